@@ -1,4 +1,4 @@
-"""Thin ctypes binding over libdbw.so: the same entry points as include/dbw.h, with
+"""Thin ctypes binding over libdbw.so: the same entry points as include/dbw.h, dbw_losses.h and dbw_measure.h, with
 argument marshalling only.  Device arrays are torch tensors (used for memory and streams,
 nothing else); every computation happens inside the library's kernels.
 
@@ -27,13 +27,17 @@ GRAD_AUTO, GRAD_LAYERS, GRAD_CHAIN = 0, 1, 2
 CAL_HBM_TRIAD, CAL_MFMA_FP32 = 0, 1
 LAYOUT_ROWS, LAYOUT_TILES = 0, 1
 TILE_COLUMNS = 64
+TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
+TEACHER_MAX, DISTILL_MAX_VOCAB = 1024, 1 << 20
 
 EXPORTS = ["dbw_create", "dbw_select", "dbw_dtur_b", "dbw_dtur_select", "dbw_dtur_reset", "dbw_dtur_get_state", "dbw_dtur_set_state",
            "dbw_get_selection",
            "dbw_get_weights", "dbw_round_time", "dbw_round", "dbw_round_eta", "dbw_consensus_rounds",
            "dbw_consensus_rounds_static",
            "dbw_convert_layout", "dbw_grad", "dbw_check", "dbw_get_links", "dbw_mix_path",
-           "dbw_destroy", "dbw_strerror", "dbw_set_timing", "dbw_get_timing", "dbw_calibrate"]
+           "dbw_destroy", "dbw_strerror", "dbw_set_timing", "dbw_get_timing", "dbw_calibrate",
+           "dbw_loss_work_bytes", "dbw_token_logp", "dbw_token_logp_grad", "dbw_distill_loss", "dbw_preference_loss",
+           "dbw_policy_loss"]
 
 
 class dbw_model(C.Structure):
@@ -44,6 +48,11 @@ class dbw_model(C.Structure):
 class dbw_opts(C.Structure):
     _fields_ = [("ld", C.c_int64), ("order", C.c_int32), ("mix_path", C.c_int32), ("layout", C.c_int32),
                 ("model", dbw_model)]
+
+
+class dbw_logits(C.Structure):
+    _fields_ = [("workers", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32), ("type", C.c_int32),
+                ("ld", C.c_int64), ("ld_grad", C.c_int64), ("scale", C.c_float)]
 
 
 class dbw_kernel_time(C.Structure):
@@ -80,6 +89,13 @@ _lib.dbw_destroy.argtypes = [_vp]
 _lib.dbw_set_timing.argtypes = [_vp, _i32]
 _lib.dbw_get_timing.argtypes = [_vp, C.POINTER(dbw_kernel_time), _i32]
 _lib.dbw_calibrate.argtypes = [_i32, _i64, _i32, C.POINTER(C.c_double), _vp]
+_lib.dbw_loss_work_bytes.restype = _i64
+_lib.dbw_loss_work_bytes.argtypes = [_vp]
+_lib.dbw_token_logp.argtypes = [_vp] * 8
+_lib.dbw_token_logp_grad.argtypes = [_vp] * 8
+_lib.dbw_distill_loss.argtypes = [_vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.dbw_preference_loss.argtypes = [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _f, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+_lib.dbw_policy_loss.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _f, _f, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 
 
 class DbwError(RuntimeError):
@@ -257,3 +273,88 @@ def dbw_calibrate(what: int, size: int, repeats: int = 10) -> float:
     res = C.c_double(0.0)
     _chk(_lib.dbw_calibrate(what, size, repeats, C.byref(res), _stream()), "dbw_calibrate")
     return res.value
+
+
+# --------------------------------------------------------------------------- losses on logits
+
+_TYPE_OF = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
+_DTYPE_OF = {number: dtype for dtype, number in _TYPE_OF.items()}
+_F32, _I32 = torch.float32, torch.int32
+
+
+def make_logits(workers: int, rows: int, vocab: int, type: int, ld: int = 0, ld_grad: int = 0, scale: float = 1.0) -> dbw_logits:
+    """type: TYPE_* (or the torch dtype) of the logits and their gradient; ld, ld_grad: row strides in elements."""
+    return dbw_logits(workers, rows, vocab, _TYPE_OF.get(type, type), ld, ld_grad, scale)
+
+
+def _arr(t, dtype, numel):
+    """Device pointer of a contiguous tensor (or None) of this type and at least this many elements."""
+    if t is None:
+        return None
+    if t.dtype is not dtype or t.numel() < numel:
+        raise ValueError(f"need at least {numel} elements of {dtype}, got {t.numel()} of {t.dtype}")
+    return _ptr(t)
+
+
+def _matrix(shape, t, ld):
+    """Device pointer of all workers' rows in a contiguous tensor (or None)."""
+    if t is None:
+        return None
+    rows = shape.workers * shape.rows
+    return _arr(t, _DTYPE_OF.get(shape.type), (rows - 1) * (ld or shape.vocab) + shape.vocab if rows > 0 else 0)
+
+
+def _work(shape, work):
+    return _arr(work, torch.uint8, dbw_loss_work_bytes(shape))
+
+
+def dbw_loss_work_bytes(shape: dbw_logits) -> int:
+    return _chk(_lib.dbw_loss_work_bytes(C.byref(shape)), "dbw_loss_work_bytes")
+
+
+def dbw_token_logp(shape, logits, tokens, logp_out, work, lse_out=None, status_out=None):
+    n = shape.workers * shape.rows
+    return _chk(_lib.dbw_token_logp(C.byref(shape), _matrix(shape, logits, shape.ld), _arr(tokens, _I32, n),
+                                    _arr(logp_out, _F32, n), _arr(lse_out, _F32, n), _arr(status_out, _I32, 1),
+                                    _work(shape, work), _stream()), "dbw_token_logp")
+
+
+def dbw_token_logp_grad(shape, logits, tokens, lse, coef, dlogits, status_out=None):
+    n = shape.workers * shape.rows
+    return _chk(_lib.dbw_token_logp_grad(C.byref(shape), _matrix(shape, logits, shape.ld), _arr(tokens, _I32, n),
+                                         _arr(lse, _F32, n), _arr(coef, _F32, n),
+                                         _matrix(shape, dlogits, shape.ld_grad or shape.ld), _arr(status_out, _I32, 1),
+                                         _stream()), "dbw_token_logp_grad")
+
+
+def dbw_distill_loss(shape, k: int, logits, teacher_index, teacher_logits, weights, loss_out, work, teacher_lse=None,
+                     row_loss_out=None, dlogits=None, status_out=None):
+    n = shape.workers * shape.rows
+    teacher_type = _TYPE_OF.get(teacher_logits.dtype, -1)
+    return _chk(_lib.dbw_distill_loss(C.byref(shape), int(k), _matrix(shape, logits, shape.ld), _arr(teacher_index, _I32, n * k),
+                                      teacher_type, _arr(teacher_logits, teacher_logits.dtype, n * k), _arr(teacher_lse, _F32, n),
+                                      _arr(weights, _F32, n), _arr(loss_out, _F32, shape.workers), _arr(row_loss_out, _F32, n),
+                                      _matrix(shape, dlogits, shape.ld_grad or shape.ld), _arr(status_out, _I32, 1),
+                                      _work(shape, work), _stream()), "dbw_distill_loss")
+
+
+def dbw_preference_loss(shape, pairs: int, logits, tokens, seq_start, ref_logp, weights, beta: float, smoothing: float, loss_out, work,
+                        margin_out, logp_out=None, dlogits=None, status_out=None):
+    n, p = shape.workers * shape.rows, shape.workers * pairs
+    return _chk(_lib.dbw_preference_loss(C.byref(shape), int(pairs), _matrix(shape, logits, shape.ld), _arr(tokens, _I32, n),
+                                         _arr(seq_start, _I32, 2 * p + 1), _arr(ref_logp, _F32, n), _arr(weights, _F32, n),
+                                         float(beta), float(smoothing), _arr(loss_out, _F32, shape.workers),
+                                         _arr(margin_out, _F32, p), _arr(logp_out, _F32, n),
+                                         _matrix(shape, dlogits, shape.ld_grad or shape.ld), _arr(status_out, _I32, 1),
+                                         _work(shape, work), _stream()), "dbw_preference_loss")
+
+
+def dbw_policy_loss(shape, logits, tokens, old_logp, ref_logp, advantage, weights, clip_low: float, clip_high: float, kl_coef: float,
+                    loss_out, work, kl_out=None, logp_out=None, dlogits=None, status_out=None):
+    n = shape.workers * shape.rows
+    return _chk(_lib.dbw_policy_loss(C.byref(shape), _matrix(shape, logits, shape.ld), _arr(tokens, _I32, n), _arr(old_logp, _F32, n),
+                                     _arr(ref_logp, _F32, n), _arr(advantage, _F32, n), _arr(weights, _F32, n), float(clip_low),
+                                     float(clip_high), float(kl_coef), _arr(loss_out, _F32, shape.workers),
+                                     _arr(kl_out, _F32, shape.workers), _arr(logp_out, _F32, n),
+                                     _matrix(shape, dlogits, shape.ld_grad or shape.ld), _arr(status_out, _I32, 1),
+                                     _work(shape, work), _stream()), "dbw_policy_loss")
