@@ -9,6 +9,7 @@
 #include <stdint.h>
 
 #include "dbw.h"
+#include "global_access.h"
 
 namespace loss {
 
@@ -91,33 +92,259 @@ __device__ __forceinline__ Base base_of(float m, float c)
 __device__ __forceinline__ float power(float x, const Base &b) { return __builtin_amdgcn_exp2f(fmaf(x, b.c, -b.M)); }
 
 // log2 of a probability, from its logit and the row's (m, Z)
-__device__ __forceinline__ float log2_p(float x, float c, float2 mz)
+template <class MZ>
+__device__ __forceinline__ float log2_p(float x, float c, const MZ &mz)
 {
-    const Base b = base_of(mz.x, c);
-    return (b.steep ? (x - mz.x) * c : fmaf(x, c, -b.M)) - log2f(mz.y);
+    const Base b = base_of(mz.m, c);
+    return (b.steep ? (x - mz.m) * c : fmaf(x, c, -b.M)) - log2f(mz.z);
 }
 
-template <int WAVES>
-__device__ __forceinline__ float block_max(float v, float *lds)
+// ---------------------------------------------------------------- reductions
+
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float shifted(float v, float identity)
 {
-    for (int d = 32; d; d >>= 1) v = fmaxf(v, __shfl_xor(v, d));
-    __syncthreads();
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
-    __syncthreads();
-    v = lds[0];
-    for (int w = 1; w < WAVES; ++w) v = fmaxf(v, lds[w]);
-    return v;
+    return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(identity), __float_as_int(v), CTRL, ROWS, 0xf, false));
 }
-template <int WAVES, class T>
-__device__ __forceinline__ T block_sum(T v, T *lds)
+__device__ __forceinline__ float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
+// Over the 64 lanes of a wave, without LDS: shifts by 1, 2, 4 and 8 within 16 lanes, then the rows' last lanes to the next rows.
+__device__ __forceinline__ float wave_max(float v)
 {
-    for (int d = 32; d; d >>= 1) v += __shfl_xor(v, d);
+    v = fmaxf(v, shifted<0x111, 0xf>(v, -INFINITY));
+    v = fmaxf(v, shifted<0x112, 0xf>(v, -INFINITY));
+    v = fmaxf(v, shifted<0x114, 0xf>(v, -INFINITY));
+    v = fmaxf(v, shifted<0x118, 0xf>(v, -INFINITY));
+    v = fmaxf(v, shifted<0x142, 0xa>(v, -INFINITY));
+    v = fmaxf(v, shifted<0x143, 0xc>(v, -INFINITY));
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+__device__ __forceinline__ float wave_sum(float v)
+{
+    v += shifted<0x111, 0xf>(v, 0.f);
+    v += shifted<0x112, 0xf>(v, 0.f);
+    v += shifted<0x114, 0xf>(v, 0.f);
+    v += shifted<0x118, 0xf>(v, 0.f);
+    v += shifted<0x142, 0xa>(v, 0.f);
+    v += shifted<0x143, 0xc>(v, 0.f);
+    return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
+}
+
+// A maximum and the sum of exponentials that count from it.
+struct MaxSum {
+    float m, z;
+};
+// The factor that takes a sum from its own maximum to another, not smaller one.
+__device__ __forceinline__ float rescale(float from, float to, float c)
+{
+    if (from == to) return 1.f;
+    if (from == -INFINITY) return 0.f;
+    const Base a = base_of(from, c), b = base_of(to, c);
+    return a.steep || b.steep ? 0.f : __builtin_amdgcn_exp2f(a.M - b.M);
+}
+__device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, float c)
+{
+    const float m = fmaxf(a.m, b.m);
+    return MaxSum{m, a.z * rescale(a.m, m, c) + b.z * rescale(b.m, m, c)};
+}
+
+// What all T threads of a row get from the waves' values, in the waves' order.  lds: T / 64 values that nothing else uses meanwhile; the
+// caller's next use of them lies behind a barrier.
+template <int T>
+__device__ __forceinline__ MaxSum row_merge(MaxSum v, float c, MaxSum *lds)
+{
+    if (T == 64) return v;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
+    float m = lds[0].m;
+    for (int w = 1; w < T / 64; ++w) m = fmaxf(m, lds[w].m);
+    float z = 0.f;
+    for (int w = 0; w < T / 64; ++w) z += lds[w].z * rescale(lds[w].m, m, c);
+    return MaxSum{uniform(m), uniform(z)};
+}
+template <int T>
+__device__ __forceinline__ float row_sum(float v, float *lds)
+{
+    v = wave_sum(v);
+    if (T == 64) return v;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     v = lds[0];
-    for (int w = 1; w < WAVES; ++w) v += lds[w];
-    return v;
+    for (int w = 1; w < T / 64; ++w) v += lds[w];
+    return uniform(v);
+}
+template <int T>
+__device__ __forceinline__ float row_max(float v, float *lds)
+{
+    v = wave_max(v);
+    if (T == 64) return v;
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = lds[0];
+    for (int w = 1; w < T / 64; ++w) v = fmaxf(v, lds[w]);
+    return uniform(v);
+}
+
+// ---------------------------------------------------------------- a row in pieces of 16 bytes
+
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+// 16 bytes that start wherever an element may
+template <class E>
+struct Piece;
+template <>
+struct Piece<float> {
+    typedef uint32_t raw __attribute__((ext_vector_type(4), aligned(4)));
+    static constexpr int N = 4;
+    static constexpr uint32_t NOTHING = 0xff800000u;      // -inf, which adds nothing to a sum of exponentials
+    static __device__ __forceinline__ void unpack(const u32x4 &w, float (&v)[N])
+    {
+        for (int i = 0; i < 4; ++i) v[i] = __uint_as_float(w[i]);
+    }
+    static __device__ __forceinline__ u32x4 pack(const float (&v)[N])
+    {
+        u32x4 w;
+        for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(v[i]);
+        return w;
+    }
+};
+template <>
+struct Piece<bf16> {
+    typedef uint32_t raw __attribute__((ext_vector_type(4), aligned(2)));
+    static constexpr int N = 8;
+    static constexpr uint32_t NOTHING = 0xff80ff80u;
+    static __device__ __forceinline__ void unpack(const u32x4 &w, float (&v)[N])
+    {
+        for (int i = 0; i < 4; ++i) {
+            v[2 * i] = __uint_as_float(w[i] << 16);
+            v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+        }
+    }
+    static __device__ __forceinline__ u32x4 pack(const float (&v)[N])
+    {
+        typedef float two __attribute__((ext_vector_type(2)));
+        typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+        u32x4 w;
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector((two){v[2 * i], v[2 * i + 1]}, bf16x2));
+        return w;
+    }
+};
+template <>
+struct Piece<f16> {
+    typedef uint32_t raw __attribute__((ext_vector_type(4), aligned(2)));
+    typedef f16 pair __attribute__((ext_vector_type(2)));
+    static constexpr int N = 8;
+    static constexpr uint32_t NOTHING = 0xfc00fc00u;
+    static __device__ __forceinline__ void unpack(const u32x4 &w, float (&v)[N])
+    {
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t bits = w[i];                   // (a cast of the vector's element itself gives the first one's bits)
+            const pair h = __builtin_bit_cast(pair, bits);
+            v[2 * i] = (float)h[0];
+            v[2 * i + 1] = (float)h[1];
+        }
+    }
+    static __device__ __forceinline__ u32x4 pack(const float (&v)[N])
+    {
+        u32x4 w;
+        for (int i = 0; i < 4; ++i) w[i] = __builtin_bit_cast(uint32_t, (pair){(f16)v[2 * i], (f16)v[2 * i + 1]});
+        return w;
+    }
+};
+
+// The elements of a row among T threads: whole pieces, thread t's are t, t + T, ...; of the fewer than 16 bytes left over thread t has
+// element t.
+template <class E, int T>
+struct RowOf {
+    typedef Piece<E> P;
+    const E *x;
+    int pieces;          // whole ones
+    int left;            // elements left over
+    __device__ __forceinline__ RowOf(const E *row, int vocab) : x(row), pieces(vocab / P::N), left(vocab % P::N) {}
+
+    // Pieces first + i T + t, i < C; what lies beyond the row adds nothing.
+    template <int C>
+    __device__ __forceinline__ void load(int first, u32x4 (&r)[C]) const
+    {
+        const global_access::bytes base = (global_access::bytes)global_access::uniform_base(x);
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int p = first + i * T + (int)threadIdx.x;
+            r[i] = (u32x4){P::NOTHING, P::NOTHING, P::NOTHING, P::NOTHING};
+            if (p < pieces) r[i] = *(const __attribute__((address_space(1))) typename P::raw *)(base + (uint32_t)p * 16u);
+        }
+    }
+    __device__ __forceinline__ int left_column() const { return pieces * P::N + (int)threadIdx.x; }
+    __device__ __forceinline__ float load_left() const { return (int)threadIdx.x < left ? widen(x[left_column()]) : -INFINITY; }
+};
+
+// Keeps the compiler from carrying pieces from one pass to the next unpacked, in twice the registers.
+template <int C>
+__device__ __forceinline__ void keep_packed(u32x4 (&r)[C])
+{
+#pragma unroll
+    for (int i = 0; i < C; ++i) asm volatile("" : "+v"(r[i]));
+}
+
+// Adds pieces to a wave's maximum and a lane's sum.  The maximum is the wave's and not the lane's, so that what the exponentials count from is
+// one number in scalar registers.
+template <class E, int C>
+__device__ __forceinline__ void add_pieces(u32x4 (&r)[C], float extra, float c, float &m, float &z)
+{
+    typedef Piece<E> P;
+    float top = extra;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        float v[P::N];
+        P::unpack(r[i], v);
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) top = fmaxf(top, v[j]);
+    }
+    top = fmaxf(wave_max(top), m);
+    z *= rescale(m, top, c);
+    m = top;
+    const Base base = base_of(m, c);
+    const Base b{uniform(base.c), uniform(base.M), false};
+    z += power(extra, b);
+    keep_packed(r);
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        float v[P::N];
+        P::unpack(r[i], v);
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < P::N; ++j) sum += power(v[j], b);
+        z += sum;
+    }
+}
+
+// Pieces of the gradient by 2^(c x - M).
+template <class E, int T, int C>
+__device__ __forceinline__ void store_pieces(E *dx, const RowOf<E, T> &row, int first, const u32x4 (&r)[C], float by, const Base &b)
+{
+    typedef Piece<E> P;
+    const global_access::bytes base = global_access::uniform_base(dx);
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+        const int p = first + i * T + (int)threadIdx.x;
+        if (p < row.pieces) {
+            float v[P::N];
+            P::unpack(r[i], v);
+#pragma unroll
+            for (int j = 0; j < P::N; ++j) v[j] = by * power(v[j], b);
+            *(__attribute__((address_space(1))) typename P::raw *)(base + (uint32_t)p * 16u) = P::pack(v);
+        }
+    }
+}
+
+template <class E, int T>
+__device__ __forceinline__ void zero_row(const Rows &R, int64_t r)
+{
+    if (!R.dx) return;
+    typedef Piece<E> P;
+    E *dx = (E *)R.dx + r * R.ld_grad;
+    const int pieces = R.vocab / P::N;
+    for (int p = threadIdx.x; p < pieces; p += T) *(typename P::raw *)(dx + (int64_t)p * P::N) = (typename P::raw)(0u);
+    const int v = pieces * P::N + (int)threadIdx.x;
+    if (v < R.vocab) dx[v] = narrow<E>(0.f);
 }
 
 // ---------------------------------------------------------------- what a row's loss needs besides its logits
@@ -125,7 +352,7 @@ __device__ __forceinline__ T block_sum(T v, T *lds)
 struct Logp {
     const int32_t *tokens;
     float *logp_out, *lse_out;
-    float2 *stats;       // (m, Z) of every row, for a gradient in a launch of its own, or null
+    struct MaxSum *stats;// (m, Z) of every row, for a gradient in a launch of its own, or null
     const float *weights;// null: no row is left out for its weight
 };
 
@@ -166,49 +393,84 @@ __device__ __forceinline__ float policy_row(const Policy &P, int64_t r, float w,
 
 // ---------------------------------------------------------------- kernels
 
-constexpr int THREADS = 256;
-constexpr int WAVES = THREADS / 64;
-
 // A grid's threads have to number less than 2^32: many rows make a second dimension.
 __device__ __forceinline__ int64_t row_of_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
-template <class E>
-__device__ __forceinline__ void zero_row(const Rows &R, int64_t r)
-{
-    if (!R.dx) return;
-    E *dx = (E *)R.dx + r * R.ld_grad;
-    for (int v = threadIdx.x; v < R.vocab; v += THREADS) dx[v] = narrow<E>(0.f);
-}
-
-// (m, Z) of a row
-template <class E>
-__device__ __forceinline__ float2 row_stats(const Rows &R, const E *x, float *lds)
-{
-    float m = -INFINITY;
-    for (int v = threadIdx.x; v < R.vocab; v += THREADS) m = fmaxf(m, widen(x[v]));
-    m = block_max<WAVES>(m, lds);
-    const Base base = base_of(m, R.c);
-    float z = 0.f;
-    for (int v = threadIdx.x; v < R.vocab; v += THREADS) z += power(widen(x[v]), base);
-    return make_float2(m, block_sum<WAVES>(z, lds));
-}
-
-// dx_v = coef ([v = y] - p_v)
-template <class E>
-__device__ __forceinline__ void row_gradient(const Rows &R, const E *x, int64_t r, int y, const Base &base, float z, float coef)
-{
-    E *dx = (E *)R.dx + r * R.ld_grad;
-    const float by = -coef / z;
-    for (int v = threadIdx.x; v < R.vocab; v += THREADS) {
-        const float e = by * power(widen(x[v]), base);
-        dx[v] = narrow<E>(v == y ? e + coef : e);
+// A workgroup of T threads takes a row in batches of T C pieces that stay in registers: one pass over them finds their maximum, one
+// their sum.  A gradient's pass starts with the last batch, which is still there: rows of up to 16 T C bytes are read once.  Longer
+// rows are read again, back to front, the latest batches first.
+template <class E, int T, int C>
+struct Walk {
+    RowOf<E, T> row;
+    u32x4 r[C];
+    float extra;
+    int last;            // the first piece of the last batch
+    __device__ __forceinline__ Walk(const E *x, int vocab) : row(x, vocab)
+    {
+        last = row.pieces > 0 ? (row.pieces - 1) / (T * C) * (T * C) : 0;
+        extra = row.load_left();
+        row.load(0, r);
     }
-}
+    // leave_out: a bit for every column that is left out of the sum, or null.  (The gradient pass may find such a column left out or not.)
+    __device__ __forceinline__ MaxSum stats(float c, MaxSum *lds, const uint8_t *leave_out = nullptr)
+    {
+        float m = -INFINITY, z = 0.f;
+        if (leave_out) {
+            const int v = row.left_column();
+            if ((int)threadIdx.x < row.left && (leave_out[v >> 3] >> (v & 7) & 1)) extra = -INFINITY;
+            leave_out_pieces(0, leave_out);
+        }
+        add_pieces<E, C>(r, extra, c, m, z);
+        for (int first = T * C; first <= last; first += T * C) {
+            row.load(first, r);
+            if (leave_out) leave_out_pieces(first, leave_out);
+            add_pieces<E, C>(r, -INFINITY, c, m, z);
+        }
+        return row_merge<T>(MaxSum{m, wave_sum(z)}, c, lds);
+    }
+    __device__ __forceinline__ void leave_out_pieces(int first, const uint8_t *bits)
+    {
+        typedef Piece<E> P;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int p = first + i * T + (int)threadIdx.x;
+            uint32_t b = p < row.pieces ? bits[P::N == 8 ? p : p >> 1] : 0u;
+            if (P::N == 4) b = b >> (p & 1) * 4 & 15u;
+            if (b) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    if (P::N == 4) {
+                        if (b >> j & 1) r[i][j] = P::NOTHING;
+                    } else {
+                        const uint32_t m = (b >> 2 * j & 1 ? 0xffffu : 0u) | (b >> 2 * j & 2 ? 0xffff0000u : 0u);
+                        r[i][j] = (r[i][j] & ~m) | (P::NOTHING & m);
+                    }
+                }
+            }
+        }
+    }
+    // dx_v = by 2^(c x_v - M), and coef more at column y (none if negative)
+    __device__ __forceinline__ void gradient(E *dx, float by, const Base &base, int y, float xy, float coef)
+    {
+        const Base b{uniform(base.c), uniform(base.M), false};
+        by = uniform(by);
+        keep_packed(r);
+        store_pieces<E, T, C>(dx, row, last, r, by, b);
+        for (int first = last - T * C; first >= 0; first -= T * C) {
+            row.load(first, r);
+            store_pieces<E, T, C>(dx, row, first, r, by, b);
+        }
+        if ((int)threadIdx.x < row.left) dx[row.left_column()] = narrow<E>(by * power(extra, b));
+        // by the thread that wrote the column before
+        const int p = y / Piece<E>::N;
+        if (y >= 0 && (int)threadIdx.x == (p < row.pieces ? p % T : y % Piece<E>::N)) dx[y] = narrow<E>(by * power(xy, b) + coef);
+    }
+};
 
-template <class E>
-__global__ __launch_bounds__(THREADS) void logp_kernel(Rows R, Logp P)
+template <class E, int T, int C>
+__global__ __launch_bounds__(T) void logp_kernel(Rows R, Logp P)
 {
-    __shared__ float lds[WAVES];
+    __shared__ MaxSum lds[T / 64];
     const int64_t r = row_of_block();
     if (r >= R.rows) return;
     const int token = P.tokens[r];
@@ -220,18 +482,20 @@ __global__ __launch_bounds__(THREADS) void logp_kernel(Rows R, Logp P)
         return;
     }
     const E *x = (const E *)R.x + r * R.ld;
-    const float2 mz = row_stats<E>(R, x, lds);
+    Walk<E, T, C> walk(x, R.vocab);
+    const float xy = widen(x[column(R, token)]);
+    const MaxSum mz = walk.stats(R.c, lds);
     if (threadIdx.x == 0) {
-        if (P.logp_out) P.logp_out[r] = LN2 * log2_p(widen(x[column(R, token)]), R.c, mz);
-        if (P.lse_out) P.lse_out[r] = fmaf(R.scale, mz.x, LN2 * log2f(mz.y));
+        if (P.logp_out) P.logp_out[r] = LN2 * log2_p(xy, R.c, mz);
+        if (P.lse_out) P.lse_out[r] = fmaf(R.scale, mz.m, LN2 * log2f(mz.z));
         if (P.stats) P.stats[r] = mz;
     }
 }
 
-template <class E>
-__global__ __launch_bounds__(THREADS) void policy_kernel(Rows R, Policy P)
+template <class E, int T, int C>
+__global__ __launch_bounds__(T) void policy_kernel(Rows R, Policy P)
 {
-    __shared__ float lds[WAVES];
+    __shared__ MaxSum lds[T / 64];
     const int64_t r = row_of_block();
     if (r >= R.rows) return;
     const int token = P.tokens[r];
@@ -241,143 +505,175 @@ __global__ __launch_bounds__(THREADS) void policy_kernel(Rows R, Policy P)
             if (P.logp_out) P.logp_out[r] = 0.f;
             P.terms[r] = make_float2(0.f, 0.f);
         }
-        zero_row<E>(R, r);
+        zero_row<E, T>(R, r);
         return;
     }
     const E *x = (const E *)R.x + r * R.ld;
+    Walk<E, T, C> walk(x, R.vocab);
     const int y = column(R, token);
     const float xy = widen(x[y]);
-    const float2 mz = row_stats<E>(R, x, lds);
+    const MaxSum mz = walk.stats(R.c, lds);
     const float logp = LN2 * log2_p(xy, R.c, mz);
     Policy once = P;
     if (threadIdx.x != 0) once.terms = nullptr;
-    const float coef = policy_row(once, r, w, logp);
+    const float coef = R.scale * policy_row(once, r, w, logp);
     if (threadIdx.x == 0 && P.logp_out) P.logp_out[r] = logp;
     if (!R.dx) return;
-    if (coef == 0.f) zero_row<E>(R, r);
-    else row_gradient<E>(R, x, r, y, base_of(mz.x, R.c), mz.y, R.scale * coef);
+    if (coef == 0.f) zero_row<E, T>(R, r);
+    else walk.gradient((E *)R.dx + r * R.ld_grad, -coef / mz.z, base_of(mz.m, R.c), y, xy, coef);
 }
 
-// The gradient alone, from (m, Z) or from L.
-template <class E>
-__global__ __launch_bounds__(THREADS) void gradient_kernel(Rows R, const int32_t *tokens, const float2 *stats, const float *lse,
-                                                           const float *coef)
+// The gradient alone, from (m, Z) or from L: a row's pieces in batches of T C.
+template <class E, int T, int C>
+__global__ __launch_bounds__(T) void gradient_kernel(Rows R, const int32_t *tokens, const MaxSum *stats, const float *lse,
+                                                     const float *coef)
 {
     const int64_t r = row_of_block();
     if (r >= R.rows) return;
     const int token = tokens[r];
-    const float g = token < 0 || !coef ? 0.f : coef[r];
+    const float g = token < 0 || !coef ? 0.f : R.scale * coef[r];
     if (g == 0.f) {
-        zero_row<E>(R, r);
+        zero_row<E, T>(R, r);
         return;
     }
     const E *x = (const E *)R.x + r * R.ld;
-    float z = 1.f;
-    Base base;
+    E *dx = (E *)R.dx + r * R.ld_grad;
+    const RowOf<E, T> row(x, R.vocab);
+    const int y = column(R, token);
+    const float xy = widen(x[y]), extra = row.load_left();
+    float by = -g;
+    Base b;
     if (stats) {
-        base = base_of(stats[r].x, R.c);
-        z = stats[r].y;
+        b = base_of(stats[r].m, R.c);
+        by /= stats[r].z;
     } else {                                              // from L: M = L log2(e), Z = 1
-        base = base_of(lse[r] / R.scale, R.c);
-        if (!base.steep) base.M = lse[r] * LOG2E;
+        b = base_of(lse[r] / R.scale, R.c);
+        if (!b.steep) b.M = lse[r] * LOG2E;
     }
-    row_gradient<E>(R, x, r, column(R, token), base, z, R.scale * g);
+    b = Base{uniform(b.c), uniform(b.M), false};
+    by = uniform(by);
+    for (int first = 0; first < row.pieces; first += T * C) {
+        u32x4 v[C];
+        row.load(first, v);
+        store_pieces<E, T, C>(dx, row, first, v, by, b);
+    }
+    if ((int)threadIdx.x < row.left) dx[row.left_column()] = narrow<E>(by * power(extra, b));
+    const int p = y / Piece<E>::N;
+    if ((int)threadIdx.x == (p < row.pieces ? p % T : y % Piece<E>::N)) dx[y] = narrow<E>(by * power(xy, b) + g);
 }
 
-template <class E>
-__global__ __launch_bounds__(THREADS) void distill_kernel(Rows R, Distill P)
+// The teacher's list of a row is in LDS: columns (-1 where absent), scaled logits, the student's logits, and a bit for every column of the
+// vocabulary that is in the list.
+template <class E, int T, int C, bool TAIL>
+__global__ __launch_bounds__(T) void distill_kernel(Rows R, Distill P)
 {
     extern __shared__ uint32_t shared[];
-    __shared__ float lds[WAVES];
+    __shared__ MaxSum lds[T / 64], lds_top[T / 64];
+    __shared__ float sums[4][T / 64];
     __shared__ int twice;
-    const int words = (R.vocab + 31) / 32;
-    int *const at = (int *)shared;                        // the teacher's columns, -1 where absent
-    float *const q = (float *)(shared + P.k);             // its probabilities
-    uint32_t *const in_top = shared + 2 * P.k;            // a bit per column: is it one of the teacher's
+    int *const at = (int *)shared;
+    float *const q = (float *)(shared + P.k);
+    float *const xs = (float *)(shared + 2 * P.k);
+    uint32_t *const in_top = shared + 3 * P.k;
 
     const int64_t r = row_of_block();
     if (r >= R.rows) return;
     const int tid = threadIdx.x;
     const float w = P.weights ? P.weights[r] : P.weight;
-    bool out = w == 0.f;
-    float norm = 0.f;
-    if (!out) {
-        for (int i = tid; i < words; i += THREADS) in_top[i] = 0;
-        if (tid == 0) twice = 0;
-        __syncthreads();
-        for (int j = tid; j < P.k; j += THREADS) {
-            int v = P.index[r * P.k + j];
-            if (v >= R.vocab) {
-                report(R.status);
-                v = -1;
-            }
-            at[j] = v;
-            q[j] = R.scale * load_as(P.value, r * P.k + j, P.value_type);
-            if (v >= 0 && (atomicOr(&in_top[v >> 5], 1u << (v & 31)) >> (v & 31) & 1)) twice = 1;
-        }
-        __syncthreads();
-        if (twice) {                                      // rare: the first entry of a column counts
-            if (tid == 0) {
-                report(R.status);
-                for (int j = 1; j < P.k; ++j)
-                    for (int i = 0; i < j; ++i)
-                        if (at[i] == at[j]) at[j] = -1;
-            }
-            __syncthreads();
-        }
-        float top = -INFINITY, any = 0.f;
-        for (int j = tid; j < P.k; j += THREADS)
-            if (at[j] >= 0) {
-                top = fmaxf(top, q[j]);
-                any = 1.f;
-            }
-        top = block_max<WAVES>(top, lds);
-        any = block_max<WAVES>(any, lds);
-        float sum = 0.f;
-        for (int j = tid; j < P.k; j += THREADS)
-            if (at[j] >= 0) sum += expf(q[j] - (top == -INFINITY ? 0.f : top));
-        sum = block_sum<WAVES>(sum, lds);
-        norm = P.teacher_lse ? P.teacher_lse[r] : top + logf(sum);
-        out = any == 0.f || (!P.teacher_lse && top == -INFINITY && sum == 0.f);
-    }
-    if (out) {
+    if (w == 0.f) {
         if (tid == 0) {
             P.terms[r] = make_float2(0.f, 0.f);
             if (P.row_loss_out) P.row_loss_out[r] = 0.f;
         }
-        zero_row<E>(R, r);
+        zero_row<E, T>(R, r);
+        return;
+    }
+    const E *x = (const E *)R.x + r * R.ld;
+    Walk<E, T, C> walk(x, R.vocab);                       // in flight while the list is looked at
+
+    const int words = (R.vocab + 31) / 32;
+    for (int i = tid; i < words; i += T) in_top[i] = 0;
+    if (tid == 0) twice = 0;
+    __syncthreads();
+    for (int j = tid; j < P.k; j += T) {
+        int v = P.index[r * P.k + j];
+        if (v >= R.vocab) {
+            report(R.status);
+            v = -1;
+        }
+        at[j] = v;
+        q[j] = R.scale * load_as(P.value, r * P.k + j, P.value_type);
+        if (v >= 0) {
+            xs[j] = widen(x[v]);
+            if (atomicOr(&in_top[v >> 5], 1u << (v & 31)) >> (v & 31) & 1) twice = 1;
+        }
+    }
+    __syncthreads();
+    if (twice) {                                          // rare: the first entry of a column counts
+        if (tid == 0) {
+            report(R.status);
+            for (int j = 1; j < P.k; ++j)
+                for (int i = 0; i < j; ++i)
+                    if (at[i] == at[j]) at[j] = -1;
+        }
+        __syncthreads();
+    }
+    float top = -INFINITY, any = 0.f, m_top = -INFINITY;
+    for (int j = tid; j < P.k; j += T)
+        if (at[j] >= 0) {
+            top = fmaxf(top, q[j]);
+            any = 1.f;
+            m_top = fmaxf(m_top, xs[j]);
+        }
+    top = row_max<T>(top, sums[0]);
+    any = row_max<T>(any, sums[1]);
+    float sum = 0.f, z_top = 0.f;
+    m_top = wave_max(m_top);
+    const Base base_top = base_of(m_top, R.c);
+    for (int j = tid; j < P.k; j += T)
+        if (at[j] >= 0) {
+            sum += expf(q[j] - (top == -INFINITY ? 0.f : top));
+            z_top += power(xs[j], base_top);
+        }
+    sum = row_sum<T>(sum, sums[2]);
+    const float norm = TAIL ? P.teacher_lse[r] : top + logf(sum);
+    if (any == 0.f || (!TAIL && top == -INFINITY && sum == 0.f)) {
+        if (tid == 0) {
+            P.terms[r] = make_float2(0.f, 0.f);
+            if (P.row_loss_out) P.row_loss_out[r] = 0.f;
+        }
+        zero_row<E, T>(R, r);
         return;
     }
 
-    const E *x = (const E *)R.x + r * R.ld;
-    const float2 mz = row_stats<E>(R, x, lds);
-    // the student's mass outside the teacher's tokens, from a maximum of its own: it may be far below the rest
-    float rest = 0.f, log_out = 0.f;
-    if (P.teacher_lse) {
-        float m = -INFINITY, z = 0.f;
-        for (int v = tid; v < R.vocab; v += THREADS)
-            if (!(in_top[v >> 5] >> (v & 31) & 1)) m = fmaxf(m, widen(x[v]));
-        m = block_max<WAVES>(m, lds);
-        const Base base = base_of(m, R.c), all = base_of(mz.x, R.c);
-        for (int v = tid; v < R.vocab; v += THREADS)
-            if (!(in_top[v >> 5] >> (v & 31) & 1)) z += power(widen(x[v]), base);
-        z = block_sum<WAVES>(z, lds);
-        log_out = LN2 * ((base.steep || all.steep ? (m - mz.x) * R.c : base.M - all.M) + (log2f(z) - log2f(mz.y)));
+    // With the tail the student's mass outside the list is summed apart, from a maximum of its own: it may be far below the rest, and as a
+    // difference from one it would be lost.
+    MaxSum mz;
+    float log_out = 0.f;
+    if (TAIL) {
+        const MaxSum in = row_merge<T>(MaxSum{m_top, wave_sum(z_top)}, R.c, lds_top);
+        const MaxSum out = walk.stats(R.c, lds, (const uint8_t *)in_top);
+        mz = merged(out, in, R.c);
+        const Base a = base_of(out.m, R.c), b = base_of(mz.m, R.c);
+        log_out = LN2 * ((a.steep || b.steep ? (out.m - mz.m) * R.c : a.M - b.M) + (log2f(out.z) - log2f(mz.z)));
+    } else {
+        mz = walk.stats(R.c, lds);
     }
+    const Base base = base_of(mz.m, R.c);
     float part = 0.f, mass = 0.f;
-    for (int j = tid; j < P.k; j += THREADS)
+    for (int j = tid; j < P.k; j += T)
         if (at[j] >= 0) {
             const float log_q = q[j] - norm, qj = expf(log_q);
-            const float log_p = LN2 * log2_p(widen(x[at[j]]), R.c, mz);
+            const float log_p = LN2 * log2_p(xs[j], R.c, mz);
             mass += qj;
             if (!(qj <= 0.f)) part += qj * (log_q - log_p);
             q[j] = expf(log_p) - qj;                      // dl/dx over s
         }
-    part = block_sum<WAVES>(part, lds);
-    mass = block_sum<WAVES>(mass, lds);
+    part = row_sum<T>(part, sums[3]);
     float factor = 1.f;
-    if (P.teacher_lse) {
-        rest = fmaxf(1.f - mass, 0.f);
+    if (TAIL) {
+        mass = row_sum<T>(mass, sums[0]);                 // (its last use lies two barriers back)
+        const float rest = fmaxf(1.f - mass, 0.f);
         if (rest > 0.f) {
             part += rest * (logf(rest) - log_out);
             factor = 1.f - expf(logf(rest) - log_out);
@@ -389,27 +685,27 @@ __global__ __launch_bounds__(THREADS) void distill_kernel(Rows R, Distill P)
     }
     if (!R.dx) return;
     E *dx = (E *)R.dx + r * R.ld_grad;
-    const Base base = base_of(mz.x, R.c);
-    const float by = R.scale * w * factor / mz.y;
-    for (int v = tid; v < R.vocab; v += THREADS)
-        if (!(in_top[v >> 5] >> (v & 31) & 1))
-            dx[v] = narrow<E>(by * power(widen(x[v]), base));
-    for (int j = tid; j < P.k; j += THREADS)
+    walk.gradient(dx, R.scale * w * factor / mz.z, base, -1, 0.f, 0.f);
+    __syncthreads();                                      // the list's columns are written over
+    for (int j = tid; j < P.k; j += T)
         if (at[j] >= 0) dx[at[j]] = narrow<E>(R.scale * w * q[j]);
 }
+
+constexpr int THREADS = 256;
+constexpr int WAVES = THREADS / 64;
 
 // loss_out[i], second_out[i] = sums of the terms of worker i's rows, always in the same order.
 __global__ __launch_bounds__(THREADS) void sum_kernel(const float2 *terms, int rows, float *loss_out, float *second_out)
 {
-    __shared__ float lds[WAVES];
+    __shared__ float lds[2][WAVES];
     const float2 *t = terms + (int64_t)blockIdx.x * rows;
     float a = 0.f, b = 0.f;
     for (int r = threadIdx.x; r < rows; r += THREADS) {
         a += t[r].x;
         b += t[r].y;
     }
-    a = block_sum<WAVES>(a, lds);
-    b = block_sum<WAVES>(b, lds);
+    a = row_sum<THREADS>(a, lds[0]);
+    b = row_sum<THREADS>(b, lds[1]);
     if (threadIdx.x == 0) {
         loss_out[blockIdx.x] = a;
         if (second_out) second_out[blockIdx.x] = b;
@@ -444,7 +740,7 @@ __global__ __launch_bounds__(THREADS) void pair_kernel(Preference P)
         const float t = P.tokens[r] < 0 || w == 0.f ? 0.f : w * (P.logp[r] - P.ref_logp[r]);
         h += r < a[1] ? t : -t;
     }
-    const float u = P.beta * block_sum<WAVES>(h, lds);
+    const float u = P.beta * row_sum<THREADS>(h, lds);
     if (tid == 0) P.margin_out[j] = u;
     const float e = expf(-fabsf(u));                      // sigma(u) = 1 / (1 + e) or e / (1 + e)
     const float sig = (u >= 0.f ? 1.f : e) / (1.f + e), sig_not = (u >= 0.f ? e : 1.f) / (1.f + e);
@@ -470,7 +766,7 @@ __global__ __launch_bounds__(THREADS) void pair_loss_kernel(const float *margin,
         // -log sigma(u) = max(-u, 0) + soft, -log sigma(-u) = max(u, 0) + soft
         l += u[j] != u[j] ? u[j] : soft + (u[j] >= 0.f ? smoothing * u[j] : (smoothing - 1.f) * u[j]);
     }
-    l = block_sum<WAVES>(l, lds);
+    l = row_sum<THREADS>(l, lds);
     if (threadIdx.x == 0) loss_out[blockIdx.x] = pairs ? l / (float)pairs : 0.f;
 }
 

@@ -14,7 +14,7 @@ constexpr int64_t MAX_GROUPS = 1 << 22;   // of kernels that take a workgroup pe
 
 struct Shape {
     int64_t rows;        // of all workers
-    int64_t ld, ld_grad;
+    int64_t ld, ld_grad, row_bytes;
     loss::Rows R;
 };
 
@@ -34,7 +34,8 @@ int check_shape(const dbw_logits *l, Shape *out)
 
 // Scratch memory: per row the maximum and the sum, and two terms of a loss (or its coefficient and its log-probability).
 struct Work {
-    float2 *stats, *terms;
+    loss::MaxSum *stats;
+    float2 *terms;
     float *coef, *logp;
 };
 constexpr int64_t WORK_PER_ROW = 16;
@@ -42,8 +43,8 @@ constexpr int64_t WORK_PER_ROW = 16;
 Work split_work(void *work, int64_t rows)
 {
     Work w;
-    w.stats = (float2 *)work;
-    w.terms = w.stats + rows;
+    w.stats = (loss::MaxSum *)work;
+    w.terms = (float2 *)(w.stats + rows);
     w.coef = (float *)w.terms;
     w.logp = w.coef + rows;
     return w;
@@ -62,6 +63,7 @@ int prepare(const dbw_logits *l, const void *logits, void *dlogits, int32_t *sta
         const size_t na = e * (size_t)((S->rows - 1) * S->ld + l->vocab), nb = e * (size_t)((S->rows - 1) * S->ld_grad + l->vocab);
         if (a < b + nb && b < a + na) return DBW_ERR_ALIAS;
     }
+    S->row_bytes = (int64_t)e * l->vocab;
     S->R = loss::Rows{logits, dlogits, S->ld, S->ld_grad, l->vocab, S->rows, l->scale, l->scale * loss::LOG2E, status};
     return DBW_OK;
 }
@@ -72,6 +74,22 @@ dim3 grid_of(int64_t rows)
     return dim3((uint32_t)x, (uint32_t)((rows + x - 1) / x));
 }
 
+// Threads and pieces a thread for rows of that many bytes.  A row of up to 16 KB a wave, or 256 KB a workgroup, stays in registers; longer ones are walked in batches.
+template <int T_, int C_>
+struct Plan {
+    static constexpr int T = T_, C = C_;
+};
+template <class F>
+void by_row(int64_t bytes, F f)
+{
+    if (bytes <= 2 * 64 * 16) f(Plan<64, 2>());
+    else if (bytes <= 8 * 64 * 16) f(Plan<64, 8>());
+    else if (bytes <= 4 * 256 * 16) f(Plan<256, 4>());
+    else if (bytes <= 8 * 256 * 16) f(Plan<256, 8>());
+    else if (bytes <= 16 * 256 * 16) f(Plan<256, 16>());
+    else if (bytes <= 16 * 512 * 16) f(Plan<512, 16>());
+    else f(Plan<1024, 16>());
+}
 // Calls f with a value of the logits' type.
 template <class F>
 void by_type(int type, F f)
@@ -79,6 +97,14 @@ void by_type(int type, F f)
     if (type == DBW_TYPE_F32) f(float());
     else if (type == DBW_TYPE_BF16) f(loss::bf16());
     else f(loss::f16());
+}
+// The kernels that only read a row, or only write one from what is known of it, need not hold it.
+template <class F>
+void by_length(int64_t bytes, F f)
+{
+    if (bytes <= 8 * 64 * 16) f(Plan<64, 2>());
+    else if (bytes <= 128 << 10) f(Plan<256, 8>());
+    else f(Plan<1024, 8>());
 }
 
 }  // namespace
@@ -100,7 +126,9 @@ extern "C" int dbw_token_logp(const dbw_logits *shape, const void *logits, const
     if (S.rows == 0) return DBW_OK;
     const loss::Logp P{tokens, logp_out, lse_out, nullptr};
     by_type(shape->type, [&](auto e) {
-        hipLaunchKernelGGL((loss::logp_kernel<decltype(e)>), grid_of(S.rows), dim3(loss::THREADS), 0, (hipStream_t)stream, S.R, P);
+        by_length(S.row_bytes, [&](auto p) {
+            hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, (hipStream_t)stream, S.R, P);
+        });
     });
     DBW_HIP(hipGetLastError());
     return DBW_OK;
@@ -115,8 +143,10 @@ extern "C" int dbw_token_logp_grad(const dbw_logits *shape, const void *logits, 
     if (S.rows > 0 && (!tokens || !lse || !coef || !dlogits)) return DBW_ERR_NULL;
     if (S.rows == 0) return DBW_OK;
     by_type(shape->type, [&](auto e) {
-        hipLaunchKernelGGL((loss::gradient_kernel<decltype(e)>), grid_of(S.rows), dim3(loss::THREADS), 0, (hipStream_t)stream, S.R,
-                           tokens, (const float2 *)nullptr, lse, coef);
+        by_length(S.row_bytes, [&](auto p) {
+            hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, (hipStream_t)stream, S.R,
+                               tokens, (const loss::MaxSum *)nullptr, lse, coef);
+        });
     });
     DBW_HIP(hipGetLastError());
     return DBW_OK;
@@ -137,13 +167,18 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
     hipStream_t s = (hipStream_t)stream;
     if (S.rows > 0) {
         const loss::Distill P{teacher_index, teacher_logits, teacher_lse, weights, 1.f / (float)shape->rows, k, teacher_type, row_loss_out, W.terms};
-        const size_t lds = 4 * ((size_t)2 * k + ((size_t)shape->vocab + 31) / 32);
+        const size_t lds = 4 * ((size_t)3 * k + ((size_t)shape->vocab + 31) / 32);
         bool fits = true;
-        by_type(shape->type, [&](auto e) {
-            auto kernel = loss::distill_kernel<decltype(e)>;
+        const auto launch = [&](auto kernel, int threads) {
             // more than 64 KB have to be asked for
             if (lds > 65536) fits = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
-            if (fits) hipLaunchKernelGGL(kernel, grid_of(S.rows), dim3(loss::THREADS), lds, s, S.R, P);
+            if (fits) hipLaunchKernelGGL(kernel, grid_of(S.rows), dim3((uint32_t)threads), lds, s, S.R, P);
+        };
+        by_type(shape->type, [&](auto e) {
+            by_row(S.row_bytes, [&](auto p) {
+                if (teacher_lse) launch(loss::distill_kernel<decltype(e), p.T, p.C, true>, p.T);
+                else launch(loss::distill_kernel<decltype(e), p.T, p.C, false>, p.T);
+            });
         });
         if (!fits) return DBW_ERR_HIP;
         DBW_HIP(hipGetLastError());
@@ -171,7 +206,9 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     if (S.rows > 0) {
         const loss::Logp P{tokens, logp, nullptr, W.stats, weights};
         by_type(shape->type, [&](auto e) {
-            hipLaunchKernelGGL((loss::logp_kernel<decltype(e)>), grid_of(S.rows), dim3(loss::THREADS), 0, s, S.R, P);
+            by_length(S.row_bytes, [&](auto p) {
+                hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
+            });
         });
         DBW_HIP(hipGetLastError());
     }
@@ -185,8 +222,10 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     DBW_HIP(hipGetLastError());
     if (dlogits && S.rows > 0) {
         by_type(shape->type, [&](auto e) {
-            hipLaunchKernelGGL((loss::gradient_kernel<decltype(e)>), grid_of(S.rows), dim3(loss::THREADS), 0, s, S.R, tokens,
-                               (const float2 *)W.stats, (const float *)nullptr, (const float *)(pairs > 0 ? W.coef : nullptr));
+            by_length(S.row_bytes, [&](auto p) {
+                hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, s, S.R, tokens,
+                                   (const loss::MaxSum *)W.stats, (const float *)nullptr, (const float *)(pairs > 0 ? W.coef : nullptr));
+            });
         });
         DBW_HIP(hipGetLastError());
     }
@@ -209,7 +248,9 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
         const loss::Policy P{tokens, old_logp, ref_logp, advantage, weights, 1.f - clip_low, 1.f + clip_high, kl_coef,
                              1.f / (float)shape->rows, logp_out, W.terms};
         by_type(shape->type, [&](auto e) {
-            hipLaunchKernelGGL((loss::policy_kernel<decltype(e)>), grid_of(S.rows), dim3(loss::THREADS), 0, s, S.R, P);
+            by_row(S.row_bytes, [&](auto p) {
+                hipLaunchKernelGGL((loss::policy_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
+            });
         });
         DBW_HIP(hipGetLastError());
     }
