@@ -40,11 +40,13 @@ extern "C" {
 
 enum { DBW_TYPE_F32 = 0, DBW_TYPE_BF16 = 1, DBW_TYPE_F16 = 2 };
 
+#define DBW_LOSS_MAX_VOCAB (1 << 28)
+
 /* Logits of all workers, and their gradient. */
 typedef struct {
     int32_t workers; /* N >= 1, at most 2^22 */
     int32_t rows;    /* T >= 0 token positions of each worker; N * T < 2^31 (DBW_ERR_UNSUPPORTED beyond) */
-    int32_t vocab;   /* V >= 1 columns */
+    int32_t vocab;   /* V >= 1 columns, at most DBW_LOSS_MAX_VOCAB (DBW_ERR_UNSUPPORTED beyond) */
     int32_t type;    /* DBW_TYPE_* of logits and dlogits */
     int64_t ld;      /* stride of the logits' rows in elements, >= V; 0 means V */
     int64_t ld_grad; /* stride of dlogits' rows, >= V; 0 means ld.  Columns [V, ld_grad) are not written */

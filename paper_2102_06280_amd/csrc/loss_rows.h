@@ -250,30 +250,82 @@ struct Piece<f16> {
     }
 };
 
-// The elements of a row among T threads: whole pieces, thread t's are t, t + T, ...; of the fewer than 16 bytes left over thread t has
-// element t.
+// The elements of a row among T threads: pieces of 16 bytes on 16-byte boundaries, thread t's are t, t + T, ...  Of the elements before
+// the first boundary thread t has element t, of those behind the last piece thread BEHIND + t: at most one of either a thread.
 template <class E, int T>
 struct RowOf {
     typedef Piece<E> P;
+    typedef const __attribute__((address_space(1))) u32x4 *place;
+    static constexpr int BEHIND = 32;
     const E *x;
-    int pieces;          // whole ones
-    int left;            // elements left over
-    __device__ __forceinline__ RowOf(const E *row, int vocab) : x(row), pieces(vocab / P::N), left(vocab % P::N) {}
+    int before;          // elements before the first boundary
+    int pieces;
+    int behind;          // elements behind the last piece
+    __device__ __forceinline__ RowOf(const E *row, int vocab) : x(row)
+    {
+        before = min(vocab, (int)(-(uintptr_t)row & 15) / (int)sizeof(E));
+        pieces = (vocab - before) / P::N;
+        behind = (vocab - before) % P::N;
+    }
 
-    // Pieces first + i T + t, i < C; what lies beyond the row adds nothing.
-    template <int C>
+    // Pieces first + i T + t, i < C, without a branch: beyond the row's end its last piece again, which clip() takes out when the pieces
+    // are looked at.  The row has a piece.  ONCE: they will not be read again, so they need not stay in the caches.
+    template <int C, bool ONCE>
     __device__ __forceinline__ void load(int first, u32x4 (&r)[C]) const
     {
-        const global_access::bytes base = (global_access::bytes)global_access::uniform_base(x);
+        const global_access::bytes base = global_access::uniform_base(x + before);
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            const int p = first + i * T + (int)threadIdx.x;
-            r[i] = (u32x4){P::NOTHING, P::NOTHING, P::NOTHING, P::NOTHING};
-            if (p < pieces) r[i] = *(const __attribute__((address_space(1))) typename P::raw *)(base + (uint32_t)p * 16u);
+            const uint32_t p = min(first + i * T + (int)threadIdx.x, pieces - 1);
+            r[i] = ONCE ? __builtin_nontemporal_load((place)(base + p * 16u)) : *(place)(base + p * 16u);
         }
     }
-    __device__ __forceinline__ int left_column() const { return pieces * P::N + (int)threadIdx.x; }
-    __device__ __forceinline__ float load_left() const { return (int)threadIdx.x < left ? widen(x[left_column()]) : -INFINITY; }
+    // Piece i of those from `first` on: beyond the row's end it adds nothing.
+    __device__ __forceinline__ void clip(int first, int i, u32x4 &r) const
+    {
+        if (first + (i + 1) * T > pieces) {               // the same for all threads
+            const bool in = first + i * T + (int)threadIdx.x < pieces;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) r[j] = in ? r[j] : P::NOTHING;
+        }
+    }
+    // Takes the columns whose bits are set out of piece i of those from `first` on.
+    __device__ __forceinline__ void leave_out(int first, int i, u32x4 &r, const uint8_t *bits) const
+    {
+        const int p = first + i * T + (int)threadIdx.x;
+        uint32_t b = p < pieces ? bits[(p + 1) * P::N >> 3] : 0u;
+        if (P::N == 4) b = b >> ((p + 1) & 1) * 4 & 15u;
+        if (b) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                if (P::N == 4) {
+                    if (b >> j & 1) r[j] = P::NOTHING;
+                } else {
+                    const uint32_t m = (b >> 2 * j & 1 ? 0xffffu : 0u) | (b >> 2 * j & 2 ? 0xffff0000u : 0u);
+                    r[j] = (r[j] & ~m) | (P::NOTHING & m);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ int piece_column(int p) const { return before + p * P::N; }
+    __device__ __forceinline__ bool has_single() const
+    {
+        const int t = threadIdx.x;
+        return t < before || (t >= BEHIND && t < BEHIND + behind);
+    }
+    __device__ __forceinline__ int single_column() const
+    {
+        const int t = threadIdx.x;
+        return t < BEHIND ? t : piece_column(pieces) + t - BEHIND;
+    }
+    __device__ __forceinline__ float load_single() const { return has_single() ? widen(x[single_column()]) : -INFINITY; }
+    // the thread that a column is with
+    __device__ __forceinline__ int owner(int v) const
+    {
+        if (v < before) return v;
+        const int p = (v - before) / P::N;
+        return p >= pieces ? BEHIND + (v - before) % P::N : p % T;
+    }
 };
 
 // Keeps the compiler from carrying pieces from one pass to the next unpacked, in twice the registers.
@@ -284,67 +336,77 @@ __device__ __forceinline__ void keep_packed(u32x4 (&r)[C])
     for (int i = 0; i < C; ++i) asm volatile("" : "+v"(r[i]));
 }
 
-// Adds pieces to a wave's maximum and a lane's sum.  The maximum is the wave's and not the lane's, so that what the exponentials count from is
-// one number in scalar registers.
-template <class E, int C>
-__device__ __forceinline__ void add_pieces(u32x4 (&r)[C], float extra, float c, float &m, float &z)
+template <class E>
+__device__ __forceinline__ float piece_max(const u32x4 &r, float top)
 {
-    typedef Piece<E> P;
-    float top = extra;
+    float v[Piece<E>::N];
+    Piece<E>::unpack(r, v);
+#pragma unroll
+    for (int j = 0; j < Piece<E>::N; ++j) top = fmaxf(top, v[j]);
+    return top;
+}
+template <class E>
+__device__ __forceinline__ float piece_sum(const u32x4 &r, const Base &b)
+{
+    float v[Piece<E>::N], sum = 0.f;
+    Piece<E>::unpack(r, v);
+#pragma unroll
+    for (int j = 0; j < Piece<E>::N; ++j) sum += power(v[j], b);
+    return sum;
+}
+
+// Adds the pieces from `first` on to a wave's maximum and a lane's sum.  The maximum is the wave's and not the lane's, so that what the exponentials count from is one number in scalar registers.
+// left_out: bits of columns that are left out of the sum (LEAVE); column v has bit v - row.before + N, so that a piece's bits are together.
+template <bool LEAVE, class E, int T, int C>
+__device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, u32x4 (&r)[C], float single, const uint8_t *left_out, float c, float &m, float &z)
+{
+    float top = single;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        float v[P::N];
-        P::unpack(r[i], v);
-#pragma unroll
-        for (int j = 0; j < P::N; ++j) top = fmaxf(top, v[j]);
+        row.clip(first, i, r[i]);
+        if (LEAVE) {
+            row.leave_out(first, i, r[i], left_out);
+            asm volatile("" : "+v"(r[i]));                // one piece after the other
+        }
+        top = piece_max<E>(r[i], top);
     }
     top = fmaxf(wave_max(top), m);
     z *= rescale(m, top, c);
     m = top;
     const Base base = base_of(m, c);
     const Base b{uniform(base.c), uniform(base.M), false};
-    z += power(extra, b);
+    z += power(single, b);
     keep_packed(r);
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        float v[P::N];
-        P::unpack(r[i], v);
-        float sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < P::N; ++j) sum += power(v[j], b);
-        z += sum;
-    }
+    for (int i = 0; i < C; ++i) z += piece_sum<E>(r[i], b);
 }
 
-// Pieces of the gradient by 2^(c x - M).
-template <class E, int T, int C>
-__device__ __forceinline__ void store_pieces(E *dx, const RowOf<E, T> &row, int first, const u32x4 (&r)[C], float by, const Base &b)
+// Piece i of the gradient of those from `first` on: by 2^(c x - M).
+template <class E, int T>
+__device__ __forceinline__ void store_piece(global_access::bytes base, int first, int pieces, int i, const u32x4 &r, float by, const Base &b)
 {
     typedef Piece<E> P;
-    const global_access::bytes base = global_access::uniform_base(dx);
+    const int p = first + i * T + (int)threadIdx.x;
+    if (p < pieces) {
+        float v[P::N];
+        P::unpack(r, v);
 #pragma unroll
-    for (int i = 0; i < C; ++i) {
-        const int p = first + i * T + (int)threadIdx.x;
-        if (p < row.pieces) {
-            float v[P::N];
-            P::unpack(r[i], v);
-#pragma unroll
-            for (int j = 0; j < P::N; ++j) v[j] = by * power(v[j], b);
-            *(__attribute__((address_space(1))) typename P::raw *)(base + (uint32_t)p * 16u) = P::pack(v);
-        }
+        for (int j = 0; j < P::N; ++j) v[j] = by * power(v[j], b);
+        __builtin_nontemporal_store((typename P::raw)P::pack(v), (__attribute__((address_space(1))) typename P::raw *)(base + (uint32_t)p * 16u));
     }
 }
 
-template <class E, int T>
+template <class E, int T, bool NT = false>
 __device__ __forceinline__ void zero_row(const Rows &R, int64_t r)
 {
     if (!R.dx) return;
-    typedef Piece<E> P;
     E *dx = (E *)R.dx + r * R.ld_grad;
-    const int pieces = R.vocab / P::N;
-    for (int p = threadIdx.x; p < pieces; p += T) *(typename P::raw *)(dx + (int64_t)p * P::N) = (typename P::raw)(0u);
-    const int v = pieces * P::N + (int)threadIdx.x;
-    if (v < R.vocab) dx[v] = narrow<E>(0.f);
+    const RowOf<E, T> row(dx, R.vocab);
+    const global_access::bytes base = global_access::uniform_base(dx + row.before);
+    for (int p = threadIdx.x; p < row.pieces; p += T)
+        if (NT) __builtin_nontemporal_store((u32x4)(0u), (__attribute__((address_space(1))) u32x4 *)(base + (uint32_t)p * 16u));
+        else *(__attribute__((address_space(1))) u32x4 *)(base + (uint32_t)p * 16u) = (u32x4)(0u);
+    if (row.has_single()) dx[row.single_column()] = narrow<E>(0.f);
 }
 
 // ---------------------------------------------------------------- what a row's loss needs besides its logits
@@ -396,78 +458,68 @@ __device__ __forceinline__ float policy_row(const Policy &P, int64_t r, float w,
 // A grid's threads have to number less than 2^32: many rows make a second dimension.
 __device__ __forceinline__ int64_t row_of_block() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
-// A workgroup of T threads takes a row in batches of T C pieces that stay in registers: one pass over them finds their maximum, one
-// their sum.  A gradient's pass starts with the last batch, which is still there: rows of up to 16 T C bytes are read once.  Longer
-// rows are read again, back to front, the latest batches first.
-template <class E, int T, int C>
+// A workgroup of T threads holds the first T C pieces of a row in registers from when they are loaded until the gradient is written: one pass
+// over them finds their maximum, one their sum, one the gradient.  The pieces that a longer row has behind them go through other registers,
+// T S at a time, and are read again for the gradient, back to front, the latest first.  (S = 0: no row is longer.)
+template <class E, int T, int C, int S>
 struct Walk {
+    static constexpr int REST = T * C;
     RowOf<E, T> row;
     u32x4 r[C];
-    float extra;
-    int last;            // the first piece of the last batch
+    float single;
     __device__ __forceinline__ Walk(const E *x, int vocab) : row(x, vocab)
     {
-        last = row.pieces > 0 ? (row.pieces - 1) / (T * C) * (T * C) : 0;
-        extra = row.load_left();
-        row.load(0, r);
+        if (row.pieces > 0) {
+            row.template load<C, true>(0, r);
+        } else {
+#pragma unroll
+            for (int i = 0; i < C; ++i) r[i] = (u32x4)(Piece<E>::NOTHING);
+        }
+        single = row.load_single();
     }
-    // leave_out: a bit for every column that is left out of the sum, or null.  (The gradient pass may find such a column left out or not.)
-    __device__ __forceinline__ MaxSum stats(float c, MaxSum *lds, const uint8_t *leave_out = nullptr)
+    // (The gradient's pass may find a column that is left out here left out or not.)
+    template <bool LEAVE = false>
+    __device__ __forceinline__ MaxSum stats(float c, MaxSum *lds, const uint8_t *left_out = nullptr)
     {
         float m = -INFINITY, z = 0.f;
-        if (leave_out) {
-            const int v = row.left_column();
-            if ((int)threadIdx.x < row.left && (leave_out[v >> 3] >> (v & 7) & 1)) extra = -INFINITY;
-            leave_out_pieces(0, leave_out);
+        if (LEAVE) {
+            const int bit = row.single_column() - row.before + Piece<E>::N;
+            if (row.has_single() && (left_out[bit >> 3] >> (bit & 7) & 1)) single = -INFINITY;
         }
-        add_pieces<E, C>(r, extra, c, m, z);
-        for (int first = T * C; first <= last; first += T * C) {
-            row.load(first, r);
-            if (leave_out) leave_out_pieces(first, leave_out);
-            add_pieces<E, C>(r, -INFINITY, c, m, z);
-        }
+        add_pieces<LEAVE>(row, 0, r, single, left_out, c, m, z);
+        if constexpr (S > 0)
+            for (int first = REST; first < row.pieces; first += T * S) {
+                u32x4 v[S];
+                row.template load<S, false>(first, v);
+                add_pieces<LEAVE>(row, first, v, -INFINITY, left_out, c, m, z);
+            }
         return row_merge<T>(MaxSum{m, wave_sum(z)}, c, lds);
     }
-    __device__ __forceinline__ void leave_out_pieces(int first, const uint8_t *bits)
-    {
-        typedef Piece<E> P;
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const int p = first + i * T + (int)threadIdx.x;
-            uint32_t b = p < row.pieces ? bits[P::N == 8 ? p : p >> 1] : 0u;
-            if (P::N == 4) b = b >> (p & 1) * 4 & 15u;
-            if (b) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    if (P::N == 4) {
-                        if (b >> j & 1) r[i][j] = P::NOTHING;
-                    } else {
-                        const uint32_t m = (b >> 2 * j & 1 ? 0xffffu : 0u) | (b >> 2 * j & 2 ? 0xffff0000u : 0u);
-                        r[i][j] = (r[i][j] & ~m) | (P::NOTHING & m);
-                    }
-                }
-            }
-        }
-    }
-    // dx_v = by 2^(c x_v - M), and coef more at column y (none if negative)
+    // dx_v = by 2^(c x - M), and coef more at column y (none if negative)
     __device__ __forceinline__ void gradient(E *dx, float by, const Base &base, int y, float xy, float coef)
     {
         const Base b{uniform(base.c), uniform(base.M), false};
         by = uniform(by);
+        const global_access::bytes out = global_access::uniform_base(dx + row.before);
+        if constexpr (S > 0)
+            if (row.pieces > REST)
+                for (int first = REST + (row.pieces - 1 - REST) / (T * S) * (T * S); first >= REST; first -= T * S) {
+                    u32x4 v[S];
+                    row.template load<S, true>(first, v);
+#pragma unroll
+                    for (int i = 0; i < S; ++i) store_piece<E, T>(out, first, row.pieces, i, v[i], by, b);
+                }
         keep_packed(r);
-        store_pieces<E, T, C>(dx, row, last, r, by, b);
-        for (int first = last - T * C; first >= 0; first -= T * C) {
-            row.load(first, r);
-            store_pieces<E, T, C>(dx, row, first, r, by, b);
-        }
-        if ((int)threadIdx.x < row.left) dx[row.left_column()] = narrow<E>(by * power(extra, b));
+#pragma unroll
+        for (int i = 0; i < C; ++i) store_piece<E, T>(out, 0, row.pieces, i, r[i], by, b);
+        if (row.has_single()) dx[row.single_column()] = narrow<E>(by * power(single, b));
         // by the thread that wrote the column before
-        const int p = y / Piece<E>::N;
-        if (y >= 0 && (int)threadIdx.x == (p < row.pieces ? p % T : y % Piece<E>::N)) dx[y] = narrow<E>(by * power(xy, b) + coef);
+        if (y >= 0 && (int)threadIdx.x == row.owner(y)) dx[y] = narrow<E>(by * power(xy, b) + coef);
     }
 };
 
-template <class E, int T, int C>
+// AGAIN: the rows will be read again soon, for their gradient.
+template <class E, int T, int C, bool AGAIN>
 __global__ __launch_bounds__(T) void logp_kernel(Rows R, Logp P)
 {
     __shared__ MaxSum lds[T / 64];
@@ -482,9 +534,15 @@ __global__ __launch_bounds__(T) void logp_kernel(Rows R, Logp P)
         return;
     }
     const E *x = (const E *)R.x + r * R.ld;
-    Walk<E, T, C> walk(x, R.vocab);
-    const float xy = widen(x[column(R, token)]);
-    const MaxSum mz = walk.stats(R.c, lds);
+    const RowOf<E, T> row(x, R.vocab);
+    float m = -INFINITY, z = 0.f;
+    for (int first = 0; first < row.pieces; first += T * C) {
+        u32x4 v[C];
+        row.template load<C, !AGAIN>(first, v);
+        add_pieces<false>(row, first, v, -INFINITY, nullptr, R.c, m, z);
+    }
+    const float single = row.load_single(), xy = widen(x[column(R, token)]), top = wave_max(single);
+    const MaxSum mz = row_merge<T>(merged(MaxSum{m, wave_sum(z)}, MaxSum{top, wave_sum(power(single, base_of(top, R.c)))}, R.c), R.c, lds);
     if (threadIdx.x == 0) {
         if (P.logp_out) P.logp_out[r] = LN2 * log2_p(xy, R.c, mz);
         if (P.lse_out) P.lse_out[r] = fmaf(R.scale, mz.m, LN2 * log2f(mz.z));
@@ -492,8 +550,8 @@ __global__ __launch_bounds__(T) void logp_kernel(Rows R, Logp P)
     }
 }
 
-template <class E, int T, int C>
-__global__ __launch_bounds__(T) void policy_kernel(Rows R, Policy P)
+template <class E, int T, int C, int S>
+__global__ __launch_bounds__(T, C == 16 ? 4 : 1) void policy_kernel(Rows R, Policy P)
 {
     __shared__ MaxSum lds[T / 64];
     const int64_t r = row_of_block();
@@ -509,7 +567,7 @@ __global__ __launch_bounds__(T) void policy_kernel(Rows R, Policy P)
         return;
     }
     const E *x = (const E *)R.x + r * R.ld;
-    Walk<E, T, C> walk(x, R.vocab);
+    Walk<E, T, C, S> walk(x, R.vocab);
     const int y = column(R, token);
     const float xy = widen(x[y]);
     const MaxSum mz = walk.stats(R.c, lds);
@@ -533,14 +591,14 @@ __global__ __launch_bounds__(T) void gradient_kernel(Rows R, const int32_t *toke
     const int token = tokens[r];
     const float g = token < 0 || !coef ? 0.f : R.scale * coef[r];
     if (g == 0.f) {
-        zero_row<E, T>(R, r);
+        zero_row<E, T, true>(R, r);
         return;
     }
     const E *x = (const E *)R.x + r * R.ld;
     E *dx = (E *)R.dx + r * R.ld_grad;
     const RowOf<E, T> row(x, R.vocab);
     const int y = column(R, token);
-    const float xy = widen(x[y]), extra = row.load_left();
+    const float xy = widen(x[y]), single = row.load_single();
     float by = -g;
     Base b;
     if (stats) {
@@ -552,20 +610,21 @@ __global__ __launch_bounds__(T) void gradient_kernel(Rows R, const int32_t *toke
     }
     b = Base{uniform(b.c), uniform(b.M), false};
     by = uniform(by);
+    const global_access::bytes out = global_access::uniform_base(dx + row.before);
     for (int first = 0; first < row.pieces; first += T * C) {
         u32x4 v[C];
-        row.load(first, v);
-        store_pieces<E, T, C>(dx, row, first, v, by, b);
+        row.template load<C, true>(first, v);
+#pragma unroll
+        for (int i = 0; i < C; ++i) store_piece<E, T>(out, first, row.pieces, i, v[i], by, b);
     }
-    if ((int)threadIdx.x < row.left) dx[row.left_column()] = narrow<E>(by * power(extra, b));
-    const int p = y / Piece<E>::N;
-    if ((int)threadIdx.x == (p < row.pieces ? p % T : y % Piece<E>::N)) dx[y] = narrow<E>(by * power(xy, b) + g);
+    if (row.has_single()) dx[row.single_column()] = narrow<E>(by * power(single, b));
+    if ((int)threadIdx.x == row.owner(y)) dx[y] = narrow<E>(by * power(xy, b) + g);
 }
 
 // The teacher's list of a row is in LDS: columns (-1 where absent), scaled logits, the student's logits, and a bit for every column of the
 // vocabulary that is in the list.
-template <class E, int T, int C, bool TAIL>
-__global__ __launch_bounds__(T) void distill_kernel(Rows R, Distill P)
+template <class E, int T, int C, int S, bool TAIL>
+__global__ __launch_bounds__(T, C == 16 ? 4 : 1) void distill_kernel(Rows R, Distill P)
 {
     extern __shared__ uint32_t shared[];
     __shared__ MaxSum lds[T / 64], lds_top[T / 64];
@@ -589,9 +648,9 @@ __global__ __launch_bounds__(T) void distill_kernel(Rows R, Distill P)
         return;
     }
     const E *x = (const E *)R.x + r * R.ld;
-    Walk<E, T, C> walk(x, R.vocab);                       // in flight while the list is looked at
+    Walk<E, T, C, S> walk(x, R.vocab);                       // in flight while the list is looked at
 
-    const int words = (R.vocab + 31) / 32;
+    const int words = (R.vocab + Piece<E>::N + 31) / 32, bit0 = Piece<E>::N - walk.row.before;
     for (int i = tid; i < words; i += T) in_top[i] = 0;
     if (tid == 0) twice = 0;
     __syncthreads();
@@ -605,7 +664,7 @@ __global__ __launch_bounds__(T) void distill_kernel(Rows R, Distill P)
         q[j] = R.scale * load_as(P.value, r * P.k + j, P.value_type);
         if (v >= 0) {
             xs[j] = widen(x[v]);
-            if (atomicOr(&in_top[v >> 5], 1u << (v & 31)) >> (v & 31) & 1) twice = 1;
+            if (atomicOr(&in_top[v + bit0 >> 5], 1u << (v + bit0 & 31)) >> (v + bit0 & 31) & 1) twice = 1;
         }
     }
     __syncthreads();
@@ -652,7 +711,7 @@ __global__ __launch_bounds__(T) void distill_kernel(Rows R, Distill P)
     float log_out = 0.f;
     if (TAIL) {
         const MaxSum in = row_merge<T>(MaxSum{m_top, wave_sum(z_top)}, R.c, lds_top);
-        const MaxSum out = walk.stats(R.c, lds, (const uint8_t *)in_top);
+        const MaxSum out = walk.template stats<true>(R.c, lds, (const uint8_t *)in_top);
         mz = merged(out, in, R.c);
         const Base a = base_of(out.m, R.c), b = base_of(mz.m, R.c);
         log_out = LN2 * ((a.steep || b.steep ? (out.m - mz.m) * R.c : a.M - b.M) + (log2f(out.z) - log2f(mz.z)));

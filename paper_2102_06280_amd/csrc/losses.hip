@@ -27,7 +27,7 @@ int check_shape(const dbw_logits *l, Shape *out)
     if (out->ld < l->vocab || out->ld_grad < l->vocab) return DBW_ERR_INVALID;
     if (!(l->scale > 0.f) || !isfinite(l->scale * loss::LOG2E)) return DBW_ERR_INVALID;
     out->rows = (int64_t)l->workers * l->rows;
-    if (l->workers > MAX_GROUPS || out->rows > INT32_MAX || out->ld > INT64_MAX / 8 / (out->rows + 1) || out->ld_grad > INT64_MAX / 8 / (out->rows + 1))
+    if (l->vocab > DBW_LOSS_MAX_VOCAB || l->workers > MAX_GROUPS || out->rows > INT32_MAX || out->ld > INT64_MAX / 8 / (out->rows + 1) || out->ld_grad > INT64_MAX / 8 / (out->rows + 1))
         return DBW_ERR_UNSUPPORTED;
     return DBW_OK;
 }
@@ -75,9 +75,9 @@ dim3 grid_of(int64_t rows)
 }
 
 // Threads and pieces a thread for rows of that many bytes.  A row of up to 16 KB a wave, or 256 KB a workgroup, stays in registers; longer ones are walked in batches.
-template <int T_, int C_>
+template <int T_, int C_, int S_ = 0>
 struct Plan {
-    static constexpr int T = T_, C = C_;
+    static constexpr int T = T_, C = C_, S = S_;
 };
 template <class F>
 void by_row(int64_t bytes, F f)
@@ -86,9 +86,9 @@ void by_row(int64_t bytes, F f)
     else if (bytes <= 8 * 64 * 16) f(Plan<64, 8>());
     else if (bytes <= 4 * 256 * 16) f(Plan<256, 4>());
     else if (bytes <= 8 * 256 * 16) f(Plan<256, 8>());
-    else if (bytes <= 16 * 256 * 16) f(Plan<256, 16>());
+    else if (bytes <= 16 * 256 * 16) f(Plan<512, 8>());
     else if (bytes <= 16 * 512 * 16) f(Plan<512, 16>());
-    else f(Plan<1024, 16>());
+    else f(Plan<512, 16, 8>());
 }
 // Calls f with a value of the logits' type.
 template <class F>
@@ -124,10 +124,13 @@ extern "C" int dbw_token_logp(const dbw_logits *shape, const void *logits, const
     if (rc != DBW_OK) return rc;
     if (!work || (S.rows > 0 && (!tokens || !logp_out))) return DBW_ERR_NULL;
     if (S.rows == 0) return DBW_OK;
-    const loss::Logp P{tokens, logp_out, lse_out, nullptr};
+    const loss::Logp P{tokens, logp_out, lse_out, nullptr, nullptr};
     by_type(shape->type, [&](auto e) {
         by_length(S.row_bytes, [&](auto p) {
-            hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, (hipStream_t)stream, S.R, P);
+            const dim3 grid = grid_of(S.rows), block(p.T);
+            // L is asked for where a gradient follows
+            if (lse_out) hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, true>), grid, block, 0, (hipStream_t)stream, S.R, P);
+            else hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, false>), grid, block, 0, (hipStream_t)stream, S.R, P);
         });
     });
     DBW_HIP(hipGetLastError());
@@ -167,7 +170,7 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
     hipStream_t s = (hipStream_t)stream;
     if (S.rows > 0) {
         const loss::Distill P{teacher_index, teacher_logits, teacher_lse, weights, 1.f / (float)shape->rows, k, teacher_type, row_loss_out, W.terms};
-        const size_t lds = 4 * ((size_t)3 * k + ((size_t)shape->vocab + 31) / 32);
+        const size_t lds = 4 * ((size_t)3 * k + ((size_t)shape->vocab + 8 + 31) / 32);
         bool fits = true;
         const auto launch = [&](auto kernel, int threads) {
             // more than 64 KB have to be asked for
@@ -176,8 +179,8 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
         };
         by_type(shape->type, [&](auto e) {
             by_row(S.row_bytes, [&](auto p) {
-                if (teacher_lse) launch(loss::distill_kernel<decltype(e), p.T, p.C, true>, p.T);
-                else launch(loss::distill_kernel<decltype(e), p.T, p.C, false>, p.T);
+                if (teacher_lse) launch(loss::distill_kernel<decltype(e), p.T, p.C, p.S, true>, p.T);
+                else launch(loss::distill_kernel<decltype(e), p.T, p.C, p.S, false>, p.T);
             });
         });
         if (!fits) return DBW_ERR_HIP;
@@ -207,7 +210,7 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
         const loss::Logp P{tokens, logp, nullptr, W.stats, weights};
         by_type(shape->type, [&](auto e) {
             by_length(S.row_bytes, [&](auto p) {
-                hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
+                hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, true>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
             });
         });
         DBW_HIP(hipGetLastError());
@@ -249,7 +252,7 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
                              1.f / (float)shape->rows, logp_out, W.terms};
         by_type(shape->type, [&](auto e) {
             by_row(S.row_bytes, [&](auto p) {
-                hipLaunchKernelGGL((loss::policy_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
+                hipLaunchKernelGGL((loss::policy_kernel<decltype(e), p.T, p.C, p.S>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
             });
         });
         DBW_HIP(hipGetLastError());

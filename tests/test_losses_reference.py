@@ -117,7 +117,7 @@ def _shape(B, **kw):
     (dict(type=-1), "ERR_INVALID"), (dict(ld=4), "ERR_INVALID"), (dict(ld_grad=4), "ERR_INVALID"), (dict(ld=-7), "ERR_INVALID"),
     (dict(scale=0.0), "ERR_INVALID"), (dict(scale=-1.0), "ERR_INVALID"), (dict(scale=math.inf), "ERR_INVALID"),
     (dict(scale=math.nan), "ERR_INVALID"), (dict(workers=1 << 20, rows=1 << 20), "ERR_UNSUPPORTED"),
-    (dict(workers=(1 << 22) + 1), "ERR_UNSUPPORTED"), (dict(ld=1 << 62), "ERR_UNSUPPORTED")])
+    (dict(workers=(1 << 22) + 1), "ERR_UNSUPPORTED"), (dict(ld=1 << 62), "ERR_UNSUPPORTED"), (dict(vocab=(1 << 28) + 1), "ERR_UNSUPPORTED")])
 def test_shapes_that_are_refused(B, kw, code):
     shape = _shape(B, **kw)
     want = getattr(B, code)
