@@ -279,7 +279,7 @@ def dbw_calibrate(what: int, size: int, repeats: int = 10) -> float:
 
 _TYPE_OF = {torch.float32: TYPE_F32, torch.bfloat16: TYPE_BF16, torch.float16: TYPE_F16}
 _DTYPE_OF = {number: dtype for dtype, number in _TYPE_OF.items()}
-_F32, _I32 = torch.float32, torch.int32
+_F32, _I32, _U8 = torch.float32, torch.int32, torch.uint8
 
 
 def make_logits(workers: int, rows: int, vocab: int, type: int, ld: int = 0, ld_grad: int = 0, scale: float = 1.0) -> dbw_logits:
@@ -291,21 +291,27 @@ def _arr(t, dtype, numel):
     """Device pointer of a contiguous tensor (or None) of this type and at least this many elements."""
     if t is None:
         return None
-    if t.dtype is not dtype or t.numel() < numel:
-        raise ValueError(f"need at least {numel} elements of {dtype}, got {t.numel()} of {t.dtype}")
-    return _ptr(t)
+    if t.dtype is dtype and t.numel() >= numel and t.is_cuda and t.is_contiguous():
+        return t.data_ptr()
+    raise ValueError(f"need a contiguous tensor on the GPU of at least {numel} elements of {dtype}, got {tuple(t.shape)} of {t.dtype} on {t.device}")
 
 
-def _matrix(shape, t, ld):
-    """Device pointer of all workers' rows in a contiguous tensor (or None)."""
-    if t is None:
-        return None
-    rows = shape.workers * shape.rows
-    return _arr(t, _DTYPE_OF.get(shape.type), (rows - 1) * (ld or shape.vocab) + shape.vocab if rows > 0 else 0)
+# What dbw_loss_work_bytes gives, without a call into the library: a tenth of a short call's time in the host.
+_WORK_FIXED, _WORK_PER_ROW = 5120, 16
 
 
-def _work(shape, work):
-    return _arr(work, torch.uint8, dbw_loss_work_bytes(shape))
+def _current():
+    """The current stream where tensors on the GPU are at hand, so that torch has been initialised."""
+    return _raw_stream(_device()) if _raw_stream is not None and _device is not None else _stream()
+
+
+def _rows(shape):
+    """Number of all workers' rows, the logits' dtype, the elements that logits and their gradient have at least, scratch bytes."""
+    n, v, ld = shape.workers * shape.rows, shape.vocab, shape.ld
+    if n <= 0:
+        return n, _DTYPE_OF.get(shape.type), 0, 0, _WORK_FIXED
+    return (n, _DTYPE_OF.get(shape.type), (n - 1) * (ld or v) + v, (n - 1) * (shape.ld_grad or ld or v) + v,
+            _WORK_FIXED + _WORK_PER_ROW * n)
 
 
 def dbw_loss_work_bytes(shape: dbw_logits) -> int:
@@ -313,48 +319,49 @@ def dbw_loss_work_bytes(shape: dbw_logits) -> int:
 
 
 def dbw_token_logp(shape, logits, tokens, logp_out, work, lse_out=None, status_out=None):
-    n = shape.workers * shape.rows
-    return _chk(_lib.dbw_token_logp(C.byref(shape), _matrix(shape, logits, shape.ld), _arr(tokens, _I32, n),
+    n, dtype, size, size_grad, scratch = _rows(shape)
+    return _chk(_lib.dbw_token_logp(C.byref(shape), _arr(logits, dtype, size), _arr(tokens, _I32, n),
                                     _arr(logp_out, _F32, n), _arr(lse_out, _F32, n), _arr(status_out, _I32, 1),
-                                    _work(shape, work), _stream()), "dbw_token_logp")
+                                    _arr(work, _U8, scratch), _current()), "dbw_token_logp")
 
 
 def dbw_token_logp_grad(shape, logits, tokens, lse, coef, dlogits, status_out=None):
-    n = shape.workers * shape.rows
-    return _chk(_lib.dbw_token_logp_grad(C.byref(shape), _matrix(shape, logits, shape.ld), _arr(tokens, _I32, n),
+    n, dtype, size, size_grad, scratch = _rows(shape)
+    return _chk(_lib.dbw_token_logp_grad(C.byref(shape), _arr(logits, dtype, size), _arr(tokens, _I32, n),
                                          _arr(lse, _F32, n), _arr(coef, _F32, n),
-                                         _matrix(shape, dlogits, shape.ld_grad or shape.ld), _arr(status_out, _I32, 1),
-                                         _stream()), "dbw_token_logp_grad")
+                                         _arr(dlogits, dtype, size_grad), _arr(status_out, _I32, 1),
+                                         _current()), "dbw_token_logp_grad")
 
 
 def dbw_distill_loss(shape, k: int, logits, teacher_index, teacher_logits, weights, loss_out, work, teacher_lse=None,
                      row_loss_out=None, dlogits=None, status_out=None):
-    n = shape.workers * shape.rows
+    n, dtype, size, size_grad, scratch = _rows(shape)
     teacher_type = _TYPE_OF.get(teacher_logits.dtype, -1)
-    return _chk(_lib.dbw_distill_loss(C.byref(shape), int(k), _matrix(shape, logits, shape.ld), _arr(teacher_index, _I32, n * k),
+    return _chk(_lib.dbw_distill_loss(C.byref(shape), int(k), _arr(logits, dtype, size), _arr(teacher_index, _I32, n * k),
                                       teacher_type, _arr(teacher_logits, teacher_logits.dtype, n * k), _arr(teacher_lse, _F32, n),
                                       _arr(weights, _F32, n), _arr(loss_out, _F32, shape.workers), _arr(row_loss_out, _F32, n),
-                                      _matrix(shape, dlogits, shape.ld_grad or shape.ld), _arr(status_out, _I32, 1),
-                                      _work(shape, work), _stream()), "dbw_distill_loss")
+                                      _arr(dlogits, dtype, size_grad), _arr(status_out, _I32, 1),
+                                      _arr(work, _U8, scratch), _current()), "dbw_distill_loss")
 
 
 def dbw_preference_loss(shape, pairs: int, logits, tokens, seq_start, ref_logp, weights, beta: float, smoothing: float, loss_out, work,
                         margin_out, logp_out=None, dlogits=None, status_out=None):
-    n, p = shape.workers * shape.rows, shape.workers * pairs
-    return _chk(_lib.dbw_preference_loss(C.byref(shape), int(pairs), _matrix(shape, logits, shape.ld), _arr(tokens, _I32, n),
+    n, dtype, size, size_grad, scratch = _rows(shape)
+    p = shape.workers * pairs
+    return _chk(_lib.dbw_preference_loss(C.byref(shape), int(pairs), _arr(logits, dtype, size), _arr(tokens, _I32, n),
                                          _arr(seq_start, _I32, 2 * p + 1), _arr(ref_logp, _F32, n), _arr(weights, _F32, n),
                                          float(beta), float(smoothing), _arr(loss_out, _F32, shape.workers),
                                          _arr(margin_out, _F32, p), _arr(logp_out, _F32, n),
-                                         _matrix(shape, dlogits, shape.ld_grad or shape.ld), _arr(status_out, _I32, 1),
-                                         _work(shape, work), _stream()), "dbw_preference_loss")
+                                         _arr(dlogits, dtype, size_grad), _arr(status_out, _I32, 1),
+                                         _arr(work, _U8, scratch), _current()), "dbw_preference_loss")
 
 
 def dbw_policy_loss(shape, logits, tokens, old_logp, ref_logp, advantage, weights, clip_low: float, clip_high: float, kl_coef: float,
                     loss_out, work, kl_out=None, logp_out=None, dlogits=None, status_out=None):
-    n = shape.workers * shape.rows
-    return _chk(_lib.dbw_policy_loss(C.byref(shape), _matrix(shape, logits, shape.ld), _arr(tokens, _I32, n), _arr(old_logp, _F32, n),
+    n, dtype, size, size_grad, scratch = _rows(shape)
+    return _chk(_lib.dbw_policy_loss(C.byref(shape), _arr(logits, dtype, size), _arr(tokens, _I32, n), _arr(old_logp, _F32, n),
                                      _arr(ref_logp, _F32, n), _arr(advantage, _F32, n), _arr(weights, _F32, n), float(clip_low),
                                      float(clip_high), float(kl_coef), _arr(loss_out, _F32, shape.workers),
                                      _arr(kl_out, _F32, shape.workers), _arr(logp_out, _F32, n),
-                                     _matrix(shape, dlogits, shape.ld_grad or shape.ld), _arr(status_out, _I32, 1),
-                                     _work(shape, work), _stream()), "dbw_policy_loss")
+                                     _arr(dlogits, dtype, size_grad), _arr(status_out, _I32, 1),
+                                     _arr(work, _U8, scratch), _current()), "dbw_policy_loss")

@@ -1,0 +1,592 @@
+// Kernels of the losses on rows of logits.
+#pragma once
+
+#include "loss_rows.h"
+
+namespace loss {
+
+constexpr int THREADS = 256;              // of workgroups that do not walk along a row
+constexpr int WAVES = THREADS / 64;
+
+// A grid's threads have to number less than 2^32: many workgroups make a second dimension.
+__device__ __forceinline__ int64_t group() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
+
+// Few and long rows are cut into slices, a workgroup each, to fill the chip; what a slice finds goes through memory to a second launch.
+struct Slices {
+    int count;           // of a row; 1: rows are whole
+    int pieces;          // of a slice (the last may have fewer)
+};
+// Slice s = first ... end - 1 of a row's pieces; slice 0 has the single elements, too.
+__device__ __forceinline__ void slice_of(const Slices &S, int s, int pieces, int &first, int &end)
+{
+    first = S.count == 1 ? 0 : s * S.pieces;
+    end = S.count == 1 ? pieces : min(first + S.pieces, pieces);
+}
+// A row's (m, Z) from its slices', on every lane of a wave; and by one thread.
+__device__ __forceinline__ MaxSum joined_by_wave(const MaxSum *slices, int count, float c)
+{
+    const int lane = threadIdx.x & 63;
+    const MaxSum own = lane < count ? slices[lane] : MaxSum{-INFINITY, 0.f};
+    const float m = wave_max(own.m);
+    return MaxSum{m, wave_sum(own.z * rescale(own.m, m, c))};
+}
+__device__ __forceinline__ MaxSum joined_by_thread(const MaxSum *slices, int count, float c)
+{
+    float m = slices[0].m, z = 0.f;
+    for (int s = 1; s < count; ++s) m = fmaxf(m, slices[s].m);
+    for (int s = 0; s < count; ++s) z += slices[s].z * rescale(slices[s].m, m, c);
+    return MaxSum{m, z};
+}
+constexpr int MAX_SLICES = 32;
+
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+
+// ---------------------------------------------------------------- log-probabilities
+
+struct Logp {
+    const int32_t *tokens;
+    const float *weights;// null: no row is left out for its weight
+    float *logp_out, *lse_out;
+    MaxSum *stats;       // (m, Z) of every slice, or null
+    float *token_logit;  // of every row where there are slices
+    Slices slices;
+};
+
+__device__ __forceinline__ bool takes_part(const Logp &P, int64_t r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
+
+// A workgroup a row, or a slice.  AGAIN: the rows will be read again soon, for their gradient.
+template <class E, int T, int C, bool AGAIN>
+__global__ __launch_bounds__(T) void logp_kernel(Rows R, Logp P)
+{
+    __shared__ MaxSum lds[T / 64];
+    const int64_t r = group() / P.slices.count;
+    const int s = (int)(group() % P.slices.count);
+    if (r >= R.rows) return;
+    if (!takes_part(P, r)) {
+        if (threadIdx.x == 0 && P.slices.count == 1) {
+            if (P.logp_out) P.logp_out[r] = 0.f;
+            if (P.lse_out) P.lse_out[r] = 0.f;
+        }
+        return;
+    }
+    const E *x = (const E *)R.x + r * R.ld;
+    const RowOf<E, T> row(x, R.vocab);
+    int first, end;
+    slice_of(P.slices, s, row.pieces, first, end);
+    float m = -INFINITY, z = 0.f;
+    for (; first < end; first += T * C) {
+        u32x4 v[C];
+        row.template load<C, !AGAIN>(first, v);
+        add_pieces<false>(row, first, end, v, -INFINITY, nullptr, R.c, m, z);
+    }
+    z = wave_sum(z);
+    if (s == 0) {
+        const float single = row.load_single(), top = wave_max(single);
+        const MaxSum both = merged(MaxSum{m, z}, MaxSum{top, wave_sum(power(single, base_of(top, R.c)))}, R.c);
+        m = both.m;
+        z = both.z;
+    }
+    const float xy = widen(x[column(R, P.tokens[r])]);
+    const MaxSum mz = row_merge<T>(MaxSum{m, z}, R.c, lds);
+    if (threadIdx.x != 0) return;
+    if (P.slices.count > 1) {
+        P.stats[r * P.slices.count + s] = mz;
+        if (s == 0) P.token_logit[r] = xy;
+        return;
+    }
+    if (P.logp_out) P.logp_out[r] = LN2 * log2_p(xy, R.c, mz);
+    if (P.lse_out) P.lse_out[r] = fmaf(R.scale, mz.m, LN2 * log2f(mz.z));
+    if (P.stats) P.stats[r] = mz;
+}
+
+// A wave a row: its log-probability from its slices.
+__global__ __launch_bounds__(64) void join_kernel(Rows R, Logp P)
+{
+    const int64_t r = blockIdx.x;
+    float logp = 0.f, lse = 0.f;
+    if (takes_part(P, r)) {
+        const MaxSum mz = joined_by_wave(P.stats + r * P.slices.count, P.slices.count, R.c);
+        logp = LN2 * log2_p(P.token_logit[r], R.c, mz);
+        lse = fmaf(R.scale, mz.m, LN2 * log2f(mz.z));
+    }
+    if (threadIdx.x != 0) return;
+    if (P.logp_out) P.logp_out[r] = logp;
+    if (P.lse_out) P.lse_out[r] = lse;
+}
+
+// dx_v = by 2^(c x - M) over pieces first ... end - 1, T C at a time, and coef more at column y if that is among them.
+template <class E, int T, int C>
+__device__ __forceinline__ void slice_gradient(const Rows &R, const RowOf<E, T> &row, int64_t r, int first, int end, float by, Base b, int y,
+                                               float coef)
+{
+    E *dx = (E *)R.dx + r * R.ld_grad;
+    const bool singles = first == 0;
+    const int yp = row.piece_of(y);
+    const bool mine = tid<T>() == row.owner(y) && (yp < 0 ? singles : yp >= first && yp < end);
+    const float xy = mine ? widen(row.x[y]) : 0.f, single = singles ? row.load_single() : 0.f;
+    b = Base{uniform(b.c), uniform(b.M), false};
+    by = uniform(by);
+    const global_access::bytes out = global_access::uniform_base(dx + row.before);
+    for (; first < end; first += T * C) {
+        u32x4 v[C];
+        row.template load<C, true>(first, v);
+#pragma unroll
+        for (int i = 0; i < C; ++i) store_piece<E, T>(out, first, end, i, v[i], by, b);
+    }
+    if (singles && row.has_single()) dx[row.single_column()] = narrow<E>(by * power(single, b));
+    if (mine) dx[y] = narrow<E>(by * power(xy, b) + coef);
+}
+
+// ---------------------------------------------------------------- pairs of sequences
+
+struct Preference {
+    const int32_t *tokens, *seq_start;
+    const float *ref_logp, *weights;
+    float beta, smoothing, c;
+    int pairs;           // of each worker
+    int64_t all_rows;
+    float *logp, *margin_out, *coef;
+    MaxSum *stats;       // of every slice, and where rows have several
+    MaxSum *joined;      // of every row
+    const float *token_logit;
+    int slices;
+    int32_t *status;
+};
+
+__device__ __forceinline__ bool takes_part(const Preference &P, int r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
+
+// The margin of a pair and the derivative of its worker's loss with respect to every log-probability of its rows.  Rows in no sequence are
+// the first and the last pair's.
+__global__ __launch_bounds__(THREADS) void pair_kernel(Preference P)
+{
+    __shared__ float lds[WAVES];
+    const int64_t j = blockIdx.x;
+    const int t = threadIdx.x, n = (int)P.all_rows;
+    int a[3];
+    for (int i = 0; i < 3; ++i) a[i] = P.seq_start[2 * j + i];
+    if (a[0] < 0 || a[1] < a[0] || a[2] < a[1] || a[2] > n) report(P.status);
+    a[0] = min(max(a[0], 0), n);
+    a[1] = min(max(a[1], a[0]), n);
+    a[2] = min(max(a[2], a[1]), n);
+    const int from = j == 0 ? 0 : a[0], to = j == gridDim.x - 1 ? n : a[2];
+    float h = 0.f;
+    for (int r = from + t; r < to; r += THREADS) {
+        const bool part = takes_part(P, r);
+        float logp = 0.f;
+        if (P.slices == 1) {
+            logp = P.logp[r];
+        } else {
+            if (part) {
+                const MaxSum mz = joined_by_thread(P.stats + (int64_t)r * P.slices, P.slices, P.c);
+                P.joined[r] = mz;
+                logp = LN2 * log2_p(P.token_logit[r], P.c, mz);
+            }
+            P.logp[r] = logp;
+        }
+        if (part && r >= a[0] && r < a[2]) {
+            const float term = (P.weights ? P.weights[r] : 1.f) * (logp - P.ref_logp[r]);
+            h += r < a[1] ? term : -term;
+        }
+    }
+    const float u = P.beta * row_sum<THREADS>(h, lds);
+    if (t == 0) P.margin_out[j] = u;
+    const float e = expf(-fabsf(u));                      // sigma(u) = 1 / (1 + e) or e / (1 + e)
+    const float sig = (u >= 0.f ? 1.f : e) / (1.f + e), sig_not = (u >= 0.f ? e : 1.f) / (1.f + e);
+    const float slope = (u != u ? u : P.smoothing * sig - (1.f - P.smoothing) * sig_not) * P.beta / (float)P.pairs;
+    for (int r = from + t; r < to; r += THREADS)
+        P.coef[r] = takes_part(P, r) && r >= a[0] && r < a[2] ? (r < a[1] ? slope : -slope) * (P.weights ? P.weights[r] : 1.f) : 0.f;
+}
+
+// A worker's mean over its pairs, from their margins.
+struct PairLoss {
+    const float *margin;
+    int workers, pairs;
+    float smoothing;
+    float *loss_out;     // null: not asked for
+};
+template <int T>
+__device__ __forceinline__ void pair_loss(const PairLoss &P, int64_t worker, float *lds)
+{
+    const float *u = P.margin + worker * P.pairs;
+    float l = 0.f;
+    for (int j = threadIdx.x; j < P.pairs; j += T) {
+        const float soft = log1pf(expf(-fabsf(u[j])));
+        // -log sigma(u) = max(-u, 0) + soft, -log sigma(-u) = max(u, 0) + soft
+        l += u[j] != u[j] ? u[j] : soft + (u[j] >= 0.f ? P.smoothing * u[j] : (P.smoothing - 1.f) * u[j]);
+    }
+    l = row_sum<T>(l, lds);
+    if (threadIdx.x == 0) P.loss_out[worker] = P.pairs ? l / (float)P.pairs : 0.f;
+}
+__global__ __launch_bounds__(THREADS) void pair_loss_kernel(PairLoss P)
+{
+    __shared__ float lds[WAVES];
+    pair_loss<THREADS>(P, blockIdx.x, lds);
+}
+
+// ---------------------------------------------------------------- a gradient alone
+
+struct Gradient {
+    const int32_t *tokens;
+    const float *coef;   // null: none
+    const MaxSum *stats; // (m, Z) of every row, or null and
+    const float *lse;    // L
+    Slices slices;
+    PairLoss pairs;      // workgroups behind the rows' give every worker's loss
+};
+
+template <class E, int T, int C>
+__global__ __launch_bounds__(T) void gradient_kernel(Rows R, Gradient P)
+{
+    __shared__ float lds[T / 64];
+    const int64_t r = group() / P.slices.count;
+    const int s = (int)(group() % P.slices.count);
+    if (r >= R.rows) {
+        const int64_t worker = group() - R.rows * P.slices.count;
+        if (P.pairs.loss_out && worker < P.pairs.workers) pair_loss<T>(P.pairs, worker, lds);
+        return;
+    }
+    const int token = P.tokens[r];
+    const float g = token < 0 || !P.coef ? 0.f : R.scale * P.coef[r];
+    const RowOf<E, T> row((const E *)R.x + r * R.ld, R.vocab);
+    if (g == 0.f) {
+        // (the pieces of the gradient's row may be one more than those of the logits')
+        zero_pieces<E, T, true>(R, r, s * P.slices.pieces, s == P.slices.count - 1 ? INT32_MAX : (s + 1) * P.slices.pieces);
+        return;
+    }
+    float by = -g;
+    Base b;
+    if (P.stats) {
+        const MaxSum mz = P.stats[r];
+        b = base_of(mz.m, R.c);
+        by /= mz.z;
+    } else {                                              // from L: M = L log2(e), Z = 1
+        b = base_of(P.lse[r] / R.scale, R.c);
+        if (!b.steep) b.M = P.lse[r] * LOG2E;
+    }
+    int first, end;
+    slice_of(P.slices, s, row.pieces, first, end);
+    slice_gradient<E, T, C>(R, row, r, first, end, by, b, column(R, token), g);
+}
+
+// ---------------------------------------------------------------- policy
+
+struct Policy {
+    const int32_t *tokens;
+    const float *old_logp, *ref_logp, *advantage, *weights;
+    float low, high, kl_coef, weight;     // the bounds of the ratio; the weight of every row where weights is null
+    float *logp_out;
+    float2 *terms;       // a row's weighted loss and KL term, for the sums over a worker's rows
+    // where rows are cut
+    const MaxSum *stats;
+    const float *token_logit;
+    Slices slices;
+    int rows;            // of each worker
+    float *loss_out, *kl_out;
+};
+
+// What a row adds to its worker's sums, and the derivative with respect to its log-probability.
+struct PolicyRow {
+    float loss, kl, slope;
+};
+__device__ __forceinline__ PolicyRow policy_of(const Policy &P, int64_t r, float w, float logp)
+{
+    const float a = P.advantage[r], rho = expf(logp - P.old_logp[r]);
+    const float product = rho * a, bounded = fminf(fmaxf(rho, P.low), P.high) * a;
+    const bool free = product <= bounded || product != product;     // (fminf and fmaxf would take a ratio that is NaN for a bound)
+    float kl = 0.f, dkl = 0.f;
+    if (P.ref_logp) {
+        const float d = P.ref_logp[r] - logp;
+        dkl = -expm1f(d);
+        kl = -dkl - d;
+    }
+    return PolicyRow{w * (P.kl_coef * kl - (free ? product : bounded)), w * kl, w * (P.kl_coef * dkl - (free ? product : 0.f))};
+}
+__device__ __forceinline__ float weight_of(const Policy &P, int64_t r)
+{
+    return P.tokens[r] < 0 ? 0.f : P.weights ? P.weights[r] : P.weight;
+}
+
+// A row's terms and its gradient, by T threads.
+template <class E, int T, int C, int S>
+__device__ __forceinline__ float2 policy_whole_row(const Rows &R, const Policy &P, int64_t r, MaxSum *lds)
+{
+    const float w = weight_of(P, r);
+    if (w == 0.f) {
+        if (tid<T>() == 0 && P.logp_out) P.logp_out[r] = 0.f;
+        zero_row<E, T>(R, r);
+        return make_float2(0.f, 0.f);
+    }
+    const E *x = (const E *)R.x + r * R.ld;
+    Walk<E, T, C, S> walk(x, R.vocab);
+    const int y = column(R, P.tokens[r]);
+    const float xy = widen(x[y]);
+    const MaxSum mz = walk.stats(R.c, lds);
+    const float logp = LN2 * log2_p(xy, R.c, mz);
+    const PolicyRow p = policy_of(P, r, w, logp);
+    if (tid<T>() == 0 && P.logp_out) P.logp_out[r] = logp;
+    if (R.dx) {
+        const float coef = R.scale * p.slope;
+        if (coef == 0.f) zero_row<E, T>(R, r);
+        else walk.gradient((E *)R.dx + r * R.ld_grad, -coef / mz.z, base_of(mz.m, R.c), y, xy, coef);
+    }
+    return make_float2(p.loss, p.kl);
+}
+
+template <class E, int T, int C, int S>
+__global__ __launch_bounds__(T, C == 16 ? 4 : 1) void policy_kernel(Rows R, Policy P)
+{
+    __shared__ MaxSum lds[T / 64];
+    const int64_t r = group();
+    if (r >= R.rows) return;
+    const float2 terms = policy_whole_row<E, T, C, S>(R, P, r, lds);
+    if (threadIdx.x == 0) P.terms[r] = terms;
+}
+
+// Sums over a workgroup's waves, in their order.
+__device__ __forceinline__ void store_sums(float a, float b, float2 *lds, float *first_out, float *second_out)
+{
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    a = b = 0.f;
+    for (unsigned w = 0; w < blockDim.x / 64; ++w) {
+        a += lds[w].x;
+        b += lds[w].y;
+    }
+    *first_out = a;
+    if (second_out) *second_out = b;
+}
+
+// All of a worker's rows in one workgroup, a wave each in turn, and their sums: one launch.
+template <class E, int C>
+__global__ __launch_bounds__(1024) void policy_worker_kernel(Rows R, Policy P)
+{
+    __shared__ float2 lds[16];
+    float a = 0.f, b = 0.f;
+    for (int t = wave_id(); t < P.rows; t += blockDim.x >> 6) {
+        const float2 terms = policy_whole_row<E, 64, C, 0>(R, P, (int64_t)blockIdx.x * P.rows + t, nullptr);
+        a += terms.x;
+        b += terms.y;
+    }
+    store_sums(a, b, lds, P.loss_out + blockIdx.x, P.kl_out ? P.kl_out + blockIdx.x : nullptr);
+}
+
+// The second launch for rows in slices: the slices' gradients, and behind them a workgroup for every worker's sums.
+template <class E, int T, int C>
+__global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
+{
+    __shared__ float2 lds[T / 64];
+    const int64_t b = blockIdx.x, cut = R.dx ? R.rows * P.slices.count : 0;
+    const int n = P.slices.count;
+    if (b >= cut) {
+        const int64_t worker = b - cut;
+        float loss = 0.f, kl = 0.f;
+        for (int t = threadIdx.x; t < P.rows; t += T) {
+            const int64_t r = worker * P.rows + t;
+            const float w = weight_of(P, r);
+            float logp = 0.f;
+            if (w != 0.f) {
+                logp = LN2 * log2_p(P.token_logit[r], R.c, joined_by_thread(P.stats + r * n, n, R.c));
+                const PolicyRow p = policy_of(P, r, w, logp);
+                loss += p.loss;
+                kl += p.kl;
+            }
+            if (P.logp_out) P.logp_out[r] = logp;
+        }
+        store_sums(wave_sum(loss), wave_sum(kl), lds, P.loss_out + worker, P.kl_out ? P.kl_out + worker : nullptr);
+        return;
+    }
+    const int64_t r = b / n;
+    const int s = (int)(b % n);
+    const float w = weight_of(P, r);
+    float coef = 0.f;
+    MaxSum mz;
+    if (w != 0.f) {
+        mz = joined_by_wave(P.stats + r * n, n, R.c);
+        coef = R.scale * policy_of(P, r, w, LN2 * log2_p(P.token_logit[r], R.c, mz)).slope;
+    }
+    if (coef == 0.f) {
+        zero_pieces<E, T>(R, r, s * P.slices.pieces, s == n - 1 ? INT32_MAX : (s + 1) * P.slices.pieces);
+        return;
+    }
+    const RowOf<E, T> row((const E *)R.x + r * R.ld, R.vocab);
+    int first, end;
+    slice_of(P.slices, s, row.pieces, first, end);
+    slice_gradient<E, T, C>(R, row, r, first, end, -coef / mz.z, base_of(mz.m, R.c), column(R, P.tokens[r]), coef);
+}
+
+// ---------------------------------------------------------------- distillation
+
+struct Distill {
+    const int32_t *index;
+    const void *value;
+    const float *teacher_lse, *weights;
+    float weight;
+    int k, value_type;
+    float *row_loss_out;
+    float2 *terms;
+    int rows;            // of each worker
+    float *loss_out;
+};
+
+// LDS words of a row: the teacher's columns (-1 where absent), its scaled logits, the student's logits, and a bit for every column of the
+// vocabulary that is in the list, which begin with Piece::N - row.before <= 8 unused ones.
+__host__ __device__ __forceinline__ int distill_words(int k, int vocab) { return 3 * k + (vocab + 8 + 31) / 32; }
+
+// A row's weighted loss, and its gradient, by T threads.
+template <class E, int T, int C, int S, bool TAIL>
+__device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill &P, int64_t r, uint32_t *shared, MaxSum *lds, MaxSum *lds_top,
+                                                   float (*sums)[T / 64])
+{
+    const int t = tid<T>();
+    const float w = P.weights ? P.weights[r] : P.weight;
+    if (w == 0.f) {
+        if (t == 0 && P.row_loss_out) P.row_loss_out[r] = 0.f;
+        zero_row<E, T>(R, r);
+        return 0.f;
+    }
+    const E *x = (const E *)R.x + r * R.ld;
+    Walk<E, T, C, S> walk(x, R.vocab);                    // in flight while the list is looked at
+
+    int *const at = (int *)shared;
+    float *const q = (float *)(shared + P.k);
+    float *const xs = (float *)(shared + 2 * P.k);
+    uint32_t *const in_top = shared + 3 * P.k;
+    const int bit0 = Piece<E>::N - walk.row.before;
+    for (int i = t; i < distill_words(P.k, R.vocab) - 3 * P.k; i += T) in_top[i] = 0;
+    row_barrier<T>();
+    float seen = 0.f, top = -INFINITY, m_top = -INFINITY;           // seen: 1 an entry, 2 a column twice
+    for (int j = t; j < P.k; j += T) {
+        int v = P.index[r * P.k + j];
+        if (v >= R.vocab) {
+            report(R.status);
+            v = -1;
+        }
+        at[j] = v;
+        q[j] = R.scale * load_as(P.value, r * P.k + j, P.value_type);
+        if (v >= 0) {
+            xs[j] = widen(x[v]);
+            const bool again = atomicOr(&in_top[(v + bit0) >> 5], 1u << ((v + bit0) & 31)) >> ((v + bit0) & 31) & 1;
+            seen = fmaxf(seen, again ? 2.f : 1.f);
+        }
+    }
+    row_barrier<T>();
+    seen = row_max<T>(seen, sums[0]);
+    if (seen == 2.f) {                                    // rare: the first entry of a column counts
+        if (t == 0) {
+            report(R.status);
+            for (int j = 1; j < P.k; ++j)
+                for (int i = 0; i < j; ++i)
+                    if (at[i] == at[j]) at[j] = -1;
+        }
+        row_barrier<T>();
+    }
+    for (int j = t; j < P.k; j += T)
+        if (at[j] >= 0) {
+            top = fmaxf(top, q[j]);
+            m_top = fmaxf(m_top, xs[j]);
+        }
+    top = row_max<T>(top, sums[1]);
+    m_top = wave_max(m_top);
+    const Base base_top = base_of(m_top, R.c);
+    float sum = 0.f, z_top = 0.f;
+    for (int j = t; j < P.k; j += T)
+        if (at[j] >= 0) {
+            sum += expf(q[j] - (top == -INFINITY ? 0.f : top));
+            z_top += power(xs[j], base_top);
+        }
+    sum = row_sum<T>(sum, sums[2]);
+    const float norm = TAIL ? P.teacher_lse[r] : top + logf(sum);
+    if (seen == 0.f || (!TAIL && top == -INFINITY && sum == 0.f)) {
+        if (t == 0 && P.row_loss_out) P.row_loss_out[r] = 0.f;
+        zero_row<E, T>(R, r);
+        return 0.f;
+    }
+
+    // With the tail the student's mass outside the list is summed apart, from a maximum of its own: it may be far below the rest, and as a
+    // difference from one it would be lost.
+    MaxSum mz;
+    float log_out = 0.f;
+    if (TAIL) {
+        const MaxSum in = row_merge<T>(MaxSum{m_top, wave_sum(z_top)}, R.c, lds_top);
+        const MaxSum out = walk.template stats<true>(R.c, lds, (const uint8_t *)in_top);
+        mz = merged(out, in, R.c);
+        const Base a = base_of(out.m, R.c), b = base_of(mz.m, R.c);
+        log_out = LN2 * ((a.steep || b.steep ? (out.m - mz.m) * R.c : a.M - b.M) + (log2f(out.z) - log2f(mz.z)));
+    } else {
+        mz = walk.stats(R.c, lds);
+    }
+    float part = 0.f, mass = 0.f;
+    for (int j = t; j < P.k; j += T)
+        if (at[j] >= 0) {
+            const float log_q = q[j] - norm, qj = expf(log_q);
+            const float log_p = LN2 * log2_p(xs[j], R.c, mz);
+            mass += qj;
+            if (!(qj <= 0.f)) part += qj * (log_q - log_p);
+            q[j] = expf(log_p) - qj;                      // dl/dx over s
+        }
+    part = row_sum<T>(part, sums[3]);
+    float factor = 1.f;
+    if (TAIL) {
+        mass = row_sum<T>(mass, sums[0]);                 // (its last use lies several barriers back)
+        const float rest = fmaxf(1.f - mass, 0.f);
+        if (rest > 0.f) {
+            part += rest * (logf(rest) - log_out);
+            factor = 1.f - expf(logf(rest) - log_out);
+        }
+    }
+    if (t == 0 && P.row_loss_out) P.row_loss_out[r] = part;
+    if (R.dx) {
+        E *dx = (E *)R.dx + r * R.ld_grad;
+        walk.gradient(dx, R.scale * w * factor / mz.z, base_of(mz.m, R.c), -1, 0.f, 0.f);
+        if (T > 64) __syncthreads();                      // the list's columns are written over
+        for (int j = t; j < P.k; j += T)
+            if (at[j] >= 0) dx[at[j]] = narrow<E>(R.scale * w * q[j]);
+    }
+    return w * part;
+}
+
+template <class E, int T, int C, int S, bool TAIL>
+__global__ __launch_bounds__(T, C == 16 ? 4 : 1) void distill_kernel(Rows R, Distill P)
+{
+    extern __shared__ uint32_t shared[];
+    __shared__ MaxSum lds[T / 64], lds_top[T / 64];
+    __shared__ float sums[4][T / 64];
+    const int64_t r = group();
+    if (r >= R.rows) return;
+    const float term = distill_whole_row<E, T, C, S, TAIL>(R, P, r, shared, lds, lds_top, sums);
+    if (threadIdx.x == 0) P.terms[r] = make_float2(term, 0.f);
+}
+
+// All of a worker's rows in one workgroup, a wave each in turn, and their sum.
+template <class E, int C, bool TAIL>
+__global__ __launch_bounds__(1024) void distill_worker_kernel(Rows R, Distill P)
+{
+    extern __shared__ uint32_t shared[];
+    __shared__ float2 lds[16];
+    const int wave = wave_id();
+    float a = 0.f;
+    for (int t = wave; t < P.rows; t += blockDim.x >> 6) {
+        a += distill_whole_row<E, 64, C, 0, TAIL>(R, P, (int64_t)blockIdx.x * P.rows + t, shared + wave * distill_words(P.k, R.vocab), nullptr,
+                                                  nullptr, nullptr);
+        row_barrier<64>();                                // the next row's list takes this one's place
+    }
+    store_sums(a, 0.f, lds, P.loss_out + blockIdx.x, nullptr);
+}
+
+// ---------------------------------------------------------------- sums
+
+// loss_out[i], second_out[i] = sums of the terms of worker i's rows, always in the same order.
+__global__ __launch_bounds__(THREADS) void sum_kernel(const float2 *terms, int rows, float *loss_out, float *second_out)
+{
+    __shared__ float2 lds[WAVES];
+    const float2 *t = terms + (int64_t)blockIdx.x * rows;
+    float a = 0.f, b = 0.f;
+    for (int r = threadIdx.x; r < rows; r += THREADS) {
+        a += t[r].x;
+        b += t[r].y;
+    }
+    store_sums(wave_sum(a), wave_sum(b), lds, loss_out + blockIdx.x, second_out ? second_out + blockIdx.x : nullptr);
+}
+
+}  // namespace loss

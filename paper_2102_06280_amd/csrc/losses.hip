@@ -4,7 +4,7 @@
 
 #include "dbw_internal.h"
 #include "dbw_losses.h"
-#include "loss_rows.h"
+#include "loss_kernels.h"
 
 namespace {
 
@@ -32,18 +32,24 @@ int check_shape(const dbw_logits *l, Shape *out)
     return DBW_OK;
 }
 
-// Scratch memory: per row the maximum and the sum, and two terms of a loss (or its coefficient and its log-probability).
+// Scratch memory: a row's maximum and sum, and the two terms of its loss or its coefficient and its log-probability; what slices of few rows found.
 struct Work {
     loss::MaxSum *stats;
     float2 *terms;
     float *coef, *logp;
+    loss::MaxSum *slices;
+    float *token_logit;
 };
 constexpr int64_t WORK_PER_ROW = 16;
+constexpr int SLICED_ROWS = 256, SLICE_GROUPS = 512;      // rows that may be cut, and workgroups that they are cut for
+constexpr int64_t WORK_FIXED = 8 * SLICE_GROUPS + 4 * SLICED_ROWS;
 
 Work split_work(void *work, int64_t rows)
 {
     Work w;
-    w.stats = (loss::MaxSum *)work;
+    w.slices = (loss::MaxSum *)work;
+    w.token_logit = (float *)(w.slices + SLICE_GROUPS);
+    w.stats = (loss::MaxSum *)(w.token_logit + SLICED_ROWS);
     w.terms = (float2 *)(w.stats + rows);
     w.coef = (float *)w.terms;
     w.logp = w.coef + rows;
@@ -68,17 +74,18 @@ int prepare(const dbw_logits *l, const void *logits, void *dlogits, int32_t *sta
     return DBW_OK;
 }
 
-dim3 grid_of(int64_t rows)
+dim3 grid_of(int64_t groups)
 {
-    const int64_t x = rows < (1 << 20) ? rows : 1 << 20;
-    return dim3((uint32_t)x, (uint32_t)((rows + x - 1) / x));
+    const int64_t x = groups < (1 << 20) ? groups : 1 << 20;
+    return dim3((uint32_t)x, (uint32_t)((groups + x - 1) / x));
 }
 
-// Threads and pieces a thread for rows of that many bytes.  A row of up to 16 KB a wave, or 256 KB a workgroup, stays in registers; longer ones are walked in batches.
+// T threads, C pieces a thread at a time (Walk: and S at a time of what lies behind them)
 template <int T_, int C_, int S_ = 0>
 struct Plan {
     static constexpr int T = T_, C = C_, S = S_;
 };
+// For the kernels that hold a row.
 template <class F>
 void by_row(int64_t bytes, F f)
 {
@@ -86,10 +93,47 @@ void by_row(int64_t bytes, F f)
     else if (bytes <= 8 * 64 * 16) f(Plan<64, 8>());
     else if (bytes <= 4 * 256 * 16) f(Plan<256, 4>());
     else if (bytes <= 8 * 256 * 16) f(Plan<256, 8>());
-    else if (bytes <= 16 * 256 * 16) f(Plan<512, 8>());
+    else if (bytes <= 8 * 512 * 16) f(Plan<512, 8>());
     else if (bytes <= 16 * 512 * 16) f(Plan<512, 16>());
     else f(Plan<512, 16, 8>());
 }
+// For those that only read it, or only write its gradient from what is known of it.
+template <class F>
+void by_length(int64_t bytes, F f)
+{
+    if (bytes <= 8 * 64 * 16) f(Plan<64, 2>());
+    else if (bytes <= 128 << 10) f(Plan<256, 8>());
+    else f(Plan<1024, 8>());
+}
+// Few rows in slices: f of the plan of a slice.
+constexpr int SLICE_LONG = 2048;                          // pieces of a slice from which threads take eight at a time
+template <class F>
+void by_slice(const loss::Slices &slices, F f)
+{
+    if (slices.pieces % SLICE_LONG == 0) f(Plan<256, 8>());
+    else f(Plan<256, 2>());
+}
+loss::Slices slices_of(const dbw_logits *l, int64_t rows)
+{
+    loss::Slices S{1, 0};
+    const int pieces = l->vocab / (16 / (int)size_of(l->type));
+    if (rows < 1 || rows > SLICED_ROWS) return S;
+    int count = SLICE_GROUPS / (int)rows;
+    if (count > loss::MAX_SLICES) count = loss::MAX_SLICES;
+    const int unit = pieces / count >= SLICE_LONG ? SLICE_LONG : 512;
+    const int units = (pieces + unit - 1) / unit;         // of whole plans
+    if (units < 2) return S;
+    S.pieces = (units + count - 1) / count * unit;
+    S.count = (pieces + S.pieces - 1) / S.pieces;
+    return S;
+}
+// All rows of a worker in one workgroup, a wave each: short rows, few enough that one compute unit takes no longer than a launch.
+bool in_one_group(const dbw_logits *l, int64_t row_bytes)
+{
+    return l->rows >= 1 && l->rows <= 64 && row_bytes <= 8 * 64 * 16 && l->rows * row_bytes <= 64 << 10;
+}
+int waves_of(const dbw_logits *l) { return l->rows < 16 ? l->rows : 16; }
+
 // Calls f with a value of the logits' type.
 template <class F>
 void by_type(int type, F f)
@@ -98,13 +142,30 @@ void by_type(int type, F f)
     else if (type == DBW_TYPE_BF16) f(loss::bf16());
     else f(loss::f16());
 }
-// The kernels that only read a row, or only write one from what is known of it, need not hold it.
-template <class F>
-void by_length(int64_t bytes, F f)
+
+// (m, Z) of every row or slice; log-probabilities where rows are whole.  again: the rows will be read again soon.
+void launch_logp(const dbw_logits *l, const Shape &S, const loss::Logp &P, bool again, hipStream_t s)
 {
-    if (bytes <= 8 * 64 * 16) f(Plan<64, 2>());
-    else if (bytes <= 128 << 10) f(Plan<256, 8>());
-    else f(Plan<1024, 8>());
+    by_type(l->type, [&](auto e) {
+        const auto launch = [&](auto p) {
+            const dim3 grid = grid_of(S.rows * P.slices.count), block(p.T);
+            if (again) hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, true>), grid, block, 0, s, S.R, P);
+            else hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, false>), grid, block, 0, s, S.R, P);
+        };
+        if (P.slices.count > 1) by_slice(P.slices, launch);
+        else by_length(S.row_bytes, launch);
+    });
+}
+void launch_gradient(const dbw_logits *l, const Shape &S, const loss::Gradient &P, hipStream_t s)
+{
+    by_type(l->type, [&](auto e) {
+        const auto launch = [&](auto p) {
+            hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>),
+                               grid_of(S.rows * P.slices.count + (P.pairs.loss_out ? P.pairs.workers : 0)), dim3(p.T), 0, s, S.R, P);
+        };
+        if (P.slices.count > 1) by_slice(P.slices, launch);
+        else by_length(S.row_bytes, launch);
+    });
 }
 
 }  // namespace
@@ -113,7 +174,7 @@ extern "C" int64_t dbw_loss_work_bytes(const dbw_logits *shape)
 {
     Shape S;
     const int rc = check_shape(shape, &S);
-    return rc == DBW_OK ? WORK_PER_ROW * (S.rows + 1) : rc;
+    return rc == DBW_OK ? WORK_FIXED + WORK_PER_ROW * S.rows : rc;
 }
 
 extern "C" int dbw_token_logp(const dbw_logits *shape, const void *logits, const int32_t *tokens, float *logp_out, float *lse_out,
@@ -124,15 +185,12 @@ extern "C" int dbw_token_logp(const dbw_logits *shape, const void *logits, const
     if (rc != DBW_OK) return rc;
     if (!work || (S.rows > 0 && (!tokens || !logp_out))) return DBW_ERR_NULL;
     if (S.rows == 0) return DBW_OK;
-    const loss::Logp P{tokens, logp_out, lse_out, nullptr, nullptr};
-    by_type(shape->type, [&](auto e) {
-        by_length(S.row_bytes, [&](auto p) {
-            const dim3 grid = grid_of(S.rows), block(p.T);
-            // L is asked for where a gradient follows
-            if (lse_out) hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, true>), grid, block, 0, (hipStream_t)stream, S.R, P);
-            else hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, false>), grid, block, 0, (hipStream_t)stream, S.R, P);
-        });
-    });
+    const Work W = split_work(work, S.rows);
+    hipStream_t s = (hipStream_t)stream;
+    const loss::Slices slices = slices_of(shape, S.rows);
+    const loss::Logp P{tokens, nullptr, logp_out, lse_out, slices.count > 1 ? W.slices : nullptr, W.token_logit, slices};
+    launch_logp(shape, S, P, lse_out != nullptr, s);      // L is asked for where a gradient follows
+    if (slices.count > 1) hipLaunchKernelGGL(loss::join_kernel, dim3((uint32_t)S.rows), dim3(64), 0, s, S.R, P);
     DBW_HIP(hipGetLastError());
     return DBW_OK;
 }
@@ -145,12 +203,8 @@ extern "C" int dbw_token_logp_grad(const dbw_logits *shape, const void *logits, 
     if (rc != DBW_OK) return rc;
     if (S.rows > 0 && (!tokens || !lse || !coef || !dlogits)) return DBW_ERR_NULL;
     if (S.rows == 0) return DBW_OK;
-    by_type(shape->type, [&](auto e) {
-        by_length(S.row_bytes, [&](auto p) {
-            hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, (hipStream_t)stream, S.R,
-                               tokens, (const loss::MaxSum *)nullptr, lse, coef);
-        });
-    });
+    const loss::Gradient P{tokens, coef, nullptr, lse, slices_of(shape, S.rows), loss::PairLoss{}};
+    launch_gradient(shape, S, P, (hipStream_t)stream);
     DBW_HIP(hipGetLastError());
     return DBW_OK;
 }
@@ -169,22 +223,34 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
     if (S.rows > 0) {
-        const loss::Distill P{teacher_index, teacher_logits, teacher_lse, weights, 1.f / (float)shape->rows, k, teacher_type, row_loss_out, W.terms};
-        const size_t lds = 4 * ((size_t)3 * k + ((size_t)shape->vocab + 8 + 31) / 32);
+        const loss::Distill P{teacher_index, teacher_logits, teacher_lse, weights, 1.f / (float)shape->rows, k, teacher_type, row_loss_out, W.terms,
+                              shape->rows, loss_out};
+        const size_t lds = 4 * (size_t)loss::distill_words(k, shape->vocab);
         bool fits = true;
-        const auto launch = [&](auto kernel, int threads) {
+        const auto launch = [&](auto kernel, dim3 grid, int threads, size_t bytes) {
             // more than 64 KB have to be asked for
-            if (lds > 65536) fits = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds) == hipSuccess;
-            if (fits) hipLaunchKernelGGL(kernel, grid_of(S.rows), dim3((uint32_t)threads), lds, s, S.R, P);
+            if (bytes > 65536) fits = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
+            if (fits) hipLaunchKernelGGL(kernel, grid, dim3((uint32_t)threads), bytes, s, S.R, P);
         };
+        const int waves = waves_of(shape);
+        const bool one_group = in_one_group(shape, S.row_bytes) && waves * lds <= 65536;
         by_type(shape->type, [&](auto e) {
             by_row(S.row_bytes, [&](auto p) {
-                if (teacher_lse) launch(loss::distill_kernel<decltype(e), p.T, p.C, p.S, true>, p.T);
-                else launch(loss::distill_kernel<decltype(e), p.T, p.C, p.S, false>, p.T);
+                typedef decltype(e) E;
+                if constexpr (p.T == 64)
+                    if (one_group) {
+                        const dim3 grid((uint32_t)shape->workers);
+                        if (teacher_lse) launch(loss::distill_worker_kernel<E, p.C, true>, grid, 64 * waves, waves * lds);
+                        else launch(loss::distill_worker_kernel<E, p.C, false>, grid, 64 * waves, waves * lds);
+                        return;
+                    }
+                if (teacher_lse) launch(loss::distill_kernel<E, p.T, p.C, p.S, true>, grid_of(S.rows), p.T, lds);
+                else launch(loss::distill_kernel<E, p.T, p.C, p.S, false>, grid_of(S.rows), p.T, lds);
             });
         });
         if (!fits) return DBW_ERR_HIP;
         DBW_HIP(hipGetLastError());
+        if (one_group) return DBW_OK;
     }
     hipLaunchKernelGGL(loss::sum_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, W.terms, shape->rows, loss_out,
                        (float *)nullptr);
@@ -206,32 +272,25 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
     float *const logp = logp_out ? logp_out : W.logp;
+    loss::Slices slices{1, 0};
     if (S.rows > 0) {
-        const loss::Logp P{tokens, logp, nullptr, W.stats, weights};
-        by_type(shape->type, [&](auto e) {
-            by_length(S.row_bytes, [&](auto p) {
-                hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, true>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
-            });
-        });
+        if (pairs > 0) slices = slices_of(shape, S.rows);  // (whose parts the pairs' kernel joins)
+        const bool cut = slices.count > 1;
+        launch_logp(shape, S, loss::Logp{tokens, weights, logp, nullptr, cut ? W.slices : W.stats, W.token_logit, slices}, dlogits != nullptr, s);
         DBW_HIP(hipGetLastError());
     }
     if (pairs > 0) {
-        const loss::Preference P{tokens, seq_start, logp, ref_logp, weights, beta, smoothing, pairs, S.rows, margin_out, W.coef, status_out};
+        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.c, pairs, S.rows, logp, margin_out, W.coef,
+                                 W.slices, W.stats, W.token_logit, slices.count, status_out};
         hipLaunchKernelGGL(loss::pair_kernel, dim3((uint32_t)(shape->workers * pairs)), dim3(loss::THREADS), 0, s, P);
         DBW_HIP(hipGetLastError());
     }
-    hipLaunchKernelGGL(loss::pair_loss_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, margin_out, pairs, smoothing,
-                       loss_out);
+    const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
+    if (dlogits && S.rows > 0)
+        launch_gradient(shape, S, loss::Gradient{tokens, pairs > 0 ? W.coef : nullptr, W.stats, nullptr, slices, mean}, s);
+    else
+        hipLaunchKernelGGL(loss::pair_loss_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, mean);
     DBW_HIP(hipGetLastError());
-    if (dlogits && S.rows > 0) {
-        by_type(shape->type, [&](auto e) {
-            by_length(S.row_bytes, [&](auto p) {
-                hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>), grid_of(S.rows), dim3(p.T), 0, s, S.R, tokens,
-                                   (const loss::MaxSum *)W.stats, (const float *)nullptr, (const float *)(pairs > 0 ? W.coef : nullptr));
-            });
-        });
-        DBW_HIP(hipGetLastError());
-    }
     return DBW_OK;
 }
 
@@ -248,14 +307,31 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
     if (S.rows > 0) {
+        const loss::Slices slices = slices_of(shape, S.rows);
+        const bool cut = slices.count > 1, one_group = in_one_group(shape, S.row_bytes);
         const loss::Policy P{tokens, old_logp, ref_logp, advantage, weights, 1.f - clip_low, 1.f + clip_high, kl_coef,
-                             1.f / (float)shape->rows, logp_out, W.terms};
+                             1.f / (float)shape->rows, logp_out, W.terms, W.slices, W.token_logit, slices, shape->rows, loss_out, kl_out};
+        if (cut) launch_logp(shape, S, loss::Logp{tokens, weights, nullptr, nullptr, W.slices, W.token_logit, slices}, dlogits != nullptr, s);
         by_type(shape->type, [&](auto e) {
-            by_row(S.row_bytes, [&](auto p) {
-                hipLaunchKernelGGL((loss::policy_kernel<decltype(e), p.T, p.C, p.S>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
-            });
+            typedef decltype(e) E;
+            if (cut)
+                by_slice(slices, [&](auto p) {
+                    const int64_t groups = (dlogits ? S.rows * slices.count : 0) + shape->workers;
+                    hipLaunchKernelGGL((loss::policy_slices_kernel<E, p.T, p.C>), dim3((uint32_t)groups), dim3(p.T), 0, s, S.R, P);
+                });
+            else
+                by_row(S.row_bytes, [&](auto p) {
+                    if constexpr (p.T == 64)
+                        if (one_group) {
+                            hipLaunchKernelGGL((loss::policy_worker_kernel<E, p.C>), dim3((uint32_t)shape->workers), dim3(64 * waves_of(shape)), 0,
+                                               s, S.R, P);
+                            return;
+                        }
+                    hipLaunchKernelGGL((loss::policy_kernel<E, p.T, p.C, p.S>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
+                });
         });
         DBW_HIP(hipGetLastError());
+        if (cut || one_group) return DBW_OK;
     }
     hipLaunchKernelGGL(loss::sum_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, W.terms, shape->rows, loss_out, kl_out);
     DBW_HIP(hipGetLastError());

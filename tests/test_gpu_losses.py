@@ -89,7 +89,8 @@ def close(got, want, bound, what=""):
 VOCABS = [1, 2, 7, 64, 65, 259, 1000, 4099, 8192, 33001]
 SHAPES = [(F32, 3, 5, 257, 0, 0), (BF16, 2, 7, 1000, 0, 0), (F16, 1, 3, 4097, 3, 1), (F32, 2, 2, 33001, 1, 3), (BF16, 1, 4, 50000, 8, 0),
           (BF16, 3, 3, 20011, 5, 7), (F16, 2, 2, 65536, 0, 0), (BF16, 1, 2, 131072, 0, 0), (F32, 1, 2, 131073, 2, 1),
-          (BF16, 1, 2, 300001, 0, 3), (F16, 40, 9, 130, 2, 1), (BF16, 1, 1, 9, 0, 0), (F32, 1, 1, 1, 4, 1), (F32, 2, 300, 33, 0, 0)]
+          (BF16, 1, 2, 300001, 0, 3), (BF16, 2, 64, 512, 0, 0), (F32, 1, 65, 129, 1, 0), (BF16, 1, 17, 4097, 0, 1), (F32, 3, 31, 2049, 0, 0),
+          (F16, 1, 256, 8200, 1, 0), (BF16, 257, 1, 8200, 0, 1), (F32, 5, 51, 4100, 0, 2), (BF16, 1, 1, 131072, 0, 0), (F16, 40, 9, 130, 2, 1), (BF16, 1, 1, 9, 0, 0), (F32, 1, 1, 1, 4, 1), (F32, 2, 300, 33, 0, 0)]
 
 
 # --------------------------------------------------------------------------- log-probabilities

@@ -188,6 +188,12 @@ def test_the_binding_refuses_wrong_tensors(B):
             B.dbw_token_logp(shape, a["x"], a["tokens"], a["out"], a["work"])
 
 
+def test_scratch_memory_as_the_binding_counts_it(B):
+    for n, t in ((1, 0), (1, 1), (3, 7), (16, 4096)):
+        shape = _shape(B, workers=n, rows=t)
+        assert B._rows(shape)[-1] == B.dbw_loss_work_bytes(shape)
+
+
 def test_logits_struct_matches_the_header(B, tmp_path):
     import os
     import subprocess
