@@ -11,6 +11,21 @@ constexpr int WAVES = THREADS / 64;
 // A grid's threads have to number less than 2^32: many workgroups make a second dimension.
 __device__ __forceinline__ int64_t group() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
+__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
+
+// Rows that are a wave's work share a workgroup, or starting workgroups would take longer than the rows.
+template <int T>
+constexpr int ROWS_OF = T == 64 ? 4 : 1;
+template <int T>
+__device__ __forceinline__ int64_t row_of_group(int64_t g) { return ROWS_OF<T> * g + (T == 64 ? wave_id() : 0); }
+
+// Workgroups go to the eight XCDs in turn: this gives each XCD rows that lie together.
+__device__ __forceinline__ int64_t row_by_xcd(int64_t g, int64_t rows)
+{
+    const int64_t each = rows / 8;
+    return g < each * 8 ? g % 8 * each + g / 8 : g;
+}
+
 // Few and long rows are cut into slices, a workgroup each, to fill the chip; what a slice finds goes through memory to a second launch.
 struct Slices {
     int count;           // of a row; 1: rows are whole
@@ -39,8 +54,6 @@ __device__ __forceinline__ MaxSum joined_by_thread(const MaxSum *slices, int cou
 }
 constexpr int MAX_SLICES = 32;
 
-__device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
-
 // ---------------------------------------------------------------- log-probabilities
 
 struct Logp {
@@ -56,14 +69,14 @@ __device__ __forceinline__ bool takes_part(const Logp &P, int64_t r) { return P.
 
 // A workgroup a row, or a slice.  AGAIN: the rows will be read again soon, for their gradient.
 template <class E, int T, int C, bool AGAIN>
-__global__ __launch_bounds__(T) void logp_kernel(Rows R, Logp P)
+__global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
 {
     __shared__ MaxSum lds[T / 64];
-    const int64_t r = group() / P.slices.count;
-    const int s = (int)(group() % P.slices.count);
+    const int64_t r = T == 64 ? row_of_group<T>(group()) : group() / P.slices.count;
+    const int s = T == 64 ? 0 : (int)(group() % P.slices.count);
     if (r >= R.rows) return;
     if (!takes_part(P, r)) {
-        if (threadIdx.x == 0 && P.slices.count == 1) {
+        if (tid<T>() == 0 && P.slices.count == 1) {
             if (P.logp_out) P.logp_out[r] = 0.f;
             if (P.lse_out) P.lse_out[r] = 0.f;
         }
@@ -88,7 +101,7 @@ __global__ __launch_bounds__(T) void logp_kernel(Rows R, Logp P)
     }
     const float xy = widen(x[column(R, P.tokens[r])]);
     const MaxSum mz = row_merge<T>(MaxSum{m, z}, R.c, lds);
-    if (threadIdx.x != 0) return;
+    if (tid<T>() != 0) return;
     if (P.slices.count > 1) {
         P.stats[r * P.slices.count + s] = mz;
         if (s == 0) P.token_logit[r] = xy;
@@ -235,16 +248,18 @@ struct Gradient {
 };
 
 template <class E, int T, int C>
-__global__ __launch_bounds__(T) void gradient_kernel(Rows R, Gradient P)
+__global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradient P)
 {
-    __shared__ float lds[T / 64];
-    const int64_t r = group() / P.slices.count;
-    const int s = (int)(group() % P.slices.count);
-    if (r >= R.rows) {
-        const int64_t worker = group() - R.rows * P.slices.count;
-        if (P.pairs.loss_out && worker < P.pairs.workers) pair_loss<T>(P.pairs, worker, lds);
+    __shared__ float lds[T * ROWS_OF<T> / 64];
+    const int64_t groups = T == 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
+    if (group() >= groups) {
+        const int64_t worker = group() - groups;
+        if (P.pairs.loss_out && worker < P.pairs.workers) pair_loss<T * ROWS_OF<T>>(P.pairs, worker, lds);
         return;
     }
+    const int64_t r = T == 64 ? row_of_group<T>(group()) : group() / P.slices.count;
+    const int s = T == 64 ? 0 : (int)(group() % P.slices.count);
+    if (r >= R.rows) return;
     const int token = P.tokens[r];
     const float g = token < 0 || !P.coef ? 0.f : R.scale * P.coef[r];
     const RowOf<E, T> row((const E *)R.x + r * R.ld, R.vocab);
@@ -284,18 +299,26 @@ struct Policy {
     float *loss_out, *kl_out;
 };
 
+// A row's figures besides its logits, all asked for at once, before the logits.
+struct PolicyFigures {
+    float w, a, old, ref;
+};
+__device__ __forceinline__ PolicyFigures figures_of(const Policy &P, int64_t r, float w)
+{
+    return PolicyFigures{w, P.advantage[r], P.old_logp[r], P.ref_logp ? P.ref_logp[r] : 0.f};
+}
 // What a row adds to its worker's sums, and the derivative with respect to its log-probability.
 struct PolicyRow {
     float loss, kl, slope;
 };
-__device__ __forceinline__ PolicyRow policy_of(const Policy &P, int64_t r, float w, float logp)
+__device__ __forceinline__ PolicyRow policy_of(const Policy &P, const PolicyFigures &F, float logp)
 {
-    const float a = P.advantage[r], rho = expf(logp - P.old_logp[r]);
+    const float w = F.w, a = F.a, rho = expf(logp - F.old);
     const float product = rho * a, bounded = fminf(fmaxf(rho, P.low), P.high) * a;
     const bool free = product <= bounded || product != product;     // (fminf and fmaxf would take a ratio that is NaN for a bound)
     float kl = 0.f, dkl = 0.f;
     if (P.ref_logp) {
-        const float d = P.ref_logp[r] - logp;
+        const float d = F.ref - logp;
         dkl = -expm1f(d);
         kl = -dkl - d;
     }
@@ -318,11 +341,12 @@ __device__ __forceinline__ float2 policy_whole_row(const Rows &R, const Policy &
     }
     const E *x = (const E *)R.x + r * R.ld;
     Walk<E, T, C, S> walk(x, R.vocab);
+    const PolicyFigures figures = figures_of(P, r, w);
     const int y = column(R, P.tokens[r]);
     const float xy = widen(x[y]);
     const MaxSum mz = walk.stats(R.c, lds);
     const float logp = LN2 * log2_p(xy, R.c, mz);
-    const PolicyRow p = policy_of(P, r, w, logp);
+    const PolicyRow p = policy_of(P, figures, logp);
     if (tid<T>() == 0 && P.logp_out) P.logp_out[r] = logp;
     if (R.dx) {
         const float coef = R.scale * p.slope;
@@ -333,13 +357,13 @@ __device__ __forceinline__ float2 policy_whole_row(const Rows &R, const Policy &
 }
 
 template <class E, int T, int C, int S>
-__global__ __launch_bounds__(T, C == 16 ? 4 : 1) void policy_kernel(Rows R, Policy P)
+__global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void policy_kernel(Rows R, Policy P)
 {
     __shared__ MaxSum lds[T / 64];
-    const int64_t r = group();
+    const int64_t r = row_of_group<T>(R.by_xcd ? row_by_xcd(group(), R.rows) : group());
     if (r >= R.rows) return;
     const float2 terms = policy_whole_row<E, T, C, S>(R, P, r, lds);
-    if (threadIdx.x == 0) P.terms[r] = terms;
+    if (tid<T>() == 0) P.terms[r] = terms;
 }
 
 // Sums over a workgroup's waves, in their order.
@@ -387,7 +411,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
             float logp = 0.f;
             if (w != 0.f) {
                 logp = LN2 * log2_p(P.token_logit[r], R.c, joined_by_thread(P.stats + r * n, n, R.c));
-                const PolicyRow p = policy_of(P, r, w, logp);
+                const PolicyRow p = policy_of(P, figures_of(P, r, w), logp);
                 loss += p.loss;
                 kl += p.kl;
             }
@@ -403,7 +427,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
     MaxSum mz;
     if (w != 0.f) {
         mz = joined_by_wave(P.stats + r * n, n, R.c);
-        coef = R.scale * policy_of(P, r, w, LN2 * log2_p(P.token_logit[r], R.c, mz)).slope;
+        coef = R.scale * policy_of(P, figures_of(P, r, w), LN2 * log2_p(P.token_logit[r], R.c, mz)).slope;
     }
     if (coef == 0.f) {
         zero_pieces<E, T>(R, r, s * P.slices.pieces, s == n - 1 ? INT32_MAX : (s + 1) * P.slices.pieces);
@@ -547,15 +571,15 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
 }
 
 template <class E, int T, int C, int S, bool TAIL>
-__global__ __launch_bounds__(T, C == 16 ? 4 : 1) void distill_kernel(Rows R, Distill P)
+__global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void distill_kernel(Rows R, Distill P)
 {
     extern __shared__ uint32_t shared[];
     __shared__ MaxSum lds[T / 64], lds_top[T / 64];
     __shared__ float sums[4][T / 64];
-    const int64_t r = group();
+    const int64_t r = row_of_group<T>(R.by_xcd ? row_by_xcd(group(), R.rows) : group());
     if (r >= R.rows) return;
-    const float term = distill_whole_row<E, T, C, S, TAIL>(R, P, r, shared, lds, lds_top, sums);
-    if (threadIdx.x == 0) P.terms[r] = make_float2(term, 0.f);
+    const float term = distill_whole_row<E, T, C, S, TAIL>(R, P, r, shared + (T == 64 ? wave_id() * distill_words(P.k, R.vocab) : 0), lds, lds_top, sums);
+    if (tid<T>() == 0) P.terms[r] = make_float2(term, 0.f);
 }
 
 // All of a worker's rows in one workgroup, a wave each in turn, and their sum.

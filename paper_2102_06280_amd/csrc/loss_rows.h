@@ -55,6 +55,7 @@ struct Rows {
     int64_t rows;      // of all workers
     float scale, c;    // s, s log2(e)
     int32_t *status;
+    bool by_xcd;       // workgroups take rows in the XCDs' order
 };
 
 __device__ __forceinline__ void report(int32_t *status)

@@ -70,7 +70,7 @@ int prepare(const dbw_logits *l, const void *logits, void *dlogits, int32_t *sta
         if (a < b + nb && b < a + na) return DBW_ERR_ALIAS;
     }
     S->row_bytes = (int64_t)e * l->vocab;
-    S->R = loss::Rows{logits, dlogits, S->ld, S->ld_grad, l->vocab, S->rows, l->scale, l->scale * loss::LOG2E, status};
+    S->R = loss::Rows{logits, dlogits, S->ld, S->ld_grad, l->vocab, S->rows, l->scale, l->scale * loss::LOG2E, status, S->row_bytes >= 65536};
     return DBW_OK;
 }
 
@@ -84,6 +84,8 @@ dim3 grid_of(int64_t groups)
 template <int T_, int C_, int S_ = 0>
 struct Plan {
     static constexpr int T = T_, C = C_, S = S_;
+    static constexpr int ROWS = loss::ROWS_OF<T>, THREADS = T * ROWS;      // of a workgroup
+    static dim3 grid(int64_t rows) { return grid_of((rows + ROWS - 1) / ROWS); }
 };
 // For the kernels that hold a row.
 template <class F>
@@ -148,7 +150,7 @@ void launch_logp(const dbw_logits *l, const Shape &S, const loss::Logp &P, bool 
 {
     by_type(l->type, [&](auto e) {
         const auto launch = [&](auto p) {
-            const dim3 grid = grid_of(S.rows * P.slices.count), block(p.T);
+            const dim3 grid = p.grid(S.rows * P.slices.count), block(p.THREADS);
             if (again) hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, true>), grid, block, 0, s, S.R, P);
             else hipLaunchKernelGGL((loss::logp_kernel<decltype(e), p.T, p.C, false>), grid, block, 0, s, S.R, P);
         };
@@ -161,7 +163,8 @@ void launch_gradient(const dbw_logits *l, const Shape &S, const loss::Gradient &
     by_type(l->type, [&](auto e) {
         const auto launch = [&](auto p) {
             hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>),
-                               grid_of(S.rows * P.slices.count + (P.pairs.loss_out ? P.pairs.workers : 0)), dim3(p.T), 0, s, S.R, P);
+                               grid_of((S.rows * P.slices.count + p.ROWS - 1) / p.ROWS + (P.pairs.loss_out ? P.pairs.workers : 0)), dim3(p.THREADS),
+                               0, s, S.R, P);
         };
         if (P.slices.count > 1) by_slice(P.slices, launch);
         else by_length(S.row_bytes, launch);
@@ -244,8 +247,8 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
                         else launch(loss::distill_worker_kernel<E, p.C, false>, grid, 64 * waves, waves * lds);
                         return;
                     }
-                if (teacher_lse) launch(loss::distill_kernel<E, p.T, p.C, p.S, true>, grid_of(S.rows), p.T, lds);
-                else launch(loss::distill_kernel<E, p.T, p.C, p.S, false>, grid_of(S.rows), p.T, lds);
+                if (teacher_lse) launch(loss::distill_kernel<E, p.T, p.C, p.S, true>, p.grid(S.rows), p.THREADS, p.ROWS * lds);
+                else launch(loss::distill_kernel<E, p.T, p.C, p.S, false>, p.grid(S.rows), p.THREADS, p.ROWS * lds);
             });
         });
         if (!fits) return DBW_ERR_HIP;
@@ -327,7 +330,7 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
                                                s, S.R, P);
                             return;
                         }
-                    hipLaunchKernelGGL((loss::policy_kernel<E, p.T, p.C, p.S>), grid_of(S.rows), dim3(p.T), 0, s, S.R, P);
+                    hipLaunchKernelGGL((loss::policy_kernel<E, p.T, p.C, p.S>), p.grid(S.rows), dim3(p.THREADS), 0, s, S.R, P);
                 });
         });
         DBW_HIP(hipGetLastError());
