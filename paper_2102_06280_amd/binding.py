@@ -297,7 +297,7 @@ def _arr(t, dtype, numel):
 
 
 # What dbw_loss_work_bytes gives, without a call into the library: a tenth of a short call's time in the host.
-_WORK_FIXED, _WORK_PER_ROW = 5120, 16
+_WORK_FIXED, _WORK_PER_ROW = 20480, 16
 
 
 def _current():

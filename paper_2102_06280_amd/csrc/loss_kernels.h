@@ -294,7 +294,8 @@ struct Policy {
     // where rows are cut
     const MaxSum *stats;
     const float *token_logit;
-    Slices slices;
+    int parts;           // slices that a row's stats are of
+    Slices slices;       // of the gradient
     int rows;            // of each worker
     float *loss_out, *kl_out;
 };
@@ -410,7 +411,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
             const float w = weight_of(P, r);
             float logp = 0.f;
             if (w != 0.f) {
-                logp = LN2 * log2_p(P.token_logit[r], R.c, joined_by_thread(P.stats + r * n, n, R.c));
+                logp = LN2 * log2_p(P.token_logit[r], R.c, joined_by_thread(P.stats + r * P.parts, P.parts, R.c));
                 const PolicyRow p = policy_of(P, figures_of(P, r, w), logp);
                 loss += p.loss;
                 kl += p.kl;
@@ -426,7 +427,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
     float coef = 0.f;
     MaxSum mz;
     if (w != 0.f) {
-        mz = joined_by_wave(P.stats + r * n, n, R.c);
+        mz = joined_by_wave(P.stats + r * P.parts, P.parts, R.c);
         coef = R.scale * policy_of(P, figures_of(P, r, w), LN2 * log2_p(P.token_logit[r], R.c, mz)).slope;
     }
     if (coef == 0.f) {

@@ -41,7 +41,8 @@ struct Work {
     float *token_logit;
 };
 constexpr int64_t WORK_PER_ROW = 16;
-constexpr int SLICED_ROWS = 256, SLICE_GROUPS = 512;      // rows that may be cut, and workgroups that they are cut for
+constexpr int SLICED_ROWS = 1024, SLICE_GROUPS = 2048;    // rows that may be cut, and workgroups that they are cut for
+constexpr int POLICY_ROWS = 128, POLICY_GROUPS = 512;     // the same where a row would be read once if it were whole
 constexpr int64_t WORK_FIXED = 8 * SLICE_GROUPS + 4 * SLICED_ROWS;
 
 Work split_work(void *work, int64_t rows)
@@ -99,7 +100,7 @@ void by_row(int64_t bytes, F f)
     else if (bytes <= 16 * 512 * 16) f(Plan<512, 16>());
     else f(Plan<512, 16, 8>());
 }
-// For those that only read it, or only write its gradient from what is known of it.
+// For those that only read it.
 template <class F>
 void by_length(int64_t bytes, F f)
 {
@@ -107,20 +108,16 @@ void by_length(int64_t bytes, F f)
     else if (bytes <= 128 << 10) f(Plan<256, 8>());
     else f(Plan<1024, 8>());
 }
-// Few rows in slices: f of the plan of a slice.
+int pieces_of(const dbw_logits *l) { return l->vocab / (16 / (int)size_of(l->type)); }
+
+// Few rows are read in slices.
 constexpr int SLICE_LONG = 2048;                          // pieces of a slice from which threads take eight at a time
-template <class F>
-void by_slice(const loss::Slices &slices, F f)
-{
-    if (slices.pieces % SLICE_LONG == 0) f(Plan<256, 8>());
-    else f(Plan<256, 2>());
-}
-loss::Slices slices_of(const dbw_logits *l, int64_t rows)
+loss::Slices slices_of(const dbw_logits *l, int64_t rows, int most_rows, int groups)
 {
     loss::Slices S{1, 0};
-    const int pieces = l->vocab / (16 / (int)size_of(l->type));
-    if (rows < 1 || rows > SLICED_ROWS) return S;
-    int count = SLICE_GROUPS / (int)rows;
+    const int pieces = pieces_of(l);
+    if (rows < 1 || rows > most_rows) return S;
+    int count = groups / (int)rows;
     if (count > loss::MAX_SLICES) count = loss::MAX_SLICES;
     const int unit = pieces / count >= SLICE_LONG ? SLICE_LONG : 512;
     const int units = (pieces + unit - 1) / unit;         // of whole plans
@@ -129,6 +126,30 @@ loss::Slices slices_of(const dbw_logits *l, int64_t rows)
     S.count = (pieces + S.pieces - 1) / S.pieces;
     return S;
 }
+template <class F>
+void by_slice(const loss::Slices &slices, F f)
+{
+    if (slices.pieces % SLICE_LONG == 0) f(Plan<256, 8>());
+    else f(Plan<256, 2>());
+}
+
+// A gradient that is written from what is known of its row is so in slices of 16 KB, or of 8 KB where those would leave compute units idle.
+constexpr int GRADIENT_GROUPS = 1536;
+loss::Slices gradient_slices_of(const dbw_logits *l, int64_t rows)
+{
+    const int pieces = pieces_of(l);
+    if (pieces <= 8 * 64) return loss::Slices{1, 0};
+    const int each = rows * ((pieces + 1023) / 1024) >= GRADIENT_GROUPS ? 1024 : 512;
+    return loss::Slices{(pieces + each - 1) / each, each};
+}
+template <class F>
+void by_gradient_slice(const loss::Slices &slices, F f)
+{
+    if (slices.pieces == 0) f(Plan<64, 2>());
+    else if (slices.pieces == 512) f(Plan<256, 2>());
+    else f(Plan<256, 4>());
+}
+
 // All rows of a worker in one workgroup, a wave each: short rows, few enough that one compute unit takes no longer than a launch.
 bool in_one_group(const dbw_logits *l, int64_t row_bytes)
 {
@@ -161,13 +182,11 @@ void launch_logp(const dbw_logits *l, const Shape &S, const loss::Logp &P, bool 
 void launch_gradient(const dbw_logits *l, const Shape &S, const loss::Gradient &P, hipStream_t s)
 {
     by_type(l->type, [&](auto e) {
-        const auto launch = [&](auto p) {
+        by_gradient_slice(P.slices, [&](auto p) {
             hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>),
                                grid_of((S.rows * P.slices.count + p.ROWS - 1) / p.ROWS + (P.pairs.loss_out ? P.pairs.workers : 0)), dim3(p.THREADS),
                                0, s, S.R, P);
-        };
-        if (P.slices.count > 1) by_slice(P.slices, launch);
-        else by_length(S.row_bytes, launch);
+        });
     });
 }
 
@@ -190,7 +209,7 @@ extern "C" int dbw_token_logp(const dbw_logits *shape, const void *logits, const
     if (S.rows == 0) return DBW_OK;
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
-    const loss::Slices slices = slices_of(shape, S.rows);
+    const loss::Slices slices = slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS);
     const loss::Logp P{tokens, nullptr, logp_out, lse_out, slices.count > 1 ? W.slices : nullptr, W.token_logit, slices};
     launch_logp(shape, S, P, lse_out != nullptr, s);      // L is asked for where a gradient follows
     if (slices.count > 1) hipLaunchKernelGGL(loss::join_kernel, dim3((uint32_t)S.rows), dim3(64), 0, s, S.R, P);
@@ -206,7 +225,7 @@ extern "C" int dbw_token_logp_grad(const dbw_logits *shape, const void *logits, 
     if (rc != DBW_OK) return rc;
     if (S.rows > 0 && (!tokens || !lse || !coef || !dlogits)) return DBW_ERR_NULL;
     if (S.rows == 0) return DBW_OK;
-    const loss::Gradient P{tokens, coef, nullptr, lse, slices_of(shape, S.rows), loss::PairLoss{}};
+    const loss::Gradient P{tokens, coef, nullptr, lse, gradient_slices_of(shape, S.rows), loss::PairLoss{}};
     launch_gradient(shape, S, P, (hipStream_t)stream);
     DBW_HIP(hipGetLastError());
     return DBW_OK;
@@ -277,7 +296,7 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     float *const logp = logp_out ? logp_out : W.logp;
     loss::Slices slices{1, 0};
     if (S.rows > 0) {
-        if (pairs > 0) slices = slices_of(shape, S.rows);  // (whose parts the pairs' kernel joins)
+        if (pairs > 0) slices = slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS);  // (whose parts the pairs' kernel joins)
         const bool cut = slices.count > 1;
         launch_logp(shape, S, loss::Logp{tokens, weights, logp, nullptr, cut ? W.slices : W.stats, W.token_logit, slices}, dlogits != nullptr, s);
         DBW_HIP(hipGetLastError());
@@ -290,7 +309,7 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     }
     const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
     if (dlogits && S.rows > 0)
-        launch_gradient(shape, S, loss::Gradient{tokens, pairs > 0 ? W.coef : nullptr, W.stats, nullptr, slices, mean}, s);
+        launch_gradient(shape, S, loss::Gradient{tokens, pairs > 0 ? W.coef : nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, s);
     else
         hipLaunchKernelGGL(loss::pair_loss_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, mean);
     DBW_HIP(hipGetLastError());
@@ -310,17 +329,20 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
     if (S.rows > 0) {
-        const loss::Slices slices = slices_of(shape, S.rows);
+        const loss::Slices slices = slices_of(shape, S.rows, POLICY_ROWS, POLICY_GROUPS);
         const bool cut = slices.count > 1, one_group = in_one_group(shape, S.row_bytes);
         const loss::Policy P{tokens, old_logp, ref_logp, advantage, weights, 1.f - clip_low, 1.f + clip_high, kl_coef,
-                             1.f / (float)shape->rows, logp_out, W.terms, W.slices, W.token_logit, slices, shape->rows, loss_out, kl_out};
+                             1.f / (float)shape->rows, logp_out, W.terms, W.slices, W.token_logit, slices.count, gradient_slices_of(shape, S.rows),
+                             shape->rows, loss_out, kl_out};
         if (cut) launch_logp(shape, S, loss::Logp{tokens, weights, nullptr, nullptr, W.slices, W.token_logit, slices}, dlogits != nullptr, s);
         by_type(shape->type, [&](auto e) {
             typedef decltype(e) E;
             if (cut)
-                by_slice(slices, [&](auto p) {
-                    const int64_t groups = (dlogits ? S.rows * slices.count : 0) + shape->workers;
-                    hipLaunchKernelGGL((loss::policy_slices_kernel<E, p.T, p.C>), dim3((uint32_t)groups), dim3(p.T), 0, s, S.R, P);
+                by_gradient_slice(P.slices, [&](auto p) {
+                    if constexpr (p.T > 64) {             // (rows that are cut are longer)
+                        const int64_t groups = (dlogits ? S.rows * P.slices.count : 0) + shape->workers;
+                        hipLaunchKernelGGL((loss::policy_slices_kernel<E, p.T, p.C>), dim3((uint32_t)groups), dim3(p.T), 0, s, S.R, P);
+                    }
                 });
             else
                 by_row(S.row_bytes, [&](auto p) {
