@@ -15,9 +15,11 @@ __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane
 
 // Rows that are a wave's work share a workgroup, or starting workgroups would take longer than the rows.
 template <int T>
-constexpr int ROWS_OF = T == 64 ? 4 : 1;
+constexpr int ROWS_OF = T <= 64 ? 256 / T : 1;
 template <int T>
-__device__ __forceinline__ int64_t row_of_group(int64_t g) { return ROWS_OF<T> * g + (T == 64 ? wave_id() : 0); }
+__device__ __forceinline__ int row_in_group() { return T == 64 ? wave_id() : T < 64 ? (int)threadIdx.x / T : 0; }
+template <int T>
+__device__ __forceinline__ int64_t row_of_group(int64_t g) { return ROWS_OF<T> * g + row_in_group<T>(); }
 
 // Workgroups go to the eight XCDs in turn: this gives each XCD rows that lie together.
 __device__ __forceinline__ int64_t row_by_xcd(int64_t g, int64_t rows)
@@ -37,20 +39,15 @@ __device__ __forceinline__ void slice_of(const Slices &S, int s, int pieces, int
     first = S.count == 1 ? 0 : s * S.pieces;
     end = S.count == 1 ? pieces : min(first + S.pieces, pieces);
 }
-// A row's (m, Z) from its slices', on every lane of a wave; and by one thread.
-__device__ __forceinline__ MaxSum joined_by_wave(const MaxSum *slices, int count, float c)
+// A row's (m, Z) from its slices', on every one of T = 1, 16 or 64 lanes.
+template <int T>
+__device__ __forceinline__ MaxSum joined(const MaxSum *slices, int count, float c)
 {
-    const int lane = threadIdx.x & 63;
-    const MaxSum own = lane < count ? slices[lane] : MaxSum{-INFINITY, 0.f};
-    const float m = wave_max(own.m);
-    return MaxSum{m, wave_sum(own.z * rescale(own.m, m, c))};
-}
-__device__ __forceinline__ MaxSum joined_by_thread(const MaxSum *slices, int count, float c)
-{
-    float m = slices[0].m, z = 0.f;
-    for (int s = 1; s < count; ++s) m = fmaxf(m, slices[s].m);
-    for (int s = 0; s < count; ++s) z += slices[s].z * rescale(slices[s].m, m, c);
-    return MaxSum{m, z};
+    MaxSum own{-INFINITY, 0.f};
+    for (int s = tid<T>(); s < count; s += T) own = merged(own, slices[s], c);
+    if (T == 1) return own;
+    const float m = lanes_max<T>(own.m);
+    return MaxSum{m, lanes_sum<T>(own.z * rescale(own.m, m, c))};
 }
 constexpr int MAX_SLICES = 32;
 
@@ -71,9 +68,9 @@ __device__ __forceinline__ bool takes_part(const Logp &P, int64_t r) { return P.
 template <class E, int T, int C, bool AGAIN>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
 {
-    __shared__ MaxSum lds[T / 64];
-    const int64_t r = T == 64 ? row_of_group<T>(group()) : group() / P.slices.count;
-    const int s = T == 64 ? 0 : (int)(group() % P.slices.count);
+    __shared__ MaxSum lds[T > 64 ? T / 64 : 1];
+    const int64_t r = T <= 64 ? row_of_group<T>(group()) : group() / P.slices.count;
+    const int s = T <= 64 ? 0 : (int)(group() % P.slices.count);
     if (r >= R.rows) return;
     if (!takes_part(P, r)) {
         if (tid<T>() == 0 && P.slices.count == 1) {
@@ -92,10 +89,10 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
         row.template load<C, !AGAIN>(first, v);
         add_pieces<false>(row, first, end, v, -INFINITY, nullptr, R.c, m, z);
     }
-    z = wave_sum(z);
+    z = lanes_sum<T>(z);
     if (s == 0) {
-        const float single = row.load_single(), top = wave_max(single);
-        const MaxSum both = merged(MaxSum{m, z}, MaxSum{top, wave_sum(power(single, base_of(top, R.c)))}, R.c);
+        const float single = row.load_single(), top = lanes_max<T>(single);
+        const MaxSum both = merged(MaxSum{m, z}, MaxSum{top, lanes_sum<T>(power(single, base_of(top, R.c)))}, R.c);
         m = both.m;
         z = both.z;
     }
@@ -118,7 +115,7 @@ __global__ __launch_bounds__(64) void join_kernel(Rows R, Logp P)
     const int64_t r = blockIdx.x;
     float logp = 0.f, lse = 0.f;
     if (takes_part(P, r)) {
-        const MaxSum mz = joined_by_wave(P.stats + r * P.slices.count, P.slices.count, R.c);
+        const MaxSum mz = joined<64>(P.stats + r * P.slices.count, P.slices.count, R.c);
         logp = LN2 * log2_p(P.token_logit[r], R.c, mz);
         lse = fmaf(R.scale, mz.m, LN2 * log2f(mz.z));
     }
@@ -137,9 +134,9 @@ __device__ __forceinline__ void slice_gradient(const Rows &R, const RowOf<E, T> 
     const int yp = row.piece_of(y);
     const bool mine = tid<T>() == row.owner(y) && (yp < 0 ? singles : yp >= first && yp < end);
     const float xy = mine ? widen(row.x[y]) : 0.f, single = singles ? row.load_single() : 0.f;
-    b = Base{uniform(b.c), uniform(b.M), false};
-    by = uniform(by);
-    const global_access::bytes out = global_access::uniform_base(dx + row.before);
+    b = Base{uniform<T>(b.c), uniform<T>(b.M), false};
+    by = uniform<T>(by);
+    const global_access::bytes out = base_address<T>(dx + row.before);
     for (; first < end; first += T * C) {
         u32x4 v[C];
         row.template load<C, true>(first, v);
@@ -168,11 +165,29 @@ struct Preference {
 
 __device__ __forceinline__ bool takes_part(const Preference &P, int r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
 
+constexpr int PAIR_THREADS = 1024;       // 64 rows at a time where their slices have to be joined
+
+// Log-probabilities of rows from their slices, T lanes a row.
+template <int T>
+__device__ __forceinline__ void join_rows(const Preference &P, int from, int to)
+{
+    const bool first = threadIdx.x % T == 0;
+    for (int r = from + (int)threadIdx.x / T; r < to; r += PAIR_THREADS / T) {
+        float logp = 0.f;
+        if (takes_part(P, r)) {
+            const MaxSum mz = joined<T>(P.stats + (int64_t)r * P.slices, P.slices, P.c);
+            logp = LN2 * log2_p(P.token_logit[r], P.c, mz);
+            if (first) P.joined[r] = mz;
+        }
+        if (first) P.logp[r] = logp;
+    }
+}
+
 // The margin of a pair and the derivative of its worker's loss with respect to every log-probability of its rows.  Rows in no sequence are
 // the first and the last pair's.
-__global__ __launch_bounds__(THREADS) void pair_kernel(Preference P)
+__global__ __launch_bounds__(PAIR_THREADS) void pair_kernel(Preference P)
 {
-    __shared__ float lds[WAVES];
+    __shared__ float lds[PAIR_THREADS / 64];
     const int64_t j = blockIdx.x;
     const int t = threadIdx.x, n = (int)P.all_rows;
     int a[3];
@@ -182,31 +197,23 @@ __global__ __launch_bounds__(THREADS) void pair_kernel(Preference P)
     a[1] = min(max(a[1], a[0]), n);
     a[2] = min(max(a[2], a[1]), n);
     const int from = j == 0 ? 0 : a[0], to = j == gridDim.x - 1 ? n : a[2];
+    if (P.slices > 1) {
+        if (P.slices > 8) join_rows<16>(P, from, to);     // few rows
+        else join_rows<1>(P, from, to);
+        __syncthreads();
+    }
     float h = 0.f;
-    for (int r = from + t; r < to; r += THREADS) {
-        const bool part = takes_part(P, r);
-        float logp = 0.f;
-        if (P.slices == 1) {
-            logp = P.logp[r];
-        } else {
-            if (part) {
-                const MaxSum mz = joined_by_thread(P.stats + (int64_t)r * P.slices, P.slices, P.c);
-                P.joined[r] = mz;
-                logp = LN2 * log2_p(P.token_logit[r], P.c, mz);
-            }
-            P.logp[r] = logp;
-        }
-        if (part && r >= a[0] && r < a[2]) {
-            const float term = (P.weights ? P.weights[r] : 1.f) * (logp - P.ref_logp[r]);
+    for (int r = a[0] + t; r < a[2]; r += PAIR_THREADS)
+        if (takes_part(P, r)) {
+            const float term = (P.weights ? P.weights[r] : 1.f) * (P.logp[r] - P.ref_logp[r]);
             h += r < a[1] ? term : -term;
         }
-    }
-    const float u = P.beta * row_sum<THREADS>(h, lds);
+    const float u = P.beta * row_sum<PAIR_THREADS>(h, lds);
     if (t == 0) P.margin_out[j] = u;
     const float e = expf(-fabsf(u));                      // sigma(u) = 1 / (1 + e) or e / (1 + e)
     const float sig = (u >= 0.f ? 1.f : e) / (1.f + e), sig_not = (u >= 0.f ? e : 1.f) / (1.f + e);
     const float slope = (u != u ? u : P.smoothing * sig - (1.f - P.smoothing) * sig_not) * P.beta / (float)P.pairs;
-    for (int r = from + t; r < to; r += THREADS)
+    for (int r = from + t; r < to; r += PAIR_THREADS)
         P.coef[r] = takes_part(P, r) && r >= a[0] && r < a[2] ? (r < a[1] ? slope : -slope) * (P.weights ? P.weights[r] : 1.f) : 0.f;
 }
 
@@ -251,14 +258,14 @@ template <class E, int T, int C>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradient P)
 {
     __shared__ float lds[T * ROWS_OF<T> / 64];
-    const int64_t groups = T == 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
+    const int64_t groups = T <= 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
     if (group() >= groups) {
         const int64_t worker = group() - groups;
         if (P.pairs.loss_out && worker < P.pairs.workers) pair_loss<T * ROWS_OF<T>>(P.pairs, worker, lds);
         return;
     }
-    const int64_t r = T == 64 ? row_of_group<T>(group()) : group() / P.slices.count;
-    const int s = T == 64 ? 0 : (int)(group() % P.slices.count);
+    const int64_t r = T <= 64 ? row_of_group<T>(group()) : group() / P.slices.count;
+    const int s = T <= 64 ? 0 : (int)(group() % P.slices.count);
     if (r >= R.rows) return;
     const int token = P.tokens[r];
     const float g = token < 0 || !P.coef ? 0.f : R.scale * P.coef[r];
@@ -360,7 +367,7 @@ __device__ __forceinline__ float2 policy_whole_row(const Rows &R, const Policy &
 template <class E, int T, int C, int S>
 __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void policy_kernel(Rows R, Policy P)
 {
-    __shared__ MaxSum lds[T / 64];
+    __shared__ MaxSum lds[T > 64 ? T / 64 : 1];
     const int64_t r = row_of_group<T>(R.by_xcd ? row_by_xcd(group(), R.rows) : group());
     if (r >= R.rows) return;
     const float2 terms = policy_whole_row<E, T, C, S>(R, P, r, lds);
@@ -406,17 +413,19 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
     if (b >= cut) {
         const int64_t worker = b - cut;
         float loss = 0.f, kl = 0.f;
-        for (int t = threadIdx.x; t < P.rows; t += T) {
+        for (int t = threadIdx.x / 16; t < P.rows; t += T / 16) {
             const int64_t r = worker * P.rows + t;
             const float w = weight_of(P, r);
             float logp = 0.f;
             if (w != 0.f) {
-                logp = LN2 * log2_p(P.token_logit[r], R.c, joined_by_thread(P.stats + r * P.parts, P.parts, R.c));
+                logp = LN2 * log2_p(P.token_logit[r], R.c, joined<16>(P.stats + r * P.parts, P.parts, R.c));
                 const PolicyRow p = policy_of(P, figures_of(P, r, w), logp);
-                loss += p.loss;
-                kl += p.kl;
+                if (threadIdx.x % 16 == 0) {
+                    loss += p.loss;
+                    kl += p.kl;
+                }
             }
-            if (P.logp_out) P.logp_out[r] = logp;
+            if (P.logp_out && threadIdx.x % 16 == 0) P.logp_out[r] = logp;
         }
         store_sums(wave_sum(loss), wave_sum(kl), lds, P.loss_out + worker, P.kl_out ? P.kl_out + worker : nullptr);
         return;
@@ -427,7 +436,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
     float coef = 0.f;
     MaxSum mz;
     if (w != 0.f) {
-        mz = joined_by_wave(P.stats + r * P.parts, P.parts, R.c);
+        mz = joined<64>(P.stats + r * P.parts, P.parts, R.c);
         coef = R.scale * policy_of(P, figures_of(P, r, w), LN2 * log2_p(P.token_logit[r], R.c, mz)).slope;
     }
     if (coef == 0.f) {
@@ -454,14 +463,14 @@ struct Distill {
     float *loss_out;
 };
 
-// LDS words of a row: the teacher's columns (-1 where absent), its scaled logits, the student's logits, and a bit for every column of the
+// LDS words of a row: the teacher's columns (-1 where absent), its logits, the student's logits, and a bit for every column of the
 // vocabulary that is in the list, which begin with Piece::N - row.before <= 8 unused ones.
 __host__ __device__ __forceinline__ int distill_words(int k, int vocab) { return 3 * k + (vocab + 8 + 31) / 32; }
 
 // A row's weighted loss, and its gradient, by T threads.
 template <class E, int T, int C, int S, bool TAIL>
 __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill &P, int64_t r, uint32_t *shared, MaxSum *lds, MaxSum *lds_top,
-                                                   float (*sums)[T / 64])
+                                                   float (*sums)[T > 64 ? T / 64 : 1])
 {
     const int t = tid<T>();
     const float w = P.weights ? P.weights[r] : P.weight;
@@ -481,18 +490,40 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     for (int i = t; i < distill_words(P.k, R.vocab) - 3 * P.k; i += T) in_top[i] = 0;
     row_barrier<T>();
     float seen = 0.f, top = -INFINITY, m_top = -INFINITY;           // seen: 1 an entry, 2 a column twice
-    for (int j = t; j < P.k; j += T) {
-        int v = P.index[r * P.k + j];
-        if (v >= R.vocab) {
-            report(R.status);
-            v = -1;
+    for (int first = t; first < P.k; first += 4 * T) {    // four entries of a thread at a time: two round trips to memory for all of them
+        int v[4];
+        float value[4], xv[4];
+#pragma unroll
+        for (int u = 0; u < 4; ++u) v[u] = P.index[r * P.k + min(first + u * T, P.k - 1)];
+        if (P.value_type == 0) {
+#pragma unroll
+            for (int u = 0; u < 4; ++u) value[u] = ((const float *)P.value)[r * P.k + min(first + u * T, P.k - 1)];
+        } else {
+            uint16_t bits[4];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) bits[u] = ((const uint16_t *)P.value)[r * P.k + min(first + u * T, P.k - 1)];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) value[u] = P.value_type == 1 ? widen(bf16{bits[u]}) : widen(__builtin_bit_cast(f16, bits[u]));
         }
-        at[j] = v;
-        q[j] = R.scale * load_as(P.value, r * P.k + j, P.value_type);
-        if (v >= 0) {
-            xs[j] = widen(x[v]);
-            const bool again = atomicOr(&in_top[(v + bit0) >> 5], 1u << ((v + bit0) & 31)) >> ((v + bit0) & 31) & 1;
-            seen = fmaxf(seen, again ? 2.f : 1.f);
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (v[u] >= R.vocab) {
+                report(R.status);
+                v[u] = -1;
+            }
+            xv[u] = widen(x[max(v[u], 0)]);
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int j = first + u * T;
+            if (j >= P.k) break;
+            at[j] = v[u];
+            q[j] = value[u];
+            xs[j] = xv[u];
+            if (v[u] >= 0) {
+                const int bit = v[u] + bit0;
+                seen = fmaxf(seen, atomicOr(&in_top[bit >> 5], 1u << (bit & 31)) >> (bit & 31) & 1 ? 2.f : 1.f);
+            }
         }
     }
     row_barrier<T>();
@@ -512,16 +543,16 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
             m_top = fmaxf(m_top, xs[j]);
         }
     top = row_max<T>(top, sums[1]);
-    m_top = wave_max(m_top);
+    m_top = lanes_max<T>(m_top);
     const Base base_top = base_of(m_top, R.c);
     float sum = 0.f, z_top = 0.f;
+    const float from = top == -INFINITY ? 0.f : top;      // differences of logits first: they may be of any size
     for (int j = t; j < P.k; j += T)
         if (at[j] >= 0) {
-            sum += expf(q[j] - (top == -INFINITY ? 0.f : top));
+            sum += __builtin_amdgcn_exp2f((q[j] - from) * R.c);
             z_top += power(xs[j], base_top);
         }
     sum = row_sum<T>(sum, sums[2]);
-    const float norm = TAIL ? P.teacher_lse[r] : top + logf(sum);
     if (seen == 0.f || (!TAIL && top == -INFINITY && sum == 0.f)) {
         if (t == 0 && P.row_loss_out) P.row_loss_out[r] = 0.f;
         zero_row<E, T>(R, r);
@@ -533,7 +564,7 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     MaxSum mz;
     float log_out = 0.f;
     if (TAIL) {
-        const MaxSum in = row_merge<T>(MaxSum{m_top, wave_sum(z_top)}, R.c, lds_top);
+        const MaxSum in = row_merge<T>(MaxSum{m_top, lanes_sum<T>(z_top)}, R.c, lds_top);
         const MaxSum out = walk.template stats<true>(R.c, lds, (const uint8_t *)in_top);
         mz = merged(out, in, R.c);
         const Base a = base_of(out.m, R.c), b = base_of(mz.m, R.c);
@@ -541,16 +572,18 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     } else {
         mz = walk.stats(R.c, lds);
     }
+    const Base base = base_of(mz.m, R.c);
+    const float log2_z = log2f(mz.z), norm = TAIL ? P.teacher_lse[r] * LOG2E : log2f(sum);
     float part = 0.f, mass = 0.f;
     for (int j = t; j < P.k; j += T)
         if (at[j] >= 0) {
-            const float log_q = q[j] - norm, qj = expf(log_q);
-            const float log_p = LN2 * log2_p(xs[j], R.c, mz);
+            const float log2_q = TAIL ? fmaf(q[j], R.c, -norm) : (q[j] - from) * R.c - norm, qj = __builtin_amdgcn_exp2f(log2_q);
+            const float log2_p = (base.steep ? (xs[j] - mz.m) * R.c : fmaf(xs[j], base.c, -base.M)) - log2_z;
             mass += qj;
-            if (!(qj <= 0.f)) part += qj * (log_q - log_p);
-            q[j] = expf(log_p) - qj;                      // dl/dx over s
+            if (!(qj <= 0.f)) part += qj * (log2_q - log2_p);
+            q[j] = __builtin_amdgcn_exp2f(log2_p) - qj;   // dl/dx over s
         }
-    part = row_sum<T>(part, sums[3]);
+    part = LN2 * row_sum<T>(part, sums[3]);
     float factor = 1.f;
     if (TAIL) {
         mass = row_sum<T>(mass, sums[0]);                 // (its last use lies several barriers back)
@@ -563,7 +596,12 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     if (t == 0 && P.row_loss_out) P.row_loss_out[r] = part;
     if (R.dx) {
         E *dx = (E *)R.dx + r * R.ld_grad;
-        walk.gradient(dx, R.scale * w * factor / mz.z, base_of(mz.m, R.c), -1, 0.f, 0.f);
+        // Single elements written over in lines that have left the L2 cost more than the streaming stores gain where they are many: 14664
+        // rows of 3920 bf16, k = 152: 75 us and 106 with streaming stores; 8192 rows of 8000, k = 64: 70 and 67.  (Kernels of longer rows have no
+        // registers left for both kinds.)
+        const float by = R.scale * w * factor / mz.z;
+        if (T <= 64 && P.k >= R.vocab / 64) walk.template gradient<true>(dx, by, base, -1, 0.f, 0.f);
+        else walk.template gradient<false>(dx, by, base, -1, 0.f, 0.f);
         if (T > 64) __syncthreads();                      // the list's columns are written over
         for (int j = t; j < P.k; j += T)
             if (at[j] >= 0) dx[at[j]] = narrow<E>(R.scale * w * q[j]);
@@ -575,11 +613,11 @@ template <class E, int T, int C, int S, bool TAIL>
 __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void distill_kernel(Rows R, Distill P)
 {
     extern __shared__ uint32_t shared[];
-    __shared__ MaxSum lds[T / 64], lds_top[T / 64];
-    __shared__ float sums[4][T / 64];
+    __shared__ MaxSum lds[T > 64 ? T / 64 : 1], lds_top[T > 64 ? T / 64 : 1];
+    __shared__ float sums[4][T > 64 ? T / 64 : 1];
     const int64_t r = row_of_group<T>(R.by_xcd ? row_by_xcd(group(), R.rows) : group());
     if (r >= R.rows) return;
-    const float term = distill_whole_row<E, T, C, S, TAIL>(R, P, r, shared + (T == 64 ? wave_id() * distill_words(P.k, R.vocab) : 0), lds, lds_top, sums);
+    const float term = distill_whole_row<E, T, C, S, TAIL>(R, P, r, shared + row_in_group<T>() * distill_words(P.k, R.vocab), lds, lds_top, sums);
     if (tid<T>() == 0) P.terms[r] = make_float2(term, 0.f);
 }
 

@@ -39,13 +39,6 @@ __device__ __forceinline__ bf16 narrow<bf16>(float v)
     return bf16{__builtin_bit_cast(uint16_t, b)};
 }
 
-__device__ __forceinline__ float load_as(const void *p, int64_t i, int type)
-{
-    if (type == 0) return ((const float *)p)[i];
-    if (type == 1) return widen(((const bf16 *)p)[i]);
-    return widen(((const f16 *)p)[i]);
-}
-
 // The rows of a call.
 struct Rows {
     const void *x;     // logits
@@ -100,14 +93,14 @@ __device__ __forceinline__ float log2_p(float x, float c, const MZ &mz)
     return (b.steep ? (x - mz.m) * c : fmaf(x, c, -b.M)) - log2f(mz.z);
 }
 
-// A row is T threads' work; a workgroup has T threads, or (T = 64) several waves with a row each.
+// A row is T threads' work; a workgroup has T threads, or several rows of 64 or 16 threads each.
 template <int T>
 __device__ __forceinline__ int tid() { return (int)threadIdx.x & (T - 1); }
 // Orders a row's accesses to LDS.
 template <int T>
 __device__ __forceinline__ void row_barrier()
 {
-    if (T == 64) {                                        // a wave's are in order; the compiler's have to be, too
+    if (T <= 64) {                                        // a wave's are in order; the compiler's have to be, too
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
     } else {
@@ -122,10 +115,23 @@ __device__ __forceinline__ float shifted(float v, float identity)
 {
     return __int_as_float(__builtin_amdgcn_update_dpp(__float_as_int(identity), __float_as_int(v), CTRL, ROWS, 0xf, false));
 }
-__device__ __forceinline__ float uniform(float v) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v))); }
-// Over the 64 lanes of a wave, without LDS: shifts by 1, 2, 4 and 8 within 16 lanes, then the rows' last lanes to the next rows.
-__device__ __forceinline__ float wave_max(float v)
+// A value that all lanes of a row's waves have, in a scalar register.  (The lanes of one wave have several rows if T < 64.)
+template <int T>
+__device__ __forceinline__ float uniform(float v)
 {
+    return T < 64 ? v : __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
+}
+// Over the 64 lanes of a wave, without LDS: shifts by 1, 2, 4 and 8 within 16 lanes, then the last lanes of 16 to the next ones.  Over 16 lanes:
+// rotations, which leave the result in all of them.
+template <int T>
+__device__ __forceinline__ float lanes_max(float v)
+{
+    if (T == 16) {
+        v = fmaxf(v, shifted<0x121, 0xf>(v, v));
+        v = fmaxf(v, shifted<0x122, 0xf>(v, v));
+        v = fmaxf(v, shifted<0x124, 0xf>(v, v));
+        return fmaxf(v, shifted<0x128, 0xf>(v, v));
+    }
     v = fmaxf(v, shifted<0x111, 0xf>(v, -INFINITY));
     v = fmaxf(v, shifted<0x112, 0xf>(v, -INFINITY));
     v = fmaxf(v, shifted<0x114, 0xf>(v, -INFINITY));
@@ -134,8 +140,15 @@ __device__ __forceinline__ float wave_max(float v)
     v = fmaxf(v, shifted<0x143, 0xc>(v, -INFINITY));
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
-__device__ __forceinline__ float wave_sum(float v)
+template <int T>
+__device__ __forceinline__ float lanes_sum(float v)
 {
+    if (T == 16) {
+        v += shifted<0x121, 0xf>(v, 0.f);
+        v += shifted<0x122, 0xf>(v, 0.f);
+        v += shifted<0x124, 0xf>(v, 0.f);
+        return v + shifted<0x128, 0xf>(v, 0.f);
+    }
     v += shifted<0x111, 0xf>(v, 0.f);
     v += shifted<0x112, 0xf>(v, 0.f);
     v += shifted<0x114, 0xf>(v, 0.f);
@@ -144,6 +157,8 @@ __device__ __forceinline__ float wave_sum(float v)
     v += shifted<0x143, 0xc>(v, 0.f);
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
+__device__ __forceinline__ float wave_max(float v) { return lanes_max<64>(v); }
+__device__ __forceinline__ float wave_sum(float v) { return lanes_sum<64>(v); }
 
 // A maximum and the sum of exponentials that count from it.
 struct MaxSum {
@@ -168,39 +183,46 @@ __device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, float c)
 template <int T>
 __device__ __forceinline__ MaxSum row_merge(MaxSum v, float c, MaxSum *lds)
 {
-    if (T == 64) return v;
+    if (T <= 64) return v;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     float m = lds[0].m;
     for (int w = 1; w < T / 64; ++w) m = fmaxf(m, lds[w].m);
     float z = 0.f;
     for (int w = 0; w < T / 64; ++w) z += lds[w].z * rescale(lds[w].m, m, c);
-    return MaxSum{uniform(m), uniform(z)};
+    return MaxSum{uniform<T>(m), uniform<T>(z)};
 }
 template <int T>
 __device__ __forceinline__ float row_sum(float v, float *lds)
 {
-    v = wave_sum(v);
-    if (T == 64) return v;
+    v = lanes_sum<T>(v);
+    if (T <= 64) return v;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     v = lds[0];
     for (int w = 1; w < T / 64; ++w) v += lds[w];
-    return uniform(v);
+    return uniform<T>(v);
 }
 template <int T>
 __device__ __forceinline__ float row_max(float v, float *lds)
 {
-    v = wave_max(v);
-    if (T == 64) return v;
+    v = lanes_max<T>(v);
+    if (T <= 64) return v;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
     __syncthreads();
     v = lds[0];
     for (int w = 1; w < T / 64; ++w) v = fmaxf(v, lds[w]);
-    return uniform(v);
+    return uniform<T>(v);
 }
 
 // ---------------------------------------------------------------- a row in pieces of 16 bytes
+
+// The address of a row, in scalar registers where it is a wave's.
+template <int T>
+__device__ __forceinline__ global_access::bytes base_address(const void *p)
+{
+    return T < 64 ? (global_access::bytes)(uint64_t)p : global_access::uniform_base(p);
+}
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 // 16 bytes that start wherever an element may
@@ -272,7 +294,7 @@ template <class E, int T>
 struct RowOf {
     typedef Piece<E> P;
     typedef const __attribute__((address_space(1))) u32x4 *place;
-    static constexpr int BEHIND = 32;
+    static constexpr int BEHIND = 8;      // (either are fewer than 8)
     const E *x;
     int before;          // elements before the first boundary
     int pieces;
@@ -289,7 +311,7 @@ struct RowOf {
     template <int C, bool ONCE>
     __device__ __forceinline__ void load(int first, u32x4 (&r)[C]) const
     {
-        const global_access::bytes base = global_access::uniform_base(x + before);
+        const global_access::bytes base = base_address<T>(x + before);
 #pragma unroll
         for (int i = 0; i < C; ++i) {
             const uint32_t p = min(first + i * T + tid<T>(), pieces - 1);
@@ -305,12 +327,16 @@ struct RowOf {
             for (int j = 0; j < 4; ++j) r[j] = in ? r[j] : P::NOTHING;
         }
     }
+    // A piece's bits of `bits`: column v has bit v - before + N, so that a piece's are together.
+    __device__ __forceinline__ uint32_t bits_of(int p, const uint8_t *bits) const
+    {
+        const uint32_t b = p < pieces ? bits[(p + 1) * P::N >> 3] : 0u;
+        return P::N == 4 ? b >> ((p + 1) & 1) * 4 & 15u : b;
+    }
     // Takes the columns whose bits are set out of piece i of those from `first` on.
     __device__ __forceinline__ void leave_out(int first, int i, u32x4 &r, const uint8_t *bits) const
     {
-        const int p = first + i * T + tid<T>();
-        uint32_t b = p < pieces ? bits[(p + 1) * P::N >> 3] : 0u;
-        if (P::N == 4) b = b >> ((p + 1) & 1) * 4 & 15u;
+        const uint32_t b = bits_of(first + i * T + tid<T>(), bits);
         if (b) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -391,11 +417,11 @@ __device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, in
         }
         top = piece_max<E>(r[i], top);
     }
-    top = fmaxf(wave_max(top), m);
+    top = fmaxf(lanes_max<T>(top), m);
     z *= rescale(m, top, c);
     m = top;
     const Base base = base_of(m, c);
-    const Base b{uniform(base.c), uniform(base.M), false};
+    const Base b{uniform<T>(base.c), uniform<T>(base.M), false};
     z += power(single, b);
     keep_packed(r);
 #pragma unroll
@@ -403,17 +429,20 @@ __device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, in
 }
 
 // Piece i of the gradient of those from `first` on: by 2^(c x - M).
-template <class E, int T>
+// LATER: parts of the row are going to be written over, so it stays in the L2 for a while.
+template <class E, int T, bool LATER = false>
 __device__ __forceinline__ void store_piece(global_access::bytes base, int first, int end, int i, const u32x4 &r, float by, const Base &b)
 {
     typedef Piece<E> P;
+    typedef __attribute__((address_space(1))) typename P::raw *place;
     const int p = first + i * T + tid<T>();
     if (p < end) {
         float v[P::N];
         P::unpack(r, v);
 #pragma unroll
         for (int j = 0; j < P::N; ++j) v[j] = by * power(v[j], b);
-        __builtin_nontemporal_store((typename P::raw)P::pack(v), (__attribute__((address_space(1))) typename P::raw *)(base + (uint32_t)p * 16u));
+        if (LATER) *(place)(base + (uint32_t)p * 16u) = P::pack(v);
+        else __builtin_nontemporal_store((typename P::raw)P::pack(v), (place)(base + (uint32_t)p * 16u));
     }
 }
 
@@ -424,7 +453,7 @@ __device__ __forceinline__ void zero_pieces(const Rows &R, int64_t r, int first,
     if (!R.dx) return;
     E *dx = (E *)R.dx + r * R.ld_grad;
     const RowOf<E, T> row(dx, R.vocab);
-    const global_access::bytes base = global_access::uniform_base(dx + row.before);
+    const global_access::bytes base = base_address<T>(dx + row.before);
     end = min(end, row.pieces);
     for (int p = first + tid<T>(); p < end; p += T) {
         __attribute__((address_space(1))) u32x4 *at = (__attribute__((address_space(1))) u32x4 *)(base + (uint32_t)p * 16u);
@@ -471,25 +500,26 @@ struct Walk {
                 row.template load<S, false>(first, v);
                 add_pieces<LEAVE>(row, first, row.pieces, v, -INFINITY, left_out, c, m, z);
             }
-        return row_merge<T>(MaxSum{m, wave_sum(z)}, c, lds);
+        return row_merge<T>(MaxSum{m, lanes_sum<T>(z)}, c, lds);
     }
     // dx_v = by 2^(c x - M), and coef more at column y (none if negative)
+    template <bool LATER = false>
     __device__ __forceinline__ void gradient(E *dx, float by, const Base &base, int y, float xy, float coef)
     {
-        const Base b{uniform(base.c), uniform(base.M), false};
-        by = uniform(by);
-        const global_access::bytes out = global_access::uniform_base(dx + row.before);
+        const Base b{uniform<T>(base.c), uniform<T>(base.M), false};
+        by = uniform<T>(by);
+        const global_access::bytes out = base_address<T>(dx + row.before);
         if constexpr (S > 0)
             if (row.pieces > REST)
                 for (int first = REST + (row.pieces - 1 - REST) / (T * S) * (T * S); first >= REST; first -= T * S) {
                     u32x4 v[S];
                     row.template load<S, true>(first, v);
 #pragma unroll
-                    for (int i = 0; i < S; ++i) store_piece<E, T>(out, first, row.pieces, i, v[i], by, b);
+                    for (int i = 0; i < S; ++i) store_piece<E, T, LATER>(out, first, row.pieces, i, v[i], by, b);
                 }
         keep_packed(r);
 #pragma unroll
-        for (int i = 0; i < C; ++i) store_piece<E, T>(out, 0, row.pieces, i, r[i], by, b);
+        for (int i = 0; i < C; ++i) store_piece<E, T, LATER>(out, 0, row.pieces, i, r[i], by, b);
         if (row.has_single()) dx[row.single_column()] = narrow<E>(by * power(single, b));
         // by the thread that wrote the column before
         if (y >= 0 && tid<T>() == row.owner(y)) dx[y] = narrow<E>(by * power(xy, b) + coef);

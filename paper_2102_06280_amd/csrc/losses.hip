@@ -88,11 +88,19 @@ struct Plan {
     static constexpr int ROWS = loss::ROWS_OF<T>, THREADS = T * ROWS;      // of a workgroup
     static dim3 grid(int64_t rows) { return grid_of((rows + ROWS - 1) / ROWS); }
 };
+constexpr int SHORT_ROW = 2048;                           // bytes of a row that 16 threads take
+template <class F>
+void by_short_row(int64_t bytes, F f)
+{
+    if (bytes <= 4 * 16 * 16) f(Plan<16, 4>());
+    else f(Plan<16, 8>());
+}
 // For the kernels that hold a row.
 template <class F>
-void by_row(int64_t bytes, F f)
+void by_row(int64_t bytes, bool by_16, F f)
 {
-    if (bytes <= 2 * 64 * 16) f(Plan<64, 2>());
+    if (by_16) by_short_row(bytes, f);
+    else if (bytes <= 2 * 64 * 16) f(Plan<64, 2>());
     else if (bytes <= 8 * 64 * 16) f(Plan<64, 8>());
     else if (bytes <= 4 * 256 * 16) f(Plan<256, 4>());
     else if (bytes <= 8 * 256 * 16) f(Plan<256, 8>());
@@ -104,7 +112,8 @@ void by_row(int64_t bytes, F f)
 template <class F>
 void by_length(int64_t bytes, F f)
 {
-    if (bytes <= 8 * 64 * 16) f(Plan<64, 2>());
+    if (bytes <= SHORT_ROW) by_short_row(bytes, f);
+    else if (bytes <= 8 * 64 * 16) f(Plan<64, 2>());
     else if (bytes <= 128 << 10) f(Plan<256, 8>());
     else f(Plan<1024, 8>());
 }
@@ -143,9 +152,10 @@ loss::Slices gradient_slices_of(const dbw_logits *l, int64_t rows)
     return loss::Slices{(pieces + each - 1) / each, each};
 }
 template <class F>
-void by_gradient_slice(const loss::Slices &slices, F f)
+void by_gradient_slice(const loss::Slices &slices, int64_t row_bytes, F f)
 {
-    if (slices.pieces == 0) f(Plan<64, 2>());
+    if (row_bytes <= SHORT_ROW) by_short_row(row_bytes, f);
+    else if (slices.pieces == 0) f(Plan<64, 2>());
     else if (slices.pieces == 512) f(Plan<256, 2>());
     else f(Plan<256, 4>());
 }
@@ -156,6 +166,12 @@ bool in_one_group(const dbw_logits *l, int64_t row_bytes)
     return l->rows >= 1 && l->rows <= 64 && row_bytes <= 8 * 64 * 16 && l->rows * row_bytes <= 64 << 10;
 }
 int waves_of(const dbw_logits *l) { return l->rows < 16 ? l->rows : 16; }
+template <class F>
+void by_wave(int64_t bytes, F f)
+{
+    if (bytes <= 2 * 64 * 16) f(Plan<64, 2>());
+    else f(Plan<64, 8>());
+}
 
 // Calls f with a value of the logits' type.
 template <class F>
@@ -182,7 +198,7 @@ void launch_logp(const dbw_logits *l, const Shape &S, const loss::Logp &P, bool 
 void launch_gradient(const dbw_logits *l, const Shape &S, const loss::Gradient &P, hipStream_t s)
 {
     by_type(l->type, [&](auto e) {
-        by_gradient_slice(P.slices, [&](auto p) {
+        by_gradient_slice(P.slices, S.row_bytes, [&](auto p) {
             hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>),
                                grid_of((S.rows * P.slices.count + p.ROWS - 1) / p.ROWS + (P.pairs.loss_out ? P.pairs.workers : 0)), dim3(p.THREADS),
                                0, s, S.R, P);
@@ -257,18 +273,18 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
         const int waves = waves_of(shape);
         const bool one_group = in_one_group(shape, S.row_bytes) && waves * lds <= 65536;
         by_type(shape->type, [&](auto e) {
-            by_row(S.row_bytes, [&](auto p) {
-                typedef decltype(e) E;
-                if constexpr (p.T == 64)
-                    if (one_group) {
-                        const dim3 grid((uint32_t)shape->workers);
-                        if (teacher_lse) launch(loss::distill_worker_kernel<E, p.C, true>, grid, 64 * waves, waves * lds);
-                        else launch(loss::distill_worker_kernel<E, p.C, false>, grid, 64 * waves, waves * lds);
-                        return;
-                    }
-                if (teacher_lse) launch(loss::distill_kernel<E, p.T, p.C, p.S, true>, p.grid(S.rows), p.THREADS, p.ROWS * lds);
-                else launch(loss::distill_kernel<E, p.T, p.C, p.S, false>, p.grid(S.rows), p.THREADS, p.ROWS * lds);
-            });
+            typedef decltype(e) E;
+            if (one_group)
+                by_wave(S.row_bytes, [&](auto p) {
+                    const dim3 grid((uint32_t)shape->workers);
+                    if (teacher_lse) launch(loss::distill_worker_kernel<E, p.C, true>, grid, 64 * waves, waves * lds);
+                    else launch(loss::distill_worker_kernel<E, p.C, false>, grid, 64 * waves, waves * lds);
+                });
+            else
+                by_row(S.row_bytes, S.row_bytes <= SHORT_ROW && 16 * lds <= 65536, [&](auto p) {
+                    if (teacher_lse) launch(loss::distill_kernel<E, p.T, p.C, p.S, true>, p.grid(S.rows), p.THREADS, p.ROWS * lds);
+                    else launch(loss::distill_kernel<E, p.T, p.C, p.S, false>, p.grid(S.rows), p.THREADS, p.ROWS * lds);
+                });
         });
         if (!fits) return DBW_ERR_HIP;
         DBW_HIP(hipGetLastError());
@@ -304,7 +320,7 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     if (pairs > 0) {
         const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.c, pairs, S.rows, logp, margin_out, W.coef,
                                  W.slices, W.stats, W.token_logit, slices.count, status_out};
-        hipLaunchKernelGGL(loss::pair_kernel, dim3((uint32_t)(shape->workers * pairs)), dim3(loss::THREADS), 0, s, P);
+        hipLaunchKernelGGL(loss::pair_kernel, dim3((uint32_t)(shape->workers * pairs)), dim3(loss::PAIR_THREADS), 0, s, P);
         DBW_HIP(hipGetLastError());
     }
     const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
@@ -338,20 +354,18 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
         by_type(shape->type, [&](auto e) {
             typedef decltype(e) E;
             if (cut)
-                by_gradient_slice(P.slices, [&](auto p) {
+                by_gradient_slice(P.slices, S.row_bytes, [&](auto p) {
                     if constexpr (p.T > 64) {             // (rows that are cut are longer)
                         const int64_t groups = (dlogits ? S.rows * P.slices.count : 0) + shape->workers;
                         hipLaunchKernelGGL((loss::policy_slices_kernel<E, p.T, p.C>), dim3((uint32_t)groups), dim3(p.T), 0, s, S.R, P);
                     }
                 });
+            else if (one_group)
+                by_wave(S.row_bytes, [&](auto p) {
+                    hipLaunchKernelGGL((loss::policy_worker_kernel<E, p.C>), dim3((uint32_t)shape->workers), dim3(64 * waves_of(shape)), 0, s, S.R, P);
+                });
             else
-                by_row(S.row_bytes, [&](auto p) {
-                    if constexpr (p.T == 64)
-                        if (one_group) {
-                            hipLaunchKernelGGL((loss::policy_worker_kernel<E, p.C>), dim3((uint32_t)shape->workers), dim3(64 * waves_of(shape)), 0,
-                                               s, S.R, P);
-                            return;
-                        }
+                by_row(S.row_bytes, S.row_bytes <= SHORT_ROW, [&](auto p) {
                     hipLaunchKernelGGL((loss::policy_kernel<E, p.T, p.C, p.S>), p.grid(S.rows), dim3(p.THREADS), 0, s, S.R, P);
                 });
         });
