@@ -389,18 +389,20 @@ __device__ __forceinline__ void store_sums(float a, float b, float2 *lds, float 
     if (second_out) *second_out = b;
 }
 
-// All of a worker's rows in one workgroup, a wave each in turn, and their sums: one launch.
-template <class E, int C>
+// All of a worker's rows in one workgroup, T threads each, and their sums: one launch.
+template <class E, int T, int C>
 __global__ __launch_bounds__(1024) void policy_worker_kernel(Rows R, Policy P)
 {
     __shared__ float2 lds[16];
     float a = 0.f, b = 0.f;
-    for (int t = wave_id(); t < P.rows; t += blockDim.x >> 6) {
-        const float2 terms = policy_whole_row<E, 64, C, 0>(R, P, (int64_t)blockIdx.x * P.rows + t, nullptr);
-        a += terms.x;
-        b += terms.y;
+    for (int t = row_in_group<T>(); t < P.rows; t += blockDim.x / T) {
+        const float2 terms = policy_whole_row<E, T, C, 0>(R, P, (int64_t)blockIdx.x * P.rows + t, nullptr);
+        if (tid<T>() == 0) {
+            a += terms.x;
+            b += terms.y;
+        }
     }
-    store_sums(a, b, lds, P.loss_out + blockIdx.x, P.kl_out ? P.kl_out + blockIdx.x : nullptr);
+    store_sums(wave_sum(a), wave_sum(b), lds, P.loss_out + blockIdx.x, P.kl_out ? P.kl_out + blockIdx.x : nullptr);
 }
 
 // The second launch for rows in slices: the slices' gradients, and behind them a workgroup for every worker's sums.
@@ -621,20 +623,20 @@ __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void distill_kerne
     if (tid<T>() == 0) P.terms[r] = make_float2(term, 0.f);
 }
 
-// All of a worker's rows in one workgroup, a wave each in turn, and their sum.
-template <class E, int C, bool TAIL>
+// All of a worker's rows in one workgroup, T threads each, and their sum.
+template <class E, int T, int C, bool TAIL>
 __global__ __launch_bounds__(1024) void distill_worker_kernel(Rows R, Distill P)
 {
     extern __shared__ uint32_t shared[];
     __shared__ float2 lds[16];
-    const int wave = wave_id();
     float a = 0.f;
-    for (int t = wave; t < P.rows; t += blockDim.x >> 6) {
-        a += distill_whole_row<E, 64, C, 0, TAIL>(R, P, (int64_t)blockIdx.x * P.rows + t, shared + wave * distill_words(P.k, R.vocab), nullptr,
-                                                  nullptr, nullptr);
-        row_barrier<64>();                                // the next row's list takes this one's place
+    for (int t = row_in_group<T>(); t < P.rows; t += blockDim.x / T) {
+        const float term = distill_whole_row<E, T, C, 0, TAIL>(R, P, (int64_t)blockIdx.x * P.rows + t,
+                                                               shared + row_in_group<T>() * distill_words(P.k, R.vocab), nullptr, nullptr, nullptr);
+        if (tid<T>() == 0) a += term;
+        row_barrier<T>();                                 // the next row's list takes this one's place
     }
-    store_sums(a, 0.f, lds, P.loss_out + blockIdx.x, nullptr);
+    store_sums(wave_sum(a), 0.f, lds, P.loss_out + blockIdx.x, nullptr);
 }
 
 // ---------------------------------------------------------------- sums

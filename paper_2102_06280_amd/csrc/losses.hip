@@ -42,7 +42,7 @@ struct Work {
 };
 constexpr int64_t WORK_PER_ROW = 16;
 constexpr int SLICED_ROWS = 1024, SLICE_GROUPS = 2048;    // rows that may be cut, and workgroups that they are cut for
-constexpr int POLICY_ROWS = 128, POLICY_GROUPS = 512;     // the same where a row would be read once if it were whole
+constexpr int POLICY_ROWS = 64, POLICY_GROUPS = 512;     // the same where a row would be read once if it were whole
 constexpr int64_t WORK_FIXED = 8 * SLICE_GROUPS + 4 * SLICED_ROWS;
 
 Work split_work(void *work, int64_t rows)
@@ -160,16 +160,19 @@ void by_gradient_slice(const loss::Slices &slices, int64_t row_bytes, F f)
     else f(Plan<256, 4>());
 }
 
-// All rows of a worker in one workgroup, a wave each: short rows, few enough that one compute unit takes no longer than a launch.
-bool in_one_group(const dbw_logits *l, int64_t row_bytes)
+// All rows of a worker in one workgroup: its threads (0: rather not) for rows of T threads each, few enough that `turns` of them one after the
+// other take no longer than a second launch.
+int one_group_threads(const dbw_logits *l, int64_t row_bytes, int turns)
 {
-    return l->rows >= 1 && l->rows <= 64 && row_bytes <= 8 * 64 * 16 && l->rows * row_bytes <= 64 << 10;
+    const int T = row_bytes <= SHORT_ROW ? 16 : 64;
+    if (l->rows < 1 || row_bytes > 8 * 64 * 16 || l->rows * T > turns * 1024 || l->rows * row_bytes > 64 << 10) return 0;
+    const int threads = (l->rows * T + 63) / 64 * 64;
+    return threads < 1024 ? threads : 1024;
 }
-int waves_of(const dbw_logits *l) { return l->rows < 16 ? l->rows : 16; }
 template <class F>
-void by_wave(int64_t bytes, F f)
+void by_group_row(int64_t bytes, F f)
 {
-    if (bytes <= 2 * 64 * 16) f(Plan<64, 2>());
+    if (bytes <= SHORT_ROW) by_short_row(bytes, f);
     else f(Plan<64, 8>());
 }
 
@@ -270,15 +273,17 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
             if (bytes > 65536) fits = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) == hipSuccess;
             if (fits) hipLaunchKernelGGL(kernel, grid, dim3((uint32_t)threads), bytes, s, S.R, P);
         };
-        const int waves = waves_of(shape);
-        const bool one_group = in_one_group(shape, S.row_bytes) && waves * lds <= 65536;
+        const int row_threads = S.row_bytes <= SHORT_ROW ? 16 : 64;
+        int group_threads = one_group_threads(shape, S.row_bytes, 1);
+        if (group_threads / row_threads * lds > 65536) group_threads = 0;
         by_type(shape->type, [&](auto e) {
             typedef decltype(e) E;
-            if (one_group)
-                by_wave(S.row_bytes, [&](auto p) {
+            if (group_threads)
+                by_group_row(S.row_bytes, [&](auto p) {
                     const dim3 grid((uint32_t)shape->workers);
-                    if (teacher_lse) launch(loss::distill_worker_kernel<E, p.C, true>, grid, 64 * waves, waves * lds);
-                    else launch(loss::distill_worker_kernel<E, p.C, false>, grid, 64 * waves, waves * lds);
+                    const size_t bytes = group_threads / p.T * lds;
+                    if (teacher_lse) launch(loss::distill_worker_kernel<E, p.T, p.C, true>, grid, group_threads, bytes);
+                    else launch(loss::distill_worker_kernel<E, p.T, p.C, false>, grid, group_threads, bytes);
                 });
             else
                 by_row(S.row_bytes, S.row_bytes <= SHORT_ROW && 16 * lds <= 65536, [&](auto p) {
@@ -288,7 +293,7 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
         });
         if (!fits) return DBW_ERR_HIP;
         DBW_HIP(hipGetLastError());
-        if (one_group) return DBW_OK;
+        if (group_threads) return DBW_OK;
     }
     hipLaunchKernelGGL(loss::sum_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, W.terms, shape->rows, loss_out,
                        (float *)nullptr);
@@ -346,7 +351,8 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
     hipStream_t s = (hipStream_t)stream;
     if (S.rows > 0) {
         const loss::Slices slices = slices_of(shape, S.rows, POLICY_ROWS, POLICY_GROUPS);
-        const bool cut = slices.count > 1, one_group = in_one_group(shape, S.row_bytes);
+        const bool cut = slices.count > 1;
+        const int group_threads = one_group_threads(shape, S.row_bytes, 2);
         const loss::Policy P{tokens, old_logp, ref_logp, advantage, weights, 1.f - clip_low, 1.f + clip_high, kl_coef,
                              1.f / (float)shape->rows, logp_out, W.terms, W.slices, W.token_logit, slices.count, gradient_slices_of(shape, S.rows),
                              shape->rows, loss_out, kl_out};
@@ -360,9 +366,9 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
                         hipLaunchKernelGGL((loss::policy_slices_kernel<E, p.T, p.C>), dim3((uint32_t)groups), dim3(p.T), 0, s, S.R, P);
                     }
                 });
-            else if (one_group)
-                by_wave(S.row_bytes, [&](auto p) {
-                    hipLaunchKernelGGL((loss::policy_worker_kernel<E, p.C>), dim3((uint32_t)shape->workers), dim3(64 * waves_of(shape)), 0, s, S.R, P);
+            else if (group_threads)
+                by_group_row(S.row_bytes, [&](auto p) {
+                    hipLaunchKernelGGL((loss::policy_worker_kernel<E, p.T, p.C>), dim3((uint32_t)shape->workers), dim3(group_threads), 0, s, S.R, P);
                 });
             else
                 by_row(S.row_bytes, S.row_bytes <= SHORT_ROW, [&](auto p) {
@@ -370,7 +376,7 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
                 });
         });
         DBW_HIP(hipGetLastError());
-        if (cut || one_group) return DBW_OK;
+        if (cut || group_threads) return DBW_OK;
     }
     hipLaunchKernelGGL(loss::sum_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, W.terms, shape->rows, loss_out, kl_out);
     DBW_HIP(hipGetLastError());
