@@ -57,6 +57,21 @@ __device__ __forceinline__ MaxSum joined(const MaxSum *slices, int count, float 
 }
 constexpr int MAX_SLICES = 32;
 
+// Sums over a workgroup's waves, in their order.
+__device__ __forceinline__ void store_sums(float a, float b, float2 *lds, float *first_out, float *second_out)
+{
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(a, b);
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    a = b = 0.f;
+    for (unsigned w = 0; w < blockDim.x / 64; ++w) {
+        a += lds[w].x;
+        b += lds[w].y;
+    }
+    *first_out = a;
+    if (second_out) *second_out = b;
+}
+
 // ---------------------------------------------------------------- log-probabilities
 
 struct Logp {
@@ -172,6 +187,35 @@ struct Preference {
 
 __device__ __forceinline__ bool takes_part(const Preference &P, int r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
 
+// Rows a[0] ... a[1] - 1 and a[1] ... a[2] - 1 of pair j, within the rows there are whatever the offsets say.
+__device__ __forceinline__ void rows_of_pair(const Preference &P, int64_t j, int (&a)[3])
+{
+    const int n = (int)P.all_rows;
+    for (int i = 0; i < 3; ++i) a[i] = P.seq_start[2 * j + i];
+    if (a[0] < 0 || a[1] < a[0] || a[2] < a[1] || a[2] > n) report(P.status);
+    a[0] = min(max(a[0], 0), n);
+    a[1] = min(max(a[1], a[0]), n);
+    a[2] = min(max(a[2], a[1]), n);
+}
+// A thread's part, one of `threads`, of the difference between the pair's summed log ratios.
+__device__ __forceinline__ float part_of_pair(const Preference &P, const int (&a)[3], int thread, int threads)
+{
+    float h = 0.f;
+    for (int r = a[0] + thread; r < a[2]; r += threads)
+        if (takes_part(P, r)) {
+            const float term = (P.weights ? P.weights[r] : 1.f) * (P.logp[r] - P.ref_logp[r]);
+            h += r < a[1] ? term : -term;
+        }
+    return h;
+}
+// The derivative of a worker's loss with respect to the difference of a pair, times beta; from the pair's margin.
+__device__ __forceinline__ float slope_of(const Preference &P, float u)
+{
+    const float e = expf(-fabsf(u));                      // sigma(u) = 1 / (1 + e) or e / (1 + e)
+    const float sig = (u >= 0.f ? 1.f : e) / (1.f + e), sig_not = (u >= 0.f ? e : 1.f) / (1.f + e);
+    return (u != u ? u : P.smoothing * sig - (1.f - P.smoothing) * sig_not) * P.beta / (float)P.pairs;
+}
+
 constexpr int PAIR_THREADS = 1024;       // 64 rows at a time where their slices have to be joined
 
 // Log-probabilities of rows from their slices, T lanes a row.
@@ -199,28 +243,16 @@ __global__ __launch_bounds__(PAIR_THREADS) void pair_kernel(Preference P)
     const int64_t j = blockIdx.x;
     const int t = threadIdx.x, n = (int)P.all_rows;
     int a[3];
-    for (int i = 0; i < 3; ++i) a[i] = P.seq_start[2 * j + i];
-    if (a[0] < 0 || a[1] < a[0] || a[2] < a[1] || a[2] > n) report(P.status);
-    a[0] = min(max(a[0], 0), n);
-    a[1] = min(max(a[1], a[0]), n);
-    a[2] = min(max(a[2], a[1]), n);
+    rows_of_pair(P, j, a);
     const int from = j == 0 ? 0 : a[0], to = j == gridDim.x - 1 ? n : a[2];
     if (P.slices > 1) {
         if (P.slices > 8) join_rows<16>(P, from, to);     // few rows
         else join_rows<1>(P, from, to);
         __syncthreads();
     }
-    float h = 0.f;
-    for (int r = a[0] + t; r < a[2]; r += PAIR_THREADS)
-        if (takes_part(P, r)) {
-            const float term = (P.weights ? P.weights[r] : 1.f) * (P.logp[r] - P.ref_logp[r]);
-            h += r < a[1] ? term : -term;
-        }
-    const float u = P.beta * row_sum<PAIR_THREADS>(h, lds);
+    const float u = P.beta * row_sum<PAIR_THREADS>(part_of_pair(P, a, t, PAIR_THREADS), lds);
     if (t == 0) P.margin_out[j] = u;
-    const float e = expf(-fabsf(u));                      // sigma(u) = 1 / (1 + e) or e / (1 + e)
-    const float sig = (u >= 0.f ? 1.f : e) / (1.f + e), sig_not = (u >= 0.f ? e : 1.f) / (1.f + e);
-    const float slope = (u != u ? u : P.smoothing * sig - (1.f - P.smoothing) * sig_not) * P.beta / (float)P.pairs;
+    const float slope = slope_of(P, u);
     for (int r = from + t; r < to; r += PAIR_THREADS)
         P.coef[r] = takes_part(P, r) && r >= a[0] && r < a[2] ? (r < a[1] ? slope : -slope) * (P.weights ? P.weights[r] : 1.f) : 0.f;
 }
@@ -232,16 +264,17 @@ struct PairLoss {
     float smoothing;
     float *loss_out;     // null: not asked for
 };
+__device__ __forceinline__ float loss_of(const PairLoss &P, float u)
+{
+    // -log sigma(u) = max(-u, 0) + soft, -log sigma(-u) = max(u, 0) + soft
+    const float soft = log1pf(expf(-fabsf(u)));
+    return u != u ? u : soft + (u >= 0.f ? P.smoothing * u : (P.smoothing - 1.f) * u);
+}
 template <int T>
 __device__ __forceinline__ void pair_loss(const PairLoss &P, int64_t worker, float *lds)
 {
-    const float *u = P.margin + worker * P.pairs;
     float l = 0.f;
-    for (int j = threadIdx.x; j < P.pairs; j += T) {
-        const float soft = log1pf(expf(-fabsf(u[j])));
-        // -log sigma(u) = max(-u, 0) + soft, -log sigma(-u) = max(u, 0) + soft
-        l += u[j] != u[j] ? u[j] : soft + (u[j] >= 0.f ? P.smoothing * u[j] : (P.smoothing - 1.f) * u[j]);
-    }
+    for (int j = threadIdx.x; j < P.pairs; j += T) l += loss_of(P, P.margin[worker * P.pairs + j]);
     l = row_sum<T>(l, lds);
     if (threadIdx.x == 0) P.loss_out[worker] = P.pairs ? l / (float)P.pairs : 0.f;
 }
@@ -262,23 +295,9 @@ struct Gradient {
     PairLoss pairs;      // workgroups behind the rows' give every worker's loss
 };
 
-// A workgroup a slice of 16 KB: the row's (m, Z) are known, so every piece is by itself.  Bound by memory: 8192 x 32768 bf16, 15 % of the rows without a part,
-// 0.99 GB in 147 us, 6.8 TB/s with what is left of the rows in the last-level cache.
 template <class E, int T, int C>
-__global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradient P)
+__device__ __forceinline__ void gradient_of_slice(const Rows &R, const Gradient &P, int64_t r, int s, int token, float g)
 {
-    __shared__ float lds[T * ROWS_OF<T> / 64];
-    const int64_t groups = T <= 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
-    if (group() >= groups) {
-        const int64_t worker = group() - groups;
-        if (P.pairs.loss_out && worker < P.pairs.workers) pair_loss<T * ROWS_OF<T>>(P.pairs, worker, lds);
-        return;
-    }
-    const int64_t r = T <= 64 ? row_of_group<T>(group()) : group() / P.slices.count;
-    const int s = T <= 64 ? 0 : (int)(group() % P.slices.count);
-    if (r >= R.rows) return;
-    const int token = P.tokens[r];
-    const float g = token < 0 || !P.coef ? 0.f : R.scale * P.coef[r];
     const RowOf<E, T> row((const E *)R.x + r * R.ld, R.vocab);
     if (g == 0.f) {
         // (the pieces of the gradient's row may be one more than those of the logits')
@@ -298,6 +317,80 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradie
     int first, end;
     slice_of(P.slices, s, row.pieces, first, end);
     slice_gradient<E, T, C>(R, row, r, first, end, by, b, column(R, token), g);
+}
+
+// A workgroup a slice of 16 KB: the row's (m, Z) are known, so every piece is by itself.  Bound by memory: 8192 x 32768 bf16, 15 % of the rows without a part,
+// 0.99 GB in 147 us, 6.8 TB/s with what is left of the rows in the last-level cache.
+template <class E, int T, int C>
+__global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradient P)
+{
+    __shared__ float lds[T * ROWS_OF<T> / 64];
+    const int64_t groups = T <= 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
+    if (group() >= groups) {
+        const int64_t worker = group() - groups;
+        if (P.pairs.loss_out && worker < P.pairs.workers) pair_loss<T * ROWS_OF<T>>(P.pairs, worker, lds);
+        return;
+    }
+    const int64_t r = T <= 64 ? row_of_group<T>(group()) : group() / P.slices.count;
+    const int s = T <= 64 ? 0 : (int)(group() % P.slices.count);
+    if (r >= R.rows) return;
+    const int token = P.tokens[r];
+    gradient_of_slice<E, T, C>(R, P, r, s, token, token < 0 || !P.coef ? 0.f : R.scale * P.coef[r]);
+}
+
+// Margins and loss of a worker with few rows and short pairs, a wave a pair, by a workgroup of THREADS.
+__device__ __forceinline__ void sums_of_pairs(const PairLoss &P, const Preference &Q, int64_t worker, float2 *lds)
+{
+    int a[3];
+    float loss = 0.f;
+    for (int j = wave_id(); j < Q.pairs; j += WAVES) {
+        rows_of_pair(Q, worker * Q.pairs + j, a);
+        const float u = Q.beta * wave_sum(part_of_pair(Q, a, threadIdx.x & 63, 64));
+        if ((threadIdx.x & 63) == 0) Q.margin_out[worker * Q.pairs + j] = u;
+        loss += loss_of(P, u);
+    }
+    store_sums(loss / (float)Q.pairs, 0.f, lds, P.loss_out + worker, nullptr);
+}
+__global__ __launch_bounds__(THREADS) void pair_sums_kernel(PairLoss P, Preference Q)
+{
+    __shared__ float2 lds[WAVES];
+    sums_of_pairs(P, Q, blockIdx.x, lds);
+}
+
+// The gradient for few rows in short pairs, with every coefficient from the log-probabilities of its pair, which the threads of a row sum up again
+// for each row; workgroups behind the rows' give margins and losses.
+template <class E, int T, int C>
+__global__ __launch_bounds__(T * ROWS_OF<T>) void pair_gradient_kernel(Rows R, Gradient P, Preference Q)
+{
+    static_assert(T * ROWS_OF<T> == THREADS, "the workgroups behind the rows' have as many threads as pair_sums_kernel's");
+    __shared__ float2 lds[WAVES];
+    constexpr int LANES = T < 64 ? T : 64;
+    const int64_t groups = T <= 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
+    int a[3];
+    if (group() >= groups) {
+        const int64_t worker = group() - groups;
+        if (worker >= P.pairs.workers) return;
+        sums_of_pairs(P.pairs, Q, worker, lds);
+        return;
+    }
+    const int64_t r = T <= 64 ? row_of_group<T>(group()) : group() / P.slices.count;
+    const int s = T <= 64 ? 0 : (int)(group() % P.slices.count);
+    if (r >= R.rows) return;
+    const int token = P.tokens[r];
+    float g = 0.f;
+    if (takes_part(Q, (int)r)) {
+        // the last sequence that starts at the row or before it
+        const int lane = threadIdx.x & (LANES - 1), sequences = 2 * P.pairs.workers * Q.pairs;
+        float starts = 0.f;
+        for (int q = lane; q < sequences; q += LANES) starts += Q.seq_start[q] <= r ? 1.f : 0.f;
+        const int q = (int)lanes_sum<LANES>(starts) - 1;
+        if (q >= 0) {
+            rows_of_pair(Q, q / 2, a);
+            const float slope = slope_of(Q, Q.beta * lanes_sum<LANES>(part_of_pair(Q, a, lane, LANES)));
+            if (r >= a[0] && r < a[2]) g = R.scale * (r < a[1] ? slope : -slope) * (Q.weights ? Q.weights[r] : 1.f);
+        }
+    }
+    gradient_of_slice<E, T, C>(R, P, r, s, token, g);
 }
 
 // ---------------------------------------------------------------- policy
@@ -384,21 +477,6 @@ __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void policy_kernel
     if (r >= R.rows) return;
     const float2 terms = policy_whole_row<E, T, C, S>(R, P, r, lds);
     if (tid<T>() == 0) P.terms[r] = terms;
-}
-
-// Sums over a workgroup's waves, in their order.
-__device__ __forceinline__ void store_sums(float a, float b, float2 *lds, float *first_out, float *second_out)
-{
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(a, b);
-    __syncthreads();
-    if (threadIdx.x != 0) return;
-    a = b = 0.f;
-    for (unsigned w = 0; w < blockDim.x / 64; ++w) {
-        a += lds[w].x;
-        b += lds[w].y;
-    }
-    *first_out = a;
-    if (second_out) *second_out = b;
 }
 
 // All of a worker's rows in one workgroup, T threads each, and their sums: one launch.

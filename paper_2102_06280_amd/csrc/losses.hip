@@ -130,8 +130,9 @@ void by_length(int64_t bytes, F f)
 }
 int pieces_of(const dbw_logits *l) { return l->vocab / (16 / (int)size_of(l->type)); }
 
-// Few rows are read in slices: 1 x 131072 8.4, by one workgroup 11.4 (its exponentials alone take 6); 300 x 100000 16.9 and 22.6; 1024 x 100000 42.6
-// and 45.7.
+// Few long rows are read in slices: 1 x 131072 9.2, by one workgroup 11.6 (its exponentials alone take 6); 200 x 80000 11.8 and 13.2, 700 x 80000 26.7
+// and 32.3.  Shorter ones are not, where a launch has to join the slices: 1 x 50000 9.4, whole 7.4; 200 x 5000 9.4 and 5.8.
+constexpr int64_t LONG_ROW = 128 << 10;
 constexpr int SLICE_LONG = 2048;                          // pieces of a slice from which threads take eight at a time
 loss::Slices slices_of(const dbw_logits *l, int64_t rows, int most_rows, int groups)
 {
@@ -213,13 +214,15 @@ void launch_logp(const dbw_logits *l, const Shape &S, const loss::Logp &P, bool 
         else by_length(S.row_bytes, launch);
     });
 }
-void launch_gradient(const dbw_logits *l, const Shape &S, const loss::Gradient &P, hipStream_t s)
+// pairs: what the kernel sums pairs up from by itself, or null
+void launch_gradient(const dbw_logits *l, const Shape &S, const loss::Gradient &P, const loss::Preference *pairs, hipStream_t s)
 {
     by_type(l->type, [&](auto e) {
+        typedef decltype(e) E;
         by_gradient_slice(P.slices, S.row_bytes, [&](auto p) {
-            hipLaunchKernelGGL((loss::gradient_kernel<decltype(e), p.T, p.C>),
-                               grid_of((S.rows * P.slices.count + p.ROWS - 1) / p.ROWS + (P.pairs.loss_out ? P.pairs.workers : 0)), dim3(p.THREADS),
-                               0, s, S.R, P);
+            const dim3 grid = grid_of((S.rows * P.slices.count + p.ROWS - 1) / p.ROWS + (P.pairs.loss_out ? P.pairs.workers : 0)), block(p.THREADS);
+            if (pairs) hipLaunchKernelGGL((loss::pair_gradient_kernel<E, p.T, p.C>), grid, block, 0, s, S.R, P, *pairs);
+            else hipLaunchKernelGGL((loss::gradient_kernel<E, p.T, p.C>), grid, block, 0, s, S.R, P);
         });
     });
 }
@@ -243,7 +246,7 @@ extern "C" int dbw_token_logp(const dbw_logits *shape, const void *logits, const
     if (S.rows == 0) return DBW_OK;
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
-    const loss::Slices slices = slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS);
+    const loss::Slices slices = S.row_bytes > LONG_ROW ? slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS) : loss::Slices{1, 0};
     const loss::Logp P{tokens, nullptr, logp_out, lse_out, slices.count > 1 ? W.slices : nullptr, W.token_logit, slices};
     launch_logp(shape, S, P, lse_out != nullptr, s);      // L is asked for where a gradient follows
     if (slices.count > 1) hipLaunchKernelGGL(loss::join_kernel, dim3((uint32_t)S.rows), dim3(64), 0, s, S.R, P);
@@ -260,7 +263,7 @@ extern "C" int dbw_token_logp_grad(const dbw_logits *shape, const void *logits, 
     if (S.rows > 0 && (!tokens || !lse || !coef || !dlogits)) return DBW_ERR_NULL;
     if (S.rows == 0) return DBW_OK;
     const loss::Gradient P{tokens, coef, nullptr, lse, gradient_slices_of(shape, S.rows), loss::PairLoss{}};
-    launch_gradient(shape, S, P, (hipStream_t)stream);
+    launch_gradient(shape, S, P, nullptr, (hipStream_t)stream);
     DBW_HIP(hipGetLastError());
     return DBW_OK;
 }
@@ -330,22 +333,32 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
     float *const logp = logp_out ? logp_out : W.logp;
+    // Few rows and short pairs: the gradient's workgroups sum their pairs up themselves, which costs less than a launch in between.  Two to four pairs
+    // of 10 to 250 rows x 80 to 3840 bf16 11.4 us, with the launch 14.7; 128 x 20000 (40 KB) 11.8 and 14.8, but 128 x 60000 20.2 and 15.8: longer rows
+    // are better read in slices, which only the launch joins.
+    const bool few = pairs > 0 && S.rows > 0 && S.rows <= 1024 && S.row_bytes <= 48 << 10 && S.rows <= (int64_t)64 * shape->workers * pairs;
     loss::Slices slices{1, 0};
     if (S.rows > 0) {
-        if (pairs > 0) slices = slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS);  // (whose parts the pairs' kernel joins)
+        if (pairs > 0 && !few) slices = slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS);  // (whose parts the pairs' kernel joins)
         const bool cut = slices.count > 1;
         launch_logp(shape, S, loss::Logp{tokens, weights, logp, nullptr, cut ? W.slices : W.stats, W.token_logit, slices}, dlogits != nullptr, s);
         DBW_HIP(hipGetLastError());
     }
+    const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
     if (pairs > 0) {
         const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.c, pairs, S.rows, logp, margin_out, W.coef,
                                  W.slices, W.stats, W.token_logit, slices.count, status_out};
+        if (few) {
+            if (dlogits) launch_gradient(shape, S, loss::Gradient{tokens, nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, &P, s);
+            else hipLaunchKernelGGL(loss::pair_sums_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, mean, P);
+            DBW_HIP(hipGetLastError());
+            return DBW_OK;
+        }
         hipLaunchKernelGGL(loss::pair_kernel, dim3((uint32_t)(shape->workers * pairs)), dim3(loss::PAIR_THREADS), 0, s, P);
         DBW_HIP(hipGetLastError());
     }
-    const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
     if (dlogits && S.rows > 0)
-        launch_gradient(shape, S, loss::Gradient{tokens, pairs > 0 ? W.coef : nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, s);
+        launch_gradient(shape, S, loss::Gradient{tokens, pairs > 0 ? W.coef : nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, nullptr, s);
     else
         hipLaunchKernelGGL(loss::pair_loss_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, mean);
     DBW_HIP(hipGetLastError());

@@ -520,6 +520,23 @@ def test_preference_over_shapes(B, dtype, n, t, v, pad, shift):
     check_preference(I, start, rf, None, 1, 0.5, 0.0, loss, margin, logp, grad)
 
 
+@pytest.mark.parametrize("dtype,n,t,v,pairs", [(BF16, 3, 70, 500, 1), (BF16, 2, 65, 24000, 1), (F32, 2, 64, 12289, 1), (BF16, 2, 129, 300, 1), (F16, 1, 1030, 120, 20),
+                                               (F32, 7, 9, 2100, 9)])
+def test_preference_pairs_of_many_and_of_few_rows(B, dtype, n, t, v, pairs):
+    """Either side of where a gradient's workgroups sum the pairs up themselves."""
+    I = Inputs(B, dtype, n, t, v, pad=3, left=2)
+    rf = (ref.token_logp(I.x, I.tokens, I.scale) + torch.randn(I.total, generator=I.g)).float()
+    start = cut(I.total, n, t, pairs, v)
+    start[0] += 1                                        # the first row in no sequence
+    start = [max(s, 1) for s in start]
+    grad = I.gradient()
+    loss, margin, logp = run_preference(I, start, rf, None, pairs, 0.2, 0.05, grad)
+    check_preference(I, start, rf, None, pairs, 0.2, 0.05, loss, margin, logp, grad)
+    again = run_preference(I, start, rf, None, pairs, 0.2, 0.05, None)
+    for a, b in zip(again, (loss, margin, logp)):
+        assert torch.equal(a, b)
+
+
 def test_preference_empty_sequences_gaps_and_large_margins(B):
     I = Inputs(B, F32, 1, 10, 60)
     rf = torch.zeros(10)
