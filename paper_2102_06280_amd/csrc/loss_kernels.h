@@ -19,7 +19,7 @@ __device__ __forceinline__ int64_t group() { return (int64_t)blockIdx.y * gridDi
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
 
-// Rows that are a wave's work share a workgroup, or starting workgroups would take longer than the rows.
+// Rows of 64 or 16 threads share a workgroup of 256.
 template <int T>
 constexpr int ROWS_OF = T <= 64 ? 256 / T : 1;
 template <int T>

@@ -111,7 +111,6 @@ template <class F>
 void by_row(int64_t bytes, bool by_16, F f)
 {
     if (by_16) by_short_row(bytes, f);
-    else if (bytes <= 2 * 64 * 16) f(Plan<64, 2>());
     else if (bytes <= 8 * 64 * 16) f(Plan<64, 8>());
     else if (bytes <= 4 * 256 * 16) f(Plan<256, 4>());
     else if (bytes <= 8 * 256 * 16) f(Plan<256, 8>());
@@ -181,9 +180,9 @@ void by_gradient_slice(const loss::Slices &slices, int64_t row_bytes, F f)
 int one_group_threads(const dbw_logits *l, int64_t row_bytes, int turns)
 {
     const int T = row_bytes <= SHORT_ROW ? 16 : 64;
-    if (l->rows < 1 || row_bytes > 8 * 64 * 16 || l->rows * T > turns * 1024 || l->rows * row_bytes > 64 << 10) return 0;
-    const int threads = (l->rows * T + 63) / 64 * 64;
-    return threads < 1024 ? threads : 1024;
+    const int64_t threads = ((int64_t)l->rows * T + 63) / 64 * 64;
+    if (l->rows < 1 || row_bytes > 8 * 64 * 16 || threads > turns * 1024 || l->rows * row_bytes > 64 << 10) return 0;
+    return threads < 1024 ? (int)threads : 1024;
 }
 template <class F>
 void by_group_row(int64_t bytes, F f)
