@@ -126,8 +126,8 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
         if (s == 0) P.token_logit[r] = xy;
         return;
     }
-    if (P.logp_out) P.logp_out[r] = LN2 * log2_p(xy, R.c, mz);
-    if (P.lse_out) P.lse_out[r] = fmaf(R.scale, mz.m, LN2 * log2f(mz.z));
+    if (P.logp_out) P.logp_out[r] = log_p(xy, R.scale, mz);
+    if (P.lse_out) P.lse_out[r] = fmaf(R.scale, mz.m, logf(mz.z));
     if (P.stats) P.stats[r] = mz;
 }
 
@@ -138,15 +138,15 @@ __global__ __launch_bounds__(64) void join_kernel(Rows R, Logp P)
     float logp = 0.f, lse = 0.f;
     if (takes_part(P, r)) {
         const MaxSum mz = joined<64>(P.stats + r * P.slices.count, P.slices.count, R.c);
-        logp = LN2 * log2_p(P.token_logit[r], R.c, mz);
-        lse = fmaf(R.scale, mz.m, LN2 * log2f(mz.z));
+        logp = log_p(P.token_logit[r], R.scale, mz);
+        lse = fmaf(R.scale, mz.m, logf(mz.z));
     }
     if (threadIdx.x != 0) return;
     if (P.logp_out) P.logp_out[r] = logp;
     if (P.lse_out) P.lse_out[r] = lse;
 }
 
-// dx_v = by 2^(c x - M) over pieces first ... end - 1, T C at a time, and coef more at column y if that is among them.
+// dx_v = by 2^(c (x - m)) over pieces first ... end - 1, T C at a time, and coef more at column y if that is among them.
 template <class E, int T, int C>
 __device__ __forceinline__ void slice_gradient(const Rows &R, const RowOf<E, T> &row, int64_t r, int first, int end, float by, Base b, int y,
                                                float coef)
@@ -156,7 +156,7 @@ __device__ __forceinline__ void slice_gradient(const Rows &R, const RowOf<E, T> 
     const int yp = row.piece_of(y);
     const bool mine = tid<T>() == row.owner(y) && (yp < 0 ? singles : yp >= first && yp < end);
     const float xy = mine ? widen(row.x[y]) : 0.f, single = singles ? row.load_single() : 0.f;
-    b = Base{uniform<T>(b.c), uniform<T>(b.M), false};
+    b = Base{uniform<T>(b.c), uniform<T>(b.m)};
     by = uniform<T>(by);
     const global_access::bytes out = base_address<T>(dx + row.before);
     for (; first < end; first += T * C) {
@@ -174,7 +174,7 @@ __device__ __forceinline__ void slice_gradient(const Rows &R, const RowOf<E, T> 
 struct Preference {
     const int32_t *tokens, *seq_start;
     const float *ref_logp, *weights;
-    float beta, smoothing, c;
+    float beta, smoothing, scale, c;
     int pairs;           // of each worker
     int64_t all_rows;
     float *logp, *margin_out, *coef;
@@ -227,7 +227,7 @@ __device__ __forceinline__ void join_rows(const Preference &P, int from, int to)
         float logp = 0.f;
         if (takes_part(P, r)) {
             const MaxSum mz = joined<T>(P.stats + (int64_t)r * P.slices, P.slices, P.c);
-            logp = LN2 * log2_p(P.token_logit[r], P.c, mz);
+            logp = log_p(P.token_logit[r], P.scale, mz);
             if (first) P.joined[r] = mz;
         }
         if (first) P.logp[r] = logp;
@@ -310,9 +310,8 @@ __device__ __forceinline__ void gradient_of_slice(const Rows &R, const Gradient 
         const MaxSum mz = P.stats[r];
         b = base_of(mz.m, R.c);
         by /= mz.z;
-    } else {                                              // from L: M = L log2(e), Z = 1
-        b = base_of(P.lse[r] / R.scale, R.c);
-        if (!b.steep) b.M = P.lse[r] * LOG2E;
+    } else {
+        b = base_of(P.lse[r] / R.scale, R.c);             // from L: as if m = L / s and Z = 1
     }
     int first, end;
     slice_of(P.slices, s, row.pieces, first, end);
@@ -456,7 +455,7 @@ __device__ __forceinline__ float2 policy_whole_row(const Rows &R, const Policy &
     const int y = column(R, P.tokens[r]);
     const float xy = widen(x[y]);
     const MaxSum mz = walk.stats(R.c, lds);
-    const float logp = LN2 * log2_p(xy, R.c, mz);
+    const float logp = log_p(xy, R.scale, mz);
     const PolicyRow p = policy_of(P, figures, logp);
     if (tid<T>() == 0 && P.logp_out) P.logp_out[r] = logp;
     if (R.dx) {
@@ -510,7 +509,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
             const float w = weight_of(P, r);
             float logp = 0.f;
             if (w != 0.f) {
-                logp = LN2 * log2_p(P.token_logit[r], R.c, joined<16>(P.stats + r * P.parts, P.parts, R.c));
+                logp = log_p(P.token_logit[r], R.scale, joined<16>(P.stats + r * P.parts, P.parts, R.c));
                 const PolicyRow p = policy_of(P, figures_of(P, r, w), logp);
                 if (threadIdx.x % 16 == 0) {
                     loss += p.loss;
@@ -529,7 +528,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
     MaxSum mz;
     if (w != 0.f) {
         mz = joined<64>(P.stats + r * P.parts, P.parts, R.c);
-        coef = R.scale * policy_of(P, figures_of(P, r, w), LN2 * log2_p(P.token_logit[r], R.c, mz)).slope;
+        coef = R.scale * policy_of(P, figures_of(P, r, w), log_p(P.token_logit[r], R.scale, mz)).slope;
     }
     if (coef == 0.f) {
         zero_pieces<E, T>(R, r, s * P.slices.pieces, s == n - 1 ? INT32_MAX : (s + 1) * P.slices.pieces);
@@ -659,8 +658,7 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
         const MaxSum in = row_merge<T>(MaxSum{m_top, lanes_sum<T>(z_top)}, R.c, lds_top);
         const MaxSum out = walk.template stats<true>(R.c, lds, (const uint8_t *)in_top);
         mz = merged(out, in, R.c);
-        const Base a = base_of(out.m, R.c), b = base_of(mz.m, R.c);
-        log_out = LN2 * ((a.steep || b.steep ? (out.m - mz.m) * R.c : a.M - b.M) + (log2f(out.z) - log2f(mz.z)));
+        log_out = R.scale * (out.m - mz.m) + (logf(out.z) - logf(mz.z));
     } else {
         mz = walk.stats(R.c, lds);
     }
@@ -670,7 +668,7 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     for (int j = t; j < P.k; j += T)
         if (at[j] >= 0) {
             const float log2_q = TAIL ? fmaf(q[j], R.c, -norm) : (q[j] - from) * R.c - norm, qj = __builtin_amdgcn_exp2f(log2_q);
-            const float log2_p = (base.steep ? (xs[j] - mz.m) * R.c : fmaf(xs[j], base.c, -base.M)) - log2_z;
+            const float log2_p = (xs[j] - mz.m) * R.c - log2_z;
             mass += qj;
             if (!(qj <= 0.f)) part += qj * (log2_q - log2_p);
             q[j] = __builtin_amdgcn_exp2f(log2_p) - qj;   // dl/dx over s

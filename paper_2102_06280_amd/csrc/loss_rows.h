@@ -1,8 +1,9 @@
 // Device side of the losses on rows of logits.
 //
-// With c = s log2(e), m the largest logit of a row and M = c m (rounded once, the same number everywhere), the row's sum is
-// Z = sum_v 2^(c x_v - M), so that log p_y = ln 2 (c x_y - M - log2 Z) and p_v = 2^(c x_v - M) / Z.  Keeping (m, Z) and not L = ln 2 (M + log2 Z)
-// keeps the rounding of a large L (2^-24 |L|), and that of M, out of every probability.
+// With c = s log2(e) and m the largest logit of a row, the row's sum is Z = sum_v 2^(c (x_v - m)), so that log p_y = s (x_y - m) - ln Z and
+// p_v = 2^(c (x_v - m)) / Z.  The difference comes first: the largest term is exactly 1, logits may be of any size (masks of a type's lowest value), and
+// keeping (m, Z) and not L = s m + ln Z keeps the rounding of a large L (2^-24 |L|) out of every probability.  A multiply-add of c x - c m
+// would save an instruction of about a dozen, and no time where memory is the bound.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -64,34 +65,12 @@ __device__ __forceinline__ int column(const Rows &R, int token)
     return R.vocab - 1;
 }
 
-// What a row's exponentials count from: 2^(c x - M).
-//
-// The rounding of M moves all of them by 2^(u |M|) and cancels in every ratio, but must not overflow: |M| <= 2^30 keeps it within 2^64.  Beyond,
-// the next number below m is at least 64 octaves away, so that nothing but the largest logits counts; then c is a power of two that
-// makes c m exact and a step below m 2^9 octaves (also where c m itself overflows, as in a row of the type's lowest value).
-// A row of nothing but -inf so far counts from 0: its terms are 2^-inf = 0 and not 2^NaN.
+// What a row's exponentials count from: 2^(c (x - m)).  A row of nothing but -inf so far counts from 0: its terms are 2^-inf = 0 and not 2^NaN.
 struct Base {
-    float c, M;
-    bool steep;      // the largest logits only
+    float c, m;
 };
-constexpr float STEEP = 1073741824.f;
-__device__ __forceinline__ Base base_of(float m, float c)
-{
-    if (m == -INFINITY) return Base{c, 0.f, false};
-    const float M = m * c;
-    if (!(fabsf(M) > STEEP) || isinf(m)) return Base{c, M, false};
-    const float unit = ldexpf(1.f, 32 - ilogbf(m));
-    return Base{unit, m * unit, true};
-}
-__device__ __forceinline__ float power(float x, const Base &b) { return __builtin_amdgcn_exp2f(fmaf(x, b.c, -b.M)); }
-
-// log2 of a probability, from its logit and the row's (m, Z)
-template <class MZ>
-__device__ __forceinline__ float log2_p(float x, float c, const MZ &mz)
-{
-    const Base b = base_of(mz.m, c);
-    return (b.steep ? (x - mz.m) * c : fmaf(x, c, -b.M)) - log2f(mz.z);
-}
+__device__ __forceinline__ Base base_of(float m, float c) { return Base{c, m == -INFINITY ? 0.f : m}; }
+__device__ __forceinline__ float power(float x, const Base &b) { return __builtin_amdgcn_exp2f((x - b.m) * b.c); }
 
 // A row is T threads' work; a workgroup has T threads, or several rows of 64 or 16 threads each.
 template <int T>
@@ -164,13 +143,13 @@ __device__ __forceinline__ float wave_sum(float v) { return lanes_sum<64>(v); }
 struct MaxSum {
     float m, z;
 };
+// The log of a probability, from its logit and the row's (m, Z)
+__device__ __forceinline__ float log_p(float x, float scale, const MaxSum &mz) { return scale * (x - mz.m) - logf(mz.z); }
 // The factor that takes a sum from its own maximum to another, not smaller one.
 __device__ __forceinline__ float rescale(float from, float to, float c)
 {
     if (from == to) return 1.f;
-    if (from == -INFINITY) return 0.f;
-    const Base a = base_of(from, c), b = base_of(to, c);
-    return a.steep || b.steep ? 0.f : __builtin_amdgcn_exp2f(a.M - b.M);
+    return from == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((from - to) * c);
 }
 __device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, float c)
 {
@@ -422,14 +401,14 @@ __device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, in
     z *= rescale(m, top, c);
     m = top;
     const Base base = base_of(m, c);
-    const Base b{uniform<T>(base.c), uniform<T>(base.M), false};
+    const Base b{uniform<T>(base.c), uniform<T>(base.m)};
     z += power(single, b);
     keep_packed(r);
 #pragma unroll
     for (int i = 0; i < C; ++i) z += piece_sum<E>(r[i], b);
 }
 
-// Piece i of the gradient of those from `first` on: by 2^(c x - M).
+// Piece i of the gradient of those from `first` on: by 2^(c (x - m)).
 // LATER: parts of the row are going to be written over, so it stays in the L2 for a while.
 template <class E, int T, bool LATER = false>
 __device__ __forceinline__ void store_piece(global_access::bytes base, int first, int end, int i, const u32x4 &r, float by, const Base &b)
@@ -503,11 +482,11 @@ struct Walk {
             }
         return row_merge<T>(MaxSum{m, lanes_sum<T>(z)}, c, lds);
     }
-    // dx_v = by 2^(c x - M), and coef more at column y (none if negative)
+    // dx_v = by 2^(c (x - m)), and coef more at column y (none if negative)
     template <bool LATER = false>
     __device__ __forceinline__ void gradient(E *dx, float by, const Base &base, int y, float xy, float coef)
     {
-        const Base b{uniform<T>(base.c), uniform<T>(base.M), false};
+        const Base b{uniform<T>(base.c), uniform<T>(base.m)};
         by = uniform<T>(by);
         const global_access::bytes out = base_address<T>(dx + row.before);
         if constexpr (S > 0)

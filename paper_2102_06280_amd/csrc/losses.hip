@@ -345,7 +345,7 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     }
     const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
     if (pairs > 0) {
-        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.c, pairs, S.rows, logp, margin_out, W.coef,
+        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, S.rows, logp, margin_out, W.coef,
                                  W.slices, W.stats, W.token_logit, slices.count, status_out};
         if (few) {
             if (dlogits) launch_gradient(shape, S, loss::Gradient{tokens, nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, &P, s);
