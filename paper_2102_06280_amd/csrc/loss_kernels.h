@@ -53,7 +53,7 @@ __device__ __forceinline__ MaxSum joined(const MaxSum *slices, int count, float 
     for (int s = tid<T>(); s < count; s += T) own = merged(own, slices[s], c);
     if (T == 1) return own;
     const float m = lanes_max<T>(own.m);
-    return MaxSum{m, lanes_sum<T>(own.z * rescale(own.m, m, c))};
+    return MaxSum{m, (float)lanes_sum<T>((double)(own.z * rescale(own.m, m, c)))};
 }
 constexpr int MAX_SLICES = 32;
 
@@ -105,13 +105,14 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
     const RowOf<E, T> row(x, R.vocab);
     int first, end;
     slice_of(P.slices, s, row.pieces, first, end);
-    float m = -INFINITY, z = 0.f;
+    float m = -INFINITY;
+    double sum = 0.;
     for (; first < end; first += T * C) {
         u32x4 v[C];
         row.template load<C, !AGAIN>(first, v);
-        add_pieces<false>(row, first, end, v, -INFINITY, nullptr, R.c, m, z);
+        add_pieces<false>(row, first, end, v, -INFINITY, nullptr, R.c, m, sum);
     }
-    z = lanes_sum<T>(z);
+    float z = (float)lanes_sum<T>(sum);
     if (s == 0) {
         const float single = row.load_single(), top = lanes_max<T>(single);
         const MaxSum both = merged(MaxSum{m, z}, MaxSum{top, lanes_sum<T>(power(single, base_of(top, R.c)))}, R.c);

@@ -136,6 +136,34 @@ __device__ __forceinline__ float lanes_sum(float v)
     v += shifted<0x143, 0xc>(v, 0.f);
     return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(v), 63));
 }
+// The same in 64 bits.
+template <int CTRL, int ROWS>
+__device__ __forceinline__ double shifted(double v)
+{
+    const int64_t b = __double_as_longlong(v);
+    const uint32_t lo = __builtin_amdgcn_update_dpp(0, (int)b, CTRL, ROWS, 0xf, false);
+    const uint32_t hi = __builtin_amdgcn_update_dpp(0, (int)(b >> 32), CTRL, ROWS, 0xf, false);
+    return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+template <int T>
+__device__ __forceinline__ double lanes_sum(double v)
+{
+    if (T == 16) {
+        v += shifted<0x121, 0xf>(v);
+        v += shifted<0x122, 0xf>(v);
+        v += shifted<0x124, 0xf>(v);
+        return v + shifted<0x128, 0xf>(v);
+    }
+    v += shifted<0x111, 0xf>(v);
+    v += shifted<0x112, 0xf>(v);
+    v += shifted<0x114, 0xf>(v);
+    v += shifted<0x118, 0xf>(v);
+    v += shifted<0x142, 0xa>(v);
+    v += shifted<0x143, 0xc>(v);
+    const int64_t b = __double_as_longlong(v);
+    const uint32_t lo = __builtin_amdgcn_readlane((int)b, 63), hi = __builtin_amdgcn_readlane((int)(b >> 32), 63);
+    return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
 __device__ __forceinline__ float wave_max(float v) { return lanes_max<64>(v); }
 __device__ __forceinline__ float wave_sum(float v) { return lanes_sum<64>(v); }
 
@@ -167,9 +195,9 @@ __device__ __forceinline__ MaxSum row_merge(MaxSum v, float c, MaxSum *lds)
     __syncthreads();
     float m = lds[0].m;
     for (int w = 1; w < T / 64; ++w) m = fmaxf(m, lds[w].m);
-    float z = 0.f;
-    for (int w = 0; w < T / 64; ++w) z += lds[w].z * rescale(lds[w].m, m, c);
-    return MaxSum{uniform<T>(m), uniform<T>(z)};
+    double z = 0.;
+    for (int w = 0; w < T / 64; ++w) z += (double)(lds[w].z * rescale(lds[w].m, m, c));
+    return MaxSum{uniform<T>(m), uniform<T>((float)z)};
 }
 template <int T>
 __device__ __forceinline__ float row_sum(float v, float *lds)
@@ -373,19 +401,24 @@ __device__ __forceinline__ float piece_max(const u32x4 &r, float top)
 template <class E>
 __device__ __forceinline__ float piece_sum(const u32x4 &r, const Base &b)
 {
-    float v[Piece<E>::N], sum = 0.f;
+    float v[Piece<E>::N];
     Piece<E>::unpack(r, v);
 #pragma unroll
-    for (int j = 0; j < Piece<E>::N; ++j) sum += power(v[j], b);
-    return sum;
+    for (int j = 0; j < Piece<E>::N; ++j) v[j] = power(v[j], b);
+#pragma unroll
+    for (int d = 1; d < Piece<E>::N; d *= 2)
+#pragma unroll
+        for (int j = 0; j < Piece<E>::N; j += 2 * d) v[j] += v[j + d];
+    return v[0];
 }
 
-// Adds the pieces from `first` on to a wave's maximum and a lane's sum.  The maximum is the wave's and not the lane's, so that what the
+// Adds the pieces from `first` on to a wave's maximum and a lane's sum, which is held in 64 bits: where one token is almost certain the sum is little more
+// than one, and each addition in 32 bits would cost the log-probability another 2^-25.  The maximum is the wave's and not the lane's, so that what the
 // exponentials count from is one number in scalar registers.
 // left_out: bits of columns that are left out of the sum (LEAVE); column v has bit v - row.before + N, so that a piece's bits are together.
 template <bool LEAVE, class E, int T, int C>
 __device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, int end, u32x4 (&r)[C], float single, const uint8_t *left_out, float c,
-                                           float &m, float &z)
+                                           float &m, double &z)
 {
     float top = single;
 #pragma unroll
@@ -405,7 +438,7 @@ __device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, in
     z += power(single, b);
     keep_packed(r);
 #pragma unroll
-    for (int i = 0; i < C; ++i) z += piece_sum<E>(r[i], b);
+    for (int i = 0; i < C; ++i) z += (double)piece_sum<E>(r[i], b);
 }
 
 // Piece i of the gradient of those from `first` on: by 2^(c (x - m)).
@@ -468,7 +501,8 @@ struct Walk {
     template <bool LEAVE = false>
     __device__ __forceinline__ MaxSum stats(float c, MaxSum *lds, const uint8_t *left_out = nullptr)
     {
-        float m = -INFINITY, z = 0.f;
+        float m = -INFINITY;
+        double z = 0.;
         if (LEAVE) {
             const int bit = row.single_column() - row.before + Piece<E>::N;
             if (row.has_single() && (left_out[bit >> 3] >> (bit & 7) & 1)) single = -INFINITY;
@@ -480,7 +514,7 @@ struct Walk {
                 row.template load<S, false>(first, v);
                 add_pieces<LEAVE>(row, first, row.pieces, v, -INFINITY, left_out, c, m, z);
             }
-        return row_merge<T>(MaxSum{m, lanes_sum<T>(z)}, c, lds);
+        return row_merge<T>(MaxSum{m, (float)lanes_sum<T>(z)}, c, lds);
     }
     // dx_v = by 2^(c (x - m)), and coef more at column y (none if negative)
     template <bool LATER = false>
