@@ -11,7 +11,7 @@
  * gradients are fp32, bf16 or fp16 and need no alignment beyond an element's; V and ld may be odd.  With s = `scale` (one
  * over the temperature) the model's distribution in a row x is p_v = exp(s x_v - L), L = log sum_v exp(s x_v).
  *
- * Precision.  Exponentials, sums, losses and gradients are computed in fp32; a gradient is rounded once to the type of the
+ * Precision.  Exponentials, losses and gradients are computed in fp32, sums in fp32 or more; a gradient is rounded once to the type of the
  * logits.  No sum depends on the order in which workgroups run: the same call gives the same bits.
  *
  * Rows that take no part.  A row whose token is negative or whose weight is 0 is not read: whatever its logits and its
