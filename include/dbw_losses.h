@@ -12,7 +12,8 @@
  * over the temperature) the model's distribution in a row x is p_v = exp(s x_v - L), L = log sum_v exp(s x_v).
  *
  * Precision.  Exponentials, losses and gradients are computed in fp32, sums in fp32 or more; a gradient is rounded once to the type of the
- * logits.  No sum depends on the order in which workgroups run: the same call gives the same bits.
+ * logits.  A log-probability is off by about 2^-24 before it is rounded to fp32, to either side alike, and enters a preference loss's sums before
+ * that rounding: they are held in 64 bits.  No sum depends on the order in which workgroups run: the same call gives the same bits.
  *
  * Rows that take no part.  A row whose token is negative or whose weight is 0 is not read: whatever its logits and its
  * other inputs hold (infinities, NaN), it adds nothing to any sum, its log-probability is given as 0 and its gradient

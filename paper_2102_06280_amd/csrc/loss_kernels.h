@@ -47,7 +47,7 @@ __device__ __forceinline__ void slice_of(const Slices &S, int s, int pieces, int
 }
 // A row's (m, Z) from its slices', on every one of T = 1, 16 or 64 lanes.
 template <int T>
-__device__ __forceinline__ MaxSum joined(const MaxSum *slices, int count, float c)
+__device__ __forceinline__ MaxSum joined(const MaxSum *slices, int count, const Factor &c)
 {
     MaxSum own{-INFINITY, 0.f};
     for (int s = tid<T>(); s < count; s += T) own = merged(own, slices[s], c);
@@ -78,11 +78,19 @@ struct Logp {
     const int32_t *tokens;
     const float *weights;// null: no row is left out for its weight
     float *logp_out, *lse_out;
+    float *low;          // what rounding to 32 bits took off every log-probability, or null
     MaxSum *stats;       // (m, Z) of every slice, or null
     float *token_logit;  // of every row where there are slices
     Slices slices;
 };
 
+// A log-probability in 32 bits, and what that leaves of it
+__device__ __forceinline__ void store_logp(double l, float *logp, float *low)
+{
+    const float rounded = (float)l;
+    *logp = rounded;
+    if (low) *low = isinf(rounded) ? 0.f : (float)(l - rounded);
+}
 __device__ __forceinline__ bool takes_part(const Logp &P, int64_t r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
 
 // A workgroup a row, or a slice: one pass, the maximum and the sum of a batch after the other.  Bound by memory: 4096 x 65536 bf16 79 us, 6.2 TB/s; a single
@@ -127,8 +135,8 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
         if (s == 0) P.token_logit[r] = xy;
         return;
     }
-    if (P.logp_out) P.logp_out[r] = log_p(xy, R.scale, mz);
-    if (P.lse_out) P.lse_out[r] = fmaf(R.scale, mz.m, logf(mz.z));
+    if (P.logp_out) store_logp(log_p(xy, R.scale, mz), P.logp_out + r, P.low ? P.low + r : nullptr);
+    if (P.lse_out) P.lse_out[r] = (float)log_sum(R.scale, mz);
     if (P.stats) P.stats[r] = mz;
 }
 
@@ -139,8 +147,8 @@ __global__ __launch_bounds__(64) void join_kernel(Rows R, Logp P)
     float logp = 0.f, lse = 0.f;
     if (takes_part(P, r)) {
         const MaxSum mz = joined<64>(P.stats + r * P.slices.count, P.slices.count, R.c);
-        logp = log_p(P.token_logit[r], R.scale, mz);
-        lse = fmaf(R.scale, mz.m, logf(mz.z));
+        logp = (float)log_p(P.token_logit[r], R.scale, mz);
+        lse = (float)log_sum(R.scale, mz);
     }
     if (threadIdx.x != 0) return;
     if (P.logp_out) P.logp_out[r] = logp;
@@ -157,7 +165,7 @@ __device__ __forceinline__ void slice_gradient(const Rows &R, const RowOf<E, T> 
     const int yp = row.piece_of(y);
     const bool mine = tid<T>() == row.owner(y) && (yp < 0 ? singles : yp >= first && yp < end);
     const float xy = mine ? widen(row.x[y]) : 0.f, single = singles ? row.load_single() : 0.f;
-    b = Base{uniform<T>(b.c), uniform<T>(b.m)};
+    b = uniform<T>(b);
     by = uniform<T>(by);
     const global_access::bytes out = base_address<T>(dx + row.before);
     for (; first < end; first += T * C) {
@@ -175,10 +183,13 @@ __device__ __forceinline__ void slice_gradient(const Rows &R, const RowOf<E, T> 
 struct Preference {
     const int32_t *tokens, *seq_start;
     const float *ref_logp, *weights;
-    float beta, smoothing, scale, c;
+    float beta, smoothing, scale;
+    Factor c;
     int pairs;           // of each worker
     int64_t all_rows;
     float *logp, *margin_out, *coef;
+    float *low;          // what log-probabilities have lost to 32 bits: of a sum over a sequence it is the larger part of the error.  The same memory as
+                         // coef, which a pair needs when its sums are known
     MaxSum *stats;       // of every slice, and where rows have several
     MaxSum *joined;      // of every row
     const float *token_logit;
@@ -199,12 +210,12 @@ __device__ __forceinline__ void rows_of_pair(const Preference &P, int64_t j, int
     a[2] = min(max(a[2], a[1]), n);
 }
 // A thread's part, one of `threads`, of the difference between the pair's summed log ratios.
-__device__ __forceinline__ float part_of_pair(const Preference &P, const int (&a)[3], int thread, int threads)
+__device__ __forceinline__ double part_of_pair(const Preference &P, const int (&a)[3], int thread, int threads)
 {
-    float h = 0.f;
+    double h = 0.;
     for (int r = a[0] + thread; r < a[2]; r += threads)
         if (takes_part(P, r)) {
-            const float term = (P.weights ? P.weights[r] : 1.f) * (P.logp[r] - P.ref_logp[r]);
+            const double term = (P.weights ? P.weights[r] : 1.f) * ((double)P.logp[r] - P.ref_logp[r] + P.low[r]);
             h += r < a[1] ? term : -term;
         }
     return h;
@@ -225,13 +236,13 @@ __device__ __forceinline__ void join_rows(const Preference &P, int from, int to)
 {
     const bool first = threadIdx.x % T == 0;
     for (int r = from + (int)threadIdx.x / T; r < to; r += PAIR_THREADS / T) {
-        float logp = 0.f;
+        double logp = 0.;
         if (takes_part(P, r)) {
             const MaxSum mz = joined<T>(P.stats + (int64_t)r * P.slices, P.slices, P.c);
             logp = log_p(P.token_logit[r], P.scale, mz);
             if (first) P.joined[r] = mz;
         }
-        if (first) P.logp[r] = logp;
+        if (first) store_logp(logp, P.logp + r, P.low + r);
     }
 }
 
@@ -240,7 +251,7 @@ __device__ __forceinline__ void join_rows(const Preference &P, int from, int to)
 // the first and the last pair's.
 __global__ __launch_bounds__(PAIR_THREADS) void pair_kernel(Preference P)
 {
-    __shared__ float lds[PAIR_THREADS / 64];
+    __shared__ double lds[PAIR_THREADS / 64];
     const int64_t j = blockIdx.x;
     const int t = threadIdx.x, n = (int)P.all_rows;
     int a[3];
@@ -251,7 +262,7 @@ __global__ __launch_bounds__(PAIR_THREADS) void pair_kernel(Preference P)
         else join_rows<1>(P, from, to);
         __syncthreads();
     }
-    const float u = P.beta * row_sum<PAIR_THREADS>(part_of_pair(P, a, t, PAIR_THREADS), lds);
+    const float u = (float)(P.beta * row_sum<PAIR_THREADS>(part_of_pair(P, a, t, PAIR_THREADS), lds));
     if (t == 0) P.margin_out[j] = u;
     const float slope = slope_of(P, u);
     for (int r = from + t; r < to; r += PAIR_THREADS)
@@ -345,7 +356,7 @@ __device__ __forceinline__ void sums_of_pairs(const PairLoss &P, const Preferenc
     float loss = 0.f;
     for (int j = wave_id(); j < Q.pairs; j += WAVES) {
         rows_of_pair(Q, worker * Q.pairs + j, a);
-        const float u = Q.beta * wave_sum(part_of_pair(Q, a, threadIdx.x & 63, 64));
+        const float u = (float)(Q.beta * wave_sum(part_of_pair(Q, a, threadIdx.x & 63, 64)));
         if ((threadIdx.x & 63) == 0) Q.margin_out[worker * Q.pairs + j] = u;
         loss += loss_of(P, u);
     }
@@ -386,7 +397,7 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void pair_gradient_kernel(Rows R, G
         const int q = (int)lanes_sum<LANES>(starts) - 1;
         if (q >= 0) {
             rows_of_pair(Q, q / 2, a);
-            const float slope = slope_of(Q, Q.beta * lanes_sum<LANES>(part_of_pair(Q, a, lane, LANES)));
+            const float slope = slope_of(Q, (float)(Q.beta * lanes_sum<LANES>(part_of_pair(Q, a, lane, LANES))));
             if (r >= a[0] && r < a[2]) g = R.scale * (r < a[1] ? slope : -slope) * (Q.weights ? Q.weights[r] : 1.f);
         }
     }
@@ -456,7 +467,7 @@ __device__ __forceinline__ float2 policy_whole_row(const Rows &R, const Policy &
     const int y = column(R, P.tokens[r]);
     const float xy = widen(x[y]);
     const MaxSum mz = walk.stats(R.c, lds);
-    const float logp = log_p(xy, R.scale, mz);
+    const float logp = (float)log_p(xy, R.scale, mz);
     const PolicyRow p = policy_of(P, figures, logp);
     if (tid<T>() == 0 && P.logp_out) P.logp_out[r] = logp;
     if (R.dx) {
@@ -510,7 +521,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
             const float w = weight_of(P, r);
             float logp = 0.f;
             if (w != 0.f) {
-                logp = log_p(P.token_logit[r], R.scale, joined<16>(P.stats + r * P.parts, P.parts, R.c));
+                logp = (float)log_p(P.token_logit[r], R.scale, joined<16>(P.stats + r * P.parts, P.parts, R.c));
                 const PolicyRow p = policy_of(P, figures_of(P, r, w), logp);
                 if (threadIdx.x % 16 == 0) {
                     loss += p.loss;
@@ -529,7 +540,7 @@ __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
     MaxSum mz;
     if (w != 0.f) {
         mz = joined<64>(P.stats + r * P.parts, P.parts, R.c);
-        coef = R.scale * policy_of(P, figures_of(P, r, w), log_p(P.token_logit[r], R.scale, mz)).slope;
+        coef = R.scale * policy_of(P, figures_of(P, r, w), (float)log_p(P.token_logit[r], R.scale, mz)).slope;
     }
     if (coef == 0.f) {
         zero_pieces<E, T>(R, r, s * P.slices.pieces, s == n - 1 ? INT32_MAX : (s + 1) * P.slices.pieces);
@@ -641,7 +652,7 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     const float from = top == -INFINITY ? 0.f : top;      // differences of logits first: they may be of any size
     for (int j = t; j < P.k; j += T)
         if (at[j] >= 0) {
-            sum += __builtin_amdgcn_exp2f((q[j] - from) * R.c);
+            sum += power(q[j], Base{R.c, from});
             z_top += power(xs[j], base_top);
         }
     sum = row_sum<T>(sum, sums[2]);
@@ -664,17 +675,17 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
         mz = walk.stats(R.c, lds);
     }
     const Base base = base_of(mz.m, R.c);
-    const float log2_z = log2f(mz.z), norm = TAIL ? P.teacher_lse[r] * LOG2E : log2f(sum);
+    const float log2_z = log2f(mz.z), norm = TAIL ? P.teacher_lse[r] * (float)LOG2E : log2f(sum);
     float part = 0.f, mass = 0.f;
     for (int j = t; j < P.k; j += T)
         if (at[j] >= 0) {
-            const float log2_q = TAIL ? fmaf(q[j], R.c, -norm) : (q[j] - from) * R.c - norm, qj = __builtin_amdgcn_exp2f(log2_q);
-            const float log2_p = (xs[j] - mz.m) * R.c - log2_z;
+            const float log2_q = TAIL ? fmaf(q[j], R.c.hi, -norm) : times(R.c, q[j] - from) - norm, qj = __builtin_amdgcn_exp2f(log2_q);
+            const float log2_p = times(R.c, xs[j] - mz.m) - log2_z;
             mass += qj;
             if (!(qj <= 0.f)) part += qj * (log2_q - log2_p);
             q[j] = __builtin_amdgcn_exp2f(log2_p) - qj;   // dl/dx over s
         }
-    part = LN2 * row_sum<T>(part, sums[3]);
+    part = (float)LN2 * row_sum<T>(part, sums[3]);
     float factor = 1.f;
     if (TAIL) {
         mass = row_sum<T>(mass, sums[0]);                 // (its last use lies several barriers back)

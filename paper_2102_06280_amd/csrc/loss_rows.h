@@ -2,8 +2,9 @@
 //
 // With c = s log2(e) and m the largest logit of a row, the row's sum is Z = sum_v 2^(c (x_v - m)), so that log p_y = s (x_y - m) - ln Z and
 // p_v = 2^(c (x_v - m)) / Z.  The difference comes first: the largest term is exactly 1, logits may be of any size (masks of a type's lowest value), and
-// keeping (m, Z) and not L = s m + ln Z keeps the rounding of a large L (2^-24 |L|) out of every probability.  A multiply-add of c x - c m
-// would save an instruction of about a dozen, and no time where memory is the bound.
+// keeping (m, Z) and not L = s m + ln Z keeps the rounding of a large L (2^-24 |L|) out of every probability.  c is a sum of two numbers: rounded to
+// one it would be off by up to 2^-24 of itself, for all terms of all rows in the same direction, which the sum over a sequence's log-probabilities
+// does not average out (at s = 0.9 every ln Z was 2.9e-7 too large).
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -14,8 +15,8 @@
 
 namespace loss {
 
-constexpr float LOG2E = 1.44269504088896340736f;
-constexpr float LN2 = 0.69314718055994530942f;
+constexpr double LOG2E = 1.44269504088896340736;
+constexpr double LN2 = 0.69314718055994530942;
 
 struct bf16 {
     uint16_t bits;
@@ -40,6 +41,11 @@ __device__ __forceinline__ bf16 narrow<bf16>(float v)
     return bf16{__builtin_bit_cast(uint16_t, b)};
 }
 
+// c = s log2(e) as hi + lo.  hi is below c and lo above zero, so that the exponent of a logit of -inf, -inf hi + -inf lo, is -inf.
+struct Factor {
+    float hi, lo;
+};
+
 // The rows of a call.
 struct Rows {
     const void *x;     // logits
@@ -47,7 +53,8 @@ struct Rows {
     int64_t ld, ld_grad;
     int vocab;
     int64_t rows;      // of all workers
-    float scale, c;    // s, s log2(e)
+    float scale;       // s
+    Factor c;          // s log2(e)
     int32_t *status;
     bool by_xcd;       // workgroups take rows in the XCDs' order
 };
@@ -67,10 +74,12 @@ __device__ __forceinline__ int column(const Rows &R, int token)
 
 // What a row's exponentials count from: 2^(c (x - m)).  A row of nothing but -inf so far counts from 0: its terms are 2^-inf = 0 and not 2^NaN.
 struct Base {
-    float c, m;
+    Factor c;
+    float m;
 };
-__device__ __forceinline__ Base base_of(float m, float c) { return Base{c, m == -INFINITY ? 0.f : m}; }
-__device__ __forceinline__ float power(float x, const Base &b) { return __builtin_amdgcn_exp2f((x - b.m) * b.c); }
+__device__ __forceinline__ Base base_of(float m, const Factor &c) { return Base{c, m == -INFINITY ? 0.f : m}; }
+__device__ __forceinline__ float times(const Factor &c, float d) { return fmaf(d, c.hi, d * c.lo); }      // rounded once, but for 2^-24 of lo's part
+__device__ __forceinline__ float power(float x, const Base &b) { return __builtin_amdgcn_exp2f(times(b.c, x - b.m)); }
 
 // A row is T threads' work; a workgroup has T threads, or several rows of 64 or 16 threads each.
 template <int T>
@@ -100,6 +109,16 @@ __device__ __forceinline__ float uniform(float v)
 {
     return T < 64 ? v : __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(v)));
 }
+template <int T>
+__device__ __forceinline__ double uniform(double v)
+{
+    const int64_t b = __double_as_longlong(v);
+    if (T < 64) return v;
+    const uint32_t lo = __builtin_amdgcn_readfirstlane((int)b), hi = __builtin_amdgcn_readfirstlane((int)(b >> 32));
+    return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
+}
+template <int T>
+__device__ __forceinline__ Base uniform(const Base &b) { return Base{{uniform<T>(b.c.hi), uniform<T>(b.c.lo)}, uniform<T>(b.m)}; }
 // Over the 64 lanes of a wave, without LDS: shifts by 1, 2, 4 and 8 within 16 lanes, then the last lanes of 16 to the next ones.  Over 16 lanes:
 // rotations, which leave the result in all of them.
 template <int T>
@@ -165,21 +184,34 @@ __device__ __forceinline__ double lanes_sum(double v)
     return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
 }
 __device__ __forceinline__ float wave_max(float v) { return lanes_max<64>(v); }
-__device__ __forceinline__ float wave_sum(float v) { return lanes_sum<64>(v); }
+template <class V>
+__device__ __forceinline__ V wave_sum(V v) { return lanes_sum<64>(v); }
 
 // A maximum and the sum of exponentials that count from it.
 struct MaxSum {
     float m, z;
 };
-// The log of a probability, from its logit and the row's (m, Z)
-__device__ __forceinline__ float log_p(float x, float scale, const MaxSum &mz) { return scale * (x - mz.m) - logf(mz.z); }
+// ln z to 2^-25, whatever its size: the logarithm in 32 bits is that of a number near one, which is small.
+__device__ __forceinline__ double ln(float z)
+{
+    float f = __builtin_amdgcn_frexp_mantf(z);            // in [1/2, 1)
+    int e = __builtin_amdgcn_frexp_expf(z);
+    if (f < 0.70710678f) {
+        f *= 2.f;
+        --e;
+    }
+    return fma((double)e, LN2, (double)logf(f));
+}
+// The log of a probability, from its logit and the row's (m, Z), and L.  Where it goes to 32 bits it is rounded once.
+__device__ __forceinline__ double log_p(float x, float scale, const MaxSum &mz) { return (double)scale * ((double)x - mz.m) - ln(mz.z); }
+__device__ __forceinline__ double log_sum(float scale, const MaxSum &mz) { return fma((double)scale, (double)mz.m, ln(mz.z)); }
 // The factor that takes a sum from its own maximum to another, not smaller one.
-__device__ __forceinline__ float rescale(float from, float to, float c)
+__device__ __forceinline__ float rescale(float from, float to, const Factor &c)
 {
     if (from == to) return 1.f;
-    return from == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((from - to) * c);
+    return from == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(times(c, from - to));
 }
-__device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, float c)
+__device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, const Factor &c)
 {
     const float m = fmaxf(a.m, b.m);
     return MaxSum{m, a.z * rescale(a.m, m, c) + b.z * rescale(b.m, m, c)};
@@ -188,7 +220,7 @@ __device__ __forceinline__ MaxSum merged(MaxSum a, MaxSum b, float c)
 // What all T threads of a row get from the waves' values, in the waves' order.  lds: T / 64 values that nothing else uses meanwhile; the
 // caller's next use of them lies behind a barrier.
 template <int T>
-__device__ __forceinline__ MaxSum row_merge(MaxSum v, float c, MaxSum *lds)
+__device__ __forceinline__ MaxSum row_merge(MaxSum v, const Factor &c, MaxSum *lds)
 {
     if (T <= 64) return v;
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
@@ -199,8 +231,8 @@ __device__ __forceinline__ MaxSum row_merge(MaxSum v, float c, MaxSum *lds)
     for (int w = 0; w < T / 64; ++w) z += (double)(lds[w].z * rescale(lds[w].m, m, c));
     return MaxSum{uniform<T>(m), uniform<T>((float)z)};
 }
-template <int T>
-__device__ __forceinline__ float row_sum(float v, float *lds)
+template <int T, class V>
+__device__ __forceinline__ V row_sum(V v, V *lds)
 {
     v = lanes_sum<T>(v);
     if (T <= 64) return v;
@@ -417,7 +449,7 @@ __device__ __forceinline__ float piece_sum(const u32x4 &r, const Base &b)
 // exponentials count from is one number in scalar registers.
 // left_out: bits of columns that are left out of the sum (LEAVE); column v has bit v - row.before + N, so that a piece's bits are together.
 template <bool LEAVE, class E, int T, int C>
-__device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, int end, u32x4 (&r)[C], float single, const uint8_t *left_out, float c,
+__device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, int end, u32x4 (&r)[C], float single, const uint8_t *left_out, const Factor &c,
                                            float &m, double &z)
 {
     float top = single;
@@ -433,8 +465,7 @@ __device__ __forceinline__ void add_pieces(const RowOf<E, T> &row, int first, in
     top = fmaxf(lanes_max<T>(top), m);
     z *= rescale(m, top, c);
     m = top;
-    const Base base = base_of(m, c);
-    const Base b{uniform<T>(base.c), uniform<T>(base.m)};
+    const Base b = uniform<T>(base_of(m, c));
     z += power(single, b);
     keep_packed(r);
 #pragma unroll
@@ -499,7 +530,7 @@ struct Walk {
     }
     // (The gradient's pass may find a column that is left out here left out or not.)
     template <bool LEAVE = false>
-    __device__ __forceinline__ MaxSum stats(float c, MaxSum *lds, const uint8_t *left_out = nullptr)
+    __device__ __forceinline__ MaxSum stats(const Factor &c, MaxSum *lds, const uint8_t *left_out = nullptr)
     {
         float m = -INFINITY;
         double z = 0.;
@@ -520,7 +551,7 @@ struct Walk {
     template <bool LATER = false>
     __device__ __forceinline__ void gradient(E *dx, float by, const Base &base, int y, float xy, float coef)
     {
-        const Base b{uniform<T>(base.c), uniform<T>(base.m)};
+        const Base b = uniform<T>(base);
         by = uniform<T>(by);
         const global_access::bytes out = base_address<T>(dx + row.before);
         if constexpr (S > 0)

@@ -25,7 +25,7 @@ int check_shape(const dbw_logits *l, Shape *out)
     out->ld = l->ld ? l->ld : l->vocab;
     out->ld_grad = l->ld_grad ? l->ld_grad : out->ld;
     if (out->ld < l->vocab || out->ld_grad < l->vocab) return DBW_ERR_INVALID;
-    if (!(l->scale > 0.f) || !isfinite(l->scale * loss::LOG2E)) return DBW_ERR_INVALID;
+    if (!(l->scale > 0.f) || !isfinite(l->scale * (float)loss::LOG2E)) return DBW_ERR_INVALID;
     out->rows = (int64_t)l->workers * l->rows;
     const int64_t most = INT64_MAX / 8 / (out->rows + 1);  // of a stride: offsets in bytes fit 64 bits
     if (l->vocab > DBW_LOSS_MAX_VOCAB || l->workers > MAX_GROUPS || out->rows > INT32_MAX || out->ld > most || out->ld_grad > most)
@@ -63,6 +63,15 @@ Work split_work(void *work, int64_t rows)
 // in turn 156; 12288 x 16384 148 and 140.
 constexpr int64_t XCD_ROW = 65536;
 
+loss::Factor factor_of(float scale)
+{
+    const double c = scale * loss::LOG2E;
+    float hi = (float)c;
+    if (hi >= c) hi = nextafterf(hi, 0.f);
+    const float lo = (float)(c - hi), least = 0x1p-149f;
+    return loss::Factor{fmaxf(hi, least), fmaxf(lo, least)};
+}
+
 // Checks that all calls have in common, and the kernels' view of the rows.
 int prepare(const dbw_logits *l, const void *logits, void *dlogits, int32_t *status, const void *work, Shape *S)
 {
@@ -77,7 +86,7 @@ int prepare(const dbw_logits *l, const void *logits, void *dlogits, int32_t *sta
         if (a < b + nb && b < a + na) return DBW_ERR_ALIAS;
     }
     S->row_bytes = (int64_t)e * l->vocab;
-    S->R = loss::Rows{logits, dlogits, S->ld, S->ld_grad, l->vocab, S->rows, l->scale, l->scale * loss::LOG2E, status, S->row_bytes >= XCD_ROW};
+    S->R = loss::Rows{logits, dlogits, S->ld, S->ld_grad, l->vocab, S->rows, l->scale, factor_of(l->scale), status, S->row_bytes >= XCD_ROW};
     return DBW_OK;
 }
 
@@ -246,7 +255,7 @@ extern "C" int dbw_token_logp(const dbw_logits *shape, const void *logits, const
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
     const loss::Slices slices = S.row_bytes > LONG_ROW ? slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS) : loss::Slices{1, 0};
-    const loss::Logp P{tokens, nullptr, logp_out, lse_out, slices.count > 1 ? W.slices : nullptr, W.token_logit, slices};
+    const loss::Logp P{tokens, nullptr, logp_out, lse_out, nullptr, slices.count > 1 ? W.slices : nullptr, W.token_logit, slices};
     launch_logp(shape, S, P, lse_out != nullptr, s);      // L is asked for where a gradient follows
     if (slices.count > 1) hipLaunchKernelGGL(loss::join_kernel, dim3((uint32_t)S.rows), dim3(64), 0, s, S.R, P);
     DBW_HIP(hipGetLastError());
@@ -340,12 +349,12 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     if (S.rows > 0) {
         if (pairs > 0 && !few) slices = slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS);  // (whose parts the pairs' kernel joins)
         const bool cut = slices.count > 1;
-        launch_logp(shape, S, loss::Logp{tokens, weights, logp, nullptr, cut ? W.slices : W.stats, W.token_logit, slices}, dlogits != nullptr, s);
+        launch_logp(shape, S, loss::Logp{tokens, weights, logp, nullptr, W.coef, cut ? W.slices : W.stats, W.token_logit, slices}, dlogits != nullptr, s);
         DBW_HIP(hipGetLastError());
     }
     const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
     if (pairs > 0) {
-        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, S.rows, logp, margin_out, W.coef,
+        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, S.rows, logp, margin_out, W.coef, W.coef,
                                  W.slices, W.stats, W.token_logit, slices.count, status_out};
         if (few) {
             if (dlogits) launch_gradient(shape, S, loss::Gradient{tokens, nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, &P, s);
@@ -383,7 +392,7 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
         const loss::Policy P{tokens, old_logp, ref_logp, advantage, weights, 1.f - clip_low, 1.f + clip_high, kl_coef,
                              1.f / (float)shape->rows, logp_out, W.terms, W.slices, W.token_logit, slices.count, gradient_slices_of(shape, S.rows),
                              shape->rows, loss_out, kl_out};
-        if (cut) launch_logp(shape, S, loss::Logp{tokens, weights, nullptr, nullptr, W.slices, W.token_logit, slices}, dlogits != nullptr, s);
+        if (cut) launch_logp(shape, S, loss::Logp{tokens, weights, nullptr, nullptr, nullptr, W.slices, W.token_logit, slices}, dlogits != nullptr, s);
         by_type(shape->type, [&](auto e) {
             typedef decltype(e) E;
             if (cut)
