@@ -573,7 +573,7 @@ __host__ __device__ __forceinline__ int distill_words(int k, int vocab) { return
 // A row's weighted loss, and its gradient, by T threads.
 template <class E, int T, int C, int S, bool TAIL>
 __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill &P, int64_t r, uint32_t *shared, MaxSum *lds, MaxSum *lds_top,
-                                                   float (*sums)[T > 64 ? T / 64 : 1])
+                                                   float (*sums)[T > 64 ? T / 64 : 1], double *masses)
 {
     const int t = tid<T>();
     const float w = P.weights ? P.weights[r] : P.weight;
@@ -670,26 +670,27 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
         const MaxSum in = row_merge<T>(MaxSum{m_top, lanes_sum<T>(z_top)}, R.c, lds_top);
         const MaxSum out = walk.template stats<true>(R.c, lds, (const uint8_t *)in_top);
         mz = merged(out, in, R.c);
-        log_out = R.scale * (out.m - mz.m) + (logf(out.z) - logf(mz.z));
+        log_out = (float)(log_p(out.m, R.scale, mz) + ln(out.z));
     } else {
         mz = walk.stats(R.c, lds);
     }
-    const Base base = base_of(mz.m, R.c);
-    const float log2_z = log2f(mz.z), norm = TAIL ? P.teacher_lse[r] * (float)LOG2E : log2f(sum);
-    float part = 0.f, mass = 0.f;
+    // With the tail the list's mass is taken from one: s t - L is rounded once, as a difference, and not its terms, which may be large.
+    const float norm = TAIL ? P.teacher_lse[r] : (float)ln(sum), ln_z = (float)ln(mz.z);
+    float part = 0.f;
+    double mass = 0.;
     for (int j = t; j < P.k; j += T)
         if (at[j] >= 0) {
-            const float log2_q = TAIL ? fmaf(q[j], R.c.hi, -norm) : times(R.c, q[j] - from) - norm, qj = __builtin_amdgcn_exp2f(log2_q);
-            const float log2_p = times(R.c, xs[j] - mz.m) - log2_z;
+            const float log_q = fmaf(R.scale, TAIL ? q[j] : q[j] - from, -norm), qj = exponential(log_q);
+            const float log_pj = fmaf(R.scale, xs[j] - mz.m, -ln_z);
             mass += qj;
-            if (!(qj <= 0.f)) part += qj * (log2_q - log2_p);
-            q[j] = __builtin_amdgcn_exp2f(log2_p) - qj;   // dl/dx over s
+            if (!(qj <= 0.f)) part += qj * (log_q - log_pj);
+            q[j] = exponential(log_pj) - qj;                     // dl/dx over s
         }
-    part = (float)LN2 * row_sum<T>(part, sums[3]);
+    part = row_sum<T>(part, sums[3]);
     float factor = 1.f;
     if (TAIL) {
-        mass = row_sum<T>(mass, sums[0]);                 // (its last use lies several barriers back)
-        const float rest = fmaxf(1.f - mass, 0.f);
+        mass = row_sum<T>(mass, masses);
+        const float rest = mass > 1. ? 0.f : (float)(1. - mass);
         if (rest > 0.f) {
             part += rest * (logf(rest) - log_out);
             factor = 1.f - expf(logf(rest) - log_out);
@@ -702,6 +703,7 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
         // rows of 3920 bf16, k = 152: 75 us and 106 with streaming stores; 8192 rows of 8000, k = 64: 70 and 67.  (Kernels of longer rows have no
         // registers left for both kinds.)
         const float by = R.scale * w * factor / mz.z;
+        const Base base = base_of(mz.m, R.c);
         if (T <= 64 && P.k >= R.vocab / 64) walk.template gradient<true>(dx, by, base, -1, 0.f, 0.f);
         else walk.template gradient<false>(dx, by, base, -1, 0.f, 0.f);
         if (T > 64) __syncthreads();                      // the list's columns are written over
@@ -719,9 +721,10 @@ __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void distill_kerne
     extern __shared__ uint32_t shared[];
     __shared__ MaxSum lds[T > 64 ? T / 64 : 1], lds_top[T > 64 ? T / 64 : 1];
     __shared__ float sums[4][T > 64 ? T / 64 : 1];
+    __shared__ double masses[T > 64 ? T / 64 : 1];
     const int64_t r = row_of_group<T>(R.by_xcd ? row_by_xcd(group(), R.rows) : group());
     if (r >= R.rows) return;
-    const float term = distill_whole_row<E, T, C, S, TAIL>(R, P, r, shared + row_in_group<T>() * distill_words(P.k, R.vocab), lds, lds_top, sums);
+    const float term = distill_whole_row<E, T, C, S, TAIL>(R, P, r, shared + row_in_group<T>() * distill_words(P.k, R.vocab), lds, lds_top, sums, masses);
     if (tid<T>() == 0) P.terms[r] = make_float2(term, 0.f);
 }
 
@@ -734,7 +737,7 @@ __global__ __launch_bounds__(1024) void distill_worker_kernel(Rows R, Distill P)
     float a = 0.f;
     for (int t = row_in_group<T>(); t < P.rows; t += blockDim.x / T) {
         const float term = distill_whole_row<E, T, C, 0, TAIL>(R, P, (int64_t)blockIdx.x * P.rows + t,
-                                                               shared + row_in_group<T>() * distill_words(P.k, R.vocab), nullptr, nullptr, nullptr);
+                                                               shared + row_in_group<T>() * distill_words(P.k, R.vocab), nullptr, nullptr, nullptr, nullptr);
         if (tid<T>() == 0) a += term;
         row_barrier<T>();                                 // the next row's list takes this one's place
     }

@@ -81,6 +81,8 @@ __device__ __forceinline__ Base base_of(float m, const Factor &c) { return Base{
 __device__ __forceinline__ float times(const Factor &c, float d) { return fmaf(d, c.hi, d * c.lo); }      // rounded once, but for 2^-24 of lo's part
 __device__ __forceinline__ float power(float x, const Base &b) { return __builtin_amdgcn_exp2f(times(b.c, x - b.m)); }
 
+__device__ __forceinline__ float exponential(float v) { return __builtin_amdgcn_exp2f(times(Factor{0x1.715474p0f, (float)(LOG2E - 0x1.715474p0)}, v)); }
+
 // A row is T threads' work; a workgroup has T threads, or several rows of 64 or 16 threads each.
 template <int T>
 __device__ __forceinline__ int tid() { return (int)threadIdx.x & (T - 1); }
