@@ -664,15 +664,15 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
 
     // With the tail the student's mass outside the list is summed apart, from a maximum of its own: it may be far below the rest, and as a
     // difference from one it would be lost.
-    MaxSum mz;
+    MaxSum mz, out;                                       // of the row; of what is not in the list, or of the row
     float log_out = 0.f;
     if (TAIL) {
         const MaxSum in = row_merge<T>(MaxSum{m_top, lanes_sum<T>(z_top)}, R.c, lds_top);
-        const MaxSum out = walk.template stats<true>(R.c, lds, (const uint8_t *)in_top);
+        out = walk.template stats<true>(R.c, lds, (const uint8_t *)in_top);
         mz = merged(out, in, R.c);
         log_out = (float)(log_p(out.m, R.scale, mz) + ln(out.z));
     } else {
-        mz = walk.stats(R.c, lds);
+        mz = out = walk.stats(R.c, lds);
     }
     // With the tail the list's mass is taken from one: s t - L is rounded once, as a difference, and not its terms, which may be large.
     const float norm = TAIL ? P.teacher_lse[r] : (float)ln(sum), ln_z = (float)ln(mz.z);
@@ -687,14 +687,13 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
             q[j] = exponential(log_pj) - qj;                     // dl/dx over s
         }
     part = row_sum<T>(part, sums[3]);
-    float factor = 1.f;
+    float mass_out = 1.f;                                 // s times this is the sum of the gradient's columns that are not in the list
     if (TAIL) {
         mass = row_sum<T>(mass, masses);
         const float rest = mass > 1. ? 0.f : (float)(1. - mass);
-        if (rest > 0.f) {
-            part += rest * (logf(rest) - log_out);
-            factor = 1.f - expf(logf(rest) - log_out);
-        }
+        if (rest > 0.f) part += rest * (logf(rest) - log_out);
+        // p_v (1 - R / S) = (S - R) p_v / S: p_v alone may be too small for 32 bits, p_v / S is not
+        mass_out = expf(log_out) - rest;
     }
     if (t == 0 && P.row_loss_out) P.row_loss_out[r] = part;
     if (R.dx) {
@@ -702,8 +701,9 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
         // Single elements written over in lines that have left the L2 cost more than the streaming stores gain where they are many: 14664
         // rows of 3920 bf16, k = 152: 75 us and 106 with streaming stores; 8192 rows of 8000, k = 64: 70 and 67.  (Kernels of longer rows have no
         // registers left for both kinds.)
-        const float by = R.scale * w * factor / mz.z;
-        const Base base = base_of(mz.m, R.c);
+        // Where nothing is outside, by is finite all the same: what it writes is a token's that cannot occur, or written over.
+        const float by = TAIL && out.z == 0.f && mz.z > 0.f ? 0.f : R.scale * w * mass_out / out.z;
+        const Base base = base_of(out.m, R.c);
         if (T <= 64 && P.k >= R.vocab / 64) walk.template gradient<true>(dx, by, base, -1, 0.f, 0.f);
         else walk.template gradient<false>(dx, by, base, -1, 0.f, 0.f);
         if (T > 64) __syncthreads();                      // the list's columns are written over

@@ -84,3 +84,21 @@ def test_a_small_rest_of_a_teacher_whose_logits_are_far_from_zero(B, dtype, rows
     value = torch.randn(rows, k, generator=I.g) + offset
     lse = (torch.logsumexp(ref.scaled(value, 0.9), 1) - math.log(0.99)).float()
     check(I, index, value, lse, f"offset {offset}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,vocab,k", SIZES)
+def test_everything_outside_the_list_far_below_it(B, dtype, rows, vocab, k):
+    for scale, gap in ((0.5, 85.0), (1.0, 90.0), (1.0, 120.0), (10.0, 95.0), (0.7, None)):
+        I, index = prepared(B, dtype, rows, vocab, k, scale, seed=int(gap or 1))
+        x = torch.randn(rows, vocab, generator=I.g)
+        if gap is None:
+            outside = torch.ones(rows, vocab, dtype=torch.bool).scatter_(1, index, False)
+            x = x.masked_fill(outside, torch.finfo(dtype).min)
+        else:
+            x = x / scale
+            x.scatter_add_(1, index, torch.full(index.shape, gap / scale))
+        student(I, x)
+        value = torch.randn(rows, k, generator=I.g)
+        lse = (torch.logsumexp(ref.scaled(value, scale), 1) - math.log(0.9)).float()
+        check(I, index, value, lse, f"scale {scale}, gap {gap}")
