@@ -76,6 +76,8 @@ int dbw_token_logp_grad(const dbw_logits *shape, const void *logits, const int32
  * With teacher_lse [dev, N*T] (the teacher's own L over its whole vocabulary) q_j = exp(s t_j - teacher_lse), and everything
  * outside K is one more class with the rest of either mass, R = max(0, 1 - sum_K q) and S = sum of p_v outside K:
  *     l = sum_K q_j log(q_j / p_j) + R log(R / S),     dl/dx_v = s (p_v - q_v) in K, s p_v (1 - R / S) outside.
+ * Where nothing can lie outside K (S = 0: K is the whole vocabulary, or all other logits are -inf) an R of up to 2^-22 (|teacher_lse| + 12) is
+ * taken for the rounding of teacher_lse and for no rest; a larger one makes the loss infinite.
  * loss_out[i] = sum over worker i's rows of weights[r] l_r; the gradient carries the weights too.  (A factor of 1 / s^2 that keeps
  * gradients comparable between temperatures goes into the weights.)
  *   k               1 <= k <= DBW_TEACHER_MAX

@@ -690,7 +690,9 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     float mass_out = 1.f;                                 // s times this is the sum of the gradient's columns that are not in the list
     if (TAIL) {
         mass = row_sum<T>(mass, masses);
-        const float rest = mass > 1. ? 0.f : (float)(1. - mass);
+        float rest = mass > 1. ? 0.f : (float)(1. - mass);
+        // Nothing outside: the list's mass is one but for the rounding of L (2^-24 |L|) and of k <= 1024 entries (2^-24 (ln k + 4)); either four times.
+        if (out.z == 0.f && rest <= 0x1p-22f * (fabsf(norm) + 12.f)) rest = 0.f;
         if (rest > 0.f) part += rest * (logf(rest) - log_out);
         // p_v (1 - R / S) = (S - R) p_v / S: p_v alone may be too small for 32 bits, p_v / S is not
         mass_out = expf(log_out) - rest;

@@ -102,3 +102,24 @@ def test_everything_outside_the_list_far_below_it(B, dtype, rows, vocab, k):
         value = torch.randn(rows, k, generator=I.g)
         lse = (torch.logsumexp(ref.scaled(value, scale), 1) - math.log(0.9)).float()
         check(I, index, value, lse, f"scale {scale}, gap {gap}")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16, F16])
+@pytest.mark.parametrize("rows,vocab,k", [(40, 40, 40), (70, 300, 300), (40, 1000, 1000), (60, 1900, 20), (40, 10007, 64), (8, 70001, 128)])
+@pytest.mark.parametrize("offset", [0.0, 200.0])
+def test_nothing_outside_the_list(B, dtype, rows, vocab, k, offset):
+    """The list is the whole vocabulary, or no other token can occur; the teacher's L is that of its list, rounded: no row or its gradient is infinite."""
+    I, index = prepared(B, dtype, rows, vocab, k, 0.9, seed=6)
+    x = torch.randn(rows, vocab, generator=I.g)
+    outside = torch.ones(rows, vocab, dtype=torch.bool).scatter_(1, index, False)
+    student(I, x.masked_fill(outside, -math.inf))
+    value = torch.randn(rows, k, generator=I.g) + offset
+    lse = torch.logsumexp(ref.scaled(value, 0.9), 1).float()
+    loss = check(I, index, value, lse)
+    assert torch.isfinite(loss).all()
+    # a rest that is no rounding: infinitely dear, and a token that cannot occur has no gradient
+    row_loss, grad = torch.empty(rows, device="cuda"), I.gradient()
+    base.run_distill(I, index, value, lse + 0.01, None, grad, row_loss)
+    assert (row_loss == math.inf).all()
+    got = I.rows_of(grad).cpu()
+    assert torch.isfinite(got).all() and (got[outside] == 0).all()
