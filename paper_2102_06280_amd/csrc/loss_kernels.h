@@ -174,8 +174,8 @@ __device__ __forceinline__ void slice_gradient(const Rows &R, const RowOf<E, T> 
 #pragma unroll
         for (int i = 0; i < C; ++i) store_piece<E, T>(out, first, end, i, v[i], by, b);
     }
-    if (singles && row.has_single()) dx[row.single_column()] = narrow<E>(by * power(single, b));
-    if (mine) dx[y] = narrow<E>(by * power(xy, b) + coef);
+    if (singles && row.has_single()) dx[row.single_column()] = narrow<E>(by * power_alone(single, b));
+    if (mine) dx[y] = narrow<E>(by * power_alone(xy, b) + coef);
 }
 
 // ---------------------------------------------------------------- pairs of sequences

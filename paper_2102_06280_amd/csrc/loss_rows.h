@@ -44,6 +44,7 @@ __device__ __forceinline__ bf16 narrow<bf16>(float v)
 // c = s log2(e) as hi + lo.  hi is below c and lo above zero, so that the exponent of a logit of -inf, -inf hi + -inf lo, is -inf.
 struct Factor {
     float hi, lo;
+    float near;          // the nearest number, for what is not summed
 };
 
 // The rows of a call.
@@ -79,9 +80,12 @@ struct Base {
 };
 __device__ __forceinline__ Base base_of(float m, const Factor &c) { return Base{c, m == -INFINITY ? 0.f : m}; }
 __device__ __forceinline__ float times(const Factor &c, float d) { return fmaf(d, c.hi, d * c.lo); }      // rounded once, but for 2^-24 of lo's part
+// Of one column, for a gradient: nothing adds these up, and the nearest factor is as good.  An instruction less: 4096 rows of 131072 bf16 distilled in
+// 426 us, with power() 439.
+__device__ __forceinline__ float power_alone(float x, const Base &b) { return __builtin_amdgcn_exp2f((x - b.m) * b.c.near); }
 __device__ __forceinline__ float power(float x, const Base &b) { return __builtin_amdgcn_exp2f(times(b.c, x - b.m)); }
 
-__device__ __forceinline__ float exponential(float v) { return __builtin_amdgcn_exp2f(times(Factor{0x1.715474p0f, (float)(LOG2E - 0x1.715474p0)}, v)); }
+__device__ __forceinline__ float exponential(float v) { return __builtin_amdgcn_exp2f(times(Factor{0x1.715474p0f, (float)(LOG2E - 0x1.715474p0), (float)LOG2E}, v)); }
 
 // A row is T threads' work; a workgroup has T threads, or several rows of 64 or 16 threads each.
 template <int T>
@@ -120,7 +124,7 @@ __device__ __forceinline__ double uniform(double v)
     return __longlong_as_double((int64_t)((uint64_t)hi << 32 | lo));
 }
 template <int T>
-__device__ __forceinline__ Base uniform(const Base &b) { return Base{{uniform<T>(b.c.hi), uniform<T>(b.c.lo)}, uniform<T>(b.m)}; }
+__device__ __forceinline__ Base uniform(const Base &b) { return Base{{uniform<T>(b.c.hi), uniform<T>(b.c.lo), uniform<T>(b.c.near)}, uniform<T>(b.m)}; }
 // Over the 64 lanes of a wave, without LDS: shifts by 1, 2, 4 and 8 within 16 lanes, then the last lanes of 16 to the next ones.  Over 16 lanes:
 // rotations, which leave the result in all of them.
 template <int T>
@@ -486,7 +490,7 @@ __device__ __forceinline__ void store_piece(global_access::bytes base, int first
         float v[P::N];
         P::unpack(r, v);
 #pragma unroll
-        for (int j = 0; j < P::N; ++j) v[j] = by * power(v[j], b);
+        for (int j = 0; j < P::N; ++j) v[j] = by * power_alone(v[j], b);
         if (LATER) *(place)(base + (uint32_t)p * 16u) = P::pack(v);
         else __builtin_nontemporal_store((typename P::raw)P::pack(v), (place)(base + (uint32_t)p * 16u));
     }
@@ -567,9 +571,9 @@ struct Walk {
         keep_packed(r);
 #pragma unroll
         for (int i = 0; i < C; ++i) store_piece<E, T, LATER>(out, 0, row.pieces, i, r[i], by, b);
-        if (row.has_single()) dx[row.single_column()] = narrow<E>(by * power(single, b));
+        if (row.has_single()) dx[row.single_column()] = narrow<E>(by * power_alone(single, b));
         // by the thread that wrote the column before
-        if (y >= 0 && tid<T>() == row.owner(y)) dx[y] = narrow<E>(by * power(xy, b) + coef);
+        if (y >= 0 && tid<T>() == row.owner(y)) dx[y] = narrow<E>(by * power_alone(xy, b) + coef);
     }
 };
 

@@ -69,7 +69,7 @@ loss::Factor factor_of(float scale)
     float hi = (float)c;
     if (hi >= c) hi = nextafterf(hi, 0.f);
     const float lo = (float)(c - hi), least = 0x1p-149f;
-    return loss::Factor{fmaxf(hi, least), fmaxf(lo, least)};
+    return loss::Factor{fmaxf(hi, least), fmaxf(lo, least), (float)c};
 }
 
 // Checks that all calls have in common, and the kernels' view of the rows.
