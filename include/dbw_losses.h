@@ -65,7 +65,9 @@ int dbw_token_logp(const dbw_logits *shape, const void *logits, const int32_t *t
                    int32_t *status_out, void *work, void *stream);
 
 /* Gradient of a function of the log-probabilities: with c_r its derivative with respect to logp_out[r] (coef [dev, N*T]),
- * dlogits[r][v] = s c_r ([v = y] - p_v).  lse as dbw_token_logp gave it.  A row with c_r = 0 takes no part. */
+ * dlogits[r][v] = s c_r ([v = y] - p_v).  lse as dbw_token_logp gave it for these logits.  A row with c_r = 0 takes no part.
+ * The rounding of L enters every p_v, by up to 2^-17 of it where |L| <= 256; a row with a larger L, of which too little of the
+ * logarithm would be left, is summed again (one workgroup takes the whole row, so many such rows cost little and a few long ones latency). */
 int dbw_token_logp_grad(const dbw_logits *shape, const void *logits, const int32_t *tokens, const float *lse,
                         const float *coef, void *dlogits, int32_t *status_out, void *stream);
 

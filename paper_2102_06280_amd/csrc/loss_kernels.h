@@ -93,6 +93,25 @@ __device__ __forceinline__ void store_logp(double l, float *logp, float *low)
 }
 __device__ __forceinline__ bool takes_part(const Logp &P, int64_t r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
 
+// (m, Z) of a wave's part of pieces first ... end - 1 of a row, and of its single elements if those are asked for.  ONCE: the pieces will not be read again.
+template <bool ONCE, class E, int T, int C>
+__device__ __forceinline__ MaxSum sums_of(const RowOf<E, T> &row, int first, int end, bool singles, const Factor &c)
+{
+    float m = -INFINITY;
+    double sum = 0.;
+    for (; first < end; first += T * C) {
+        u32x4 v[C];
+        row.template load<C, ONCE>(first, v);
+        add_pieces<false>(row, first, end, v, -INFINITY, nullptr, c, m, sum);
+    }
+    MaxSum mz{m, (float)lanes_sum<T>(sum)};
+    if (singles) {
+        const float single = row.load_single(), top = lanes_max<T>(single);
+        mz = merged(mz, MaxSum{top, lanes_sum<T>(power(single, base_of(top, c)))}, c);
+    }
+    return mz;
+}
+
 // A workgroup a row, or a slice: one pass, the maximum and the sum of a batch after the other.  Bound by memory: 4096 x 65536 bf16 79 us, 6.2 TB/s; a single
 // row by latency.  AGAIN: the rows will be read again soon, for their gradient.
 template <class E, int T, int C, bool AGAIN>
@@ -113,22 +132,9 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
     const RowOf<E, T> row(x, R.vocab);
     int first, end;
     slice_of(P.slices, s, row.pieces, first, end);
-    float m = -INFINITY;
-    double sum = 0.;
-    for (; first < end; first += T * C) {
-        u32x4 v[C];
-        row.template load<C, !AGAIN>(first, v);
-        add_pieces<false>(row, first, end, v, -INFINITY, nullptr, R.c, m, sum);
-    }
-    float z = (float)lanes_sum<T>(sum);
-    if (s == 0) {
-        const float single = row.load_single(), top = lanes_max<T>(single);
-        const MaxSum both = merged(MaxSum{m, z}, MaxSum{top, lanes_sum<T>(power(single, base_of(top, R.c)))}, R.c);
-        m = both.m;
-        z = both.z;
-    }
+    const MaxSum part = sums_of<!AGAIN, E, T, C>(row, first, end, s == 0, R.c);
     const float xy = widen(x[column(R, P.tokens[r])]);
-    const MaxSum mz = row_merge<T>(MaxSum{m, z}, R.c, lds);
+    const MaxSum mz = row_merge<T>(part, R.c, lds);
     if (tid<T>() != 0) return;
     if (P.slices.count > 1) {
         P.stats[r * P.slices.count + s] = mz;
@@ -301,14 +307,20 @@ __global__ __launch_bounds__(THREADS) void pair_loss_kernel(PairLoss P)
 struct Gradient {
     const int32_t *tokens;
     const float *coef;   // null: none
-    const MaxSum *stats; // (m, Z) of every row, or null and
+    const MaxSum *stats; // (m, Z) of every row, or (FROM_L)
     const float *lse;    // L
     Slices slices;
     PairLoss pairs;      // workgroups behind the rows' give every worker's loss
 };
 
-template <class E, int T, int C>
-__device__ __forceinline__ void gradient_of_slice(const Rows &R, const Gradient &P, int64_t r, int s, int token, float g)
+// Largest |L| that is taken as it is: in 32 bits it is off by 2^-17, and so is every probability, of itself.  Larger ones have lost too much of ln Z (all of it in
+// a row of equal logits of 1e30), or are infinite where their row is not.
+constexpr float MOST_L = 256.f;
+
+// FROM_L: a row whose L is larger than that is summed again, whole and by the workgroup of its first slice, which then also writes it all: in place, nobody
+// else may write what is still to be read.
+template <class E, int T, int C, bool FROM_L>
+__device__ __forceinline__ void gradient_of_slice(const Rows &R, const Gradient &P, int64_t r, int s, int token, float g, MaxSum *lds)
 {
     const RowOf<E, T> row((const E *)R.x + r * R.ld, R.vocab);
     if (g == 0.f) {
@@ -316,26 +328,39 @@ __device__ __forceinline__ void gradient_of_slice(const Rows &R, const Gradient 
         zero_pieces<E, T, true>(R, r, s * P.slices.pieces, s == P.slices.count - 1 ? INT32_MAX : (s + 1) * P.slices.pieces);
         return;
     }
-    float by = -g;
-    Base b;
-    if (P.stats) {
-        const MaxSum mz = P.stats[r];
-        b = base_of(mz.m, R.c);
-        by /= mz.z;
-    } else {
-        b = base_of(P.lse[r] / R.scale, R.c);             // from L: as if m = L / s and Z = 1
-    }
     int first, end;
     slice_of(P.slices, s, row.pieces, first, end);
+    float by;
+    MaxSum mz;
+    bool summed = !FROM_L;
+    if (FROM_L) {
+        const float L = P.lse[r], m = L / R.scale;
+        summed = !(fabsf(L) <= MOST_L && fabsf(m) < INFINITY);
+        if (summed) {
+            if (s != 0) return;
+            first = 0;
+            end = row.pieces;
+            mz = row_merge<T>(sums_of<false, E, T, C>(row, first, end, true, R.c), R.c, lds);
+        } else {
+            // p = exp(s (x - m) - d) with d = L - s m, what the division's rounding has left
+            mz.m = m;
+            by = fmaf(g, fmaf(-R.scale, m, L), -g);
+        }
+    } else {
+        mz = P.stats[r];
+    }
+    if (summed) by = -g / mz.z;
+    const Base b = base_of(mz.m, R.c);
     slice_gradient<E, T, C>(R, row, r, first, end, by, b, column(R, token), g);
 }
 
 // A workgroup a slice of 16 KB: the row's (m, Z) are known, so every piece is by itself.  Bound by memory: 8192 x 32768 bf16, 15 % of the rows without a part,
 // 0.99 GB in 147 us, 6.8 TB/s with what is left of the rows in the last-level cache.
-template <class E, int T, int C>
+template <class E, int T, int C, bool FROM_L>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradient P)
 {
     __shared__ float lds[T * ROWS_OF<T> / 64];
+    __shared__ MaxSum lds_row[T > 64 ? T / 64 : 1];
     const int64_t groups = T <= 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
     if (group() >= groups) {
         const int64_t worker = group() - groups;
@@ -346,7 +371,7 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradie
     const int s = T <= 64 ? 0 : (int)(group() % P.slices.count);
     if (r >= R.rows) return;
     const int token = P.tokens[r];
-    gradient_of_slice<E, T, C>(R, P, r, s, token, token < 0 || !P.coef ? 0.f : R.scale * P.coef[r]);
+    gradient_of_slice<E, T, C, FROM_L>(R, P, r, s, token, token < 0 || !P.coef ? 0.f : R.scale * P.coef[r], lds_row);
 }
 
 // Margins and loss of a worker with few rows and short pairs, a wave a pair, by a workgroup of THREADS.
@@ -401,7 +426,7 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void pair_gradient_kernel(Rows R, G
             if (r >= a[0] && r < a[2]) g = R.scale * (r < a[1] ? slope : -slope) * (Q.weights ? Q.weights[r] : 1.f);
         }
     }
-    gradient_of_slice<E, T, C>(R, P, r, s, token, g);
+    gradient_of_slice<E, T, C, false>(R, P, r, s, token, g, nullptr);
 }
 
 // ---------------------------------------------------------------- policy

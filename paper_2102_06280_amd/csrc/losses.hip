@@ -230,7 +230,8 @@ void launch_gradient(const dbw_logits *l, const Shape &S, const loss::Gradient &
         by_gradient_slice(P.slices, S.row_bytes, [&](auto p) {
             const dim3 grid = grid_of((S.rows * P.slices.count + p.ROWS - 1) / p.ROWS + (P.pairs.loss_out ? P.pairs.workers : 0)), block(p.THREADS);
             if (pairs) hipLaunchKernelGGL((loss::pair_gradient_kernel<E, p.T, p.C>), grid, block, 0, s, S.R, P, *pairs);
-            else hipLaunchKernelGGL((loss::gradient_kernel<E, p.T, p.C>), grid, block, 0, s, S.R, P);
+            else if (P.stats) hipLaunchKernelGGL((loss::gradient_kernel<E, p.T, p.C, false>), grid, block, 0, s, S.R, P);
+            else hipLaunchKernelGGL((loss::gradient_kernel<E, p.T, p.C, true>), grid, block, 0, s, S.R, P);
         });
     });
 }
