@@ -57,19 +57,19 @@ __device__ __forceinline__ MaxSum joined(const MaxSum *slices, int count, const 
 }
 constexpr int MAX_SLICES = 32;
 
-// Sums over a workgroup's waves, in their order.
-__device__ __forceinline__ void store_sums(float a, float b, float2 *lds, float *first_out, float *second_out)
+// Sums over a workgroup's waves, in their order.  A worker's sums are held in 64 bits: of thousands of terms that are alike, roundings to 32 bits have one sign.
+__device__ __forceinline__ void store_sums(double a, double b, double2 *lds, float *first_out, float *second_out)
 {
-    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_float2(a, b);
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_double2(a, b);
     __syncthreads();
     if (threadIdx.x != 0) return;
-    a = b = 0.f;
+    a = b = 0.;
     for (unsigned w = 0; w < blockDim.x / 64; ++w) {
         a += lds[w].x;
         b += lds[w].y;
     }
-    *first_out = a;
-    if (second_out) *second_out = b;
+    *first_out = (float)a;
+    if (second_out) *second_out = (float)b;
 }
 
 // ---------------------------------------------------------------- log-probabilities
@@ -289,16 +289,16 @@ __device__ __forceinline__ float loss_of(const PairLoss &P, float u)
     return u != u ? u : soft + (u >= 0.f ? P.smoothing * u : (P.smoothing - 1.f) * u);
 }
 template <int T>
-__device__ __forceinline__ void pair_loss(const PairLoss &P, int64_t worker, float *lds)
+__device__ __forceinline__ void pair_loss(const PairLoss &P, int64_t worker, double *lds)
 {
-    float l = 0.f;
+    double l = 0.;
     for (int j = threadIdx.x; j < P.pairs; j += T) l += loss_of(P, P.margin[worker * P.pairs + j]);
     l = row_sum<T>(l, lds);
-    if (threadIdx.x == 0) P.loss_out[worker] = P.pairs ? l / (float)P.pairs : 0.f;
+    if (threadIdx.x == 0) P.loss_out[worker] = P.pairs ? (float)(l / P.pairs) : 0.f;
 }
 __global__ __launch_bounds__(THREADS) void pair_loss_kernel(PairLoss P)
 {
-    __shared__ float lds[WAVES];
+    __shared__ double lds[WAVES];
     pair_loss<THREADS>(P, blockIdx.x, lds);
 }
 
@@ -359,7 +359,7 @@ __device__ __forceinline__ void gradient_of_slice(const Rows &R, const Gradient 
 template <class E, int T, int C, bool FROM_L>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradient P)
 {
-    __shared__ float lds[T * ROWS_OF<T> / 64];
+    __shared__ double lds[T * ROWS_OF<T> / 64];
     __shared__ MaxSum lds_row[T > 64 ? T / 64 : 1];
     const int64_t groups = T <= 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
     if (group() >= groups) {
@@ -375,21 +375,21 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradie
 }
 
 // Margins and loss of a worker with few rows and short pairs, a wave a pair, by a workgroup of THREADS.
-__device__ __forceinline__ void sums_of_pairs(const PairLoss &P, const Preference &Q, int64_t worker, float2 *lds)
+__device__ __forceinline__ void sums_of_pairs(const PairLoss &P, const Preference &Q, int64_t worker, double2 *lds)
 {
     int a[3];
-    float loss = 0.f;
+    double loss = 0.;
     for (int j = wave_id(); j < Q.pairs; j += WAVES) {
         rows_of_pair(Q, worker * Q.pairs + j, a);
         const float u = (float)(Q.beta * wave_sum(part_of_pair(Q, a, threadIdx.x & 63, 64)));
         if ((threadIdx.x & 63) == 0) Q.margin_out[worker * Q.pairs + j] = u;
         loss += loss_of(P, u);
     }
-    store_sums(loss / (float)Q.pairs, 0.f, lds, P.loss_out + worker, nullptr);
+    store_sums(loss / Q.pairs, 0., lds, P.loss_out + worker, nullptr);
 }
 __global__ __launch_bounds__(THREADS) void pair_sums_kernel(PairLoss P, Preference Q)
 {
-    __shared__ float2 lds[WAVES];
+    __shared__ double2 lds[WAVES];
     sums_of_pairs(P, Q, blockIdx.x, lds);
 }
 
@@ -399,7 +399,7 @@ template <class E, int T, int C>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void pair_gradient_kernel(Rows R, Gradient P, Preference Q)
 {
     static_assert(T * ROWS_OF<T> == THREADS, "the workgroups behind the rows' have as many threads as pair_sums_kernel's");
-    __shared__ float2 lds[WAVES];
+    __shared__ double2 lds[WAVES];
     constexpr int LANES = T < 64 ? T : 64;
     const int64_t groups = T <= 64 ? (R.rows + ROWS_OF<T> - 1) / ROWS_OF<T> : R.rows * P.slices.count;
     int a[3];
@@ -519,8 +519,8 @@ __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void policy_kernel
 template <class E, int T, int C>
 __global__ __launch_bounds__(1024) void policy_worker_kernel(Rows R, Policy P)
 {
-    __shared__ float2 lds[16];
-    float a = 0.f, b = 0.f;
+    __shared__ double2 lds[16];
+    double a = 0., b = 0.;
     for (int t = row_in_group<T>(); t < P.rows; t += blockDim.x / T) {
         const float2 terms = policy_whole_row<E, T, C, 0>(R, P, (int64_t)blockIdx.x * P.rows + t, nullptr);
         if (tid<T>() == 0) {
@@ -535,12 +535,12 @@ __global__ __launch_bounds__(1024) void policy_worker_kernel(Rows R, Policy P)
 template <class E, int T, int C>
 __global__ __launch_bounds__(T) void policy_slices_kernel(Rows R, Policy P)
 {
-    __shared__ float2 lds[T / 64];
+    __shared__ double2 lds[T / 64];
     const int64_t b = blockIdx.x, cut = R.dx ? R.rows * P.slices.count : 0;
     const int n = P.slices.count;
     if (b >= cut) {
         const int64_t worker = b - cut;
-        float loss = 0.f, kl = 0.f;
+        double loss = 0., kl = 0.;
         for (int t = threadIdx.x / 16; t < P.rows; t += T / 16) {
             const int64_t r = worker * P.rows + t;
             const float w = weight_of(P, r);
@@ -760,15 +760,15 @@ template <class E, int T, int C, bool TAIL>
 __global__ __launch_bounds__(1024) void distill_worker_kernel(Rows R, Distill P)
 {
     extern __shared__ uint32_t shared[];
-    __shared__ float2 lds[16];
-    float a = 0.f;
+    __shared__ double2 lds[16];
+    double a = 0.;
     for (int t = row_in_group<T>(); t < P.rows; t += blockDim.x / T) {
         const float term = distill_whole_row<E, T, C, 0, TAIL>(R, P, (int64_t)blockIdx.x * P.rows + t,
                                                                shared + row_in_group<T>() * distill_words(P.k, R.vocab), nullptr, nullptr, nullptr, nullptr);
         if (tid<T>() == 0) a += term;
         row_barrier<T>();                                 // the next row's list takes this one's place
     }
-    store_sums(wave_sum(a), 0.f, lds, P.loss_out + blockIdx.x, nullptr);
+    store_sums(wave_sum(a), 0., lds, P.loss_out + blockIdx.x, nullptr);
 }
 
 // ---------------------------------------------------------------- sums
@@ -776,9 +776,9 @@ __global__ __launch_bounds__(1024) void distill_worker_kernel(Rows R, Distill P)
 // loss_out[i], second_out[i] = sums of the terms of worker i's rows, always in the same order.
 __global__ __launch_bounds__(THREADS) void sum_kernel(const float2 *terms, int rows, float *loss_out, float *second_out)
 {
-    __shared__ float2 lds[WAVES];
+    __shared__ double2 lds[WAVES];
     const float2 *t = terms + (int64_t)blockIdx.x * rows;
-    float a = 0.f, b = 0.f;
+    double a = 0., b = 0.;
     for (int r = threadIdx.x; r < rows; r += THREADS) {
         a += t[r].x;
         b += t[r].y;
