@@ -461,7 +461,9 @@ struct PolicyRow {
 __device__ __forceinline__ PolicyRow policy_of(const Policy &P, const PolicyFigures &F, float logp)
 {
     const float w = F.w, a = F.a, rho = expf(logp - F.old);
-    const float product = rho * a, bounded = fminf(fmaxf(rho, P.low), P.high) * a;
+    // A factor of zero takes its term out also where the other one is beyond 32 bits (a ratio that is NaN stays so).
+    const bool no_ratio = a == 0.f && rho == rho;
+    const float product = no_ratio ? 0.f : rho * a, bounded = no_ratio ? 0.f : fminf(fmaxf(rho, P.low), P.high) * a;
     const bool free = product <= bounded || product != product;     // (fminf and fmaxf would take a ratio that is NaN for a bound)
     float kl = 0.f, dkl = 0.f;
     if (P.ref_logp) {
@@ -469,7 +471,9 @@ __device__ __forceinline__ PolicyRow policy_of(const Policy &P, const PolicyFigu
         dkl = -expm1f(d);
         kl = -dkl - d;
     }
-    return PolicyRow{w * (P.kl_coef * kl - (free ? product : bounded)), w * kl, w * (P.kl_coef * dkl - (free ? product : 0.f))};
+    const bool no_kl = P.kl_coef == 0.f && dkl == dkl;
+    const float kl_term = no_kl ? 0.f : P.kl_coef * kl, kl_slope = no_kl ? 0.f : P.kl_coef * dkl;
+    return PolicyRow{w * (kl_term - (free ? product : bounded)), w * kl, w * (kl_slope - (free ? product : 0.f))};
 }
 __device__ __forceinline__ float weight_of(const Policy &P, int64_t r)
 {
