@@ -660,13 +660,23 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
     }
     row_barrier<T>();
     seen = row_max<T>(seen, sums[0]);
-    if (seen == 2.f) {                                    // rare: the first entry of a column counts
-        if (t == 0) {
-            report(R.status);
-            for (int j = 1; j < P.k; ++j)
-                for (int i = 0; i < j; ++i)
-                    if (at[i] == at[j]) at[j] = -1;
+    if (seen == 2.f) {                                    // the first entry of a column counts
+        if (t == 0) report(R.status);
+        // An entry looks for its column among those before it.  One that has found it says so beside its column, which later ones still compare
+        // with, and goes when all have looked.  3 rows of 33001 f16 with 1024 entries, half of them the first again: 61 us; 25 ms by one thread.
+        constexpr int AGAIN = 1 << 30;                    // columns are below 2^20
+        for (int j = t; j < P.k; j += T) {
+            const int v = at[j];
+            if (v < 0) continue;
+            for (int i = 0; i < j; ++i)
+                if ((at[i] & ~AGAIN) == v) {
+                    at[j] = v | AGAIN;
+                    break;
+                }
         }
+        row_barrier<T>();
+        for (int j = t; j < P.k; j += T)
+            if (at[j] >= AGAIN) at[j] = -1;
         row_barrier<T>();
     }
     for (int j = t; j < P.k; j += T)
