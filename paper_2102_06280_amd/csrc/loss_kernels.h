@@ -15,6 +15,7 @@ constexpr int THREADS = 256;              // of workgroups that do not walk alon
 constexpr int WAVES = THREADS / 64;
 
 // A grid's threads have to number less than 2^32: many workgroups make a second dimension.
+// As pairs or workers may be 2^22 and a workgroup has up to 1024 threads, that goes for those as well.
 __device__ __forceinline__ int64_t group() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
@@ -192,7 +193,7 @@ struct Preference {
     float beta, smoothing, scale;
     Factor c;
     int pairs;           // of each worker
-    int64_t all_rows;
+    int64_t all_pairs, all_rows;
     float *logp, *margin_out, *coef;
     float *low;          // what log-probabilities have lost to 32 bits: of a sum over a sequence it is the larger part of the error.  The same memory as
                          // coef, which a pair needs when its sums are known
@@ -258,11 +259,12 @@ __device__ __forceinline__ void join_rows(const Preference &P, int from, int to)
 __global__ __launch_bounds__(PAIR_THREADS) void pair_kernel(Preference P)
 {
     __shared__ double lds[PAIR_THREADS / 64];
-    const int64_t j = blockIdx.x;
+    const int64_t j = group();
+    if (j >= P.all_pairs) return;
     const int t = threadIdx.x, n = (int)P.all_rows;
     int a[3];
     rows_of_pair(P, j, a);
-    const int from = j == 0 ? 0 : a[0], to = j == gridDim.x - 1 ? n : a[2];
+    const int from = j == 0 ? 0 : a[0], to = j == P.all_pairs - 1 ? n : a[2];
     if (P.slices > 1) {
         if (P.slices > 8) join_rows<16>(P, from, to);     // few rows
         else join_rows<1>(P, from, to);
@@ -524,15 +526,17 @@ template <class E, int T, int C>
 __global__ __launch_bounds__(1024) void policy_worker_kernel(Rows R, Policy P)
 {
     __shared__ double2 lds[16];
+    const int64_t worker = group();
+    if (worker * P.rows >= R.rows) return;
     double a = 0., b = 0.;
     for (int t = row_in_group<T>(); t < P.rows; t += blockDim.x / T) {
-        const float2 terms = policy_whole_row<E, T, C, 0>(R, P, (int64_t)blockIdx.x * P.rows + t, nullptr);
+        const float2 terms = policy_whole_row<E, T, C, 0>(R, P, worker * P.rows + t, nullptr);
         if (tid<T>() == 0) {
             a += terms.x;
             b += terms.y;
         }
     }
-    store_sums(wave_sum(a), wave_sum(b), lds, P.loss_out + blockIdx.x, P.kl_out ? P.kl_out + blockIdx.x : nullptr);
+    store_sums(wave_sum(a), wave_sum(b), lds, P.loss_out + worker, P.kl_out ? P.kl_out + worker : nullptr);
 }
 
 // The second launch for rows in slices: the slices' gradients, and behind them a workgroup for every worker's sums.
@@ -775,14 +779,16 @@ __global__ __launch_bounds__(1024) void distill_worker_kernel(Rows R, Distill P)
 {
     extern __shared__ uint32_t shared[];
     __shared__ double2 lds[16];
+    const int64_t worker = group();
+    if (worker * P.rows >= R.rows) return;
     double a = 0.;
     for (int t = row_in_group<T>(); t < P.rows; t += blockDim.x / T) {
-        const float term = distill_whole_row<E, T, C, 0, TAIL>(R, P, (int64_t)blockIdx.x * P.rows + t,
+        const float term = distill_whole_row<E, T, C, 0, TAIL>(R, P, worker * P.rows + t,
                                                                shared + row_in_group<T>() * distill_words(P.k, R.vocab), nullptr, nullptr, nullptr, nullptr);
         if (tid<T>() == 0) a += term;
         row_barrier<T>();                                 // the next row's list takes this one's place
     }
-    store_sums(wave_sum(a), 0., lds, P.loss_out + blockIdx.x, nullptr);
+    store_sums(wave_sum(a), 0., lds, P.loss_out + worker, nullptr);
 }
 
 // ---------------------------------------------------------------- sums

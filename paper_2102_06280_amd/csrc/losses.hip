@@ -10,7 +10,7 @@ namespace {
 
 size_t size_of(int type) { return type == DBW_TYPE_F32 ? 4 : 2; }
 
-constexpr int64_t MAX_GROUPS = 1 << 22;   // of kernels that take a workgroup per worker or pair
+constexpr int64_t MAX_GROUPS = 1 << 22;   // of workers and of pairs: of one dimension where they have a workgroup of at most 512 threads each
 
 struct Shape {
     int64_t rows;        // of all workers
@@ -307,7 +307,7 @@ extern "C" int dbw_distill_loss(const dbw_logits *shape, int32_t k, const void *
             typedef decltype(e) E;
             if (group_threads)
                 by_group_row(S.row_bytes, [&](auto p) {
-                    const dim3 grid((uint32_t)shape->workers);
+                    const dim3 grid = grid_of(shape->workers);
                     const size_t bytes = group_threads / p.T * lds;
                     if (teacher_lse) launch(loss::distill_worker_kernel<E, p.T, p.C, true>, grid, group_threads, bytes);
                     else launch(loss::distill_worker_kernel<E, p.T, p.C, false>, grid, group_threads, bytes);
@@ -360,7 +360,7 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     }
     const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
     if (pairs > 0) {
-        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, S.rows, logp, margin_out, W.coef, W.coef,
+        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, (int64_t)shape->workers * pairs, S.rows, logp, margin_out, W.coef, W.coef,
                                  W.slices, W.stats, W.token_logit, slices.count, status_out};
         if (few) {
             if (dlogits) launch_gradient(shape, S, loss::Gradient{tokens, nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, &P, s);
@@ -368,7 +368,7 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
             DBW_HIP(hipGetLastError());
             return DBW_OK;
         }
-        hipLaunchKernelGGL(loss::pair_kernel, dim3((uint32_t)(shape->workers * pairs)), dim3(loss::PAIR_THREADS), 0, s, P);
+        hipLaunchKernelGGL(loss::pair_kernel, grid_of(P.all_pairs), dim3(loss::PAIR_THREADS), 0, s, P);
         DBW_HIP(hipGetLastError());
     }
     if (dlogits && S.rows > 0)
@@ -410,7 +410,7 @@ extern "C" int dbw_policy_loss(const dbw_logits *shape, const void *logits, cons
                 });
             else if (group_threads)
                 by_group_row(S.row_bytes, [&](auto p) {
-                    hipLaunchKernelGGL((loss::policy_worker_kernel<E, p.T, p.C>), dim3((uint32_t)shape->workers), dim3(group_threads), 0, s, S.R, P);
+                    hipLaunchKernelGGL((loss::policy_worker_kernel<E, p.T, p.C>), grid_of(shape->workers), dim3(group_threads), 0, s, S.R, P);
                 });
             else
                 by_row(S.row_bytes, [&](auto p) {
