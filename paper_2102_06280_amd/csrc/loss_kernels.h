@@ -204,8 +204,9 @@ struct Preference {
     int32_t *status;
 };
 
-__device__ __forceinline__ bool takes_part(const Preference &P, int r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
+__device__ __forceinline__ bool takes_part(const Preference &P, int64_t r) { return P.tokens[r] >= 0 && !(P.weights && P.weights[r] == 0.f); }
 
+// (Numbers of rows go up to 2^31 - 2: those that count on in steps of a workgroup's threads need 64 bits.)
 // Rows a[0] ... a[1] - 1 and a[1] ... a[2] - 1 of pair j, within the rows there are whatever the offsets say.
 __device__ __forceinline__ void rows_of_pair(const Preference &P, int64_t j, int (&a)[3])
 {
@@ -220,7 +221,7 @@ __device__ __forceinline__ void rows_of_pair(const Preference &P, int64_t j, int
 __device__ __forceinline__ double part_of_pair(const Preference &P, const int (&a)[3], int thread, int threads)
 {
     double h = 0.;
-    for (int r = a[0] + thread; r < a[2]; r += threads)
+    for (int64_t r = (int64_t)a[0] + thread; r < a[2]; r += threads)
         if (takes_part(P, r)) {
             const double term = (P.weights ? P.weights[r] : 1.f) * ((double)P.logp[r] - P.ref_logp[r] + P.low[r]);
             h += r < a[1] ? term : -term;
@@ -242,10 +243,10 @@ template <int T>
 __device__ __forceinline__ void join_rows(const Preference &P, int from, int to)
 {
     const bool first = threadIdx.x % T == 0;
-    for (int r = from + (int)threadIdx.x / T; r < to; r += PAIR_THREADS / T) {
+    for (int64_t r = (int64_t)from + threadIdx.x / T; r < to; r += PAIR_THREADS / T) {
         double logp = 0.;
         if (takes_part(P, r)) {
-            const MaxSum mz = joined<T>(P.stats + (int64_t)r * P.slices, P.slices, P.c);
+            const MaxSum mz = joined<T>(P.stats + r * P.slices, P.slices, P.c);
             logp = log_p(P.token_logit[r], P.scale, mz);
             if (first) P.joined[r] = mz;
         }
@@ -273,7 +274,7 @@ __global__ __launch_bounds__(PAIR_THREADS) void pair_kernel(Preference P)
     const float u = (float)(P.beta * row_sum<PAIR_THREADS>(part_of_pair(P, a, t, PAIR_THREADS), lds));
     if (t == 0) P.margin_out[j] = u;
     const float slope = slope_of(P, u);
-    for (int r = from + t; r < to; r += PAIR_THREADS)
+    for (int64_t r = (int64_t)from + t; r < to; r += PAIR_THREADS)
         P.coef[r] = takes_part(P, r) && r >= a[0] && r < a[2] ? (r < a[1] ? slope : -slope) * (P.weights ? P.weights[r] : 1.f) : 0.f;
 }
 
@@ -416,7 +417,7 @@ __global__ __launch_bounds__(T * ROWS_OF<T>) void pair_gradient_kernel(Rows R, G
     if (r >= R.rows) return;
     const int token = P.tokens[r];
     float g = 0.f;
-    if (takes_part(Q, (int)r)) {
+    if (takes_part(Q, r)) {
         // the last sequence that starts at the row or before it
         const int lane = threadIdx.x & (LANES - 1), sequences = 2 * P.pairs.workers * Q.pairs;
         float starts = 0.f;
@@ -799,7 +800,7 @@ __global__ __launch_bounds__(THREADS) void sum_kernel(const float2 *terms, int r
     __shared__ double2 lds[WAVES];
     const float2 *t = terms + (int64_t)blockIdx.x * rows;
     double a = 0., b = 0.;
-    for (int r = threadIdx.x; r < rows; r += THREADS) {
+    for (int64_t r = threadIdx.x; r < rows; r += THREADS) {
         a += t[r].x;
         b += t[r].y;
     }

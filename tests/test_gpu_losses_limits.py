@@ -65,3 +65,32 @@ def test_the_most_workers_in_one_workgroup_each(B):
     B.dbw_distill_loss(shape, 1, x, tokens, torch.zeros(total, device="cuda"), None, loss, work, dlogits=grad)
     assert ((loss - math.log(2)).abs() < 1e-6).all()
     assert torch.equal(grad, want.to(BF16).expand(total, 2))
+
+
+def test_the_most_rows(B):
+    """Row numbers up to 2^31 - 2, in steps of a workgroup's threads."""
+    rows, vocab, pairs, last = (1 << 31) - 1, 2, 2048, 1500
+    x = torch.zeros(rows * vocab, dtype=BF16, device="cuda")
+    tokens = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    shape = B.make_logits(1, rows, vocab, BF16)
+    work = torch.empty(B.dbw_loss_work_bytes(shape), dtype=torch.uint8, device="cuda")
+    rf = torch.full((rows,), -math.log(2), device="cuda")
+    rf[-last:] = -1.0
+    start = torch.linspace(0, rows - last, 2 * pairs, dtype=torch.float64).long()
+    start = torch.cat([start, torch.tensor([rows])]).int().cuda()           # the last sequence: the last rows
+    loss, margin = torch.full((1,), 7.0, device="cuda"), torch.full((pairs,), 7.0, device="cuda")
+    grad = torch.full_like(x, 7.0)
+    B.dbw_preference_loss(shape, pairs, x, tokens, start, rf, None, 0.01, 0.0, loss, work, margin, dlogits=grad)
+    u = -0.01 * last * (1 - math.log(2))
+    assert (margin[:-1].abs() < 1e-3).all() and abs(margin[-1].item() - u) < 1e-3
+    slope = lambda u: -0.01 / pairs / (1 + math.exp(u))
+    tail = grad[-2 * last:].view(last, 2).double().cpu()
+    want = torch.tensor([-0.5, 0.5], dtype=torch.float64) * slope(u)
+    assert ((tail - want).abs() <= 2.0 ** -7 * want.abs()).all()
+    head = grad[:2000].view(1000, 2).double().cpu()
+    want = torch.tensor([0.5, -0.5], dtype=torch.float64) * slope(0.0)
+    assert ((head - want).abs() <= 2.0 ** -7 * want.abs()).all()
+    del grad, start
+    B.dbw_policy_loss(shape, x, tokens, rf, None, torch.ones(rows, device="cuda"), None, 0.2, 10.0, 0.0, loss, work)
+    want = -((rows - last) + last * math.e / 2) / rows
+    assert abs(loss.item() - want) < 1e-6
