@@ -343,14 +343,17 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     if (rc != DBW_OK) return rc;
     if (!work || !loss_out || !seq_start || (pairs > 0 && !margin_out) || (S.rows > 0 && (!tokens || !ref_logp))) return DBW_ERR_NULL;
     if (pairs < 0 || !isfinite(beta) || !(smoothing >= 0.f && smoothing <= 1.f)) return DBW_ERR_INVALID;
-    if ((int64_t)shape->workers * pairs > MAX_GROUPS) return DBW_ERR_UNSUPPORTED;
+    const int64_t all_pairs = (int64_t)shape->workers * pairs;
+    if (all_pairs > MAX_GROUPS) return DBW_ERR_UNSUPPORTED;
     const Work W = split_work(work, S.rows);
     hipStream_t s = (hipStream_t)stream;
     float *const logp = logp_out ? logp_out : W.logp;
-    // Few rows and short pairs: the gradient's workgroups sum their pairs up themselves, which costs less than a launch in between.  Two to four pairs
-    // of 10 to 250 rows x 80 to 3840 bf16 11.4 us, with the launch 14.7; 128 x 20000 (40 KB) 11.8 and 14.8, but 128 x 60000 20.2 and 15.8: longer rows
-    // are better read in slices, which only the launch joins.
-    const bool few = pairs > 0 && S.rows > 0 && S.rows <= 1024 && S.row_bytes <= 48 << 10 && S.rows <= (int64_t)64 * shape->workers * pairs;
+    // Few rows in few and short pairs: the gradient's workgroups sum their pairs up themselves, which costs less than a launch in between.  Two to four
+    // pairs of 10 to 250 rows x 80 to 3840 bf16 11.4 us, with the launch 14.7; 128 x 20000 (40 KB) 11.8 and 14.8, but 128 x 60000 20.2 and 15.8:
+    // longer rows are better read in slices, which only the launch joins.  A worker's pairs are one workgroup's, four at a time: of 1000 x 500 16 pairs
+    // 13.7 and 14.2, 64 23 and 14.2, 500 116 and 14.2; and every row looks for its sequence among all: 128 pairs of 16 workers 11.1 and 14.2,
+    // 512 of 64 or more workers 14.5 and 14.2.
+    const bool few = pairs > 0 && pairs <= 16 && all_pairs <= 256 && S.rows > 0 && S.rows <= 1024 && S.row_bytes <= 48 << 10 && S.rows <= 64 * all_pairs;
     loss::Slices slices{1, 0};
     if (S.rows > 0) {
         if (pairs > 0 && !few) slices = slices_of(shape, S.rows, SLICED_ROWS, SLICE_GROUPS);  // (whose parts the pairs' kernel joins)
@@ -360,7 +363,7 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     }
     const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
     if (pairs > 0) {
-        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, (int64_t)shape->workers * pairs, S.rows, logp, margin_out, W.coef, W.coef,
+        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, all_pairs, S.rows, logp, margin_out, W.coef, W.coef,
                                  W.slices, W.stats, W.token_logit, slices.count, status_out};
         if (few) {
             if (dlogits) launch_gradient(shape, S, loss::Gradient{tokens, nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, &P, s);
