@@ -1,7 +1,9 @@
 // Kernels of the losses on rows of logits.
 //
-// All of them are bound by memory where rows are many: a bf16 logit is two bytes to read and two to write, for two exponentials (a quarter of the rate
-// of other instructions) and about a dozen other instructions, which take about half as long as its bytes.  The rows are independent, so a
+// Where rows are many and long, those that write gradients are bound by memory (vector units busy 33 to 73 % of the time), those that only read by their
+// instructions as much (86 %): a bf16 logit is two bytes to read for an exponential, at a quarter of the rate of other instructions, and six or seven of
+// those.  Pieces beyond a row's end are computed as well, so short rows, and rows a little longer than a whole number of a workgroup's passes, are
+// bound by instructions.  The rows are independent, so a
 // row belongs to one workgroup, or its part of one, from its first byte to its gradient, and only the sums over a worker's rows cross workgroups:
 // through memory and a second, small launch, in a fixed order (no atomics on floating point).  Figures: us on MI355X, logits read and gradients
 // written at the rate named; a plain copy with streaming accesses reaches 6.5 TB/s here.
@@ -113,8 +115,8 @@ __device__ __forceinline__ MaxSum sums_of(const RowOf<E, T> &row, int first, int
     return mz;
 }
 
-// A workgroup a row, or a slice: one pass, the maximum and the sum of a batch after the other.  Bound by memory: 4096 x 65536 bf16 79 us, 6.2 TB/s; a single
-// row by latency.  AGAIN: the rows will be read again soon, for their gradient.
+// A workgroup a row, or a slice: one pass, the maximum and the sum of a batch after the other.  4096 x 65536 bf16, a tenth of the rows without
+// a part, 0.48 GB in 83 us, 5.8 TB/s, bound by memory and instructions; a single row by latency.  AGAIN: the rows will be read again soon, for their gradient.
 template <class E, int T, int C, bool AGAIN>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void logp_kernel(Rows R, Logp P)
 {
@@ -358,7 +360,7 @@ __device__ __forceinline__ void gradient_of_slice(const Rows &R, const Gradient 
 }
 
 // A workgroup a slice of 16 KB: the row's (m, Z) are known, so every piece is by itself.  Bound by memory: 8192 x 32768 bf16, 15 % of the rows without a part,
-// 0.99 GB in 147 us, 6.8 TB/s with what is left of the rows in the last-level cache.
+// 0.99 GB in 148 us, 6.7 TB/s with what is left of the rows in the last-level cache.
 template <class E, int T, int C, bool FROM_L>
 __global__ __launch_bounds__(T * ROWS_OF<T>) void gradient_kernel(Rows R, Gradient P)
 {
@@ -511,7 +513,7 @@ __device__ __forceinline__ float2 policy_whole_row(const Rows &R, const Policy &
 }
 
 // A workgroup a row, which is read once and stays in registers until its gradient is written: the coefficient needs nothing but the row's own sum.
-// Bound by memory: 4096 x 32768 bf16 0.5 GB in 87 us, 5.7 TB/s.
+// Bound by memory: 4096 x 32768 bf16, 15 % of the rows without a part, 0.5 GB in 88 us, 5.7 TB/s.
 template <class E, int T, int C, int S>
 __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void policy_kernel(Rows R, Policy P)
 {
@@ -760,7 +762,7 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
 }
 
 // As policy_kernel, with the list in LDS beside it.  Bound by memory, and by what the list costs a row (five short loops over it with barriers between):
-// 2048 x 32000 bf16, 64 entries, 0.25 GB in 57 us, 4.4 TB/s; 4096 x 131072, 128 entries, 2.15 GB in 417 us, 5.2 TB/s.
+// 2048 x 32000 bf16, 64 entries, 0.25 GB in 57 us, 4.4 TB/s; 4096 x 131072, 128 entries, 2.15 GB in 420 us, 5.1 TB/s.
 template <class E, int T, int C, int S, bool TAIL>
 __global__ __launch_bounds__(T * ROWS_OF<T>, C == 16 ? 4 : 1) void distill_kernel(Rows R, Distill P)
 {

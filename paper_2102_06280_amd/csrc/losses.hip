@@ -97,7 +97,8 @@ dim3 grid_of(int64_t groups)
 }
 
 // Which kernel takes a row, by its length in bytes: T threads, C pieces a thread at a time (Walk: and S at a time of what lies behind them).
-// Times below in us, bf16 unless said otherwise, rows x vocabulary.
+// Times below in us, bf16 unless said otherwise, rows x vocabulary.  (Those of one plan or rule against another were taken when a term of a sum took an
+// instruction less: kernels that only read a row take 4 % more now, those of many short rows 4 to 12 %, on either side.)
 template <int T_, int C_, int S_ = 0>
 struct Plan {
     static constexpr int T = T_, C = C_, S = S_;
@@ -127,7 +128,7 @@ void by_row(int64_t bytes, F f)
     else if (bytes <= 16 * 512 * 16) f(Plan<512, 16>());
     else f(Plan<512, 16, 8>());
 }
-// For those that only read it: 4096 x 65536 in 78 to 79, 6.2 TB/s.
+// For those that only read it: 4096 x 65536, a tenth of the rows without a part, in 83, 5.8 TB/s.
 template <class F>
 void by_length(int64_t bytes, F f)
 {
