@@ -16,8 +16,7 @@ namespace loss {
 constexpr int THREADS = 256;              // of workgroups that do not walk along a row
 constexpr int WAVES = THREADS / 64;
 
-// A grid's threads have to number less than 2^32: many workgroups make a second dimension.
-// As pairs or workers may be 2^22 and a workgroup has up to 1024 threads, that goes for those as well.
+// A grid's threads have to number less than 2^32: many workgroups make a second dimension (2^22 pairs or workers of 1024 threads would be as many).
 __device__ __forceinline__ int64_t group() { return (int64_t)blockIdx.y * gridDim.x + blockIdx.x; }
 
 __device__ __forceinline__ int wave_id() { return __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6); }
@@ -60,7 +59,8 @@ __device__ __forceinline__ MaxSum joined(const MaxSum *slices, int count, const 
 }
 constexpr int MAX_SLICES = 32;
 
-// Sums over a workgroup's waves, in their order.  A worker's sums are held in 64 bits: of thousands of terms that are alike, roundings to 32 bits have one sign.
+// Sums over a workgroup's waves, in their order.  A worker's sums are held in 64 bits: of thousands of terms that are alike, roundings to 32 bits have
+// one sign.
 __device__ __forceinline__ void store_sums(double a, double b, double2 *lds, float *first_out, float *second_out)
 {
     if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = make_double2(a, b);
@@ -318,8 +318,8 @@ struct Gradient {
     PairLoss pairs;      // workgroups behind the rows' give every worker's loss
 };
 
-// Largest |L| that is taken as it is: in 32 bits it is off by 2^-17, and so is every probability, of itself.  Larger ones have lost too much of ln Z (all of it in
-// a row of equal logits of 1e30), or are infinite where their row is not.
+// Largest |L| that is taken as it is: in 32 bits it is off by up to 2^-17, and so is every probability, of itself.  Larger ones have lost too much of ln Z
+// (all of it in a row of equal logits of 1e30), or are infinite where their row is not.
 constexpr float MOST_L = 256.f;
 
 // FROM_L: a row whose L is larger than that is summed again, whole and by the workgroup of its first slice, which then also writes it all: in place, nobody
@@ -730,7 +730,7 @@ __device__ __forceinline__ float distill_whole_row(const Rows &R, const Distill 
             const float log_pj = fmaf(R.scale, xs[j] - mz.m, -ln_z);
             mass += qj;
             if (!(qj <= 0.f)) part += qj * (log_q - log_pj);
-            q[j] = exponential(log_pj) - qj;                     // dl/dx over s
+            q[j] = exponential(log_pj) - qj;              // dl/dx over s
         }
     part = row_sum<T>(part, sums[3]);
     float mass_out = 1.f;                                 // s times this is the sum of the gradient's columns that are not in the list

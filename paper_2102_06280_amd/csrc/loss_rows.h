@@ -85,7 +85,12 @@ __device__ __forceinline__ float times(const Factor &c, float d) { return fmaf(d
 __device__ __forceinline__ float power_alone(float x, const Base &b) { return __builtin_amdgcn_exp2f((x - b.m) * b.c.near); }
 __device__ __forceinline__ float power(float x, const Base &b) { return __builtin_amdgcn_exp2f(times(b.c, x - b.m)); }
 
-__device__ __forceinline__ float exponential(float v) { return __builtin_amdgcn_exp2f(times(Factor{0x1.715474p0f, (float)(LOG2E - 0x1.715474p0), (float)LOG2E}, v)); }
+// e^v: log2(e) likewise
+__device__ __forceinline__ float exponential(float v)
+{
+    constexpr float HI = 0x1.715474p0f;
+    return __builtin_amdgcn_exp2f(times(Factor{HI, (float)(LOG2E - HI), (float)LOG2E}, v));
+}
 
 // A row is T threads' work; a workgroup has T threads, or several rows of 64 or 16 threads each.
 template <int T>

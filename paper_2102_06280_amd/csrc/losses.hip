@@ -10,7 +10,7 @@ namespace {
 
 size_t size_of(int type) { return type == DBW_TYPE_F32 ? 4 : 2; }
 
-constexpr int64_t MAX_GROUPS = 1 << 22;   // of workers and of pairs: of one dimension where they have a workgroup of at most 512 threads each
+constexpr int64_t MAX_GROUPS = 1 << 22;   // of workers, and of pairs
 
 struct Shape {
     int64_t rows;        // of all workers
@@ -364,8 +364,8 @@ extern "C" int dbw_preference_loss(const dbw_logits *shape, int32_t pairs, const
     }
     const loss::PairLoss mean{margin_out, shape->workers, pairs, smoothing, loss_out};
     if (pairs > 0) {
-        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, all_pairs, S.rows, logp, margin_out, W.coef, W.coef,
-                                 W.slices, W.stats, W.token_logit, slices.count, status_out};
+        const loss::Preference P{tokens, seq_start, ref_logp, weights, beta, smoothing, S.R.scale, S.R.c, pairs, all_pairs, S.rows, logp, margin_out, W.coef,
+                                 W.coef, W.slices, W.stats, W.token_logit, slices.count, status_out};
         if (few) {
             if (dlogits) launch_gradient(shape, S, loss::Gradient{tokens, nullptr, W.stats, nullptr, gradient_slices_of(shape, S.rows), mean}, &P, s);
             else hipLaunchKernelGGL(loss::pair_sums_kernel, dim3((uint32_t)shape->workers), dim3(loss::THREADS), 0, s, mean, P);
