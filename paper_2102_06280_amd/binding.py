@@ -1,5 +1,5 @@
-"""Thin ctypes binding over libdbw.so: the same entry points as include/dbw.h, dbw_losses.h and dbw_measure.h, with
-argument marshalling only.  Device arrays are torch tensors (used for memory and streams,
+"""Thin ctypes binding over libdbw.so: the same entry points as include/dbw.h, dbw_losses.h, dbw_layers.h and
+dbw_measure.h, with argument marshalling only.  Device arrays are torch tensors (used for memory and streams,
 nothing else); every computation happens inside the library's kernels.
 
 There is no fallback: if the library has not been built, importing this module raises.
@@ -29,6 +29,7 @@ LAYOUT_ROWS, LAYOUT_TILES = 0, 1
 TILE_COLUMNS = 64
 TYPE_F32, TYPE_BF16, TYPE_F16 = 0, 1, 2
 TEACHER_MAX, DISTILL_MAX_VOCAB = 1024, 1 << 20
+LAYER_MAX_WIDTH, EXPERTS_MAX = 1 << 20, 1024
 
 EXPORTS = ["dbw_create", "dbw_select", "dbw_dtur_b", "dbw_dtur_select", "dbw_dtur_reset", "dbw_dtur_get_state", "dbw_dtur_set_state",
            "dbw_get_selection",
@@ -37,7 +38,10 @@ EXPORTS = ["dbw_create", "dbw_select", "dbw_dtur_b", "dbw_dtur_select", "dbw_dtu
            "dbw_convert_layout", "dbw_grad", "dbw_check", "dbw_get_links", "dbw_mix_path",
            "dbw_destroy", "dbw_strerror", "dbw_set_timing", "dbw_get_timing", "dbw_calibrate",
            "dbw_loss_work_bytes", "dbw_token_logp", "dbw_token_logp_grad", "dbw_distill_loss", "dbw_preference_loss",
-           "dbw_policy_loss"]
+           "dbw_policy_loss",
+           "dbw_checkpoint_bytes", "dbw_checkpoint_store", "dbw_checkpoint_load", "dbw_layer_norm", "dbw_layer_norm_work_bytes",
+           "dbw_layer_norm_grad", "dbw_expert_work_bytes", "dbw_expert_sort", "dbw_expert_gather", "dbw_expert_combine",
+           "dbw_expert_combine_grad", "dbw_checkpoint_weight_grad_work_bytes", "dbw_checkpoint_weight_grad"]
 
 
 class dbw_model(C.Structure):
@@ -53,6 +57,20 @@ class dbw_opts(C.Structure):
 class dbw_logits(C.Structure):
     _fields_ = [("workers", C.c_int32), ("rows", C.c_int32), ("vocab", C.c_int32), ("type", C.c_int32),
                 ("ld", C.c_int64), ("ld_grad", C.c_int64), ("scale", C.c_float)]
+
+
+class dbw_rows(C.Structure):
+    _fields_ = [("workers", C.c_int32), ("rows", C.c_int32), ("width", C.c_int32), ("type", C.c_int32),
+                ("ld", C.c_int64), ("ld_out", C.c_int64)]
+
+
+class dbw_routing(C.Structure):
+    _fields_ = [("workers", C.c_int32), ("tokens", C.c_int32), ("k", C.c_int32), ("experts", C.c_int32)]
+
+
+class dbw_linear(C.Structure):
+    _fields_ = [("workers", C.c_int32), ("rows", C.c_int32), ("inputs", C.c_int32), ("outputs", C.c_int32), ("type", C.c_int32),
+                ("experts", C.c_int32), ("tokens", C.c_int32), ("k", C.c_int32), ("ld", C.c_int64)]
 
 
 class dbw_kernel_time(C.Structure):
@@ -96,6 +114,19 @@ _lib.dbw_token_logp_grad.argtypes = [_vp] * 8
 _lib.dbw_distill_loss.argtypes = [_vp, _i32, _vp, _vp, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.dbw_preference_loss.argtypes = [_vp, _i32, _vp, _vp, _vp, _vp, _vp, _f, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
 _lib.dbw_policy_loss.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _f, _f, _f, _vp, _vp, _vp, _vp, _vp, _vp, _vp]
+
+for _name in ("dbw_checkpoint_bytes", "dbw_layer_norm_work_bytes", "dbw_expert_work_bytes", "dbw_checkpoint_weight_grad_work_bytes"):
+    getattr(_lib, _name).restype = _i64
+    getattr(_lib, _name).argtypes = [_vp]
+_lib.dbw_checkpoint_store.argtypes = [_vp] * 5
+_lib.dbw_checkpoint_load.argtypes = [_vp] * 4
+_lib.dbw_layer_norm.argtypes = [_vp, _vp, _vp, _vp, _i64, _i64, _i64, _f, _vp, _vp, _vp, _vp]
+_lib.dbw_layer_norm_grad.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _i64, _vp, _vp]
+_lib.dbw_expert_sort.argtypes = [_vp] * 8
+_lib.dbw_expert_gather.argtypes = [_vp] * 7
+_lib.dbw_expert_combine.argtypes = [_vp] * 8
+_lib.dbw_expert_combine_grad.argtypes = [_vp] * 10
+_lib.dbw_checkpoint_weight_grad.argtypes = [_vp, _vp, _vp, _vp, _vp, _vp, _i64, _i64, _i64, _vp, _vp, _vp]
 
 
 class DbwError(RuntimeError):
@@ -365,3 +396,141 @@ def dbw_policy_loss(shape, logits, tokens, old_logp, ref_logp, advantage, weight
                                      _arr(kl_out, _F32, shape.workers), _arr(logp_out, _F32, n),
                                      _arr(dlogits, dtype, size_grad), _arr(status_out, _I32, 1),
                                      _arr(work, _U8, scratch), _current()), "dbw_policy_loss")
+
+
+# --------------------------------------------------------------------------- between the products of a language model
+
+def make_rows(workers: int, rows: int, width: int, type: int, ld: int = 0, ld_out: int = 0) -> dbw_rows:
+    """type: TYPE_* (or the torch dtype) of the arrays of rows; ld, ld_out: strides of what goes in and comes out, in elements."""
+    return dbw_rows(workers, rows, width, _TYPE_OF.get(type, type), ld, ld_out)
+
+
+def make_routing(workers: int, tokens: int, k: int, experts: int) -> dbw_routing:
+    return dbw_routing(workers, tokens, k, experts)
+
+
+def make_linear(workers: int, rows: int, inputs: int, outputs: int, type: int, experts: int = 1, tokens: int = None, k: int = 1,
+                ld: int = 0) -> dbw_linear:
+    """type: TYPE_* (or the torch dtype) of dy, ld the stride of its rows; tokens: rows of the checkpoint of each worker, by default as many as of dy."""
+    return dbw_linear(workers, rows, inputs, outputs, _TYPE_OF.get(type, type), experts, rows if tokens is None else tokens, k, ld)
+
+
+def _size(shape, name):
+    return _chk(getattr(_lib, name)(C.byref(shape)), name)
+
+
+def dbw_checkpoint_bytes(shape: dbw_rows) -> int:
+    return _size(shape, "dbw_checkpoint_bytes")
+
+
+def dbw_layer_norm_work_bytes(shape: dbw_rows) -> int:
+    return _size(shape, "dbw_layer_norm_work_bytes")
+
+
+def dbw_expert_work_bytes(routing: dbw_routing) -> int:
+    return _size(routing, "dbw_expert_work_bytes")
+
+
+def dbw_checkpoint_weight_grad_work_bytes(shape: dbw_linear) -> int:
+    return _size(shape, "dbw_checkpoint_weight_grad_work_bytes")
+
+
+def _spans(shape):
+    """Number of all workers' rows, their dtype, the elements that arrays of stride ld and of stride ld_out have at least."""
+    n, d = shape.workers * shape.rows, shape.width
+    ld = shape.ld or d
+    if n <= 0:
+        return n, _DTYPE_OF.get(shape.type), 0, 0
+    return n, _DTYPE_OF.get(shape.type), (n - 1) * ld + d, (n - 1) * (shape.ld_out or ld) + d
+
+
+def _mask(mask, n):
+    return None if mask is None else _arr(mask, torch.bool if mask.dtype is torch.bool else _U8, n)
+
+
+def _parameters(t, workers):
+    """Pointer and stride of the workers' rows of parameters or gradients, [N, ld]."""
+    if t is None:
+        return None, 0
+    if t.dim() != 2 or t.shape[0] != workers:
+        raise ValueError(f"need a row of parameters for each of {workers} workers, got {tuple(t.shape)}")
+    return _arr(t, _F32, 0), t.shape[1]
+
+
+def dbw_checkpoint_store(shape, x, checkpoint, mask=None):
+    n, dtype, size, _ = _spans(shape)
+    return _chk(_lib.dbw_checkpoint_store(C.byref(shape), _arr(x, dtype, size), _mask(mask, n),
+                                          _arr(checkpoint, _U8, dbw_checkpoint_bytes(shape)), _current()), "dbw_checkpoint_store")
+
+
+def dbw_checkpoint_load(shape, checkpoint, x_out):
+    n, dtype, _, size = _spans(shape)
+    return _chk(_lib.dbw_checkpoint_load(C.byref(shape), _arr(checkpoint, _U8, dbw_checkpoint_bytes(shape)), _arr(x_out, dtype, size),
+                                         _current()), "dbw_checkpoint_load")
+
+
+def dbw_layer_norm(shape, x, params, y, weight_at: int = -1, bias_at: int = -1, eps: float = 1e-5, mask=None, stats_out=None, checkpoint=None):
+    """params [N, ld]: the workers' rows of parameters."""
+    n, dtype, size, size_out = _spans(shape)
+    rows, ld = _parameters(params, shape.workers)
+    kept = None if checkpoint is None else _arr(checkpoint, _U8, dbw_checkpoint_bytes(shape))
+    return _chk(_lib.dbw_layer_norm(C.byref(shape), _arr(x, dtype, size), _mask(mask, n), rows, ld, weight_at, bias_at, eps,
+                                    _arr(y, dtype, size_out), _arr(stats_out, _F32, 2 * n), kept, _current()), "dbw_layer_norm")
+
+
+def dbw_layer_norm_grad(shape, dy, x, stats, params, dx, grads, work, weight_at: int = -1, bias_at: int = -1, mask=None, checkpoint=None):
+    """x None: from the checkpoint.  grads [N, ld]: the workers' rows of gradients, or None."""
+    n, dtype, size, size_out = _spans(shape)
+    rows, ld = _parameters(params, shape.workers)
+    to, ld_grads = _parameters(grads, shape.workers)
+    kept = None if checkpoint is None else _arr(checkpoint, _U8, dbw_checkpoint_bytes(shape))
+    return _chk(_lib.dbw_layer_norm_grad(C.byref(shape), _arr(dy, dtype, size_out), _arr(x, dtype, size), kept, _mask(mask, n),
+                                         _arr(stats, _F32, 2 * n), rows, ld, weight_at, bias_at, _arr(dx, dtype, size), to, ld_grads,
+                                         _arr(work, _U8, dbw_layer_norm_work_bytes(shape)), _current()), "dbw_layer_norm_grad")
+
+
+def dbw_expert_sort(routing, expert, start_out, place_out, source_out, work, status_out=None):
+    n = routing.workers * routing.tokens * routing.k
+    return _chk(_lib.dbw_expert_sort(C.byref(routing), _arr(expert, _I32, n), _arr(start_out, _I32, routing.workers * (routing.experts + 1)),
+                                     _arr(place_out, _I32, n), _arr(source_out, _I32, n), _arr(status_out, _I32, 1),
+                                     _arr(work, _U8, dbw_expert_work_bytes(routing)), _current()), "dbw_expert_sort")
+
+
+def _moved(routing, shape):
+    """Number of slots, dtype, elements of the tokens' rows and of the sorted rows."""
+    n, dtype, size, _ = _spans(shape)
+    slots = n * routing.k
+    return slots, dtype, size, (slots - 1) * (shape.ld_out or shape.ld or shape.width) + shape.width if slots > 0 else 0
+
+
+def dbw_expert_gather(routing, shape, x, place, sorted, status_out=None):
+    n, dtype, size, size_sorted = _moved(routing, shape)
+    return _chk(_lib.dbw_expert_gather(C.byref(routing), C.byref(shape), _arr(x, dtype, size), _arr(place, _I32, n),
+                                       _arr(sorted, dtype, size_sorted), _arr(status_out, _I32, 1), _current()), "dbw_expert_gather")
+
+
+def dbw_expert_combine(routing, shape, sorted, place, y, weights=None, status_out=None):
+    n, dtype, size, size_sorted = _moved(routing, shape)
+    return _chk(_lib.dbw_expert_combine(C.byref(routing), C.byref(shape), _arr(sorted, dtype, size_sorted), _arr(place, _I32, n),
+                                        _arr(weights, _F32, n), _arr(y, dtype, size), _arr(status_out, _I32, 1), _current()), "dbw_expert_combine")
+
+
+def dbw_expert_combine_grad(routing, shape, dy, sorted, place, dsorted, weights=None, dweights=None, status_out=None):
+    n, dtype, size, size_sorted = _moved(routing, shape)
+    return _chk(_lib.dbw_expert_combine_grad(C.byref(routing), C.byref(shape), _arr(dy, dtype, size), _arr(sorted, dtype, size_sorted),
+                                             _arr(place, _I32, n), _arr(weights, _F32, n), _arr(dsorted, dtype, size_sorted),
+                                             _arr(dweights, _F32, n), _arr(status_out, _I32, 1), _current()), "dbw_expert_combine_grad")
+
+
+def dbw_checkpoint_weight_grad(shape, dy, checkpoint, grads, work, weight_at: int, bias_at: int = -1, start=None, source=None, status_out=None):
+    """grads [N, ld]: the workers' rows of gradients."""
+    n, dtype = shape.workers * shape.rows, _DTYPE_OF.get(shape.type)
+    size = (n - 1) * (shape.ld or shape.outputs) + shape.outputs if n > 0 else 0
+    to, ld = _parameters(grads, shape.workers)
+    padded = -(-shape.inputs // 32) * 32
+    return _chk(_lib.dbw_checkpoint_weight_grad(C.byref(shape), _arr(dy, dtype, size),
+                                                _arr(checkpoint, _U8, shape.workers * shape.tokens * (padded + padded // 32)),
+                                                _arr(start, _I32, shape.workers * (shape.experts + 1)), _arr(source, _I32, n), to, ld, weight_at,
+                                                bias_at, _arr(status_out, _I32, 1),
+                                                _arr(work, _U8, dbw_checkpoint_weight_grad_work_bytes(shape)), _current()),
+                "dbw_checkpoint_weight_grad")

@@ -1,0 +1,434 @@
+// Entry points of what lies between the products of a language model (dbw_layers.h): argument checks and launches.  No context and no
+// allocation: what the kernels need beyond inputs and outputs is the caller's scratch memory.
+#include <math.h>
+
+#include "dbw_internal.h"
+#include "dbw_layers.h"
+#include "layer_experts.h"
+#include "layer_norm.h"
+#include "layer_wgrad.h"
+
+namespace {
+
+constexpr int64_t MAX_GROUPS = 1 << 22;                   // workers
+
+size_t size_of(int type) { return type == DBW_TYPE_F32 ? 4 : 2; }
+bool no_type(int type) { return type < DBW_TYPE_F32 || type > DBW_TYPE_F16; }
+bool off(const void *p, size_t boundary) { return (uintptr_t)p % boundary != 0; }
+// A stride of which so many rows' offsets in bytes fit 64 bits.
+bool too_long(int64_t ld, int64_t rows) { return ld > INT64_MAX / 8 / (rows + 1); }
+
+template <class F>
+void by_type(int type, F f)
+{
+    if (type == DBW_TYPE_F32) f(float());
+    else if (type == DBW_TYPE_BF16) f(loss::bf16());
+    else f(loss::f16());
+}
+dim3 grid_of(int64_t groups)
+{
+    const int64_t x = groups < (1 << 20) ? groups : 1 << 20;
+    return dim3((uint32_t)x, (uint32_t)((groups + x - 1) / x));
+}
+
+struct Shape {
+    int64_t rows, ld, ld_out;
+    size_t e;                                             // bytes of an element
+};
+int check_shape(const dbw_rows *l, Shape *S)
+{
+    if (!l) return DBW_ERR_NULL;
+    if (l->workers < 1 || l->rows < 0 || l->width < 1 || no_type(l->type)) return DBW_ERR_INVALID;
+    S->ld = l->ld ? l->ld : l->width;
+    S->ld_out = l->ld_out ? l->ld_out : S->ld;
+    if (S->ld < l->width || S->ld_out < l->width) return DBW_ERR_INVALID;
+    S->rows = (int64_t)l->workers * l->rows;
+    S->e = size_of(l->type);
+    if (l->width > DBW_LAYER_MAX_WIDTH || l->workers > MAX_GROUPS || S->rows > INT32_MAX || too_long(S->ld, S->rows) || too_long(S->ld_out, S->rows))
+        return DBW_ERR_UNSUPPORTED;
+    return DBW_OK;
+}
+// Whether arrays of rows share memory.
+bool overlap(const void *a, int64_t rows_a, int64_t ld_a, const void *b, int64_t rows_b, int64_t ld_b, int64_t width, size_t e)
+{
+    if (!a || !b || rows_a < 1 || rows_b < 1) return false;
+    const uintptr_t p = (uintptr_t)a, q = (uintptr_t)b;
+    const size_t na = e * (size_t)((rows_a - 1) * ld_a + width), nb = e * (size_t)((rows_b - 1) * ld_b + width);
+    return p < q + nb && q < p + na;
+}
+// Columns of the parameters' rows: `count` from `at` on, or none (at < 0).
+bool outside(int64_t at, int64_t count, int64_t ld) { return at >= 0 && (count > ld || at > ld - count); }
+
+layer::Kept kept_of(const void *checkpoint, const Shape &S, const dbw_rows *l) { return layer::kept_of((void *)checkpoint, S.rows, l->width); }
+int64_t checkpoint_bytes(int64_t rows, int64_t width) { return rows * (layer::padded(width) + layer::padded(width) / layer::BLOCK); }
+
+// Which kernel takes a row of a norm: T threads, C pieces each.
+template <int T_, int C_>
+struct Plan {
+    static constexpr int T = T_, C = C_, ROWS = layer::ROWS_OF<T>;
+};
+template <class F>
+bool by_row(int64_t bytes, F f)
+{
+    if (bytes <= 16 * 16) f(Plan<16, 1>());
+    else if (bytes <= 4 * 16 * 16) f(Plan<16, 4>());
+    else if (bytes <= 4 * 64 * 16) f(Plan<64, 4>());
+    else if (bytes <= 2 * 256 * 16) f(Plan<256, 2>());
+    else if (bytes <= 4 * 256 * 16) f(Plan<256, 4>());
+    else if (bytes <= 4 * 1024 * 16) f(Plan<1024, 4>());
+    else return false;
+    return true;
+}
+constexpr int LONG_THREADS = 1024, LONG_GRAD_THREADS = 256;
+
+// The backward pass: T threads a row, C pieces each, ROWS rows of a workgroup at a time.
+template <int T_, int C_, int ROWS_>
+struct GradPlan {
+    static constexpr int T = T_, C = C_, ROWS = ROWS_;
+};
+template <class F>
+bool by_grad_row(int64_t bytes, F f)
+{
+    if (bytes <= 16 * 16) f(GradPlan<16, 1, 16>());
+    else if (bytes <= 64 * 16) f(GradPlan<64, 1, 4>());
+    else if (bytes <= 2 * 64 * 16) f(GradPlan<64, 2, 8>());
+    else if (bytes <= 4 * 64 * 16) f(GradPlan<64, 4, 4>());
+    else if (bytes <= 2 * 256 * 16) f(GradPlan<256, 2, 1>());
+    else if (bytes <= 2 * 512 * 16) f(GradPlan<512, 2, 1>());
+    else if (bytes <= 2 * 1024 * 16) f(GradPlan<1024, 2, 1>());
+    else return false;
+    return true;
+}
+constexpr int STRIPS = 512;                               // workgroups that all workers' rows are cut for
+struct Strips {
+    int count, rows;                                      // of a worker, and of a strip
+};
+Strips strips_of(const dbw_rows *l, const Shape &S)
+{
+    int at_once = 1;
+    by_grad_row(S.e * l->width, [&](auto p) { at_once = p.ROWS; });
+    const int64_t most = (STRIPS + l->workers - 1) / l->workers, least_rows = 4 * at_once;
+    int64_t count = (l->rows + least_rows - 1) / least_rows;
+    if (count > most) count = most;
+    if (count < 1) count = 1;
+    const int rows = (int)((l->rows + count - 1) / count);
+    return Strips{rows ? (int)((l->rows + rows - 1) / rows) : 1, rows};
+}
+int64_t part_ld(const dbw_rows *l) { return (l->width + 3) / 4 * 4; }
+
+}  // namespace
+
+extern "C" int64_t dbw_checkpoint_bytes(const dbw_rows *shape)
+{
+    Shape S;
+    const int rc = check_shape(shape, &S);
+    return rc == DBW_OK ? checkpoint_bytes(S.rows, shape->width) : rc;
+}
+
+extern "C" int dbw_checkpoint_store(const dbw_rows *shape, const void *x, const uint8_t *mask, void *checkpoint, void *stream)
+{
+    Shape S;
+    const int rc = check_shape(shape, &S);
+    if (rc != DBW_OK) return rc;
+    if (S.rows > 0 && (!x || !checkpoint)) return DBW_ERR_NULL;
+    if (off(x, S.e) || off(checkpoint, 16)) return DBW_ERR_INVALID;
+    if (S.rows == 0) return DBW_OK;
+    const layer::Store P{x, mask, nullptr, S.ld, S.rows, shape->width, kept_of(checkpoint, S, shape)};
+    by_type(shape->type, [&](auto e) {
+        typedef decltype(e) E;
+        const int64_t pieces = S.rows * (P.kept.stride / layer::Piece<E>::N);
+        hipLaunchKernelGGL(layer::store_kernel<E>, grid_of((pieces + layer::STORE_THREADS - 1) / layer::STORE_THREADS), dim3(layer::STORE_THREADS), 0,
+                           (hipStream_t)stream, P);
+    });
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
+
+extern "C" int dbw_checkpoint_load(const dbw_rows *shape, const void *checkpoint, void *x_out, void *stream)
+{
+    Shape S;
+    const int rc = check_shape(shape, &S);
+    if (rc != DBW_OK) return rc;
+    if (S.rows > 0 && (!x_out || !checkpoint)) return DBW_ERR_NULL;
+    if (off(x_out, S.e) || off(checkpoint, 16)) return DBW_ERR_INVALID;
+    if (S.rows == 0) return DBW_OK;
+    const layer::Store P{nullptr, nullptr, x_out, S.ld_out, S.rows, shape->width, kept_of(checkpoint, S, shape)};
+    by_type(shape->type, [&](auto e) {
+        typedef decltype(e) E;
+        const int64_t pieces = S.rows * (P.kept.stride / layer::Piece<E>::N);
+        hipLaunchKernelGGL(layer::load_kernel<E>, grid_of((pieces + layer::STORE_THREADS - 1) / layer::STORE_THREADS), dim3(layer::STORE_THREADS), 0,
+                           (hipStream_t)stream, P);
+    });
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
+
+extern "C" int dbw_layer_norm(const dbw_rows *shape, const void *x, const uint8_t *mask, const float *params, int64_t ld_params,
+                              int64_t weight_at, int64_t bias_at, float eps, void *y, float *stats_out, void *checkpoint, void *stream)
+{
+    Shape S;
+    const int rc = check_shape(shape, &S);
+    if (rc != DBW_OK) return rc;
+    if ((S.rows > 0 && (!x || !y)) || ((weight_at >= 0 || bias_at >= 0) && !params)) return DBW_ERR_NULL;
+    if (off(x, S.e) || off(y, S.e) || off(checkpoint, 16) || off(params, 4) || !(eps > 0.f) || !isfinite(eps)) return DBW_ERR_INVALID;
+    if (outside(weight_at, shape->width, ld_params) || outside(bias_at, shape->width, ld_params)) return DBW_ERR_INVALID;
+    if ((weight_at >= 0 || bias_at >= 0) && too_long(ld_params, shape->workers)) return DBW_ERR_UNSUPPORTED;
+    if (!(x == y && S.ld == S.ld_out) && overlap(x, S.rows, S.ld, y, S.rows, S.ld_out, shape->width, S.e)) return DBW_ERR_ALIAS;
+    if (S.rows == 0) return DBW_OK;
+    layer::Norm P{x, mask, params, S.ld, S.ld_out, ld_params, weight_at, bias_at, S.rows, shape->rows, shape->width, eps, y, stats_out,
+                  kept_of(checkpoint, S, shape)};
+    if (!checkpoint) P.kept.codes = nullptr;
+    hipStream_t s = (hipStream_t)stream;
+    by_type(shape->type, [&](auto e) {
+        typedef decltype(e) E;
+        if (!by_row(S.e * shape->width, [&](auto p) {
+                hipLaunchKernelGGL((layer::norm_kernel<E, p.T, p.C>), grid_of((S.rows + p.ROWS - 1) / p.ROWS), dim3(p.T * p.ROWS), 0, s, P);
+            }))
+            hipLaunchKernelGGL((layer::norm_long_kernel<E, LONG_THREADS>), grid_of(S.rows), dim3(LONG_THREADS), 0, s, P);
+    });
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
+
+extern "C" int64_t dbw_layer_norm_work_bytes(const dbw_rows *shape)
+{
+    Shape S;
+    const int rc = check_shape(shape, &S);
+    if (rc != DBW_OK) return rc;
+    const Strips strips = strips_of(shape, S);
+    int64_t bytes = strips.count > 1 ? (int64_t)shape->workers * strips.count * 2 * part_ld(shape) * 4 : 0;
+    if (!by_grad_row(S.e * shape->width, [](auto) {})) bytes += 8 * S.rows;
+    return bytes + 16;
+}
+
+extern "C" int dbw_layer_norm_grad(const dbw_rows *shape, const void *dy, const void *x, const void *checkpoint, const uint8_t *mask,
+                                   const float *stats, const float *params, int64_t ld_params, int64_t weight_at, int64_t bias_at, void *dx,
+                                   float *grads, int64_t ld_grads, void *work, void *stream)
+{
+    Shape S;
+    const int rc = check_shape(shape, &S);
+    if (rc != DBW_OK) return rc;
+    if (!work || (S.rows > 0 && (!dy || !dx || !stats || (!x && !checkpoint))) || (weight_at >= 0 && !params)) return DBW_ERR_NULL;
+    if (x && checkpoint) return DBW_ERR_INVALID;
+    if (off(dy, S.e) || off(x, S.e) || off(dx, S.e) || off(checkpoint, 16) || off(work, 16) || off(params, 4) || off(grads, 4)) return DBW_ERR_INVALID;
+    if (outside(weight_at, shape->width, ld_params)) return DBW_ERR_INVALID;
+    if (grads && (outside(weight_at, shape->width, ld_grads) || outside(bias_at, shape->width, ld_grads))) return DBW_ERR_INVALID;
+    if (grads && weight_at >= 0 && bias_at >= 0 && weight_at < bias_at + shape->width && bias_at < weight_at + shape->width) return DBW_ERR_ALIAS;
+    if ((weight_at >= 0 && too_long(ld_params, shape->workers)) || (grads && too_long(ld_grads, shape->workers))) return DBW_ERR_UNSUPPORTED;
+    if (dx != x && overlap(x, S.rows, S.ld, dx, S.rows, S.ld, shape->width, S.e)) return DBW_ERR_ALIAS;
+    if (!(dx == dy && S.ld == S.ld_out) && overlap(dy, S.rows, S.ld_out, dx, S.rows, S.ld, shape->width, S.e)) return DBW_ERR_ALIAS;
+    if (weight_at < 0 && bias_at < 0) grads = nullptr;
+    const Strips strips = strips_of(shape, S);
+    layer::NormGrad P{dy, x, kept_of(checkpoint, S, shape), mask, stats, params, S.ld, S.ld_out, ld_params, ld_grads, weight_at, bias_at, S.rows,
+                      shape->rows, shape->width, shape->workers, strips.count, strips.rows, dx, grads, nullptr, part_ld(shape), nullptr};
+    hipStream_t s = (hipStream_t)stream;
+    if (S.rows == 0) {
+        const int slices = (shape->width + 255) / 256;
+        if (grads) hipLaunchKernelGGL(layer::norm_zero_kernel, grid_of((int64_t)slices * shape->workers), dim3(256), 0, s, P, slices);
+        DBW_HIP(hipGetLastError());
+        return DBW_OK;
+    }
+    const int64_t groups = (int64_t)shape->workers * strips.count;
+    if (strips.count > 1) P.parts = (float *)work;
+    P.means = (layer::f32x2 *)((float *)work + (strips.count > 1 ? groups * 2 * P.part_ld : 0));
+    by_type(shape->type, [&](auto e) {
+        typedef decltype(e) E;
+        const auto rows = [&](auto p) {
+            const size_t lds = (size_t)(p.ROWS - 1) * p.T * p.C * layer::Piece<E>::N * 4;
+            if (x) hipLaunchKernelGGL((layer::norm_grad_kernel<E, p.T, p.C, p.ROWS, false>), grid_of(groups), dim3(p.T * p.ROWS), lds, s, P);
+            else hipLaunchKernelGGL((layer::norm_grad_kernel<E, p.T, p.C, p.ROWS, true>), grid_of(groups), dim3(p.T * p.ROWS), lds, s, P);
+        };
+        if (!by_grad_row(S.e * shape->width, rows)) {
+            constexpr int T = LONG_GRAD_THREADS, COLUMNS = T * layer::Piece<E>::N;
+            const int slices = (shape->width + COLUMNS - 1) / COLUMNS;
+            if (x) {
+                hipLaunchKernelGGL((layer::norm_means_kernel<E, LONG_THREADS, false>), grid_of(S.rows), dim3(LONG_THREADS), 0, s, P);
+                hipLaunchKernelGGL((layer::norm_grad_long_kernel<E, T, false>), grid_of(groups * slices), dim3(T), 0, s, P, slices);
+            } else {
+                hipLaunchKernelGGL((layer::norm_means_kernel<E, LONG_THREADS, true>), grid_of(S.rows), dim3(LONG_THREADS), 0, s, P);
+                hipLaunchKernelGGL((layer::norm_grad_long_kernel<E, T, true>), grid_of(groups * slices), dim3(T), 0, s, P, slices);
+            }
+        }
+    });
+    if (grads && strips.count > 1) {
+        const int slices = (shape->width + layer::SUM_COLUMNS - 1) / layer::SUM_COLUMNS;
+        hipLaunchKernelGGL(layer::norm_sum_kernel, grid_of((int64_t)shape->workers * slices * 2), dim3(layer::SUM_COLUMNS * layer::SUM_ROWS), 0, s, P, slices);
+    }
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
+
+// ---------------------------------------------------------------- experts
+
+namespace {
+
+constexpr int SORT_CHUNK = 4096;                          // slots of a workgroup
+int chunks_of(const dbw_routing *l) { return (int)(((int64_t)l->tokens * l->k + SORT_CHUNK - 1) / SORT_CHUNK); }
+
+int check_routing(const dbw_routing *l)
+{
+    if (!l) return DBW_ERR_NULL;
+    if (l->workers < 1 || l->tokens < 0 || l->k < 1 || l->experts < 1) return DBW_ERR_INVALID;
+    const int64_t slots = (int64_t)l->tokens * l->k;
+    if (l->workers > MAX_GROUPS || slots > INT32_MAX || slots * l->workers > INT32_MAX || l->experts > DBW_EXPERTS_MAX ||
+        (int64_t)l->workers * (l->experts + 1) > INT32_MAX)
+        return DBW_ERR_UNSUPPORTED;
+    return DBW_OK;
+}
+// Checks that the calls on rows have in common, and the kernels' view of them.
+int check_move(const dbw_routing *routing, const dbw_rows *shape, const void *tokens, const void *sorted, const int32_t *place,
+               const float *weights, int32_t *status, Shape *S, layer::Move *P)
+{
+    int rc = check_routing(routing);
+    if (rc == DBW_OK) rc = check_shape(shape, S);
+    if (rc != DBW_OK) return rc;
+    if (shape->workers != routing->workers || shape->rows != routing->tokens) return DBW_ERR_INVALID;
+    const int64_t slots = (int64_t)routing->tokens * routing->k, all = slots * routing->workers;
+    if (too_long(S->ld_out, all)) return DBW_ERR_UNSUPPORTED;
+    if (S->rows > 0 && (!tokens || !sorted || !place)) return DBW_ERR_NULL;
+    if (off(tokens, S->e) || off(sorted, S->e)) return DBW_ERR_INVALID;
+    if (overlap(tokens, S->rows, S->ld, sorted, all, S->ld_out, shape->width, S->e)) return DBW_ERR_ALIAS;
+    *P = layer::Move{nullptr, nullptr, nullptr, nullptr, place, weights, nullptr, status, S->ld, S->ld_out, S->rows, slots, shape->rows, shape->width,
+                     routing->k};
+    return DBW_OK;
+}
+dim3 move_grid(int64_t rows) { return grid_of((rows + layer::MOVE_THREADS / 64 - 1) / (layer::MOVE_THREADS / 64)); }
+
+}  // namespace
+
+extern "C" int64_t dbw_expert_work_bytes(const dbw_routing *routing)
+{
+    const int rc = check_routing(routing);
+    if (rc != DBW_OK) return rc;
+    const int64_t chunks = chunks_of(routing);
+    return 16 + (chunks > 1 ? routing->workers * chunks * routing->experts * 4 : 0);
+}
+
+extern "C" int dbw_expert_sort(const dbw_routing *routing, const int32_t *expert, int32_t *start_out, int32_t *place_out, int32_t *source_out,
+                               int32_t *status_out, void *work, void *stream)
+{
+    const int rc = check_routing(routing);
+    if (rc != DBW_OK) return rc;
+    const int64_t slots = (int64_t)routing->tokens * routing->k;
+    if (!start_out || !work || (slots > 0 && (!expert || !place_out || !source_out))) return DBW_ERR_NULL;
+    if (off(work, 16)) return DBW_ERR_INVALID;
+    const int chunks = slots > 0 ? chunks_of(routing) : 1;
+    const layer::Sort P{expert, start_out, place_out, source_out, status_out, (int32_t *)work, routing->workers, (int)slots, routing->experts, SORT_CHUNK,
+                        chunks};
+    hipStream_t s = (hipStream_t)stream;
+    const dim3 grid = grid_of((int64_t)routing->workers * chunks), block(layer::SORT_THREADS);
+    if (chunks > 1) hipLaunchKernelGGL(layer::sort_count_kernel, grid, block, routing->experts * 4, s, P);
+    hipLaunchKernelGGL(layer::sort_kernel, grid, block, (layer::SORT_WAVES * routing->experts + layer::SORT_WAVES) * 4, s, P);
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
+
+extern "C" int dbw_expert_gather(const dbw_routing *routing, const dbw_rows *shape, const void *x, const int32_t *place, void *sorted,
+                                 int32_t *status_out, void *stream)
+{
+    Shape S;
+    layer::Move P;
+    const int rc = check_move(routing, shape, x, sorted, place, nullptr, status_out, &S, &P);
+    if (rc != DBW_OK) return rc;
+    if (S.rows == 0) return DBW_OK;
+    P.tokens = x;
+    P.sorted_out = sorted;
+    by_type(shape->type, [&](auto e) {
+        hipLaunchKernelGGL(layer::gather_kernel<decltype(e)>, move_grid(S.rows), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P);
+    });
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
+
+extern "C" int dbw_expert_combine(const dbw_routing *routing, const dbw_rows *shape, const void *sorted, const int32_t *place, const float *weights,
+                                  void *y, int32_t *status_out, void *stream)
+{
+    Shape S;
+    layer::Move P;
+    const int rc = check_move(routing, shape, y, sorted, place, weights, status_out, &S, &P);
+    if (rc != DBW_OK) return rc;
+    if (S.rows == 0) return DBW_OK;
+    P.sorted_in = sorted;
+    P.out = y;
+    by_type(shape->type, [&](auto e) {
+        hipLaunchKernelGGL(layer::combine_kernel<decltype(e)>, move_grid(S.rows), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P);
+    });
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
+
+extern "C" int dbw_expert_combine_grad(const dbw_routing *routing, const dbw_rows *shape, const void *dy, const void *sorted, const int32_t *place,
+                                       const float *weights, void *dsorted, float *dweights, int32_t *status_out, void *stream)
+{
+    Shape S;
+    layer::Move P;
+    const int rc = check_move(routing, shape, dy, dsorted, place, weights, status_out, &S, &P);
+    if (rc != DBW_OK) return rc;
+    const int64_t all = S.rows * routing->k;
+    if (S.rows > 0 && dweights && !sorted) return DBW_ERR_NULL;
+    if (off(sorted, S.e)) return DBW_ERR_INVALID;
+    if (dweights && sorted != dsorted && overlap(sorted, all, S.ld_out, dsorted, all, S.ld_out, shape->width, S.e)) return DBW_ERR_ALIAS;
+    if (S.rows == 0) return DBW_OK;
+    P.tokens = dy;
+    P.sorted_in = sorted;
+    P.sorted_out = dsorted;
+    P.dweights = dweights;
+    by_type(shape->type, [&](auto e) {
+        hipLaunchKernelGGL(layer::combine_grad_kernel<decltype(e)>, move_grid(S.rows), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P);
+    });
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
+
+// ---------------------------------------------------------------- weight gradient
+
+namespace {
+
+int check_linear(const dbw_linear *l, int64_t *ld)
+{
+    if (!l) return DBW_ERR_NULL;
+    if (l->workers < 1 || l->rows < 0 || l->inputs < 1 || l->outputs < 1 || no_type(l->type) || l->experts < 1 || l->tokens < 0 || l->k < 1) return DBW_ERR_INVALID;
+    *ld = l->ld ? l->ld : l->outputs;
+    if (*ld < l->outputs) return DBW_ERR_INVALID;
+    const int64_t rows = (int64_t)l->workers * l->rows;
+    if (l->workers > MAX_GROUPS || rows > INT32_MAX || (int64_t)l->workers * l->tokens > INT32_MAX || l->inputs > DBW_LAYER_MAX_WIDTH ||
+        l->outputs > DBW_LAYER_MAX_WIDTH || l->experts > DBW_EXPERTS_MAX || (int64_t)l->workers * (l->experts + 1) > INT32_MAX || too_long(*ld, rows))
+        return DBW_ERR_UNSUPPORTED;
+    return DBW_OK;
+}
+
+}  // namespace
+
+extern "C" int64_t dbw_checkpoint_weight_grad_work_bytes(const dbw_linear *shape)
+{
+    int64_t ld;
+    const int rc = check_linear(shape, &ld);
+    return rc == DBW_OK ? 16 : rc;
+}
+
+extern "C" int dbw_checkpoint_weight_grad(const dbw_linear *shape, const void *dy, const void *checkpoint, const int32_t *start,
+                                          const int32_t *source, float *grads, int64_t ld_grads, int64_t weight_at, int64_t bias_at,
+                                          int32_t *status_out, void *work, void *stream)
+{
+    int64_t ld;
+    const int rc = check_linear(shape, &ld);
+    if (rc != DBW_OK) return rc;
+    if (!work || !grads || (shape->rows > 0 && !dy) || (shape->rows > 0 && shape->tokens > 0 && !checkpoint) || (!start && shape->experts > 1))
+        return DBW_ERR_NULL;
+    const size_t e = size_of(shape->type);
+    const int64_t count = (int64_t)shape->experts * shape->outputs, weights = count * shape->inputs;   // at most 2^50
+    if (off(dy, e) || off(checkpoint, 16) || off(work, 16) || off(grads, 4) || (!source && shape->rows != shape->tokens)) return DBW_ERR_INVALID;
+    if (weight_at < 0 || outside(weight_at, weights, ld_grads) || outside(bias_at, count, ld_grads)) return DBW_ERR_INVALID;
+    if (bias_at >= 0 && bias_at < weight_at + weights && weight_at < bias_at + count) return DBW_ERR_ALIAS;
+    if (too_long(ld_grads, shape->workers)) return DBW_ERR_UNSUPPORTED;
+    const int64_t tokens = (int64_t)shape->workers * shape->tokens;
+    const layer::Linear P{dy, layer::kept_of((void *)checkpoint, tokens, shape->inputs), start, source, status_out, grads, ld, ld_grads, weight_at, bias_at,
+                          shape->workers, shape->rows, shape->inputs, shape->outputs, shape->experts, shape->tokens, shape->k};
+    const int64_t tiles_out = (shape->outputs + layer::TILE - 1) / layer::TILE, tiles_in = (shape->inputs + layer::TILE - 1) / layer::TILE;
+    const int64_t groups = tiles_out * tiles_in * shape->workers * shape->experts;
+    by_type(shape->type, [&](auto v) {
+        hipLaunchKernelGGL(layer::weight_grad_kernel<decltype(v)>, grid_of(groups), dim3(256), 0, (hipStream_t)stream, P, (int)tiles_out, (int)tiles_in);
+    });
+    DBW_HIP(hipGetLastError());
+    return DBW_OK;
+}
