@@ -1,9 +1,20 @@
-// The weight gradient of a linear layer whose input was kept in 8 bits (dbw_layers.h).
+// The weight gradient of a linear layer whose input was kept in 8 bits (dbw_layers.h): dW = sum over rows of dy x'.
+//
+// What a code stands for is exact in bf16, and so is dy as one (bf16), two (fp16) or three (fp32) bf16 numbers: every product on the bf16
+// matrix instruction is exact, and fp32 sums are all that rounds.
 #pragma once
 
+#include "global_access.h"
 #include "layer_rows.h"
 
 namespace layer {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f32x16 __attribute__((ext_vector_type(16)));
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef short s16x8 __attribute__((ext_vector_type(8)));
+typedef __attribute__((address_space(3))) char *lds_bytes;
 
 struct Linear {
     const void *dy;
@@ -14,6 +25,8 @@ struct Linear {
     int64_t ld, ld_grads, weight_at, bias_at;
     int64_t workers;
     int rows, in, out, experts, tokens, k;                // rows, tokens: of a worker
+    int tiles_out, tiles_in, splits;
+    float *parts;                                         // [split][weights of all layers, then their biases], where the rows are split
 };
 // The rows of dy of a worker's layer.
 struct Range {
@@ -29,62 +42,287 @@ __device__ __forceinline__ Range range_of(const Linear &P, int64_t worker, int e
     return Range{low, low};
 }
 // The checkpoint's row of a row of dy, or -1.
-__device__ __forceinline__ int64_t input_row(const Linear &P, int64_t worker, int64_t row)
+__device__ __forceinline__ int input_row(const Linear &P, int64_t worker, int64_t row)
 {
-    if (!P.source) return row;
     const int64_t low = worker * P.tokens;
     const int32_t slot = P.source[row];
-    const int64_t r = slot < 0 ? -1 : slot / P.k;
+    const int r = slot < 0 ? -1 : slot / P.k;
     if (r >= low && r < low + P.tokens) return r;
     report(P.status);
     return -1;
 }
 
-constexpr int TILE = 64, STEP = 16;
+// A piece of dy as bf16 planes, the large parts first.
 template <class E>
-__global__ __launch_bounds__(256) void weight_grad_kernel(Linear P, int tiles_out, int tiles_in)
+struct Planes;
+template <>
+struct Planes<bf16> {
+    static constexpr int COUNT = 1;
+    static __device__ __forceinline__ void split(const u32x4 &w, u32x4 (&p)[1]) { p[0] = w; }
+};
+__device__ __forceinline__ uint32_t nearest(float a, float b)
 {
-    __shared__ float d[STEP][TILE], x[STEP][TILE];
-    const int64_t group = group_number();
-    const int64_t layer = group / ((int64_t)tiles_out * tiles_in);
-    const int tile = (int)(group % ((int64_t)tiles_out * tiles_in));
-    const int64_t worker = layer / P.experts;
-    const int expert = (int)(layer % P.experts);
-    if (worker >= P.workers) return;
-    const int o0 = tile / tiles_in * TILE, i0 = tile % tiles_in * TILE;
-    const Range range = range_of(P, worker, expert);
-    const int column = threadIdx.x % TILE, q = threadIdx.x / TILE, to = threadIdx.x / 16 * 4, ti = threadIdx.x % 16 * 4;
-    float acc[4][4] = {}, bias[4] = {};
-    for (int64_t r0 = range.first; r0 < range.end; r0 += STEP) {
-        __syncthreads();
-        for (int s = q; s < STEP; s += 256 / TILE) {
-            const int64_t r = r0 + s;
-            const int64_t in = r < range.end ? input_row(P, worker, r) : -1;
-            d[s][column] = in >= 0 && o0 + column < P.out ? loss::widen(((const E *)P.dy)[r * P.ld + o0 + column]) : 0.f;
-            float v[4] = {0.f, 0.f, 0.f, 0.f};
-            if (in >= 0 && i0 + column < P.in) {
-                const int c = i0 + column;
-                const float by = power_of_two((int)P.kept.exponents[in * (P.kept.stride / BLOCK) + c / BLOCK] - 127);
-                decode4(P.kept.codes[in * P.kept.stride + c], by, v);
-            }
-            x[s][column] = v[0];
+    const bf16x2 r = {(__bf16)a, (__bf16)b};
+    return __builtin_bit_cast(uint32_t, r);
+}
+__device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
+__device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
+// What is left of v without its larger part; nothing of an infinity.
+__device__ __forceinline__ float rest_of(float v, float part) { return fabsf(v) < INFINITY ? v - part : 0.f; }
+template <>
+struct Planes<f16> {                                      // 11 bits: the nearest eight and what is left
+    static constexpr int COUNT = 2;
+    static __device__ __forceinline__ void split(const u32x4 &w, u32x4 (&p)[2])
+    {
+        float v[8];
+        Piece<f16>::unpack(w, v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            p[0][i] = nearest(v[2 * i], v[2 * i + 1]);
+            p[1][i] = nearest(rest_of(v[2 * i], low_half(p[0][i])), rest_of(v[2 * i + 1], high_half(p[0][i])));
         }
-        __syncthreads();
-        for (int s = 0; s < STEP; ++s)
-            for (int a = 0; a < 4; ++a) {
-                const float g = d[s][to + a];
-                bias[a] += g;
-                for (int b = 0; b < 4; ++b) acc[a][b] = fmaf(g, x[s][ti + b], acc[a][b]);
+    }
+};
+template <>
+struct Planes<float> {                                    // 24 bits: the upper eight towards zero, so that they stay finite, the nearest eight of the rest, what is left
+    static constexpr int COUNT = 3;
+    static __device__ __forceinline__ void split(const u32x4 &w, u32x2 (&p)[3])
+    {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const float a = __uint_as_float(w[2 * i]), b = __uint_as_float(w[2 * i + 1]);
+            p[0][i] = __builtin_amdgcn_perm(w[2 * i + 1], w[2 * i], 0x07060302u);
+            const float c = rest_of(a, high_half(w[2 * i])), d = rest_of(b, high_half(w[2 * i + 1]));
+            p[1][i] = nearest(c, d);
+            p[2][i] = nearest(c - low_half(p[1][i]), d - high_half(p[1][i]));
+        }
+    }
+};
+
+// Tiles in LDS: rows of COLUMNS bf16, in units of 16 columns.  The transposing read takes of 16 lanes four rows' 32 bytes each, a
+// matrix instruction's operand four such blocks, of four rows by two units and of another four rows.  Units of neighbouring rows are
+// exchanged so that those of half a wave lie on different banks.
+template <int COLUMNS>
+__device__ __forceinline__ int unit_place(int row, int unit)
+{
+    static_assert(COLUMNS >= 64, "four units at least");
+    return unit ^ (COLUMNS >= 128 ? 2 * (row & 3) : 2 * ((row >> 1) & 1));
+}
+template <int COLUMNS>
+__device__ __forceinline__ int lds_offset(int row, int column)     // column: a multiple of 4
+{
+    return row * (COLUMNS * 2) + unit_place<COLUMNS>(row, column >> 4) * 32 + (column & 15) * 2;
+}
+// An operand of v_mfma_f32_32x32x16_bf16 from rows row ... row + 15: a lane has column l % 32, and of its eight numbers the first four are those of rows 4 (l / 32)
+// and on, the others of rows 8 + 4 (l / 32) and on.  (Both operands take the rows in this order.)
+template <int COLUMNS>
+__device__ __forceinline__ bf16x8 operand(lds_bytes tile, int row, int column)
+{
+    const int l = threadIdx.x & 63, i = l & 15;
+    const int r = row + 4 * (l >> 5) + (i >> 2), c = column + 16 * ((l >> 4) & 1) + 4 * (i & 3);
+    typedef __attribute__((address_space(3))) s16x4 *place;
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(tile + lds_offset<COLUMNS>(r, c)));
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(tile + lds_offset<COLUMNS>(r + 8, c)));
+    return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
+}
+
+// A workgroup's tile: OUT x IN of a layer's weights, by WO x WI waves, STEP rows at a time.
+template <int OUT_, int IN_, int WO_, int WI_, int STEP_>
+struct Tile {
+    static constexpr int OUT = OUT_, IN = IN_, WO = WO_, WI = WI_, STEP = STEP_;
+    static constexpr int THREADS = 64 * WO * WI;
+};
+template <class E, class T>
+constexpr int tile_lds() { return 2 * T::STEP * 2 * (Planes<E>::COUNT * T::OUT + T::IN) + 2 * T::STEP * 4; }
+
+template <class E, class T, bool SOURCED>
+__global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
+{
+    constexpr int N = Piece<E>::N, PLANES = Planes<E>::COUNT;
+    constexpr int A_PIECES = T::OUT / N, A_ROWS = T::THREADS / A_PIECES, A_COUNT = T::STEP / A_ROWS;
+    constexpr int B_PIECES = T::IN / 16, B_ROWS = T::THREADS / B_PIECES, B_COUNT = T::STEP / B_ROWS;
+    static_assert(A_COUNT * A_ROWS == T::STEP && B_COUNT * B_ROWS == T::STEP, "whole turns");
+    constexpr int MI = T::OUT / T::WO / 32, NI = T::IN / T::WI / 32;
+    constexpr int A_BYTES = T::STEP * T::OUT * 2, B_BYTES = T::STEP * T::IN * 2, BUFFER = PLANES * A_BYTES + B_BYTES;
+    extern __shared__ char shared[];
+    const lds_bytes lds = (lds_bytes)shared;
+    int32_t *const rows_of = (int32_t *)(shared + 2 * BUFFER);       // [2][STEP]: the checkpoint's rows
+
+    int64_t group = group_number();
+    const int64_t per_layer = (int64_t)P.tiles_out * P.tiles_in, groups = per_layer * P.splits * P.experts * P.workers;
+    if (group >= groups) return;
+    const int tile = (int)(group % per_layer);
+    group /= per_layer;
+    const int split = (int)(group % P.splits);
+    group /= P.splits;
+    const int expert = (int)(group % P.experts);
+    const int64_t worker = group / P.experts;
+    const int o0 = tile / P.tiles_in * T::OUT, i0 = tile % P.tiles_in * T::IN;
+    Range range = range_of(P, worker, expert);
+    if (P.splits > 1) {
+        const int64_t part = ((range.end - range.first + P.splits - 1) / P.splits + T::STEP - 1) / T::STEP * T::STEP;
+        range.first = min(range.first + split * part, range.end);
+        range.end = min(range.first + part, range.end);
+    }
+    const int length = (int)(range.end - range.first), steps = (length + T::STEP - 1) / T::STEP;
+
+    const int t = threadIdx.x;
+    const int ac = t % A_PIECES * N, ar = t / A_PIECES, bc = t % B_PIECES * 16, br = t / B_PIECES;
+    const bool a_in = o0 + ac < P.out, a_whole = o0 + ac + N <= P.out, b_in = i0 + bc < P.kept.stride;
+    const int64_t exponents_stride = P.kept.stride / BLOCK;
+    u32x4 a[A_COUNT], b[B_COUNT];
+    uint32_t e[B_COUNT];
+    const bool with_bias = P.bias_at >= 0 && i0 == 0;
+    float bias[N] = {};
+
+    const auto load = [&](int step) {
+        const int32_t *const rows = rows_of + (step & 1) * T::STEP;
+#pragma unroll
+        for (int i = 0; i < A_COUNT; ++i) {
+            const int s = ar + i * A_ROWS;
+            const int64_t r = range.first + (int64_t)step * T::STEP + s;
+            a[i] = (u32x4)0u;
+            if (a_in && step * T::STEP + s < length && (!SOURCED || rows[s] >= 0)) {
+                const E *const row = (const E *)P.dy + r * P.ld;
+                a[i] = load_piece<E>(row, o0 + ac, a_whole ? INT32_MAX : P.out);
             }
+        }
+#pragma unroll
+        for (int i = 0; i < B_COUNT; ++i) {
+            const int s = br + i * B_ROWS;
+            const int64_t r = SOURCED ? rows[s] : range.first + (int64_t)step * T::STEP + s;
+            b[i] = (u32x4)0u;
+            e[i] = 127;
+            if (b_in && step * T::STEP + s < length && r >= 0) {
+                b[i] = *(const __attribute__((address_space(1))) u32x4 *)(uint64_t)(P.kept.codes + r * P.kept.stride + i0 + bc);
+                e[i] = *(const __attribute__((address_space(1))) uint8_t *)(uint64_t)(P.kept.exponents + r * exponents_stride + (i0 + bc) / BLOCK);
+            }
+        }
+    };
+    const auto put = [&](int buffer) {
+        const lds_bytes at = lds + buffer * BUFFER;
+#pragma unroll
+        for (int i = 0; i < A_COUNT; ++i) {
+            const int to = lds_offset<T::OUT>(ar + i * A_ROWS, ac);
+            if constexpr (N == 8) {
+                u32x4 p[PLANES];
+                Planes<E>::split(a[i], p);
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) *(__attribute__((address_space(3))) u32x4 *)(at + q * A_BYTES + to) = p[q];
+            } else {
+                u32x2 p[PLANES];
+                Planes<E>::split(a[i], p);
+#pragma unroll
+                for (int q = 0; q < PLANES; ++q) *(__attribute__((address_space(3))) u32x2 *)(at + q * A_BYTES + to) = p[q];
+            }
+            if (with_bias) {
+                float v[N];
+                Piece<E>::unpack(a[i], v);
+#pragma unroll
+                for (int j = 0; j < N; ++j) bias[j] += v[j];
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < B_COUNT; ++i) {
+            const float by = __uint_as_float(e[i] << 23);
+            u32x4 w[2];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const uint32_t code = b[i][q];
+                w[q / 2][q % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, by, false));
+                w[q / 2][q % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, by, true));
+            }
+            const lds_bytes to = at + PLANES * A_BYTES + lds_offset<T::IN>(br + i * B_ROWS, bc);
+            *(__attribute__((address_space(3))) u32x4 *)to = w[0];
+            *(__attribute__((address_space(3))) u32x4 *)(to + 16) = w[1];
+        }
+    };
+    // The checkpoint's rows of a step, looked up by its first threads two steps ahead.
+    const auto look_up = [&](int step) {
+        if (SOURCED && t < T::STEP) {
+            const int s = step * T::STEP + t;
+            rows_of[(step & 1) * T::STEP + t] = s < length ? input_row(P, worker, range.first + s) : -1;
+        }
+    };
+
+    f32x16 acc[MI][NI] = {};
+    const int wave = t >> 6, wo = wave / T::WI * (T::OUT / T::WO), wi = wave % T::WI * (T::IN / T::WI);
+    if (steps > 0) {
+        look_up(0);
+        look_up(1);
+        __syncthreads();
+        load(0);
+        put(0);
+        if (steps > 1) load(1);
+        __syncthreads();
     }
-    float *const grads = P.grads + worker * P.ld_grads;
-    for (int a = 0; a < 4; ++a) {
-        const int o = o0 + to + a;
-        if (o >= P.out) continue;
-        for (int b = 0; b < 4; ++b)
-            if (i0 + ti + b < P.in) grads[P.weight_at + ((int64_t)expert * P.out + o) * P.in + i0 + ti + b] = acc[a][b];
-        if (i0 == 0 && ti == 0 && P.bias_at >= 0) grads[P.bias_at + (int64_t)expert * P.out + o] = bias[a];
+    for (int step = 0; step < steps; ++step) {
+        const lds_bytes at = lds + (step & 1) * BUFFER;
+        look_up(step + 2);                                // (whose place was last read before the barrier)
+#pragma unroll
+        for (int s = 0; s < T::STEP; s += 16) {
+            bf16x8 x[NI];
+#pragma unroll
+            for (int j = 0; j < NI; ++j) x[j] = operand<T::IN>(at + PLANES * A_BYTES, s, wi + 32 * j);
+#pragma unroll
+            for (int q = PLANES - 1; q >= 0; --q)
+#pragma unroll
+                for (int i = 0; i < MI; ++i) {
+                    const bf16x8 d = operand<T::OUT>(at + q * A_BYTES, s, wo + 32 * i);
+#pragma unroll
+                    for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d, x[j], acc[i][j], 0, 0, 0);
+                }
+        }
+        if (step + 1 < steps) put((step + 1) & 1);
+        __syncthreads();
+        if (step + 2 < steps) load(step + 2);
     }
+
+    const int64_t layer = worker * P.experts + expert, weights = (int64_t)P.out * P.in;
+    const int64_t all = P.workers * P.experts;
+    float *const to = P.splits > 1 ? P.parts + split * all * (weights + P.out) + layer * weights
+                                   : P.grads + worker * P.ld_grads + P.weight_at + expert * weights;
+    const int l = t & 63;
+#pragma unroll
+    for (int i = 0; i < MI; ++i)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+            const int o = o0 + wo + 32 * i + 8 * (v / 4) + 4 * (l >> 5) + v % 4;
+#pragma unroll
+            for (int j = 0; j < NI; ++j) {
+                const int c = i0 + wi + 32 * j + (l & 31);
+                if (o < P.out && c < P.in) to[(int64_t)o * P.in + c] = acc[i][j][v];
+            }
+        }
+    if (with_bias) {
+        // the sums of the threads that have the same columns, in their order
+        float *const sums = (float *)shared;              // [A_ROWS][OUT]
+        __syncthreads();
+#pragma unroll
+        for (int j = 0; j < N; ++j) sums[ar * T::OUT + ac + j] = bias[j];
+        __syncthreads();
+        float *const biases = P.splits > 1 ? P.parts + split * all * (weights + P.out) + all * weights + layer * P.out
+                                           : P.grads + worker * P.ld_grads + P.bias_at + (int64_t)expert * P.out;
+        for (int c = t; c < T::OUT; c += T::THREADS) {
+            float v = 0.f;
+            for (int r = 0; r < A_ROWS; ++r) v += sums[r * T::OUT + c];
+            if (o0 + c < P.out) biases[o0 + c] = v;
+        }
+    }
+}
+
+// The splits' shares, in their order.
+constexpr int SUM_THREADS = 256;
+__global__ __launch_bounds__(SUM_THREADS) void weight_grad_sum_kernel(Linear P)
+{
+    const int64_t weights = (int64_t)P.experts * P.out * P.in, biases = (int64_t)P.experts * P.out, each = weights + (P.bias_at >= 0 ? biases : 0);
+    const int64_t i = group_number() * SUM_THREADS + threadIdx.x;
+    const int64_t worker = i / each, c = i % each;
+    if (worker >= P.workers) return;
+    const int64_t at = c < weights ? worker * weights + c : P.workers * weights + worker * biases + c - weights;
+    float v = 0.f;
+    for (int s = 0; s < P.splits; ++s) v += P.parts[s * P.workers * (weights + biases) + at];
+    P.grads[worker * P.ld_grads + (c < weights ? P.weight_at + c : P.bias_at + c - weights)] = v;
 }
 
 }  // namespace layer

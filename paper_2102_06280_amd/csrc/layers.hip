@@ -397,13 +397,47 @@ int check_linear(const dbw_linear *l, int64_t *ld)
     return DBW_OK;
 }
 
+// Tiles of the weights, a workgroup each, and into how many parts a layer's rows are split.
+typedef layer::Tile<256, 256, 2, 4, 32> Large;
+typedef layer::Tile<128, 256, 2, 4, 32> LargeSplit;       // of operands in parts
+typedef layer::Tile<128, 128, 2, 2, 32> Middle;
+typedef layer::Tile<64, 64, 2, 2, 64> Small;
+struct Cut {
+    int tile;                                             // 0: small, 1: middle, 2: large
+    int64_t tiles_out, tiles_in, layers;
+    int splits;
+};
+constexpr int64_t CHIP = 256;
+Cut cut_of(const dbw_linear *l)
+{
+    Cut c;
+    c.layers = (int64_t)l->workers * l->experts;
+    c.splits = 1;
+    for (c.tile = 2; c.tile >= 0; --c.tile) {
+        const int out = c.tile == 2 ? (l->type == DBW_TYPE_BF16 ? Large::OUT : LargeSplit::OUT) : c.tile == 1 ? Middle::OUT : Small::OUT;
+        const int in = c.tile == 2 ? Large::IN : c.tile == 1 ? Middle::IN : Small::IN;
+        c.tiles_out = (l->outputs + out - 1) / out;
+        c.tiles_in = (l->inputs + in - 1) / in;
+        if (c.tile == 0 || c.tiles_out * c.tiles_in * c.layers >= CHIP) break;
+    }
+    const int64_t groups = c.tiles_out * c.tiles_in * c.layers, rows = l->rows / l->experts;
+    if (groups < CHIP) {
+        int64_t splits = (2 * CHIP + groups - 1) / groups;
+        if (splits > rows / 256) splits = rows / 256;
+        if (splits > 1) c.splits = (int)splits;
+    }
+    return c;
+}
+
 }  // namespace
 
 extern "C" int64_t dbw_checkpoint_weight_grad_work_bytes(const dbw_linear *shape)
 {
     int64_t ld;
     const int rc = check_linear(shape, &ld);
-    return rc == DBW_OK ? 16 : rc;
+    if (rc != DBW_OK) return rc;
+    const Cut cut = cut_of(shape);
+    return 16 + (cut.splits > 1 ? 4 * cut.splits * shape->workers * shape->experts * (int64_t)shape->outputs * (shape->inputs + 1) : 0);
 }
 
 extern "C" int dbw_checkpoint_weight_grad(const dbw_linear *shape, const void *dy, const void *checkpoint, const int32_t *start,
@@ -422,13 +456,36 @@ extern "C" int dbw_checkpoint_weight_grad(const dbw_linear *shape, const void *d
     if (bias_at >= 0 && bias_at < weight_at + weights && weight_at < bias_at + count) return DBW_ERR_ALIAS;
     if (too_long(ld_grads, shape->workers)) return DBW_ERR_UNSUPPORTED;
     const int64_t tokens = (int64_t)shape->workers * shape->tokens;
-    const layer::Linear P{dy, layer::kept_of((void *)checkpoint, tokens, shape->inputs), start, source, status_out, grads, ld, ld_grads, weight_at, bias_at,
-                          shape->workers, shape->rows, shape->inputs, shape->outputs, shape->experts, shape->tokens, shape->k};
-    const int64_t tiles_out = (shape->outputs + layer::TILE - 1) / layer::TILE, tiles_in = (shape->inputs + layer::TILE - 1) / layer::TILE;
-    const int64_t groups = tiles_out * tiles_in * shape->workers * shape->experts;
+    const Cut cut = cut_of(shape);
+    const int64_t groups = cut.tiles_out * cut.tiles_in * cut.layers * cut.splits;
+    const layer::Linear P{dy, layer::kept_of((void *)checkpoint, tokens, shape->inputs), start, source, status_out, grads, ld, ld_grads, weight_at,
+                          bias_at, shape->workers, shape->rows, shape->inputs, shape->outputs, shape->experts, shape->tokens, shape->k, (int)cut.tiles_out,
+                          (int)cut.tiles_in, cut.splits, (float *)work};
+    hipStream_t s = (hipStream_t)stream;
+    bool fits = true;
     by_type(shape->type, [&](auto v) {
-        hipLaunchKernelGGL(layer::weight_grad_kernel<decltype(v)>, grid_of(groups), dim3(256), 0, (hipStream_t)stream, P, (int)tiles_out, (int)tiles_in);
+        typedef decltype(v) E;
+        const auto launch = [&](auto tile) {
+            typedef decltype(tile) T;
+            constexpr int lds = layer::tile_lds<E, T>();
+            const auto run = [&](auto kernel) {
+                // more than 64 KB have to be asked for
+                if (lds > 65536) fits = hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, lds) == hipSuccess;
+                if (fits) hipLaunchKernelGGL(kernel, grid_of(groups), dim3(T::THREADS), lds, s, P);
+            };
+            if (source) run(layer::weight_grad_kernel<E, T, true>);
+            else run(layer::weight_grad_kernel<E, T, false>);
+        };
+        if (cut.tile == 0) launch(Small());
+        else if (cut.tile == 1) launch(Middle());
+        else if constexpr (layer::Planes<E>::COUNT == 1) launch(Large());
+        else launch(LargeSplit());
     });
+    if (!fits) return DBW_ERR_HIP;
+    if (cut.splits > 1) {
+        const int64_t all = (int64_t)shape->workers * (weights + (bias_at >= 0 ? count : 0));
+        hipLaunchKernelGGL(layer::weight_grad_sum_kernel, grid_of((all + layer::SUM_THREADS - 1) / layer::SUM_THREADS), dim3(layer::SUM_THREADS), 0, s, P);
+    }
     DBW_HIP(hipGetLastError());
     return DBW_OK;
 }
