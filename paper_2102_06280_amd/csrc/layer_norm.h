@@ -11,7 +11,8 @@ struct Norm {
     const float *params;
     int64_t ld, ld_out, ld_params, weight_at, bias_at;
     int64_t rows;                                         // of all workers
-    int per_worker, width;
+    int per_worker, width, workers;
+    int strips, strip_rows;                               // of a worker
     float eps;
     void *y;
     float *stats;
@@ -32,60 +33,91 @@ __device__ __forceinline__ f32x2 row_sums(f32x2 v, f32x2 *lds)
     return v;
 }
 
-// A row in the registers of T threads, C pieces each.  The mean comes first, then the sums of the differences from it and of their squares:
-// the first of these is what the rounding of the mean left, which counts where a row's mean is large beside its spread.
-template <class E, int T, int C>
-__global__ __launch_bounds__(ROWS_OF<T> * T) void norm_kernel(Norm P)
+// A row in the registers of T threads, C pieces each; a workgroup walks over a strip of a worker's rows, ROWS at a time, with the weights in registers and
+// the next row on its way.  The mean comes first, then the sums of the differences from it and of their squares: the first of these is what the
+// rounding of the mean left, which counts where a row's mean is large beside its spread.
+template <class E, int T, int C, int ROWS>
+__global__ __launch_bounds__(T * ROWS) void norm_kernel(Norm P)
 {
-    constexpr int N = Piece<E>::N, ROWS = ROWS_OF<T>;
-    __shared__ f32x2 sums[2][(T + 63) / 64];
-    const int64_t r = group_number() * ROWS + threadIdx.x / T;
-    const int t = loss::tid<T>();
-    if (r >= P.rows) return;                              // (whole waves' worth of lanes that share a row; T > 64: one row a workgroup)
-    const bool on = !P.mask || P.mask[r];
-    const E *const x = (const E *)P.x + r * P.ld;
-    E *const y = (E *)P.y + r * P.ld_out;
-    float v[C][N];
-    float total = 0.f;
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-        u32x4 w = (u32x4)0u;
-        if (on) w = load_piece<E>(x, (i * T + t) * N, P.width);
-        Piece<E>::unpack(w, v[i]);
-#pragma unroll
-        for (int j = 0; j < N; ++j) total += v[i][j];
-    }
+    constexpr int N = Piece<E>::N;
+    constexpr bool WIDE = T * C > 16;
+    __shared__ f32x2 sums[2][ROWS][(T + 63) / 64];
+    const int64_t group = group_number();
+    if (group >= (int64_t)P.workers * P.strips) return;
+    const Strip strip = strip_of((uint32_t)group, P.strips, P.strip_rows, P.per_worker);
+    const int t = loss::tid<T>(), slot = slot_of<T>();
+    const int64_t base = (int64_t)strip.worker * P.per_worker;
     const float inverse = 1.f / (float)P.width;
-    const float mean = row_sums<T>((f32x2){total, 0.f}, sums[0])[0] * inverse;
-    f32x2 s = (f32x2)0.f;
+    u32x4 next[C];
+    bool next_on = false;
+    const auto load = [&](int at) {
+        const int64_t r = base + at + slot;
+        next_on = at + slot < strip.end && (!P.mask || P.mask[r]);
+        if (next_on)
 #pragma unroll
-    for (int i = 0; i < C; ++i)
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const float d = (i * T + t) * N + j < P.width ? v[i][j] - mean : 0.f;
-            s[0] += d;
-            s[1] = fmaf(d, d, s[1]);
-        }
-    s = row_sums<T>(s, sums[1]);
-    const float rest = s[0] * inverse;
-    const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[1] * inverse) + P.eps);
-    if (P.stats && t == 0) {
-        P.stats[2 * r] = on ? mean + rest : 0.f;
-        P.stats[2 * r + 1] = on ? rstd : 0.f;
-    }
-    const float *const params = P.params + r / P.per_worker * P.ld_params;
+            for (int i = 0; i < C; ++i) next[i] = load_raw<E, WIDE>((const E *)P.x + r * P.ld, (i * T + t) * N, P.width);
+    };
+    load(strip.first);
+    float w[C][N], b[C][N];
+    const float *const params = P.params + strip.worker * P.ld_params;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-        const int c = (i * T + t) * N;
-        if (P.kept.codes && c < (int)P.kept.stride) keep_piece<N>(P.kept, r, c, v[i]);
-        if (c >= P.width) continue;
-        float w[N], b[N];
-        for (int j = 0; j < N; ++j) w[j] = 1.f, b[j] = 0.f;
-        if (P.weight_at >= 0) load_floats<N>(params + P.weight_at, c, P.width, w);
-        if (P.bias_at >= 0) load_floats<N>(params + P.bias_at, c, P.width, b);
+        for (int j = 0; j < N; ++j) w[i][j] = 1.f, b[i][j] = 0.f;
+        if (P.weight_at >= 0) load_floats<N, WIDE>(params + P.weight_at, (i * T + t) * N, P.width, w[i]);
+        if (P.bias_at >= 0) load_floats<N, WIDE>(params + P.bias_at, (i * T + t) * N, P.width, b[i]);
+    }
+    for (int at = strip.first; at < strip.end; at += ROWS) {
+        const bool on = next_on, there = at + slot < strip.end;
+        const int64_t r = base + at + slot;
+        float v[C][N];
+        f32x2 s = (f32x2)0.f;
 #pragma unroll
-        for (int j = 0; j < N; ++j) v[i][j] = on ? fmaf((v[i][j] - mean - rest) * rstd, w[j], b[j]) : 0.f;
-        store_piece<E>(y, c, P.width, Piece<E>::pack(v[i]));
+        for (int i = 0; i < C; ++i) {
+            const u32x4 raw = on ? settled<E, WIDE>(next[i], (i * T + t) * N, P.width) : (u32x4)0u;
+            if (P.kept.codes && there && (i * T + t) * N < (int)P.kept.stride) keep_piece<E>(P.kept, r, (i * T + t) * N, raw);
+            Piece<E>::unpack(raw, v[i]);
+        }
+        load(at + ROWS);
+        if (!on) {                                        // (T > 64: a row is the workgroup's)
+            if (there) {
+                if (P.stats && t == 0) *(__attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r) = s;
+#pragma unroll
+                for (int i = 0; i < C; ++i) store_piece<E>((E *)P.y + r * P.ld_out, (i * T + t) * N, P.width, (u32x4)0u);
+            }
+            continue;
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+#pragma unroll
+            for (int j = 0; j < N; ++j) s[j & 1] += v[i][j];
+        const float mean = row_sums<T>((f32x2){s[0] + s[1], 0.f}, sums[0][slot])[0] * inverse;
+        s = (f32x2)0.f;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int c = (i * T + t) * N;
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[i][j] -= mean;
+            if (c + N > P.width)
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[i][j] = c + j < P.width ? v[i][j] : 0.f;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                s[0] += v[i][j];
+                s[1] = fmaf(v[i][j], v[i][j], s[1]);
+            }
+        }
+        s = row_sums<T>(s, sums[1][slot]);
+        const float rest = s[0] * inverse;
+        const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[1] * inverse) + P.eps);
+        if (P.stats && t == 0) *(__attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r) = (f32x2){mean + rest, rstd};
+        const float less = -rest * rstd;
+#pragma unroll
+        for (int i = 0; i < C; ++i) {
+            const int c = (i * T + t) * N;
+#pragma unroll
+            for (int j = 0; j < N; ++j) v[i][j] = fmaf(fmaf(v[i][j], rstd, less), w[i][j], b[i][j]);
+            store_piece<E>((E *)P.y + r * P.ld_out, c, P.width, Piece<E>::pack(v[i]));
+        }
     }
 }
 
@@ -105,7 +137,7 @@ __global__ __launch_bounds__(T) void norm_long_kernel(Norm P)
     float total = 0.f;
     if (on)
         for (int c = t * N; c < P.width; c += T * N) {
-            Piece<E>::unpack(load_piece<E>(x, c, P.width), v);
+            Piece<E>::unpack(load_piece<E, true>(x, c, P.width), v);
             float part = 0.f;
             for (int j = 0; j < N; ++j) part += v[j];
             total += part;
@@ -115,7 +147,7 @@ __global__ __launch_bounds__(T) void norm_long_kernel(Norm P)
     f32x2 s = (f32x2)0.f;
     if (on)
         for (int c = t * N; c < P.width; c += T * N) {
-            Piece<E>::unpack(load_piece<E>(x, c, P.width), v);
+            Piece<E>::unpack(load_piece<E, true>(x, c, P.width), v);
             f32x2 part = (f32x2)0.f;
             for (int j = 0; j < N; ++j) {
                 const float d = c + j < P.width ? v[j] - mean : 0.f;
@@ -133,14 +165,14 @@ __global__ __launch_bounds__(T) void norm_long_kernel(Norm P)
     }
     const float *const params = P.params + r / P.per_worker * P.ld_params;
     for (int c = t * N; c < (int)padded(P.width); c += T * N) {
-        for (int j = 0; j < N; ++j) v[j] = 0.f;
-        if (on) Piece<E>::unpack(load_piece<E>(x, c, P.width), v);
-        if (P.kept.codes) keep_piece<N>(P.kept, r, c, v);
+        const u32x4 raw = on ? load_piece<E, true>(x, c, P.width) : (u32x4)0u;
+        if (P.kept.codes) keep_piece<E>(P.kept, r, c, raw);
+        Piece<E>::unpack(raw, v);
         if (c >= P.width) continue;
         float w[N], b[N];
         for (int j = 0; j < N; ++j) w[j] = 1.f, b[j] = 0.f;
-        if (P.weight_at >= 0) load_floats<N>(params + P.weight_at, c, P.width, w);
-        if (P.bias_at >= 0) load_floats<N>(params + P.bias_at, c, P.width, b);
+        if (P.weight_at >= 0) load_floats<N, true>(params + P.weight_at, c, P.width, w);
+        if (P.bias_at >= 0) load_floats<N, true>(params + P.bias_at, c, P.width, b);
         for (int j = 0; j < N; ++j) v[j] = on ? fmaf((v[j] - mean - rest) * rstd, w[j], b[j]) : 0.f;
         store_piece<E>(y, c, P.width, Piece<E>::pack(v));
     }
@@ -164,11 +196,29 @@ struct NormGrad {
     f32x2 *means;                                         // of long rows: mean of g and of g u
 };
 
+// A piece of the input as it is read, and its numbers.
+template <class E, bool KEPT>
+struct Input {
+    u32x4 raw;
+    template <bool WIDE>
+    __device__ __forceinline__ void load(const NormGrad &P, int64_t r, int c) { raw = load_raw<E, WIDE>((const E *)P.x + r * P.ld, c, P.width); }
+    template <bool WIDE>
+    __device__ __forceinline__ void unpack(int c, int width, float (&v)[Piece<E>::N]) const { Piece<E>::unpack(settled<E, WIDE>(raw, c, width), v); }
+};
+template <class E>
+struct Input<E, true> {
+    Codes<Piece<E>::N> raw;
+    template <bool>
+    __device__ __forceinline__ void load(const NormGrad &P, int64_t r, int c) { raw = load_codes<Piece<E>::N>(P.kept, r, c < P.width ? c : 0); }
+    template <bool>
+    __device__ __forceinline__ void unpack(int, int, float (&v)[Piece<E>::N]) const { unpack_codes<Piece<E>::N>(raw, v); }
+};
 template <class E, bool KEPT>
 __device__ __forceinline__ void input_piece(const NormGrad &P, int64_t r, int c, float (&v)[Piece<E>::N])
 {
-    if (KEPT) kept_piece<Piece<E>::N>(P.kept, r, c, v);
-    else Piece<E>::unpack(load_piece<E>((const E *)P.x + r * P.ld, c, P.width), v);
+    Input<E, KEPT> in;
+    in.template load<true>(P, r, c);
+    in.template unpack<true>(c, P.width, v);
 }
 // Where a workgroup's share of dw (which = 0) or db goes, or null.
 __device__ __forceinline__ float *part_of(const NormGrad &P, int worker, int strip, int which)
@@ -185,55 +235,80 @@ template <class E, int T, int C, int ROWS, bool KEPT>
 __global__ __launch_bounds__(T * ROWS) void norm_grad_kernel(NormGrad P)
 {
     constexpr int N = Piece<E>::N;
+    constexpr bool WIDE = T * C > 16;
     __shared__ f32x2 sums[2][ROWS][(T + 63) / 64];
     extern __shared__ float joined[];                     // [ROWS - 1][T][C * N], one of dw and db after the other
     const int64_t group = group_number();
     if (group >= (int64_t)P.workers * P.strips) return;
-    const int worker = (int)(group / P.strips), strip = (int)(group % P.strips);
-    const int t = loss::tid<T>(), slot = threadIdx.x / T;
-    const int first = strip * P.strip_rows, end = min(first + P.strip_rows, P.per_worker);
+    const Strip cut = strip_of((uint32_t)group, P.strips, P.strip_rows, P.per_worker);
+    const int worker = cut.worker, strip = cut.number;
+    const int t = loss::tid<T>(), slot = slot_of<T>();
+    const int64_t base = (int64_t)worker * P.per_worker;
     const float inverse = 1.f / (float)P.width;
+    u32x4 next_dy[C];
+    Input<E, KEPT> next[C];
+    f32x2 next_stats = (f32x2)0.f;
+    bool next_on = false;
+    const auto load = [&](int at) {
+        const int64_t r = base + at + slot;
+        next_on = at + slot < cut.end && (!P.mask || P.mask[r]);
+        if (next_on) {
+            next_stats = *(const __attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r);
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+                const int c = (i * T + t) * N;
+                next_dy[i] = load_raw<E, WIDE>((const E *)P.dy + r * P.ld_out, c, P.width);
+                next[i].template load<WIDE>(P, r, c);
+            }
+        }
+    };
+    load(cut.first);
     float w[C][N], dw[C][N], db[C][N];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
         for (int j = 0; j < N; ++j) w[i][j] = 1.f, dw[i][j] = db[i][j] = 0.f;
-        if (P.weight_at >= 0 && P.params) load_floats<N>(P.params + worker * P.ld_params + P.weight_at, (i * T + t) * N, P.width, w[i]);
+        if (P.weight_at >= 0) load_floats<N, WIDE>(P.params + worker * P.ld_params + P.weight_at, (i * T + t) * N, P.width, w[i]);
     }
     int turn = 0;
-    for (int at = first; at < end; at += ROWS, turn ^= 1) {
-        const bool there = at + slot < end;
-        const int64_t r = (int64_t)worker * P.per_worker + at + slot;
-        const bool on = there && (!P.mask || P.mask[r]);
+    for (int at = cut.first; at < cut.end; at += ROWS) {
+        const bool there = at + slot < cut.end, on = next_on;
+        const int64_t r = base + at + slot;
         float g[C][N], u[C][N];
-        const float mean = on ? P.stats[2 * r] : 0.f, rstd = on ? P.stats[2 * r + 1] : 0.f;
+        const float mean = next_stats[0], rstd = next_stats[1];
         f32x2 s = (f32x2)0.f;
 #pragma unroll
         for (int i = 0; i < C; ++i) {
-            const int c = (i * T + t) * N;
-            for (int j = 0; j < N; ++j) g[i][j] = u[i][j] = 0.f;
-            if (on && c < P.width) {
-                Piece<E>::unpack(load_piece<E>((const E *)P.dy + r * P.ld_out, c, P.width), g[i]);
-                input_piece<E, KEPT>(P, r, c, u[i]);
-            }
+            Piece<E>::unpack(settled<E, WIDE>(next_dy[i], (i * T + t) * N, P.width), g[i]);
+            next[i].template unpack<WIDE>((i * T + t) * N, P.width, u[i]);
+        }
+        load(at + ROWS);
+        if (!on) {                                        // (T > 64: a row is the workgroup's)
+            if (there)
+#pragma unroll
+                for (int i = 0; i < C; ++i) store_piece<E>((E *)P.dx + r * P.ld, (i * T + t) * N, P.width, (u32x4)0u);
+            continue;
+        }
+        // (columns beyond the width: dy, and with it all sums, is zero there)
+#pragma unroll
+        for (int i = 0; i < C; ++i)
 #pragma unroll
             for (int j = 0; j < N; ++j) {
-                u[i][j] = on && c + j < P.width ? (u[i][j] - mean) * rstd : 0.f;
+                u[i][j] = (u[i][j] - mean) * rstd;
                 dw[i][j] = fmaf(g[i][j], u[i][j], dw[i][j]);
                 db[i][j] += g[i][j];
                 g[i][j] *= w[i][j];
                 s[0] += g[i][j];
                 s[1] = fmaf(g[i][j], u[i][j], s[1]);
             }
-        }
         s = row_sums<T>(s, sums[turn][slot]) * inverse;
-        if (there)
+        turn ^= 1;
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const int c = (i * T + t) * N;
-                if (c >= P.width) continue;
-                for (int j = 0; j < N; ++j) g[i][j] = on ? rstd * (g[i][j] - s[0] - u[i][j] * s[1]) : 0.f;
-                store_piece<E>((E *)P.dx + r * P.ld, c, P.width, Piece<E>::pack(g[i]));
-            }
+        for (int i = 0; i < C; ++i) {
+            const int c = (i * T + t) * N;
+#pragma unroll
+            for (int j = 0; j < N; ++j) g[i][j] = rstd * fmaf(-s[1], u[i][j], g[i][j] - s[0]);
+            store_piece<E>((E *)P.dx + r * P.ld, c, P.width, Piece<E>::pack(g[i]));
+        }
     }
     for (int which = 0; which < 2; ++which) {
         float *const to = part_of(P, worker, strip, which);
@@ -270,8 +345,8 @@ __global__ __launch_bounds__(T) void norm_means_kernel(NormGrad P)
     for (int c = threadIdx.x * N; c < P.width; c += T * N) {
         float g[N], u[N], w[N];
         for (int j = 0; j < N; ++j) w[j] = 1.f;
-        if (P.weight_at >= 0 && P.params) load_floats<N>(P.params + worker * P.ld_params + P.weight_at, c, P.width, w);
-        Piece<E>::unpack(load_piece<E>((const E *)P.dy + r * P.ld_out, c, P.width), g);
+        if (P.weight_at >= 0) load_floats<N, true>(P.params + worker * P.ld_params + P.weight_at, c, P.width, w);
+        Piece<E>::unpack(load_piece<E, true>((const E *)P.dy + r * P.ld_out, c, P.width), g);
         input_piece<E, KEPT>(P, r, c, u);
         f32x2 part = (f32x2)0.f;
         for (int j = 0; j < N; ++j) {
@@ -298,7 +373,7 @@ __global__ __launch_bounds__(T) void norm_grad_long_kernel(NormGrad P, int slice
     const int first = strip * P.strip_rows, end = min(first + P.strip_rows, P.per_worker);
     float w[N], dw[N], db[N];
     for (int j = 0; j < N; ++j) w[j] = 1.f, dw[j] = db[j] = 0.f;
-    if (P.weight_at >= 0 && P.params) load_floats<N>(P.params + worker * P.ld_params + P.weight_at, c, P.width, w);
+    if (P.weight_at >= 0) load_floats<N, true>(P.params + worker * P.ld_params + P.weight_at, c, P.width, w);
     for (int at = first; at < end; ++at) {
         const int64_t r = (int64_t)worker * P.per_worker + at;
         float g[N], u[N];
@@ -306,7 +381,7 @@ __global__ __launch_bounds__(T) void norm_grad_long_kernel(NormGrad P, int slice
         if (!P.mask || P.mask[r]) {
             const float mean = P.stats[2 * r], rstd = P.stats[2 * r + 1];
             const f32x2 s = P.means[r];
-            Piece<E>::unpack(load_piece<E>((const E *)P.dy + r * P.ld_out, c, P.width), g);
+            Piece<E>::unpack(load_piece<E, true>((const E *)P.dy + r * P.ld_out, c, P.width), g);
             input_piece<E, KEPT>(P, r, c, u);
             for (int j = 0; j < N; ++j) {
                 u[j] = (u[j] - mean) * rstd;
@@ -365,32 +440,72 @@ struct Store {
     int width;
     Kept kept;
 };
-constexpr int STORE_THREADS = 256;
-// A thread has a piece of a row; a row is `pieces` threads'.
+// A workgroup has STORE_PIECES x STORE_THREADS pieces that follow one another, a thread every STORE_THREADS-th; a row is a multiple of the pieces of a
+// block.
+constexpr int STORE_THREADS = 256, STORE_PIECES = 4;
+struct Spot {
+    int64_t r;
+    int c;
+};
+// Where a workgroup's pieces lie: the first one's row and place in it, and, to divide by, one over a row's pieces (at most 2^18, so that what is divided
+// is below 2^19 and a quotient in fp32 is off by one at most).
+template <int N>
+struct Pieces {
+    int64_t row;
+    int in_row, pieces;
+    float inverse;
+    __device__ __forceinline__ Pieces(const Store &P)
+    {
+        pieces = (int)(P.kept.stride / N);
+        const int64_t first = group_number() * (STORE_THREADS * STORE_PIECES);
+        row = first / pieces;
+        in_row = (int)(first % pieces);
+        inverse = 1.f / (float)pieces;
+    }
+    __device__ __forceinline__ Spot spot(int i) const
+    {
+        const int at = in_row + i * STORE_THREADS + (int)threadIdx.x;
+        int q = (int)((float)at * inverse), rest = at - q * pieces;
+        if (rest < 0) --q, rest += pieces;
+        if (rest >= pieces) ++q, rest -= pieces;
+        return Spot{row + q, rest * N};
+    }
+};
 template <class E>
 __global__ __launch_bounds__(STORE_THREADS) void store_kernel(Store P)
 {
-    constexpr int N = Piece<E>::N;
-    const int64_t pieces = P.kept.stride / N, piece = group_number() * STORE_THREADS + threadIdx.x;
-    const int64_t r = piece / pieces;
-    const int c = (int)(piece % pieces) * N;
-    if (r >= P.rows) return;                              // (a block's lanes together)
-    float v[N];
-    for (int j = 0; j < N; ++j) v[j] = 0.f;
-    if (!P.mask || P.mask[r]) Piece<E>::unpack(load_piece<E>((const E *)P.x + r * P.ld, c, P.width), v);
-    keep_piece<N>(P.kept, r, c, v);
+    const Pieces<Piece<E>::N> pieces(P);
+    u32x4 w[STORE_PIECES];
+#pragma unroll
+    for (int i = 0; i < STORE_PIECES; ++i) {
+        const Spot s = pieces.spot(i);
+        w[i] = (u32x4)0u;
+        if (s.r < P.rows && (!P.mask || P.mask[s.r])) w[i] = load_piece<E>((const E *)P.x + s.r * P.ld, s.c, P.width);
+    }
+#pragma unroll
+    for (int i = 0; i < STORE_PIECES; ++i) {
+        const Spot s = pieces.spot(i);
+        if (s.r < P.rows) keep_piece<E>(P.kept, s.r, s.c, w[i]);
+    }
 }
 template <class E>
 __global__ __launch_bounds__(STORE_THREADS) void load_kernel(Store P)
 {
     constexpr int N = Piece<E>::N;
-    const int64_t pieces = P.kept.stride / N, piece = group_number() * STORE_THREADS + threadIdx.x;
-    const int64_t r = piece / pieces;
-    const int c = (int)(piece % pieces) * N;
-    if (r >= P.rows || c >= P.width) return;
-    float v[N];
-    kept_piece<N>(P.kept, r, c, v);
-    store_piece<E>((E *)P.out + r * P.ld, c, P.width, Piece<E>::pack(v));
+    const Pieces<N> pieces(P);
+    Codes<N> w[STORE_PIECES];
+#pragma unroll
+    for (int i = 0; i < STORE_PIECES; ++i) {
+        const Spot s = pieces.spot(i);
+        if (s.r < P.rows) w[i] = load_codes<N>(P.kept, s.r, s.c);
+    }
+#pragma unroll
+    for (int i = 0; i < STORE_PIECES; ++i) {
+        const Spot s = pieces.spot(i);
+        float v[N];
+        unpack_codes<N>(w[i], v);
+        if (s.r < P.rows) store_piece<E>((E *)P.out + s.r * P.ld, s.c, P.width, Piece<E>::pack(v));
+    }
 }
 
 }  // namespace layer

@@ -9,7 +9,6 @@
 
 namespace layer {
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef float f32x16 __attribute__((ext_vector_type(16)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
@@ -168,7 +167,7 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
 
     const int t = threadIdx.x;
     const int ac = t % A_PIECES * N, ar = t / A_PIECES, bc = t % B_PIECES * 16, br = t / B_PIECES;
-    const bool a_in = o0 + ac < P.out, a_whole = o0 + ac + N <= P.out, b_in = i0 + bc < P.kept.stride;
+    const bool a_in = o0 + ac < P.out, b_in = i0 + bc < P.kept.stride;
     const int64_t exponents_stride = P.kept.stride / BLOCK;
     u32x4 a[A_COUNT], b[B_COUNT];
     uint32_t e[B_COUNT];
@@ -184,7 +183,7 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
             a[i] = (u32x4)0u;
             if (a_in && step * T::STEP + s < length && (!SOURCED || rows[s] >= 0)) {
                 const E *const row = (const E *)P.dy + r * P.ld;
-                a[i] = load_piece<E>(row, o0 + ac, a_whole ? INT32_MAX : P.out);
+                a[i] = load_piece<E>(row, o0 + ac, P.out);
             }
         }
 #pragma unroll

@@ -62,57 +62,50 @@ bool outside(int64_t at, int64_t count, int64_t ld) { return at >= 0 && (count >
 layer::Kept kept_of(const void *checkpoint, const Shape &S, const dbw_rows *l) { return layer::kept_of((void *)checkpoint, S.rows, l->width); }
 int64_t checkpoint_bytes(int64_t rows, int64_t width) { return rows * (layer::padded(width) + layer::padded(width) / layer::BLOCK); }
 
-// Which kernel takes a row of a norm: T threads, C pieces each.
-template <int T_, int C_>
+// Which kernel takes a row of a norm: T threads, C pieces each, ROWS rows of a workgroup at a time.
+template <int T_, int C_, int ROWS_>
 struct Plan {
-    static constexpr int T = T_, C = C_, ROWS = layer::ROWS_OF<T>;
+    static constexpr int T = T_, C = C_, ROWS = ROWS_;
 };
 template <class F>
 bool by_row(int64_t bytes, F f)
 {
-    if (bytes <= 16 * 16) f(Plan<16, 1>());
-    else if (bytes <= 4 * 16 * 16) f(Plan<16, 4>());
-    else if (bytes <= 4 * 64 * 16) f(Plan<64, 4>());
-    else if (bytes <= 2 * 256 * 16) f(Plan<256, 2>());
-    else if (bytes <= 4 * 256 * 16) f(Plan<256, 4>());
-    else if (bytes <= 4 * 1024 * 16) f(Plan<1024, 4>());
+    if (bytes <= 16 * 16) f(Plan<16, 1, 16>());
+    else if (bytes <= 64 * 16) f(Plan<64, 1, 4>());
+    else if (bytes <= 2 * 64 * 16) f(Plan<64, 2, 4>());
+    else if (bytes <= 4 * 64 * 16) f(Plan<64, 4, 4>());
+    else if (bytes <= 2 * 256 * 16) f(Plan<256, 2, 1>());
+    else if (bytes <= 2 * 512 * 16) f(Plan<512, 2, 1>());
+    else if (bytes <= 2 * 1024 * 16) f(Plan<1024, 2, 1>());
     else return false;
     return true;
 }
 constexpr int LONG_THREADS = 1024, LONG_GRAD_THREADS = 256;
 
-// The backward pass: T threads a row, C pieces each, ROWS rows of a workgroup at a time.
-template <int T_, int C_, int ROWS_>
-struct GradPlan {
-    static constexpr int T = T_, C = C_, ROWS = ROWS_;
-};
-template <class F>
-bool by_grad_row(int64_t bytes, F f)
-{
-    if (bytes <= 16 * 16) f(GradPlan<16, 1, 16>());
-    else if (bytes <= 64 * 16) f(GradPlan<64, 1, 4>());
-    else if (bytes <= 2 * 64 * 16) f(GradPlan<64, 2, 8>());
-    else if (bytes <= 4 * 64 * 16) f(GradPlan<64, 4, 4>());
-    else if (bytes <= 2 * 256 * 16) f(GradPlan<256, 2, 1>());
-    else if (bytes <= 2 * 512 * 16) f(GradPlan<512, 2, 1>());
-    else if (bytes <= 2 * 1024 * 16) f(GradPlan<1024, 2, 1>());
-    else return false;
-    return true;
-}
-constexpr int STRIPS = 512;                               // workgroups that all workers' rows are cut for
+// A worker's rows in strips of whole turns: as many rows as leave `groups` workgroups for all workers, at least `turns` turns.
 struct Strips {
     int count, rows;                                      // of a worker, and of a strip
 };
-Strips strips_of(const dbw_rows *l, const Shape &S)
+Strips strips_of(const dbw_rows *l, int rows_at_once, int64_t groups, int turns)
 {
-    int at_once = 1;
-    by_grad_row(S.e * l->width, [&](auto p) { at_once = p.ROWS; });
-    const int64_t most = (STRIPS + l->workers - 1) / l->workers, least_rows = 4 * at_once;
-    int64_t count = (l->rows + least_rows - 1) / least_rows;
-    if (count > most) count = most;
-    if (count < 1) count = 1;
-    const int rows = (int)((l->rows + count - 1) / count);
-    return Strips{rows ? (int)((l->rows + rows - 1) / rows) : 1, rows};
+    const int64_t most = (groups + l->workers - 1) / l->workers, least = (int64_t)turns * rows_at_once;
+    int64_t rows = (l->rows + most - 1) / most;
+    if (rows < least) rows = least;
+    rows = (rows + rows_at_once - 1) / rows_at_once * rows_at_once;
+    return Strips{l->rows > rows ? (int)((l->rows + rows - 1) / rows) : 1, (int)(rows < INT32_MAX ? rows : INT32_MAX)};
+}
+int rows_at_once(const dbw_rows *l, const Shape &S)
+{
+    int n = 1;
+    by_row(S.e * l->width, [&](auto p) { n = p.ROWS; });
+    return n;
+}
+constexpr int NORM_GROUPS = 2048, GRAD_GROUPS = 512;      // workgroups of a strip each
+Strips grad_strips_of(const dbw_rows *l, const Shape &S) { return strips_of(l, rows_at_once(l, S), GRAD_GROUPS, 4); }
+dim3 store_grid(int64_t pieces)
+{
+    constexpr int each = layer::STORE_THREADS * layer::STORE_PIECES;
+    return grid_of((pieces + each - 1) / each);
 }
 int64_t part_ld(const dbw_rows *l) { return (l->width + 3) / 4 * 4; }
 
@@ -137,7 +130,7 @@ extern "C" int dbw_checkpoint_store(const dbw_rows *shape, const void *x, const 
     by_type(shape->type, [&](auto e) {
         typedef decltype(e) E;
         const int64_t pieces = S.rows * (P.kept.stride / layer::Piece<E>::N);
-        hipLaunchKernelGGL(layer::store_kernel<E>, grid_of((pieces + layer::STORE_THREADS - 1) / layer::STORE_THREADS), dim3(layer::STORE_THREADS), 0,
+        hipLaunchKernelGGL(layer::store_kernel<E>, store_grid(pieces), dim3(layer::STORE_THREADS), 0,
                            (hipStream_t)stream, P);
     });
     DBW_HIP(hipGetLastError());
@@ -156,7 +149,7 @@ extern "C" int dbw_checkpoint_load(const dbw_rows *shape, const void *checkpoint
     by_type(shape->type, [&](auto e) {
         typedef decltype(e) E;
         const int64_t pieces = S.rows * (P.kept.stride / layer::Piece<E>::N);
-        hipLaunchKernelGGL(layer::load_kernel<E>, grid_of((pieces + layer::STORE_THREADS - 1) / layer::STORE_THREADS), dim3(layer::STORE_THREADS), 0,
+        hipLaunchKernelGGL(layer::load_kernel<E>, store_grid(pieces), dim3(layer::STORE_THREADS), 0,
                            (hipStream_t)stream, P);
     });
     DBW_HIP(hipGetLastError());
@@ -175,14 +168,15 @@ extern "C" int dbw_layer_norm(const dbw_rows *shape, const void *x, const uint8_
     if ((weight_at >= 0 || bias_at >= 0) && too_long(ld_params, shape->workers)) return DBW_ERR_UNSUPPORTED;
     if (!(x == y && S.ld == S.ld_out) && overlap(x, S.rows, S.ld, y, S.rows, S.ld_out, shape->width, S.e)) return DBW_ERR_ALIAS;
     if (S.rows == 0) return DBW_OK;
-    layer::Norm P{x, mask, params, S.ld, S.ld_out, ld_params, weight_at, bias_at, S.rows, shape->rows, shape->width, eps, y, stats_out,
-                  kept_of(checkpoint, S, shape)};
+    const Strips strips = strips_of(shape, rows_at_once(shape, S), NORM_GROUPS, 1);
+    layer::Norm P{x, mask, params, S.ld, S.ld_out, ld_params, weight_at, bias_at, S.rows, shape->rows, shape->width, shape->workers, strips.count,
+                  strips.rows, eps, y, stats_out, kept_of(checkpoint, S, shape)};
     if (!checkpoint) P.kept.codes = nullptr;
     hipStream_t s = (hipStream_t)stream;
     by_type(shape->type, [&](auto e) {
         typedef decltype(e) E;
         if (!by_row(S.e * shape->width, [&](auto p) {
-                hipLaunchKernelGGL((layer::norm_kernel<E, p.T, p.C>), grid_of((S.rows + p.ROWS - 1) / p.ROWS), dim3(p.T * p.ROWS), 0, s, P);
+                hipLaunchKernelGGL((layer::norm_kernel<E, p.T, p.C, p.ROWS>), grid_of((int64_t)shape->workers * strips.count), dim3(p.T * p.ROWS), 0, s, P);
             }))
             hipLaunchKernelGGL((layer::norm_long_kernel<E, LONG_THREADS>), grid_of(S.rows), dim3(LONG_THREADS), 0, s, P);
     });
@@ -195,9 +189,9 @@ extern "C" int64_t dbw_layer_norm_work_bytes(const dbw_rows *shape)
     Shape S;
     const int rc = check_shape(shape, &S);
     if (rc != DBW_OK) return rc;
-    const Strips strips = strips_of(shape, S);
+    const Strips strips = grad_strips_of(shape, S);
     int64_t bytes = strips.count > 1 ? (int64_t)shape->workers * strips.count * 2 * part_ld(shape) * 4 : 0;
-    if (!by_grad_row(S.e * shape->width, [](auto) {})) bytes += 8 * S.rows;
+    if (!by_row(S.e * shape->width, [](auto) {})) bytes += 8 * S.rows;
     return bytes + 16;
 }
 
@@ -218,7 +212,7 @@ extern "C" int dbw_layer_norm_grad(const dbw_rows *shape, const void *dy, const 
     if (dx != x && overlap(x, S.rows, S.ld, dx, S.rows, S.ld, shape->width, S.e)) return DBW_ERR_ALIAS;
     if (!(dx == dy && S.ld == S.ld_out) && overlap(dy, S.rows, S.ld_out, dx, S.rows, S.ld, shape->width, S.e)) return DBW_ERR_ALIAS;
     if (weight_at < 0 && bias_at < 0) grads = nullptr;
-    const Strips strips = strips_of(shape, S);
+    const Strips strips = grad_strips_of(shape, S);
     layer::NormGrad P{dy, x, kept_of(checkpoint, S, shape), mask, stats, params, S.ld, S.ld_out, ld_params, ld_grads, weight_at, bias_at, S.rows,
                       shape->rows, shape->width, shape->workers, strips.count, strips.rows, dx, grads, nullptr, part_ld(shape), nullptr};
     hipStream_t s = (hipStream_t)stream;
@@ -238,7 +232,7 @@ extern "C" int dbw_layer_norm_grad(const dbw_rows *shape, const void *dy, const 
             if (x) hipLaunchKernelGGL((layer::norm_grad_kernel<E, p.T, p.C, p.ROWS, false>), grid_of(groups), dim3(p.T * p.ROWS), lds, s, P);
             else hipLaunchKernelGGL((layer::norm_grad_kernel<E, p.T, p.C, p.ROWS, true>), grid_of(groups), dim3(p.T * p.ROWS), lds, s, P);
         };
-        if (!by_grad_row(S.e * shape->width, rows)) {
+        if (!by_row(S.e * shape->width, rows)) {
             constexpr int T = LONG_GRAD_THREADS, COLUMNS = T * layer::Piece<E>::N;
             const int slices = (shape->width + COLUMNS - 1) / COLUMNS;
             if (x) {
