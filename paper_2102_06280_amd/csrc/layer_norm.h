@@ -12,50 +12,80 @@ struct Norm {
     int64_t ld, ld_out, ld_params, weight_at, bias_at;
     int64_t rows;                                         // of all workers
     int per_worker, width, workers;
-    int strips, strip_rows;                               // of a worker
+    int strips;                                           // workgroups of a worker
     float eps;
     void *y;
     float *stats;
     Kept kept;                                            // codes null: not wanted
 };
 
-// Sums of two numbers over a row's T threads.  lds: 2 T / 64 floats of the row's that nothing else uses until the next barrier.
-template <int T>
-__device__ __forceinline__ f32x2 row_sums(f32x2 v, f32x2 *lds)
+// Sums of K numbers over a row's T threads.  lds: T / 64 times K floats of the row's that nothing else uses until the next barrier but one.
+template <int T, int K>
+__device__ __forceinline__ void row_sums(float (&v)[K], float (*lds)[K])
 {
-    v = (f32x2){loss::lanes_sum<T>(v[0]), loss::lanes_sum<T>(v[1])};
-    if (T <= 64) return v;
-    if ((threadIdx.x & 63) == 0) lds[(threadIdx.x & (T - 1)) >> 6] = v;
-    __syncthreads();
-    v = lds[0];
 #pragma unroll
-    for (int w = 1; w < T / 64; ++w) v += lds[w];
-    return v;
+    for (int k = 0; k < K; ++k) v[k] = loss::lanes_sum<T>(v[k]);
+    if (T <= 64) return;
+    if ((threadIdx.x & 63) == 0)
+#pragma unroll
+        for (int k = 0; k < K; ++k) lds[(threadIdx.x & (T - 1)) >> 6][k] = v[k];
+    __syncthreads();
+#pragma unroll
+    for (int k = 0; k < K; ++k) {
+        v[k] = lds[0][k];
+#pragma unroll
+        for (int w = 1; w < T / 64; ++w) v[k] += lds[w][k];
+    }
 }
 
-// A row in the registers of T threads, C pieces each; a workgroup walks over a strip of a worker's rows, ROWS at a time, with the weights in registers and
-// the next row on its way.  The mean comes first, then the sums of the differences from it and of their squares: the first of these is what the
-// rounding of the mean left, which counts where a row's mean is large beside its spread.
-template <class E, int T, int C, int ROWS>
-__global__ __launch_bounds__(T * ROWS) void norm_kernel(Norm P)
+// Which of a group's next rows take part, looked up a turn before their loads, which would wait for it otherwise.
+template <int R, int SLOTS>
+struct Ahead {
+    const uint8_t *mask;                                  // of the group's first row
+    int64_t end;
+    uint8_t rows[R];
+    __device__ __forceinline__ Ahead(const uint8_t *all, int64_t first, int64_t rows_left) : mask(all ? all + first : nullptr), end(rows_left) {}
+    __device__ __forceinline__ void look(int64_t at)
+    {
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            rows[q] = 1;
+            if (mask && at + q * SLOTS < end) rows[q] = ((const __attribute__((address_space(1))) uint8_t *)(uint64_t)mask)[at + q * SLOTS];
+        }
+    }
+    __device__ __forceinline__ bool on(int64_t at, int q) const { return at + q * SLOTS < end && rows[q]; }
+};
+
+// A row in the registers of T threads, C pieces each.  A workgroup has SLOTS such groups of threads and walks over a strip of a worker's rows, R rows a
+// group at a time, with the weights in registers and the next rows on their way; the rows' sums share their barriers.  The mean comes first, then the
+// sums of the differences from it and of their squares: the first of these is what the rounding of the mean left, which counts where a row's mean is
+// large beside its spread.
+template <class E, int T, int C, int SLOTS, int R>
+__global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P)
 {
-    constexpr int N = Piece<E>::N;
+    constexpr int N = Piece<E>::N, WAVES = (T + 63) / 64;
     constexpr bool WIDE = T * C > 16;
-    __shared__ f32x2 sums[2][ROWS][(T + 63) / 64];
+    __shared__ float totals[SLOTS][WAVES][R], sums[SLOTS][WAVES][2 * R];
     const int64_t group = group_number();
     if (group >= (int64_t)P.workers * P.strips) return;
-    const Strip strip = strip_of((uint32_t)group, P.strips, P.strip_rows, P.per_worker);
+    const Strip strip = strip_of((uint32_t)group, P.strips, R * SLOTS, P.per_worker);
     const int t = loss::tid<T>(), slot = slot_of<T>();
     const int64_t base = (int64_t)strip.worker * P.per_worker;
     const float inverse = 1.f / (float)P.width;
-    u32x4 next[C];
-    bool next_on = false;
-    const auto load = [&](int at) {
-        const int64_t r = base + at + slot;
-        next_on = at + slot < strip.end && (!P.mask || P.mask[r]);
-        if (next_on)
+    u32x4 next[R][C];
+    bool next_on[R];
+    Ahead<R, SLOTS> ahead(P.mask, base + slot, strip.end - slot);
+    ahead.look(strip.first);
+    const auto load = [&](int64_t at) {
 #pragma unroll
-            for (int i = 0; i < C; ++i) next[i] = load_raw<E, WIDE>((const E *)P.x + r * P.ld, (i * T + t) * N, P.width);
+        for (int q = 0; q < R; ++q) {
+            const int64_t r = base + at + q * SLOTS + slot;
+            next_on[q] = ahead.on(at, q);
+            if (next_on[q])
+#pragma unroll
+                for (int i = 0; i < C; ++i) next[q][i] = load_raw<E, WIDE>((const E *)P.x + r * P.ld, (i * T + t) * N, P.width);
+        }
+        ahead.look(at + strip.stride);
     };
     load(strip.first);
     float w[C][N], b[C][N];
@@ -66,59 +96,86 @@ __global__ __launch_bounds__(T * ROWS) void norm_kernel(Norm P)
         if (P.weight_at >= 0) load_floats<N, WIDE>(params + P.weight_at, (i * T + t) * N, P.width, w[i]);
         if (P.bias_at >= 0) load_floats<N, WIDE>(params + P.bias_at, (i * T + t) * N, P.width, b[i]);
     }
-    for (int at = strip.first; at < strip.end; at += ROWS) {
-        const bool on = next_on, there = at + slot < strip.end;
-        const int64_t r = base + at + slot;
-        float v[C][N];
-        f32x2 s = (f32x2)0.f;
+    // Rows are written a turn later, in front of the loads of the rows behind the next: waiting for loads is waiting for all that was asked for before
+    // them, and nothing then waits for stores that have just begun.  (Backwards from 8 bits with a mask, 8 x 2048 x 2048 bf16: 48 us -> 37.)
+    u32x4 out[R][C];
+    int64_t last = -1;
+    const auto store = [&](int64_t at) {
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const u32x4 raw = on ? settled<E, WIDE>(next[i], (i * T + t) * N, P.width) : (u32x4)0u;
-            if (P.kept.codes && there && (i * T + t) * N < (int)P.kept.stride) keep_piece<E>(P.kept, r, (i * T + t) * N, raw);
-            Piece<E>::unpack(raw, v[i]);
+        for (int q = 0; q < R; ++q) {
+            const int64_t row = at + q * SLOTS + slot;
+            if (row < strip.end)
+#pragma unroll
+                for (int i = 0; i < C; ++i) store_piece<E>((E *)P.y + (base + row) * P.ld_out, (i * T + t) * N, P.width, out[q][i]);
         }
-        load(at + ROWS);
-        if (!on) {                                        // (T > 64: a row is the workgroup's)
-            if (there) {
-                if (P.stats && t == 0) *(__attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r) = s;
+    };
+    for (int64_t at = strip.first; at < strip.end; at += strip.stride) {
+        bool on[R];
+        float v[R][C][N], total[R], s[2 * R];
+        u32x4 raw[R][C];
 #pragma unroll
-                for (int i = 0; i < C; ++i) store_piece<E>((E *)P.y + r * P.ld_out, (i * T + t) * N, P.width, (u32x4)0u);
-            }
-            continue;
+        for (int q = 0; q < R; ++q) {
+            on[q] = next_on[q];
+#pragma unroll
+            for (int i = 0; i < C; ++i) raw[q][i] = on[q] ? settled<E, WIDE>(next[q][i], (i * T + t) * N, P.width) : (u32x4)0u;
         }
+        if (last >= 0) store(last);
 #pragma unroll
-        for (int i = 0; i < C; ++i)
+        for (int q = 0; q < R; ++q) {
+            const int64_t row = at + q * SLOTS + slot;
+            total[q] = 0.f;
 #pragma unroll
-            for (int j = 0; j < N; ++j) s[j & 1] += v[i][j];
-        const float mean = row_sums<T>((f32x2){s[0] + s[1], 0.f}, sums[0][slot])[0] * inverse;
-        s = (f32x2)0.f;
+            for (int i = 0; i < C; ++i) {
+                const int c = (i * T + t) * N;
+                if (P.kept.codes && row < strip.end && c < (int)P.kept.stride) keep_piece<E>(P.kept, base + row, c, raw[q][i]);
+                Piece<E>::unpack(raw[q][i], v[q][i]);
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const int c = (i * T + t) * N;
-#pragma unroll
-            for (int j = 0; j < N; ++j) v[i][j] -= mean;
-            if (c + N > P.width)
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[i][j] = c + j < P.width ? v[i][j] : 0.f;
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                s[0] += v[i][j];
-                s[1] = fmaf(v[i][j], v[i][j], s[1]);
+                for (int j = 0; j < N; ++j) total[q] += v[q][i][j];
             }
         }
-        s = row_sums<T>(s, sums[1][slot]);
-        const float rest = s[0] * inverse;
-        const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[1] * inverse) + P.eps);
-        if (P.stats && t == 0) *(__attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r) = (f32x2){mean + rest, rstd};
-        const float less = -rest * rstd;
+        load(at + strip.stride);
+        row_sums<T>(total, totals[slot]);
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const int c = (i * T + t) * N;
+        for (int q = 0; q < R; ++q) {
+            total[q] *= inverse;                          // the mean
+            s[2 * q] = s[2 * q + 1] = 0.f;
 #pragma unroll
-            for (int j = 0; j < N; ++j) v[i][j] = fmaf(fmaf(v[i][j], rstd, less), w[i][j], b[i][j]);
-            store_piece<E>((E *)P.y + r * P.ld_out, c, P.width, Piece<E>::pack(v[i]));
+            for (int i = 0; i < C; ++i) {
+                const int c = (i * T + t) * N;
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[q][i][j] -= total[q];
+                if (c + N > P.width)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) v[q][i][j] = c + j < P.width ? v[q][i][j] : 0.f;
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    s[2 * q] += v[q][i][j];
+                    s[2 * q + 1] = fmaf(v[q][i][j], v[q][i][j], s[2 * q + 1]);
+                }
+            }
         }
+        row_sums<T>(s, sums[slot]);
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const int64_t row = at + q * SLOTS + slot;
+            if (row >= strip.end) continue;
+            const int64_t r = base + row;
+            const float rest = s[2 * q] * inverse;
+            const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[2 * q + 1] * inverse) + P.eps);
+            if (P.stats && t == 0)
+                *(__attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r) = on[q] ? (f32x2){total[q] + rest, rstd} : (f32x2)0.f;
+            const float less = -rest * rstd;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) v[q][i][j] = fmaf(fmaf(v[q][i][j], rstd, less), w[i][j], b[i][j]);
+                const u32x4 packed = Piece<E>::pack(v[q][i]);
+                out[q][i] = on[q] ? packed : (u32x4)0u;
+            }
+        }
+        last = at;
     }
+    if (last >= 0) store(last);
 }
 
 // Rows that registers do not hold: read three times, by one workgroup.
@@ -126,37 +183,38 @@ template <class E, int T>
 __global__ __launch_bounds__(T) void norm_long_kernel(Norm P)
 {
     constexpr int N = Piece<E>::N;
-    __shared__ f32x2 sums[2][T / 64];
+    __shared__ float totals[T / 64][1], sums[T / 64][2];
     const int64_t r = group_number();
     const int t = threadIdx.x;
     if (r >= P.rows) return;
     const bool on = !P.mask || P.mask[r];
     const E *const x = (const E *)P.x + r * P.ld;
     E *const y = (E *)P.y + r * P.ld_out;
-    float v[N];
-    float total = 0.f;
+    float v[N], total[1] = {0.f};
     if (on)
         for (int c = t * N; c < P.width; c += T * N) {
             Piece<E>::unpack(load_piece<E, true>(x, c, P.width), v);
             float part = 0.f;
             for (int j = 0; j < N; ++j) part += v[j];
-            total += part;
+            total[0] += part;
         }
     const float inverse = 1.f / (float)P.width;
-    const float mean = row_sums<T>((f32x2){total, 0.f}, sums[0])[0] * inverse;
-    f32x2 s = (f32x2)0.f;
+    row_sums<T>(total, totals);
+    const float mean = total[0] * inverse;
+    float s[2] = {0.f, 0.f};
     if (on)
         for (int c = t * N; c < P.width; c += T * N) {
             Piece<E>::unpack(load_piece<E, true>(x, c, P.width), v);
-            f32x2 part = (f32x2)0.f;
+            float part[2] = {0.f, 0.f};
             for (int j = 0; j < N; ++j) {
                 const float d = c + j < P.width ? v[j] - mean : 0.f;
                 part[0] += d;
                 part[1] = fmaf(d, d, part[1]);
             }
-            s += part;
+            s[0] += part[0];
+            s[1] += part[1];
         }
-    s = row_sums<T>(s, sums[1]);
+    row_sums<T>(s, sums);
     const float rest = s[0] * inverse;
     const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[1] * inverse) + P.eps);
     if (P.stats && t == 0) {
@@ -188,7 +246,7 @@ struct NormGrad {
     int64_t ld, ld_out, ld_params, ld_grads, weight_at, bias_at;
     int64_t rows;
     int per_worker, width, workers;
-    int strips, strip_rows;                               // a worker's rows are cut into strips, a workgroup each
+    int strips;                                           // workgroups of a worker
     void *dx;
     float *grads;                                         // null: not wanted
     float *parts;                                         // [worker][strip][2][part_ld]: dw and db of the strips; null: one strip, straight into grads
@@ -203,7 +261,10 @@ struct Input {
     template <bool WIDE>
     __device__ __forceinline__ void load(const NormGrad &P, int64_t r, int c) { raw = load_raw<E, WIDE>((const E *)P.x + r * P.ld, c, P.width); }
     template <bool WIDE>
-    __device__ __forceinline__ void unpack(int c, int width, float (&v)[Piece<E>::N]) const { Piece<E>::unpack(settled<E, WIDE>(raw, c, width), v); }
+    __device__ __forceinline__ void unpack(bool on, int c, int width, float (&v)[Piece<E>::N]) const
+    {
+        Piece<E>::unpack(on ? settled<E, WIDE>(raw, c, width) : (u32x4)0u, v);
+    }
 };
 template <class E>
 struct Input<E, true> {
@@ -211,14 +272,20 @@ struct Input<E, true> {
     template <bool>
     __device__ __forceinline__ void load(const NormGrad &P, int64_t r, int c) { raw = load_codes<Piece<E>::N>(P.kept, r, c < P.width ? c : 0); }
     template <bool>
-    __device__ __forceinline__ void unpack(int, int, float (&v)[Piece<E>::N]) const { unpack_codes<Piece<E>::N>(raw, v); }
+    __device__ __forceinline__ void unpack(bool on, int, int, float (&v)[Piece<E>::N]) const
+    {
+        Codes<Piece<E>::N> codes = raw;
+        for (uint32_t &w : codes.w) w = on ? w : 0u;
+        codes.exponent = on ? codes.exponent : 127u;
+        unpack_codes<Piece<E>::N>(codes, v);
+    }
 };
 template <class E, bool KEPT>
 __device__ __forceinline__ void input_piece(const NormGrad &P, int64_t r, int c, float (&v)[Piece<E>::N])
 {
     Input<E, KEPT> in;
     in.template load<true>(P, r, c);
-    in.template unpack<true>(c, P.width, v);
+    in.template unpack<true>(true, c, P.width, v);
 }
 // Where a workgroup's share of dw (which = 0) or db goes, or null.
 __device__ __forceinline__ float *part_of(const NormGrad &P, int worker, int strip, int which)
@@ -229,105 +296,133 @@ __device__ __forceinline__ float *part_of(const NormGrad &P, int worker, int str
     return P.grads + worker * P.ld_grads + at;
 }
 
-// A workgroup walks over its strip, T threads a row and ROWS rows at a time; every thread's columns are the same in all rows, so that it sums
-// dw and db in registers.
-template <class E, int T, int C, int ROWS, bool KEPT>
-__global__ __launch_bounds__(T * ROWS) void norm_grad_kernel(NormGrad P)
+// As norm_kernel; every thread's columns are the same in all rows, so that it sums dw and db in registers.  Rows that take no part are zeros with a mean and
+// a scale of zero.
+template <class E, int T, int C, int SLOTS, int R, bool KEPT>
+__global__ __launch_bounds__(T * SLOTS) void norm_grad_kernel(NormGrad P)
 {
-    constexpr int N = Piece<E>::N;
+    constexpr int N = Piece<E>::N, WAVES = (T + 63) / 64;
     constexpr bool WIDE = T * C > 16;
-    __shared__ f32x2 sums[2][ROWS][(T + 63) / 64];
-    extern __shared__ float joined[];                     // [ROWS - 1][T][C * N], one of dw and db after the other
+    __shared__ float sums[2][SLOTS][WAVES][2 * R];
+    extern __shared__ float joined[];                     // [SLOTS][C * N][T], one of dw and db after the other
     const int64_t group = group_number();
     if (group >= (int64_t)P.workers * P.strips) return;
-    const Strip cut = strip_of((uint32_t)group, P.strips, P.strip_rows, P.per_worker);
-    const int worker = cut.worker, strip = cut.number;
+    const Strip strip = strip_of((uint32_t)group, P.strips, R * SLOTS, P.per_worker);
     const int t = loss::tid<T>(), slot = slot_of<T>();
-    const int64_t base = (int64_t)worker * P.per_worker;
+    const int64_t base = (int64_t)strip.worker * P.per_worker;
     const float inverse = 1.f / (float)P.width;
-    u32x4 next_dy[C];
-    Input<E, KEPT> next[C];
-    f32x2 next_stats = (f32x2)0.f;
-    bool next_on = false;
-    const auto load = [&](int at) {
-        const int64_t r = base + at + slot;
-        next_on = at + slot < cut.end && (!P.mask || P.mask[r]);
-        if (next_on) {
-            next_stats = *(const __attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r);
+    u32x4 next_dy[R][C];
+    Input<E, KEPT> next[R][C];
+    f32x2 next_stats[R];
+    bool next_on[R];
+    Ahead<R, SLOTS> ahead(P.mask, base + slot, strip.end - slot);
+    ahead.look(strip.first);
+    const auto load = [&](int64_t at) {
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const int c = (i * T + t) * N;
-                next_dy[i] = load_raw<E, WIDE>((const E *)P.dy + r * P.ld_out, c, P.width);
-                next[i].template load<WIDE>(P, r, c);
+        for (int q = 0; q < R; ++q) {
+            const int64_t r = base + at + q * SLOTS + slot;
+            next_on[q] = ahead.on(at, q);
+            next_stats[q] = (f32x2)0.f;
+            if (next_on[q]) {
+                next_stats[q] = *(const __attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r);
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    next_dy[q][i] = load_raw<E, WIDE>((const E *)P.dy + r * P.ld_out, (i * T + t) * N, P.width);
+                    next[q][i].template load<WIDE>(P, r, (i * T + t) * N);
+                }
             }
         }
+        ahead.look(at + strip.stride);
     };
-    load(cut.first);
+    load(strip.first);
     float w[C][N], dw[C][N], db[C][N];
 #pragma unroll
     for (int i = 0; i < C; ++i) {
         for (int j = 0; j < N; ++j) w[i][j] = 1.f, dw[i][j] = db[i][j] = 0.f;
-        if (P.weight_at >= 0) load_floats<N, WIDE>(P.params + worker * P.ld_params + P.weight_at, (i * T + t) * N, P.width, w[i]);
+        if (P.weight_at >= 0) load_floats<N, WIDE>(P.params + strip.worker * P.ld_params + P.weight_at, (i * T + t) * N, P.width, w[i]);
     }
+    u32x4 out[R][C];
+    int64_t last = -1;
+    const auto store = [&](int64_t at) {
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const int64_t row = at + q * SLOTS + slot;
+            if (row < strip.end)
+#pragma unroll
+                for (int i = 0; i < C; ++i) store_piece<E>((E *)P.dx + (base + row) * P.ld, (i * T + t) * N, P.width, out[q][i]);
+        }
+    };
     int turn = 0;
-    for (int at = cut.first; at < cut.end; at += ROWS) {
-        const bool there = at + slot < cut.end, on = next_on;
-        const int64_t r = base + at + slot;
-        float g[C][N], u[C][N];
-        const float mean = next_stats[0], rstd = next_stats[1];
-        f32x2 s = (f32x2)0.f;
+    for (int64_t at = strip.first; at < strip.end; at += strip.stride, turn ^= 1) {
+        float g[R][C][N], u[R][C][N], s[2 * R], rstd[R];
 #pragma unroll
-        for (int i = 0; i < C; ++i) {
-            Piece<E>::unpack(settled<E, WIDE>(next_dy[i], (i * T + t) * N, P.width), g[i]);
-            next[i].template unpack<WIDE>((i * T + t) * N, P.width, u[i]);
-        }
-        load(at + ROWS);
-        if (!on) {                                        // (T > 64: a row is the workgroup's)
-            if (there)
+        for (int q = 0; q < R; ++q) {
+            const float mean = next_stats[q][0];
+            rstd[q] = next_stats[q][1];
+            s[2 * q] = s[2 * q + 1] = 0.f;
 #pragma unroll
-                for (int i = 0; i < C; ++i) store_piece<E>((E *)P.dx + r * P.ld, (i * T + t) * N, P.width, (u32x4)0u);
-            continue;
-        }
-        // (columns beyond the width: dy, and with it all sums, is zero there)
+            for (int i = 0; i < C; ++i) {
+                const int c = (i * T + t) * N;
+                Piece<E>::unpack(next_on[q] ? settled<E, WIDE>(next_dy[q][i], c, P.width) : (u32x4)0u, g[q][i]);
+                next[q][i].template unpack<WIDE>(next_on[q], c, P.width, u[q][i]);
+                // (columns beyond the width: dy, and with it all sums, is zero there)
 #pragma unroll
-        for (int i = 0; i < C; ++i)
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                u[i][j] = (u[i][j] - mean) * rstd;
-                dw[i][j] = fmaf(g[i][j], u[i][j], dw[i][j]);
-                db[i][j] += g[i][j];
-                g[i][j] *= w[i][j];
-                s[0] += g[i][j];
-                s[1] = fmaf(g[i][j], u[i][j], s[1]);
+                for (int j = 0; j < N; ++j) u[q][i][j] = (u[q][i][j] - mean) * rstd[q];
             }
-        s = row_sums<T>(s, sums[turn][slot]) * inverse;
-        turn ^= 1;
-#pragma unroll
-        for (int i = 0; i < C; ++i) {
-            const int c = (i * T + t) * N;
-#pragma unroll
-            for (int j = 0; j < N; ++j) g[i][j] = rstd * fmaf(-s[1], u[i][j], g[i][j] - s[0]);
-            store_piece<E>((E *)P.dx + r * P.ld, c, P.width, Piece<E>::pack(g[i]));
         }
-    }
-    for (int which = 0; which < 2; ++which) {
-        float *const to = part_of(P, worker, strip, which);
-        if (!to) continue;
-        if (ROWS > 1) {
-            __syncthreads();
-            if (slot)
-                for (int i = 0; i < C; ++i)
-                    for (int j = 0; j < N; ++j) joined[((slot - 1) * C * N + i * N + j) * T + t] = which ? db[i][j] : dw[i][j];
-            __syncthreads();
-            if (slot == 0)
-                for (int i = 0; i < C; ++i)
-                    for (int j = 0; j < N; ++j)
-                        for (int q = 0; q < ROWS - 1; ++q) (which ? db : dw)[i][j] += joined[(q * C * N + i * N + j) * T + t];
-        }
-        if (slot == 0)
+        if (last >= 0) store(last);
+        load(at + strip.stride);
+#pragma unroll
+        for (int q = 0; q < R; ++q)
 #pragma unroll
             for (int i = 0; i < C; ++i)
-                if ((i * T + t) * N < P.width) store_floats<N>(to, (i * T + t) * N, P.width, which ? db[i] : dw[i]);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    dw[i][j] = fmaf(g[q][i][j], u[q][i][j], dw[i][j]);
+                    db[i][j] += g[q][i][j];
+                    g[q][i][j] *= w[i][j];
+                    s[2 * q] += g[q][i][j];
+                    s[2 * q + 1] = fmaf(g[q][i][j], u[q][i][j], s[2 * q + 1]);
+                }
+        row_sums<T>(s, sums[turn][slot]);
+#pragma unroll
+        for (int q = 0; q < R; ++q) {
+            const float mean_g = s[2 * q] * inverse, mean_gu = s[2 * q + 1] * inverse;
+#pragma unroll
+            for (int i = 0; i < C; ++i) {
+#pragma unroll
+                for (int j = 0; j < N; ++j) g[q][i][j] = rstd[q] * fmaf(-mean_gu, u[q][i][j], g[q][i][j] - mean_g);
+                out[q][i] = Piece<E>::pack(g[q][i]);
+            }
+        }
+        last = at;
+    }
+    if (last >= 0) store(last);
+    // the groups' sums, piece i of all of them by group i mod SLOTS
+#pragma unroll
+    for (int which = 0; which < 2; ++which) {
+        float *const to = part_of(P, strip.worker, strip.number, which);
+        if (!to) continue;
+        float (&mine)[C][N] = which ? db : dw;
+        if (SLOTS > 1) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+#pragma unroll
+                for (int j = 0; j < N; ++j) joined[((slot * C + i) * N + j) * T + t] = mine[i][j];
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < C; ++i)
+                if (i % SLOTS == slot)
+#pragma unroll
+                    for (int j = 0; j < N; ++j) {
+                        mine[i][j] = joined[(i * N + j) * T + t];
+                        for (int q = 1; q < SLOTS; ++q) mine[i][j] += joined[((q * C + i) * N + j) * T + t];
+                    }
+        }
+#pragma unroll
+        for (int i = 0; i < C; ++i)
+            if (i % SLOTS == slot && (i * T + t) * N < P.width) store_floats<N>(to, (i * T + t) * N, P.width, mine[i]);
     }
 }
 
@@ -336,28 +431,30 @@ template <class E, int T, bool KEPT>
 __global__ __launch_bounds__(T) void norm_means_kernel(NormGrad P)
 {
     constexpr int N = Piece<E>::N;
-    __shared__ f32x2 sums[T / 64];
+    __shared__ float sums[T / 64][2];
     const int64_t r = group_number();
     if (r >= P.rows || (P.mask && !P.mask[r])) return;
     const int worker = (int)(r / P.per_worker);
     const float mean = P.stats[2 * r], rstd = P.stats[2 * r + 1];
-    f32x2 s = (f32x2)0.f;
+    float s[2] = {0.f, 0.f};
     for (int c = threadIdx.x * N; c < P.width; c += T * N) {
         float g[N], u[N], w[N];
         for (int j = 0; j < N; ++j) w[j] = 1.f;
         if (P.weight_at >= 0) load_floats<N, true>(P.params + worker * P.ld_params + P.weight_at, c, P.width, w);
         Piece<E>::unpack(load_piece<E, true>((const E *)P.dy + r * P.ld_out, c, P.width), g);
         input_piece<E, KEPT>(P, r, c, u);
-        f32x2 part = (f32x2)0.f;
+        float part[2] = {0.f, 0.f};
         for (int j = 0; j < N; ++j) {
             const float d = g[j] * w[j];
             part[0] += d;
             part[1] = c + j < P.width ? fmaf(d, (u[j] - mean) * rstd, part[1]) : part[1];
         }
-        s += part;
+        s[0] += part[0];
+        s[1] += part[1];
     }
-    s = row_sums<T>(s, sums) * (1.f / (float)P.width);
-    if (threadIdx.x == 0) P.means[r] = s;
+    row_sums<T>(s, sums);
+    const float inverse = 1.f / (float)P.width;
+    if (threadIdx.x == 0) P.means[r] = (f32x2){s[0] * inverse, s[1] * inverse};
 }
 // ... then, a slice of the columns at a time, the rest.
 template <class E, int T, bool KEPT>
@@ -370,11 +467,10 @@ __global__ __launch_bounds__(T) void norm_grad_long_kernel(NormGrad P, int slice
     const int worker = (int)(which_strip / P.strips), strip = (int)(which_strip % P.strips);
     const int c = ((int)(group % slices) * T + threadIdx.x) * N;
     if (c >= P.width) return;
-    const int first = strip * P.strip_rows, end = min(first + P.strip_rows, P.per_worker);
     float w[N], dw[N], db[N];
     for (int j = 0; j < N; ++j) w[j] = 1.f, dw[j] = db[j] = 0.f;
     if (P.weight_at >= 0) load_floats<N, true>(P.params + worker * P.ld_params + P.weight_at, c, P.width, w);
-    for (int at = first; at < end; ++at) {
+    for (int64_t at = strip; at < P.per_worker; at += P.strips) {
         const int64_t r = (int64_t)worker * P.per_worker + at;
         float g[N], u[N];
         for (int j = 0; j < N; ++j) g[j] = 0.f;
@@ -397,26 +493,37 @@ __global__ __launch_bounds__(T) void norm_grad_long_kernel(NormGrad P, int slice
         if (to) store_floats<N>(to, c, P.width, which ? db : dw);
     }
 }
-// The strips' shares, added in the strips' order: 32 columns a workgroup, its 8 rows of threads every eighth strip.
-constexpr int SUM_COLUMNS = 32, SUM_ROWS = 8;
-__global__ __launch_bounds__(SUM_COLUMNS * SUM_ROWS) void norm_sum_kernel(NormGrad P, int slices)
+// The strips' shares: 64 columns a workgroup, four a thread, its 16 rows of threads every sixteenth strip, eight loads on their way at a time.  One worker
+// of 4096 x 2048 in 512 strips with 32 columns a workgroup, 8 rows of threads and one load after the other: 25 us.
+constexpr int SUM_COLUMNS = 64, SUM_ROWS = 16;
+__global__ __launch_bounds__(SUM_COLUMNS / 4 * SUM_ROWS) void norm_sum_kernel(NormGrad P, int slices)
 {
-    __shared__ float lds[SUM_ROWS][SUM_COLUMNS];
+    __shared__ f32x4 lds[SUM_ROWS][SUM_COLUMNS / 4];
     const int64_t group = group_number();
     const int which = (int)(group % 2);
     const int slice = (int)(group / 2 % slices);
     const int64_t worker = group / 2 / slices;
     const int64_t at = which ? P.bias_at : P.weight_at;
     if (worker >= P.workers || at < 0) return;
-    const int q = threadIdx.x / SUM_COLUMNS, c = slice * SUM_COLUMNS + threadIdx.x % SUM_COLUMNS;
-    float v = 0.f;
-    if (c < P.width)
-        for (int s = q; s < P.strips; s += SUM_ROWS) v += P.parts[((worker * P.strips + s) * 2 + which) * P.part_ld + c];
-    lds[q][threadIdx.x % SUM_COLUMNS] = v;
+    const int q = threadIdx.x / (SUM_COLUMNS / 4), k = threadIdx.x % (SUM_COLUMNS / 4), c = slice * SUM_COLUMNS + 4 * k;
+    f32x4 v = (f32x4)0.f;
+    if (c < P.width) {
+        const float *const part = P.parts + (worker * P.strips * 2 + which) * P.part_ld + c;
+        const int64_t stride = 2 * P.part_ld;
+        for (int s = q; s < P.strips; s += 8 * SUM_ROWS) {
+            f32x4 w[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = s + i * SUM_ROWS < P.strips ? *(const f32x4 *)(part + (s + i * SUM_ROWS) * stride) : (f32x4)0.f;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v += w[i];
+        }
+    }
+    lds[q][k] = v;
     __syncthreads();
     if (q == 0 && c < P.width) {
-        for (int s = 1; s < SUM_ROWS; ++s) v += lds[s][threadIdx.x];
-        P.grads[worker * P.ld_grads + at + c] = v;
+        for (int s = 1; s < SUM_ROWS; ++s) v += lds[s][k];
+        float to[4] = {v[0], v[1], v[2], v[3]};
+        store_floats<4>(P.grads + worker * P.ld_grads + at, c, P.width, to);
     }
 }
 // Workers without rows.

@@ -14,6 +14,7 @@ using loss::report;
 
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 
 // Rows of T threads each in a workgroup.
 template <int T>
@@ -31,15 +32,16 @@ __device__ __forceinline__ int slot_of()
     const int slot = threadIdx.x / T;
     return T < 64 ? slot : __builtin_amdgcn_readfirstlane(slot);
 }
-// A worker's rows in strips, a workgroup each, walked over several rows at a time.
+// A worker's rows among `strips` workgroups, which take `step` rows each in turn, so that those that run at a time read and write rows that lie together:
+// 8 x 8192 x 2048 bf16 forwards 96.5 us, with a contiguous strip for each 107.
 struct Strip {
-    int worker, number, first, end;                       // rows of the worker
+    int worker, number;
+    int64_t first, stride, end;                           // rows of the worker
 };
-__device__ __forceinline__ Strip strip_of(uint32_t group, uint32_t strips, int strip_rows, int per_worker)
+__device__ __forceinline__ Strip strip_of(uint32_t group, uint32_t strips, int step, int per_worker)
 {
     const int worker = (int)(group / strips), number = (int)(group % strips);
-    const int64_t first = (int64_t)number * strip_rows, end = first + strip_rows;
-    return Strip{worker, number, (int)min(first, (int64_t)per_worker), (int)min(end, (int64_t)per_worker)};
+    return Strip{worker, number, (int64_t)number * step, (int64_t)strips * step, per_worker};
 }
 
 template <class E>

@@ -2,6 +2,8 @@
 // allocation: what the kernels need beyond inputs and outputs is the caller's scratch memory.
 #include <math.h>
 
+#include <type_traits>
+
 #include "dbw_internal.h"
 #include "dbw_layers.h"
 #include "layer_experts.h"
@@ -62,46 +64,53 @@ bool outside(int64_t at, int64_t count, int64_t ld) { return at >= 0 && (count >
 layer::Kept kept_of(const void *checkpoint, const Shape &S, const dbw_rows *l) { return layer::kept_of((void *)checkpoint, S.rows, l->width); }
 int64_t checkpoint_bytes(int64_t rows, int64_t width) { return rows * (layer::padded(width) + layer::padded(width) / layer::BLOCK); }
 
-// Which kernel takes a row of a norm: T threads, C pieces each, ROWS rows of a workgroup at a time.
-template <int T_, int C_, int ROWS_>
+// Which kernel takes a row of a norm: T threads, C pieces each, SLOTS such groups of threads in a workgroup, R rows of a group at a time.  A wave a row as long
+// as its registers hold it: no barriers.  Microseconds, workers x rows x width, bf16 unless said otherwise: forwards 8 x 2048 x 2048 by a wave 23.5, by 256
+// threads, four rows between two barriers, 24.8; 4 x 2048 x 4096 by 256 threads 23.3, by 128 28.5, by 512 28.0; backwards from 8 bits
+// 8 x 2048 x 4096 by 128 threads, two rows at a time, 75.8, by 256 one row at a time 78.7, by 512 79.9.  16 x 64 x 16 fp32 by 16 threads a row, four rows
+// each, 7.9, one each 11.4.
+template <int T_, int C_, int SLOTS_, int R_>
 struct Plan {
-    static constexpr int T = T_, C = C_, ROWS = ROWS_;
+    static constexpr int T = T_, C = C_, SLOTS = SLOTS_, R = R_;
 };
-template <class F>
+template <bool BACK, class F>
 bool by_row(int64_t bytes, F f)
 {
-    if (bytes <= 16 * 16) f(Plan<16, 1, 16>());
-    else if (bytes <= 64 * 16) f(Plan<64, 1, 4>());
-    else if (bytes <= 2 * 64 * 16) f(Plan<64, 2, 4>());
-    else if (bytes <= 4 * 64 * 16) f(Plan<64, 4, 4>());
-    else if (bytes <= 2 * 256 * 16) f(Plan<256, 2, 1>());
-    else if (bytes <= 2 * 512 * 16) f(Plan<512, 2, 1>());
-    else if (bytes <= 2 * 1024 * 16) f(Plan<1024, 2, 1>());
+    if (bytes <= 16 * 16) f(Plan<16, 1, 16, 4>());
+    else if (bytes <= 64 * 16) f(Plan<64, 1, 4, 1>());
+    else if (bytes <= 2 * 64 * 16) f(Plan<64, 2, 4, 1>());
+    else if (bytes <= 4 * 64 * 16) f(Plan<64, 4, 4, 1>());
+    else if (bytes <= 2 * 256 * 16) f(std::conditional_t<BACK, Plan<128, 4, 2, 1>, Plan<256, 2, 1, 1>>());
+    else if (bytes <= 2 * 512 * 16) f(Plan<512, 2, 1, 1>());
+    else if (bytes <= 2 * 1024 * 16) f(Plan<1024, 2, 1, 1>());
     else return false;
     return true;
 }
 constexpr int LONG_THREADS = 1024, LONG_GRAD_THREADS = 256;
 
-// A worker's rows in strips of whole turns: as many rows as leave `groups` workgroups for all workers, at least `turns` turns.
-struct Strips {
-    int count, rows;                                      // of a worker, and of a strip
-};
-Strips strips_of(const dbw_rows *l, int rows_at_once, int64_t groups, int turns)
+// Workgroups of a worker, which take rows_at_once rows each in turn: `groups` for all workers, if there are so many rows for at least `turns` turns.
+int strips_of(const dbw_rows *l, int rows_at_once, int64_t groups, int turns)
 {
-    const int64_t most = (groups + l->workers - 1) / l->workers, least = (int64_t)turns * rows_at_once;
-    int64_t rows = (l->rows + most - 1) / most;
-    if (rows < least) rows = least;
-    rows = (rows + rows_at_once - 1) / rows_at_once * rows_at_once;
-    return Strips{l->rows > rows ? (int)((l->rows + rows - 1) / rows) : 1, (int)(rows < INT32_MAX ? rows : INT32_MAX)};
+    const int64_t most = (groups + l->workers - 1) / l->workers, each = (int64_t)turns * rows_at_once;
+    const int64_t count = (l->rows + each - 1) / each;
+    return (int)(count < 1 ? 1 : count < most ? count : most);
 }
+template <bool BACK>
 int rows_at_once(const dbw_rows *l, const Shape &S)
 {
     int n = 1;
-    by_row(S.e * l->width, [&](auto p) { n = p.ROWS; });
+    by_row<BACK>(S.e * l->width, [&](auto p) { n = p.SLOTS * p.R; });
     return n;
 }
-constexpr int NORM_GROUPS = 2048, GRAD_GROUPS = 512;      // workgroups of a strip each
-Strips grad_strips_of(const dbw_rows *l, const Shape &S) { return strips_of(l, rows_at_once(l, S), GRAD_GROUPS, 4); }
+// Forwards, 8 x 2048 x 2048: 1024 workgroups 23.1, 4096 32.  Backwards every workgroup has 8 bytes a column to add up in the end: 512 of them, or as
+// many as have 64 rows each, up to 1024.  From 8 bits 8 x 2048 x 2048 with 512 and 1024 37.8 and 42.8, 8 x 8192 x 2048 145 and 133, 4 x 2048 x 4096
+// 42.0 and 54.2.
+constexpr int NORM_GROUPS = 2048, GRAD_GROUPS = 512;
+int grad_strips_of(const dbw_rows *l, const Shape &S)
+{
+    const int64_t groups = S.rows / 64;
+    return strips_of(l, rows_at_once<true>(l, S), groups < GRAD_GROUPS ? GRAD_GROUPS : groups < 2 * GRAD_GROUPS ? groups : 2 * GRAD_GROUPS, 2);
+}
 dim3 store_grid(int64_t pieces)
 {
     constexpr int each = layer::STORE_THREADS * layer::STORE_PIECES;
@@ -168,15 +177,14 @@ extern "C" int dbw_layer_norm(const dbw_rows *shape, const void *x, const uint8_
     if ((weight_at >= 0 || bias_at >= 0) && too_long(ld_params, shape->workers)) return DBW_ERR_UNSUPPORTED;
     if (!(x == y && S.ld == S.ld_out) && overlap(x, S.rows, S.ld, y, S.rows, S.ld_out, shape->width, S.e)) return DBW_ERR_ALIAS;
     if (S.rows == 0) return DBW_OK;
-    const Strips strips = strips_of(shape, rows_at_once(shape, S), NORM_GROUPS, 1);
-    layer::Norm P{x, mask, params, S.ld, S.ld_out, ld_params, weight_at, bias_at, S.rows, shape->rows, shape->width, shape->workers, strips.count,
-                  strips.rows, eps, y, stats_out, kept_of(checkpoint, S, shape)};
+    const int strips = strips_of(shape, rows_at_once<false>(shape, S), NORM_GROUPS, 1);
+    layer::Norm P{x, mask, params, S.ld, S.ld_out, ld_params, weight_at, bias_at, S.rows, shape->rows, shape->width, shape->workers, strips, eps, y, stats_out, kept_of(checkpoint, S, shape)};
     if (!checkpoint) P.kept.codes = nullptr;
     hipStream_t s = (hipStream_t)stream;
     by_type(shape->type, [&](auto e) {
         typedef decltype(e) E;
-        if (!by_row(S.e * shape->width, [&](auto p) {
-                hipLaunchKernelGGL((layer::norm_kernel<E, p.T, p.C, p.ROWS>), grid_of((int64_t)shape->workers * strips.count), dim3(p.T * p.ROWS), 0, s, P);
+        if (!by_row<false>(S.e * shape->width, [&](auto p) {
+                hipLaunchKernelGGL((layer::norm_kernel<E, p.T, p.C, p.SLOTS, p.R>), grid_of((int64_t)shape->workers * strips), dim3(p.T * p.SLOTS), 0, s, P);
             }))
             hipLaunchKernelGGL((layer::norm_long_kernel<E, LONG_THREADS>), grid_of(S.rows), dim3(LONG_THREADS), 0, s, P);
     });
@@ -189,9 +197,9 @@ extern "C" int64_t dbw_layer_norm_work_bytes(const dbw_rows *shape)
     Shape S;
     const int rc = check_shape(shape, &S);
     if (rc != DBW_OK) return rc;
-    const Strips strips = grad_strips_of(shape, S);
-    int64_t bytes = strips.count > 1 ? (int64_t)shape->workers * strips.count * 2 * part_ld(shape) * 4 : 0;
-    if (!by_row(S.e * shape->width, [](auto) {})) bytes += 8 * S.rows;
+    const int strips = grad_strips_of(shape, S);
+    int64_t bytes = strips > 1 ? (int64_t)shape->workers * strips * 2 * part_ld(shape) * 4 : 0;
+    if (!by_row<true>(S.e * shape->width, [](auto) {})) bytes += 8 * S.rows;
     return bytes + 16;
 }
 
@@ -212,9 +220,9 @@ extern "C" int dbw_layer_norm_grad(const dbw_rows *shape, const void *dy, const 
     if (dx != x && overlap(x, S.rows, S.ld, dx, S.rows, S.ld, shape->width, S.e)) return DBW_ERR_ALIAS;
     if (!(dx == dy && S.ld == S.ld_out) && overlap(dy, S.rows, S.ld_out, dx, S.rows, S.ld, shape->width, S.e)) return DBW_ERR_ALIAS;
     if (weight_at < 0 && bias_at < 0) grads = nullptr;
-    const Strips strips = grad_strips_of(shape, S);
+    const int strips = grad_strips_of(shape, S);
     layer::NormGrad P{dy, x, kept_of(checkpoint, S, shape), mask, stats, params, S.ld, S.ld_out, ld_params, ld_grads, weight_at, bias_at, S.rows,
-                      shape->rows, shape->width, shape->workers, strips.count, strips.rows, dx, grads, nullptr, part_ld(shape), nullptr};
+                      shape->rows, shape->width, shape->workers, strips, dx, grads, nullptr, part_ld(shape), nullptr};
     hipStream_t s = (hipStream_t)stream;
     if (S.rows == 0) {
         const int slices = (shape->width + 255) / 256;
@@ -222,17 +230,17 @@ extern "C" int dbw_layer_norm_grad(const dbw_rows *shape, const void *dy, const 
         DBW_HIP(hipGetLastError());
         return DBW_OK;
     }
-    const int64_t groups = (int64_t)shape->workers * strips.count;
-    if (strips.count > 1) P.parts = (float *)work;
-    P.means = (layer::f32x2 *)((float *)work + (strips.count > 1 ? groups * 2 * P.part_ld : 0));
+    const int64_t groups = (int64_t)shape->workers * strips;
+    if (strips > 1) P.parts = (float *)work;
+    P.means = (layer::f32x2 *)((float *)work + (strips > 1 ? groups * 2 * P.part_ld : 0));
     by_type(shape->type, [&](auto e) {
         typedef decltype(e) E;
         const auto rows = [&](auto p) {
-            const size_t lds = (size_t)(p.ROWS - 1) * p.T * p.C * layer::Piece<E>::N * 4;
-            if (x) hipLaunchKernelGGL((layer::norm_grad_kernel<E, p.T, p.C, p.ROWS, false>), grid_of(groups), dim3(p.T * p.ROWS), lds, s, P);
-            else hipLaunchKernelGGL((layer::norm_grad_kernel<E, p.T, p.C, p.ROWS, true>), grid_of(groups), dim3(p.T * p.ROWS), lds, s, P);
+            const size_t lds = (size_t)(p.SLOTS > 1 ? p.SLOTS : 0) * p.T * p.C * layer::Piece<E>::N * 4;
+            if (x) hipLaunchKernelGGL((layer::norm_grad_kernel<E, p.T, p.C, p.SLOTS, p.R, false>), grid_of(groups), dim3(p.T * p.SLOTS), lds, s, P);
+            else hipLaunchKernelGGL((layer::norm_grad_kernel<E, p.T, p.C, p.SLOTS, p.R, true>), grid_of(groups), dim3(p.T * p.SLOTS), lds, s, P);
         };
-        if (!by_row(S.e * shape->width, rows)) {
+        if (!by_row<true>(S.e * shape->width, rows)) {
             constexpr int T = LONG_GRAD_THREADS, COLUMNS = T * layer::Piece<E>::N;
             const int slices = (shape->width + COLUMNS - 1) / COLUMNS;
             if (x) {
@@ -244,9 +252,9 @@ extern "C" int dbw_layer_norm_grad(const dbw_rows *shape, const void *dy, const 
             }
         }
     });
-    if (grads && strips.count > 1) {
+    if (grads && strips > 1) {
         const int slices = (shape->width + layer::SUM_COLUMNS - 1) / layer::SUM_COLUMNS;
-        hipLaunchKernelGGL(layer::norm_sum_kernel, grid_of((int64_t)shape->workers * slices * 2), dim3(layer::SUM_COLUMNS * layer::SUM_ROWS), 0, s, P, slices);
+        hipLaunchKernelGGL(layer::norm_sum_kernel, grid_of((int64_t)shape->workers * slices * 2), dim3(layer::SUM_COLUMNS / 4 * layer::SUM_ROWS), 0, s, P, slices);
     }
     DBW_HIP(hipGetLastError());
     return DBW_OK;
