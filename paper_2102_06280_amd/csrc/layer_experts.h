@@ -141,82 +141,165 @@ struct Move {
     int64_t slots;                                        // of a worker
     int per_worker, width, k;
 };
-// The sorted row of a token's slot, or -1.
-__device__ __forceinline__ int64_t place_of(const Move &P, int64_t slot, int64_t first)
+
+// A wave has a token, or some of its columns, C pieces a lane at a time.  Of up to 64 slots of the token each lane has one: its sorted row, or -1, and its
+// weight, which go to the whole wave when they are used.
+constexpr int MOVE_WAVES = 4, MOVE_THREADS = 64 * MOVE_WAVES;
+struct Token {
+    int64_t row;
+    int chunk;                                            // of its columns
+};
+__device__ __forceinline__ Token token_of(uint32_t chunks)
 {
-    const int32_t p = P.place[slot];
-    if (p < 0) return -1;
-    if (p >= first && p < first + P.slots) return p;
-    report(P.status);
-    return -1;
+    const int64_t wave = group_number() * MOVE_WAVES + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (chunks == 1) return Token{wave, 0};
+    return Token{wave / chunks, (int)(wave % chunks)};
+}
+struct Slots {
+    int place;
+    float weight;
+    __device__ __forceinline__ Slots(const Move &P, int64_t row, int first_slot)
+    {
+        const int j = first_slot + (threadIdx.x & 63);
+        const int64_t slot = row * P.k + j, first = (uint32_t)row / (uint32_t)P.per_worker * P.slots;
+        place = -1;
+        weight = 0.f;
+        if (j >= P.k) return;
+        const int32_t p = ((const __attribute__((address_space(1))) int32_t *)(uint64_t)P.place)[slot];
+        weight = P.weights ? ((const __attribute__((address_space(1))) float *)(uint64_t)P.weights)[slot] : 1.f;
+        if (p >= first && p < first + P.slots) place = p;
+        else if (p >= 0) report(P.status);
+    }
+    __device__ __forceinline__ int place_of(int j) const { return __builtin_amdgcn_readlane(place, j); }
+    __device__ __forceinline__ float weight_of(int j) const { return __int_as_float(__builtin_amdgcn_readlane(__float_as_int(weight), j)); }
+};
+
+template <class E, int C>
+__global__ __launch_bounds__(MOVE_THREADS) void gather_kernel(Move P, int chunks)
+{
+    constexpr int N = Piece<E>::N;
+    const Token token = token_of(chunks);
+    if (token.row >= P.rows) return;
+    const int c0 = (token.chunk * C * 64 + (threadIdx.x & 63)) * N;
+    u32x4 w[C];
+#pragma unroll
+    for (int i = 0; i < C; ++i) w[i] = load_raw<E, false>((const E *)P.tokens + token.row * P.ld, c0 + i * 64 * N, P.width);
+    for (int j0 = 0; j0 < P.k; j0 += 64) {
+        const Slots slots(P, token.row, j0);
+        if (j0 == 0)
+#pragma unroll
+            for (int i = 0; i < C; ++i) w[i] = settled<E, false>(w[i], c0 + i * 64 * N, P.width);
+        const int count = min(64, P.k - j0);
+        for (int j = 0; j < count; ++j) {
+            const int p = slots.place_of(j);
+            if (p < 0) continue;
+            E *const to = (E *)P.sorted_out + p * P.ld_sorted;
+#pragma unroll
+            for (int i = 0; i < C; ++i) store_piece<E>(to, c0 + i * 64 * N, P.width, w[i]);
+        }
+    }
 }
 
-constexpr int MOVE_THREADS = 256;
-// A wave has a token.
-template <class E>
-__global__ __launch_bounds__(MOVE_THREADS) void gather_kernel(Move P)
+constexpr int TOGETHER = 4;                               // slots whose rows are asked for before the first is used
+template <class E, int C>
+__global__ __launch_bounds__(MOVE_THREADS) void combine_kernel(Move P, int chunks)
 {
     constexpr int N = Piece<E>::N;
-    const int64_t r = group_number() * (MOVE_THREADS / 64) + (threadIdx.x >> 6);
-    if (r >= P.rows) return;
-    const int64_t first = r / P.per_worker * P.slots;
-    for (int c = (threadIdx.x & 63) * N; c < P.width; c += 64 * N) {
-        const u32x4 w = load_piece<E>((const E *)P.tokens + r * P.ld, c, P.width);
-        for (int j = 0; j < P.k; ++j) {
-            const int64_t p = place_of(P, r * P.k + j, first);
-            if (p >= 0) store_piece<E>((E *)P.sorted_out + p * P.ld_sorted, c, P.width, w);
-        }
-    }
-}
-template <class E>
-__global__ __launch_bounds__(MOVE_THREADS) void combine_kernel(Move P)
-{
-    constexpr int N = Piece<E>::N;
-    const int64_t r = group_number() * (MOVE_THREADS / 64) + (threadIdx.x >> 6);
-    if (r >= P.rows) return;
-    const int64_t first = r / P.per_worker * P.slots;
-    for (int c = (threadIdx.x & 63) * N; c < P.width; c += 64 * N) {
-        float v[N], z[N];
-        for (int i = 0; i < N; ++i) v[i] = 0.f;
-        for (int j = 0; j < P.k; ++j) {
-            const int64_t p = place_of(P, r * P.k + j, first);
-            if (p < 0) continue;
-            const float w = P.weights ? P.weights[r * P.k + j] : 1.f;
-            Piece<E>::unpack(load_piece<E>((const E *)P.sorted_in + p * P.ld_sorted, c, P.width), z);
-            for (int i = 0; i < N; ++i) v[i] = fmaf(w, z[i], v[i]);
-        }
-        store_piece<E>((E *)P.out + r * P.ld, c, P.width, Piece<E>::pack(v));
-    }
-}
-template <class E>
-__global__ __launch_bounds__(MOVE_THREADS) void combine_grad_kernel(Move P)
-{
-    constexpr int N = Piece<E>::N;
-    const int64_t r = group_number() * (MOVE_THREADS / 64) + (threadIdx.x >> 6);
-    if (r >= P.rows) return;
-    const int64_t first = r / P.per_worker * P.slots;
-    for (int j = 0; j < P.k; ++j) {
-        const int64_t slot = r * P.k + j, p = place_of(P, slot, first);
-        float dot = 0.f;
-        if (p >= 0) {
-            const float w = P.weights ? P.weights[slot] : 1.f;
-            for (int c = (threadIdx.x & 63) * N; c < P.width; c += 64 * N) {
-                float d[N], z[N];
-                Piece<E>::unpack(load_piece<E>((const E *)P.tokens + r * P.ld, c, P.width), d);
-                if (P.dweights) {
-                    Piece<E>::unpack(load_piece<E>((const E *)P.sorted_in + p * P.ld_sorted, c, P.width), z);
-                    float part = 0.f;
-                    for (int i = 0; i < N; ++i) part = fmaf(d[i], z[i], part);
-                    dot += part;
+    const Token token = token_of(chunks);
+    if (token.row >= P.rows) return;
+    const int c0 = (token.chunk * C * 64 + (threadIdx.x & 63)) * N;
+    float v[C][N] = {};
+    for (int j0 = 0; j0 < P.k; j0 += 64) {
+        const Slots slots(P, token.row, j0);
+        const int count = min(64, P.k - j0);
+        for (int j = 0; j < count; j += TOGETHER) {
+            u32x4 z[TOGETHER][C];
+#pragma unroll
+            for (int q = 0; q < TOGETHER; ++q) {
+                const int p = j + q < count ? slots.place_of(j + q) : -1;
+#pragma unroll
+                for (int i = 0; i < C; ++i) z[q][i] = (u32x4)0u;
+                if (p >= 0)
+#pragma unroll
+                    for (int i = 0; i < C; ++i) z[q][i] = load_raw<E, false>((const E *)P.sorted_in + p * P.ld_sorted, c0 + i * 64 * N, P.width);
+            }
+#pragma unroll
+            for (int q = 0; q < TOGETHER; ++q) {
+                if (j + q >= count || slots.place_of(j + q) < 0) continue;
+                const float by = slots.weight_of(j + q);
+#pragma unroll
+                for (int i = 0; i < C; ++i) {
+                    float x[N];
+                    Piece<E>::unpack(settled<E, false>(z[q][i], c0 + i * 64 * N, P.width), x);
+#pragma unroll
+                    for (int n = 0; n < N; ++n) v[i][n] = fmaf(by, x[n], v[i][n]);
                 }
-                for (int i = 0; i < N; ++i) d[i] *= w;
-                store_piece<E>((E *)P.sorted_out + p * P.ld_sorted, c, P.width, Piece<E>::pack(d));
             }
         }
-        if (P.dweights) {
-            dot = loss::lanes_sum<64>(dot);
-            if ((threadIdx.x & 63) == 0) P.dweights[slot] = dot;
+    }
+#pragma unroll
+    for (int i = 0; i < C; ++i) store_piece<E>((E *)P.out + token.row * P.ld, c0 + i * 64 * N, P.width, Piece<E>::pack(v[i]));
+}
+
+// Here a wave has the whole token, as many columns at a time as its lanes hold; what it has of a few slots' products is summed over the lanes in the end.
+template <class E, int C>
+__global__ __launch_bounds__(MOVE_THREADS) void combine_grad_kernel(Move P)
+{
+    constexpr int N = Piece<E>::N, Q = 2;                 // slots at a time
+    const Token token = token_of(1);
+    if (token.row >= P.rows) return;
+    const E *const dy = (const E *)P.tokens + token.row * P.ld;
+    for (int j0 = 0; j0 < P.k; j0 += 64) {
+        const Slots slots(P, token.row, j0);
+        const int count = min(64, P.k - j0);
+        float mine = 0.f;                                 // of the slot that is the lane's
+        for (int j = 0; j < count; j += Q) {
+            int p[Q];
+            float dot[Q] = {};
+            for (int q = 0; q < Q; ++q) p[q] = j + q < count ? slots.place_of(j + q) : -1;
+            for (int c0 = (threadIdx.x & 63) * N; c0 < P.width; c0 += C * 64 * N) {
+                u32x4 d[C], z[Q][C];
+#pragma unroll
+                for (int i = 0; i < C; ++i) d[i] = load_raw<E, false>(dy, c0 + i * 64 * N, P.width);
+                if (P.dweights)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q)
+                        if (p[q] >= 0)
+#pragma unroll
+                            for (int i = 0; i < C; ++i)
+                                z[q][i] = load_raw<E, false>((const E *)P.sorted_in + p[q] * P.ld_sorted, c0 + i * 64 * N, P.width);
+                float g[C][N];
+#pragma unroll
+                for (int i = 0; i < C; ++i) Piece<E>::unpack(settled<E, false>(d[i], c0 + i * 64 * N, P.width), g[i]);
+#pragma unroll
+                for (int q = 0; q < Q; ++q) {
+                    if (p[q] < 0) continue;
+                    const float by = slots.weight_of(j + q);
+                    float part = 0.f;
+#pragma unroll
+                    for (int i = 0; i < C; ++i) {
+                        const int c = c0 + i * 64 * N;
+                        float x[N];
+                        if (P.dweights) {
+                            Piece<E>::unpack(settled<E, false>(z[q][i], c, P.width), x);
+#pragma unroll
+                            for (int n = 0; n < N; ++n) part = fmaf(g[i][n], x[n], part);
+                        }
+#pragma unroll
+                        for (int n = 0; n < N; ++n) x[n] = by * g[i][n];
+                        store_piece<E>((E *)P.sorted_out + p[q] * P.ld_sorted, c, P.width, Piece<E>::pack(x));
+                    }
+                    dot[q] += part;
+                }
+            }
+            if (P.dweights)
+                for (int q = 0; q < Q; ++q) {
+                    const float sum = loss::lanes_sum<64>(dot[q]);
+                    if ((int)(threadIdx.x & 63) == j + q) mine = sum;
+                }
         }
+        const int j = threadIdx.x & 63;
+        if (P.dweights && j < count) ((__attribute__((address_space(1))) float *)(uint64_t)P.dweights)[token.row * P.k + j0 + j] = mine;
     }
 }
 

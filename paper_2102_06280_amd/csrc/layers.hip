@@ -264,7 +264,7 @@ extern "C" int dbw_layer_norm_grad(const dbw_rows *shape, const void *dy, const 
 
 namespace {
 
-constexpr int SORT_CHUNK = 4096;                          // slots of a workgroup
+constexpr int SORT_CHUNK = 1024;                          // slots of a workgroup
 int chunks_of(const dbw_routing *l) { return (int)(((int64_t)l->tokens * l->k + SORT_CHUNK - 1) / SORT_CHUNK); }
 
 int check_routing(const dbw_routing *l)
@@ -294,7 +294,17 @@ int check_move(const dbw_routing *routing, const dbw_rows *shape, const void *to
                      routing->k};
     return DBW_OK;
 }
-dim3 move_grid(int64_t rows) { return grid_of((rows + layer::MOVE_THREADS / 64 - 1) / (layer::MOVE_THREADS / 64)); }
+dim3 move_grid(int64_t waves) { return grid_of((waves + layer::MOVE_WAVES - 1) / layer::MOVE_WAVES); }
+// Pieces of a lane: rows in chunks of 64 C pieces, a wave each, four pieces a lane where that leaves waves enough.
+constexpr int64_t MOVE_ENOUGH = 4096;
+template <class F>
+void by_chunk(int64_t rows, int64_t row_bytes, F f)
+{
+    const auto chunks = [&](int c) { return (int)((row_bytes + 1024 * c - 1) / (1024 * c)); };
+    if (row_bytes > 2048 && rows * chunks(4) >= MOVE_ENOUGH) f(std::integral_constant<int, 4>(), chunks(4));
+    else if (row_bytes > 1024 && rows * chunks(2) >= MOVE_ENOUGH) f(std::integral_constant<int, 2>(), chunks(2));
+    else f(std::integral_constant<int, 1>(), chunks(1));
+}
 
 }  // namespace
 
@@ -336,7 +346,10 @@ extern "C" int dbw_expert_gather(const dbw_routing *routing, const dbw_rows *sha
     P.tokens = x;
     P.sorted_out = sorted;
     by_type(shape->type, [&](auto e) {
-        hipLaunchKernelGGL(layer::gather_kernel<decltype(e)>, move_grid(S.rows), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P);
+        by_chunk(S.rows, S.e * shape->width, [&](auto c, int chunks) {
+            hipLaunchKernelGGL((layer::gather_kernel<decltype(e), c.value>), move_grid(S.rows * chunks), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P,
+                               chunks);
+        });
     });
     DBW_HIP(hipGetLastError());
     return DBW_OK;
@@ -353,7 +366,10 @@ extern "C" int dbw_expert_combine(const dbw_routing *routing, const dbw_rows *sh
     P.sorted_in = sorted;
     P.out = y;
     by_type(shape->type, [&](auto e) {
-        hipLaunchKernelGGL(layer::combine_kernel<decltype(e)>, move_grid(S.rows), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P);
+        by_chunk(S.rows, S.e * shape->width, [&](auto c, int chunks) {
+            hipLaunchKernelGGL((layer::combine_kernel<decltype(e), c.value>), move_grid(S.rows * chunks), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P,
+                               chunks);
+        });
     });
     DBW_HIP(hipGetLastError());
     return DBW_OK;
@@ -376,7 +392,11 @@ extern "C" int dbw_expert_combine_grad(const dbw_routing *routing, const dbw_row
     P.sorted_out = dsorted;
     P.dweights = dweights;
     by_type(shape->type, [&](auto e) {
-        hipLaunchKernelGGL(layer::combine_grad_kernel<decltype(e)>, move_grid(S.rows), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P);
+        typedef decltype(e) E;
+        const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, move_grid(S.rows), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P); };
+        if (S.e * shape->width > 2048) launch(layer::combine_grad_kernel<E, 4>);
+        else if (S.e * shape->width > 1024) launch(layer::combine_grad_kernel<E, 2>);
+        else launch(layer::combine_grad_kernel<E, 1>);
     });
     DBW_HIP(hipGetLastError());
     return DBW_OK;
