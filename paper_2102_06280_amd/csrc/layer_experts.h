@@ -200,7 +200,7 @@ __global__ __launch_bounds__(MOVE_THREADS) void gather_kernel(Move P, int chunks
     }
 }
 
-constexpr int TOGETHER = 4;                               // slots whose rows are asked for before the first is used
+constexpr int TOGETHER = 2;                               // slots whose rows are asked for before the first is used
 template <class E, int C>
 __global__ __launch_bounds__(MOVE_THREADS) void combine_kernel(Move P, int chunks)
 {

@@ -548,8 +548,8 @@ struct Store {
     Kept kept;
 };
 // A workgroup has STORE_PIECES x STORE_THREADS pieces that follow one another, a thread every STORE_THREADS-th; a row is a multiple of the pieces of a
-// block.
-constexpr int STORE_THREADS = 256, STORE_PIECES = 4;
+// block.  4 x 4096 x 4096 bf16 stored and loaded with one, two and four pieces a thread 73, 67.6 and 71 us.
+constexpr int STORE_THREADS = 256, STORE_PIECES = 2;
 struct Spot {
     int64_t r;
     int c;

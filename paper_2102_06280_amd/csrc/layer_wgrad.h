@@ -4,6 +4,8 @@
 // matrix instruction is exact, and fp32 sums are all that rounds.
 #pragma once
 
+#include <type_traits>
+
 #include "global_access.h"
 #include "layer_rows.h"
 
@@ -112,16 +114,21 @@ __device__ __forceinline__ int lds_offset(int row, int column)     // column: a 
 {
     return row * (COLUMNS * 2) + unit_place<COLUMNS>(row, column >> 4) * 32 + (column & 15) * 2;
 }
-// An operand of v_mfma_f32_32x32x16_bf16 from rows row ... row + 15: a lane has column l % 32, and of its eight numbers the first four are those of rows 4 (l / 32)
-// and on, the others of rows 8 + 4 (l / 32) and on.  (Both operands take the rows in this order.)
+// An operand of v_mfma_f32_32x32x16_bf16 from 16 rows: a lane has column l % 32, and of its eight numbers the first four are those of rows 4 (l / 32)
+// and on, the others of rows 8 + 4 (l / 32) and on.  (Both operands take the rows in this order.)  Where in a tile a lane reads for the columns from
+// `column` on, of rows 0 to 15; other sixteens lie 16 rows further.
 template <int COLUMNS>
-__device__ __forceinline__ bf16x8 operand(lds_bytes tile, int row, int column)
+__device__ __forceinline__ int operand_place(int column)
 {
     const int l = threadIdx.x & 63, i = l & 15;
-    const int r = row + 4 * (l >> 5) + (i >> 2), c = column + 16 * ((l >> 4) & 1) + 4 * (i & 3);
+    return lds_offset<COLUMNS>(4 * (l >> 5) + (i >> 2), column + 16 * ((l >> 4) & 1) + 4 * (i & 3));
+}
+template <int COLUMNS>
+__device__ __forceinline__ bf16x8 operand(lds_bytes at)
+{
     typedef __attribute__((address_space(3))) s16x4 *place;
-    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(tile + lds_offset<COLUMNS>(r, c)));
-    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(tile + lds_offset<COLUMNS>(r + 8, c)));
+    const s16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)at);
+    const s16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((place)(at + 8 * COLUMNS * 2));
     return __builtin_bit_cast(bf16x8, __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7));
 }
 
@@ -131,8 +138,9 @@ struct Tile {
     static constexpr int OUT = OUT_, IN = IN_, WO = WO_, WI = WI_, STEP = STEP_;
     static constexpr int THREADS = 64 * WO * WI;
 };
+constexpr int BUFFERS = 3;
 template <class E, class T>
-constexpr int tile_lds() { return 2 * T::STEP * 2 * (Planes<E>::COUNT * T::OUT + T::IN) + 2 * T::STEP * 4; }
+constexpr int tile_lds() { return BUFFERS * T::STEP * 2 * (Planes<E>::COUNT * T::OUT + T::IN) + 2 * T::STEP * 4; }
 
 template <class E, class T, bool SOURCED>
 __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
@@ -145,7 +153,7 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     constexpr int A_BYTES = T::STEP * T::OUT * 2, B_BYTES = T::STEP * T::IN * 2, BUFFER = PLANES * A_BYTES + B_BYTES;
     extern __shared__ char shared[];
     const lds_bytes lds = (lds_bytes)shared;
-    int32_t *const rows_of = (int32_t *)(shared + 2 * BUFFER);       // [2][STEP]: the checkpoint's rows
+    int32_t *const rows_of = (int32_t *)(shared + BUFFERS * BUFFER);       // [2][STEP]: the checkpoint's rows
 
     int64_t group = group_number();
     const int64_t per_layer = (int64_t)P.tiles_out * P.tiles_in, groups = per_layer * P.splits * P.experts * P.workers;
@@ -158,65 +166,69 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     const int64_t worker = group / P.experts;
     const int o0 = tile / P.tiles_in * T::OUT, i0 = tile % P.tiles_in * T::IN;
     Range range = range_of(P, worker, expert);
+    if (P.tokens == 0) range.end = range.first;           // (of which none is a row's)
     if (P.splits > 1) {
         const int64_t part = ((range.end - range.first + P.splits - 1) / P.splits + T::STEP - 1) / T::STEP * T::STEP;
         range.first = min(range.first + split * part, range.end);
         range.end = min(range.first + part, range.end);
     }
-    const int length = (int)(range.end - range.first), steps = (length + T::STEP - 1) / T::STEP;
+    const uint32_t length = (uint32_t)(range.end - range.first), steps = (length + T::STEP - 1) / T::STEP;    // (rows beyond it: below 2^32)
 
     const int t = threadIdx.x;
     const int ac = t % A_PIECES * N, ar = t / A_PIECES, bc = t % B_PIECES * 16, br = t / B_PIECES;
     const bool a_in = o0 + ac < P.out, b_in = i0 + bc < P.kept.stride;
     const int64_t exponents_stride = P.kept.stride / BLOCK;
+    const int b_column = min(i0 + bc, (int)P.kept.stride - 16);
     u32x4 a[A_COUNT], b[B_COUNT];
     uint32_t e[B_COUNT];
+    bool a_on[A_COUNT], b_on[B_COUNT];
     const bool with_bias = P.bias_at >= 0 && i0 == 0;
     float bias[N] = {};
 
-    const auto load = [&](int step) {
+    // A step's rows: loads without a condition, of rows and columns that are there, and what of them counts.
+    const auto load = [&](uint32_t step) {
         const int32_t *const rows = rows_of + (step & 1) * T::STEP;
 #pragma unroll
         for (int i = 0; i < A_COUNT; ++i) {
             const int s = ar + i * A_ROWS;
-            const int64_t r = range.first + (int64_t)step * T::STEP + s;
-            a[i] = (u32x4)0u;
-            if (a_in && step * T::STEP + s < length && (!SOURCED || rows[s] >= 0)) {
-                const E *const row = (const E *)P.dy + r * P.ld;
-                a[i] = load_piece<E>(row, o0 + ac, P.out);
-            }
+            const uint32_t at = step * T::STEP + s;
+            a_on[i] = a_in && at < length && (!SOURCED || rows[s] >= 0);
+            a[i] = load_raw<E, false>((const E *)P.dy + (range.first + min(at, length - 1)) * P.ld, o0 + ac, P.out);
         }
 #pragma unroll
         for (int i = 0; i < B_COUNT; ++i) {
             const int s = br + i * B_ROWS;
-            const int64_t r = SOURCED ? rows[s] : range.first + (int64_t)step * T::STEP + s;
-            b[i] = (u32x4)0u;
-            e[i] = 127;
-            if (b_in && step * T::STEP + s < length && r >= 0) {
-                b[i] = *(const __attribute__((address_space(1))) u32x4 *)(uint64_t)(P.kept.codes + r * P.kept.stride + i0 + bc);
-                e[i] = *(const __attribute__((address_space(1))) uint8_t *)(uint64_t)(P.kept.exponents + r * exponents_stride + (i0 + bc) / BLOCK);
-            }
+            const uint32_t at = step * T::STEP + s;
+            const int64_t r = SOURCED ? max(rows[s], 0) : range.first + min(at, length - 1);
+            b_on[i] = b_in && at < length && (!SOURCED || rows[s] >= 0);
+            b[i] = *(const __attribute__((address_space(1))) u32x4 *)(uint64_t)(P.kept.codes + r * P.kept.stride + b_column);
+            e[i] = *(const __attribute__((address_space(1))) uint8_t *)(uint64_t)(P.kept.exponents + r * exponents_stride + b_column / BLOCK);
         }
     };
-    const auto put = [&](int buffer) {
-        const lds_bytes at = lds + buffer * BUFFER;
+    int a_to[A_COUNT], b_to[B_COUNT];
+#pragma unroll
+    for (int i = 0; i < A_COUNT; ++i) a_to[i] = lds_offset<T::OUT>(ar + i * A_ROWS, ac);
+#pragma unroll
+    for (int i = 0; i < B_COUNT; ++i) b_to[i] = lds_offset<T::IN>(br + i * B_ROWS, bc);
+    const auto put = [&](auto buffer) {
+        const lds_bytes at = lds + decltype(buffer)::value * BUFFER;
 #pragma unroll
         for (int i = 0; i < A_COUNT; ++i) {
-            const int to = lds_offset<T::OUT>(ar + i * A_ROWS, ac);
+            const u32x4 w = a_on[i] ? settled<E, false>(a[i], o0 + ac, P.out) : (u32x4)0u;
             if constexpr (N == 8) {
                 u32x4 p[PLANES];
-                Planes<E>::split(a[i], p);
+                Planes<E>::split(w, p);
 #pragma unroll
-                for (int q = 0; q < PLANES; ++q) *(__attribute__((address_space(3))) u32x4 *)(at + q * A_BYTES + to) = p[q];
+                for (int q = 0; q < PLANES; ++q) *(__attribute__((address_space(3))) u32x4 *)(at + q * A_BYTES + a_to[i]) = p[q];
             } else {
                 u32x2 p[PLANES];
-                Planes<E>::split(a[i], p);
+                Planes<E>::split(w, p);
 #pragma unroll
-                for (int q = 0; q < PLANES; ++q) *(__attribute__((address_space(3))) u32x2 *)(at + q * A_BYTES + to) = p[q];
+                for (int q = 0; q < PLANES; ++q) *(__attribute__((address_space(3))) u32x2 *)(at + q * A_BYTES + a_to[i]) = p[q];
             }
             if (with_bias) {
                 float v[N];
-                Piece<E>::unpack(a[i], v);
+                Piece<E>::unpack(w, v);
 #pragma unroll
                 for (int j = 0; j < N; ++j) bias[j] += v[j];
             }
@@ -227,54 +239,102 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
             u32x4 w[2];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t code = b[i][q];
+                const uint32_t code = b_on[i] ? b[i][q] : 0u;
                 w[q / 2][q % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, by, false));
                 w[q / 2][q % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, by, true));
             }
-            const lds_bytes to = at + PLANES * A_BYTES + lds_offset<T::IN>(br + i * B_ROWS, bc);
+            const lds_bytes to = at + PLANES * A_BYTES + b_to[i];
             *(__attribute__((address_space(3))) u32x4 *)to = w[0];
             *(__attribute__((address_space(3))) u32x4 *)(to + 16) = w[1];
         }
     };
-    // The checkpoint's rows of a step, looked up by its first threads two steps ahead.
-    const auto look_up = [&](int step) {
+    // The checkpoint's rows of a step, looked up by its first threads.
+    const auto look_up = [&](uint32_t step) {
         if (SOURCED && t < T::STEP) {
-            const int s = step * T::STEP + t;
+            const uint32_t s = step * T::STEP + t;
             rows_of[(step & 1) * T::STEP + t] = s < length ? input_row(P, worker, range.first + s) : -1;
         }
     };
 
     f32x16 acc[MI][NI] = {};
     const int wave = t >> 6, wo = wave / T::WI * (T::OUT / T::WO), wi = wave % T::WI * (T::IN / T::WI);
+    int d_at[MI], x_at[NI];
+#pragma unroll
+    for (int i = 0; i < MI; ++i) d_at[i] = operand_place<T::OUT>(wo + 32 * i);
+#pragma unroll
+    for (int j = 0; j < NI; ++j) x_at[j] = operand_place<T::IN>(wi + 32 * j);
+    // 16 rows' operands, and their products.
+    struct Operands {
+        bf16x8 x[NI], d[PLANES][MI];
+    };
+    const auto fetch = [&](Operands &f, auto buffer, auto row) {
+        const lds_bytes at = lds + decltype(buffer)::value * BUFFER;
+        constexpr int s = decltype(row)::value;
+#pragma unroll
+        for (int j = 0; j < NI; ++j) f.x[j] = operand<T::IN>(at + (PLANES * A_BYTES + s * T::IN * 2) + x_at[j]);
+#pragma unroll
+        for (int q = PLANES - 1; q >= 0; --q)
+#pragma unroll
+            for (int i = 0; i < MI; ++i) f.d[q][i] = operand<T::OUT>(at + (q * A_BYTES + s * T::OUT * 2) + d_at[i]);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    const auto multiply = [&](const Operands &f) {
+#pragma unroll
+        for (int q = PLANES - 1; q >= 0; --q)
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.d[q][i], f.x[j], acc[i][j], 0, 0, 0);
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // A step's rows go through three buffers: step s is multiplied, step s + 1 lies ready, so that its first operands are fetched in front of the barrier,
+    // and step s + 2, which has come meanwhile, is put into the third, where step s - 1 was; step s + 3 is asked for.  Operands are fetched while the ones
+    // before them are multiplied.  Rows are looked up two steps ahead of their loads: their place was last read in front of the barrier before this step's.
+    Operands even, odd;
+    const auto turn = [&](uint32_t step, auto buffer) {
+        constexpr int B = decltype(buffer)::value;
+        typedef std::integral_constant<int, (B + 1) % BUFFERS> Next;
+        typedef std::integral_constant<int, (B + 2) % BUFFERS> Third;
+        if constexpr (T::STEP == 32) {
+            fetch(odd, buffer, std::integral_constant<int, 16>());
+            multiply(even);
+        } else {
+            fetch(odd, buffer, std::integral_constant<int, 16>());
+            multiply(even);
+            fetch(even, buffer, std::integral_constant<int, 32>());
+            multiply(odd);
+            fetch(odd, buffer, std::integral_constant<int, 48>());
+            multiply(even);
+        }
+        put(Third());
+        load(step + 3);
+        look_up(step + 4);
+        fetch(even, Next(), std::integral_constant<int, 0>());
+        multiply(odd);
+        __syncthreads();
+    };
     if (steps > 0) {
+        typedef std::integral_constant<int, 0> First;
+        typedef std::integral_constant<int, 1> Second;
+        typedef std::integral_constant<int, 2> Third;
         look_up(0);
         look_up(1);
-        __syncthreads();
+        if (SOURCED) __syncthreads();
         load(0);
-        put(0);
-        if (steps > 1) load(1);
+        put(First());
+        load(1);
+        put(Second());
         __syncthreads();
-    }
-    for (int step = 0; step < steps; ++step) {
-        const lds_bytes at = lds + (step & 1) * BUFFER;
-        look_up(step + 2);                                // (whose place was last read before the barrier)
-#pragma unroll
-        for (int s = 0; s < T::STEP; s += 16) {
-            bf16x8 x[NI];
-#pragma unroll
-            for (int j = 0; j < NI; ++j) x[j] = operand<T::IN>(at + PLANES * A_BYTES, s, wi + 32 * j);
-#pragma unroll
-            for (int q = PLANES - 1; q >= 0; --q)
-#pragma unroll
-                for (int i = 0; i < MI; ++i) {
-                    const bf16x8 d = operand<T::OUT>(at + q * A_BYTES, s, wo + 32 * i);
-#pragma unroll
-                    for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(d, x[j], acc[i][j], 0, 0, 0);
-                }
+        look_up(2);
+        look_up(3);
+        if (SOURCED) __syncthreads();
+        load(2);
+        fetch(even, First(), std::integral_constant<int, 0>());
+        for (uint32_t step = 0; step < steps; step += BUFFERS) {
+            turn(step, First());
+            if (step + 1 < steps) turn(step + 1, Second());
+            if (step + 2 < steps) turn(step + 2, Third());
         }
-        if (step + 1 < steps) put((step + 1) & 1);
-        __syncthreads();
-        if (step + 2 < steps) load(step + 2);
     }
 
     const int64_t layer = worker * P.experts + expert, weights = (int64_t)P.out * P.in;
