@@ -42,15 +42,63 @@ __device__ __forceinline__ Range range_of(const Linear &P, int64_t worker, int e
     report(P.status);
     return Range{low, low};
 }
-// The checkpoint's row of a row of dy, or -1.
-__device__ __forceinline__ int input_row(const Linear &P, int64_t worker, int64_t row)
+// The checkpoint's row that belongs to a slot, or -1.
+__device__ __forceinline__ int input_row(const Linear &P, int64_t worker, int32_t slot)
 {
     const int64_t low = worker * P.tokens;
-    const int32_t slot = P.source[row];
     const int r = slot < 0 ? -1 : slot / P.k;
     if (r >= low && r < low + P.tokens) return r;
     report(P.status);
     return -1;
+}
+
+// A workgroup's tile.  Workgroups go to the XCDs in turn, each with an L2 of its own: an XCD gets tiles that follow one another, which read the same rows
+// (4 x 4096 x 2048 x 2048 bf16 145 us, tiles to the XCDs in turn 153).  With experts the work of a workgroup is what its expert has of rows; so
+// every layer's tiles are shared out to all XCDs, and the workers' longest layers come first (2 x 4096 x 1024 x 2048, two of eight experts, the most popular
+// four times as popular as the least NOTE), which a wave finds by counting, up to 64 experts.
+constexpr int XCDS = 8, SORTED_EXPERTS = 64;
+struct Share {
+    int64_t worker;
+    int expert, split, tile;
+};
+__device__ __forceinline__ int expert_of_rank(const Linear &P, int64_t worker, int rank)
+{
+    const int lane = threadIdx.x & 63;
+    int length = -1;
+    if (lane < P.experts) {
+        const Range range = range_of(P, worker, lane);
+        length = (int)(range.end - range.first);
+    }
+    int longer = 0;
+    for (int e = 0; e < P.experts; ++e) {
+        const int other = __builtin_amdgcn_readlane(length, e);
+        longer += other > length || (other == length && e < lane);
+    }
+    return __builtin_ctzll(__ballot(lane < P.experts && longer == rank));
+}
+__device__ __forceinline__ Share share_of(const Linear &P)
+{
+    const uint32_t per_layer = (uint32_t)P.tiles_out * (uint32_t)P.tiles_in;
+    int64_t group = group_number();
+    Share s;
+    if (!P.start) {
+        const int64_t groups = (int64_t)per_layer * P.splits * P.workers, xcd = group % XCDS;
+        if (group >= groups) return Share{P.workers, 0, 0, 0};
+        group = xcd * (groups / XCDS) + min(xcd, groups % XCDS) + group / XCDS;
+    }
+    s.tile = (int)(group % per_layer);
+    group /= per_layer;
+    s.split = (int)(group % P.splits);
+    group /= P.splits;
+    s.worker = group % P.workers;
+    const int64_t rank = group / P.workers;
+    if (rank >= P.experts) return Share{P.workers, 0, 0, 0};
+    s.expert = (int)rank;
+    if (P.start) {
+        if (per_layer % XCDS == 0) s.tile = s.tile % XCDS * (int)(per_layer / XCDS) + s.tile / XCDS;
+        if (P.experts > 1 && P.experts <= SORTED_EXPERTS) s.expert = expert_of_rank(P, s.worker, s.expert);
+    }
+    return s;
 }
 
 // A piece of dy as bf16 planes, the large parts first.
@@ -155,15 +203,10 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     const lds_bytes lds = (lds_bytes)shared;
     int32_t *const rows_of = (int32_t *)(shared + BUFFERS * BUFFER);       // [2][STEP]: the checkpoint's rows
 
-    int64_t group = group_number();
-    const int64_t per_layer = (int64_t)P.tiles_out * P.tiles_in, groups = per_layer * P.splits * P.experts * P.workers;
-    if (group >= groups) return;
-    const int tile = (int)(group % per_layer);
-    group /= per_layer;
-    const int split = (int)(group % P.splits);
-    group /= P.splits;
-    const int expert = (int)(group % P.experts);
-    const int64_t worker = group / P.experts;
+    const Share mine = share_of(P);
+    if (mine.worker >= P.workers) return;
+    const int tile = mine.tile, split = mine.split, expert = mine.expert;
+    const int64_t worker = mine.worker;
     const int o0 = tile / P.tiles_in * T::OUT, i0 = tile % P.tiles_in * T::IN;
     Range range = range_of(P, worker, expert);
     if (P.tokens == 0) range.end = range.first;           // (of which none is a row's)
@@ -185,22 +228,30 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     const bool with_bias = P.bias_at >= 0 && i0 == 0;
     float bias[N] = {};
 
+    // The checkpoint's rows of a step, which a load goes by: read a step ahead.
+    int a_row[A_COUNT], b_row[B_COUNT];
+    const auto take = [&](uint32_t step) {
+        if (!SOURCED) return;
+#pragma unroll
+        for (int i = 0; i < A_COUNT; ++i) a_row[i] = rows_of[(step & 1) * T::STEP + ar + i * A_ROWS];
+#pragma unroll
+        for (int i = 0; i < B_COUNT; ++i) b_row[i] = rows_of[(step & 1) * T::STEP + br + i * B_ROWS];
+    };
     // A step's rows: loads without a condition, of rows and columns that are there, and what of them counts.
     const auto load = [&](uint32_t step) {
-        const int32_t *const rows = rows_of + (step & 1) * T::STEP;
 #pragma unroll
         for (int i = 0; i < A_COUNT; ++i) {
             const int s = ar + i * A_ROWS;
             const uint32_t at = step * T::STEP + s;
-            a_on[i] = a_in && at < length && (!SOURCED || rows[s] >= 0);
+            a_on[i] = a_in && at < length && (!SOURCED || a_row[i] >= 0);
             a[i] = load_raw<E, false>((const E *)P.dy + (range.first + min(at, length - 1)) * P.ld, o0 + ac, P.out);
         }
 #pragma unroll
         for (int i = 0; i < B_COUNT; ++i) {
             const int s = br + i * B_ROWS;
             const uint32_t at = step * T::STEP + s;
-            const int64_t r = SOURCED ? max(rows[s], 0) : range.first + min(at, length - 1);
-            b_on[i] = b_in && at < length && (!SOURCED || rows[s] >= 0);
+            const int64_t r = SOURCED ? max(b_row[i], 0) : range.first + min(at, length - 1);
+            b_on[i] = b_in && at < length && (!SOURCED || b_row[i] >= 0);
             b[i] = *(const __attribute__((address_space(1))) u32x4 *)(uint64_t)(P.kept.codes + r * P.kept.stride + b_column);
             e[i] = *(const __attribute__((address_space(1))) uint8_t *)(uint64_t)(P.kept.exponents + r * exponents_stride + b_column / BLOCK);
         }
@@ -248,13 +299,18 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
             *(__attribute__((address_space(3))) u32x4 *)(to + 16) = w[1];
         }
     };
-    // The checkpoint's rows of a step, looked up by its first threads.
-    const auto look_up = [&](uint32_t step) {
-        if (SOURCED && t < T::STEP) {
-            const uint32_t s = step * T::STEP + t;
-            rows_of[(step & 1) * T::STEP + t] = s < length ? input_row(P, worker, range.first + s) : -1;
-        }
+    // The checkpoint's rows of a step, looked up by its first threads; the next step's slots are asked for a step ahead.
+    int32_t next_slot = -1;
+    const auto ask = [&](uint32_t step) {
+        const uint32_t s = step * T::STEP + t;
+        if (t < T::STEP && s < length) next_slot = ((const __attribute__((address_space(1))) int32_t *)(uint64_t)P.source)[range.first + s];
     };
+    const auto look_up = [&](uint32_t step) {
+        if (!SOURCED) return;
+        if (t < T::STEP) rows_of[(step & 1) * T::STEP + t] = step * T::STEP + t < length ? input_row(P, worker, next_slot) : -1;
+        ask(step + 1);
+    };
+    if (SOURCED) ask(0);
 
     f32x16 acc[MI][NI] = {};
     const int wave = t >> 6, wo = wave / T::WI * (T::OUT / T::WO), wi = wave % T::WI * (T::IN / T::WI);
@@ -276,7 +332,6 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
         for (int q = PLANES - 1; q >= 0; --q)
 #pragma unroll
             for (int i = 0; i < MI; ++i) f.d[q][i] = operand<T::OUT>(at + (q * A_BYTES + s * T::OUT * 2) + d_at[i]);
-        __builtin_amdgcn_sched_barrier(0);
     };
     const auto multiply = [&](const Operands &f) {
 #pragma unroll
@@ -285,11 +340,11 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
             for (int i = 0; i < MI; ++i)
 #pragma unroll
                 for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(f.d[q][i], f.x[j], acc[i][j], 0, 0, 0);
-        __builtin_amdgcn_sched_barrier(0);
     };
     // A step's rows go through three buffers: step s is multiplied, step s + 1 lies ready, so that its first operands are fetched in front of the barrier,
     // and step s + 2, which has come meanwhile, is put into the third, where step s - 1 was; step s + 3 is asked for.  Operands are fetched while the ones
-    // before them are multiplied.  Rows are looked up two steps ahead of their loads: their place was last read in front of the barrier before this step's.
+    // before them are multiplied.  The rows that step s + 4 takes of the checkpoint are read from LDS and those of step s + 5 looked up, into the place that
+    // step s + 3 had, read in front of the last barrier.
     Operands even, odd;
     const auto turn = [&](uint32_t step, auto buffer) {
         constexpr int B = decltype(buffer)::value;
@@ -308,7 +363,8 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
         }
         put(Third());
         load(step + 3);
-        look_up(step + 4);
+        take(step + 4);
+        look_up(step + 5);
         fetch(even, Next(), std::integral_constant<int, 0>());
         multiply(odd);
         __syncthreads();
@@ -320,7 +376,9 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
         look_up(0);
         look_up(1);
         if (SOURCED) __syncthreads();
+        take(0);
         load(0);
+        take(1);
         put(First());
         load(1);
         put(Second());
@@ -328,7 +386,12 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
         look_up(2);
         look_up(3);
         if (SOURCED) __syncthreads();
+        take(2);
         load(2);
+        take(3);
+        if (SOURCED) __syncthreads();
+        look_up(4);
+        if (SOURCED) __syncthreads();
         fetch(even, First(), std::integral_constant<int, 0>());
         for (uint32_t step = 0; step < steps; step += BUFFERS) {
             turn(step, First());
