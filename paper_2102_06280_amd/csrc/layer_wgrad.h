@@ -413,7 +413,7 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
 #pragma unroll
             for (int j = 0; j < NI; ++j) {
                 const int c = i0 + wi + 32 * j + (l & 31);
-                if (o < P.out && c < P.in) to[(int64_t)o * P.in + c] = acc[i][j][v];
+                if (o < P.out && c < P.in) __builtin_nontemporal_store(acc[i][j][v], to + (int64_t)o * P.in + c);
             }
         }
     if (with_bias) {

@@ -429,23 +429,28 @@ struct Cut {
     int64_t tiles_out, tiles_in, layers;
     int splits;
 };
-constexpr int64_t CHIP = 256;
+// Large tiles where they fill the chip.  Else middle ones where there are two for a compute unit or so much to do that splitting the rows pays: 1 x 4096 x
+// 2048 x 2048 bf16 67.7 us (small tiles 82, large ones 71.9), 1 x 8192 x 1024 x 1024 40.9 (50, 53), but 8 x 1024 x 512 x 512 29 and small ones
+// 15.3, 2 x 1024 x 768 x 2304 34 and 25.4.  Parts have 512 rows at least: 2 x 512 x 500 x 700 fp32 whole 15.8, in halves 26.6.
+constexpr int64_t CHIP = 256, MUCH = 400000, PART = 512;
 Cut cut_of(const dbw_linear *l)
 {
     Cut c;
     c.layers = (int64_t)l->workers * l->experts;
     c.splits = 1;
+    const int64_t rows = l->rows / l->experts;
+    int64_t groups = 0;
     for (c.tile = 2; c.tile >= 0; --c.tile) {
         const int out = c.tile == 2 ? (l->type == DBW_TYPE_BF16 ? Large::OUT : LargeSplit::OUT) : c.tile == 1 ? Middle::OUT : Small::OUT;
         const int in = c.tile == 2 ? Large::IN : c.tile == 1 ? Middle::IN : Small::IN;
         c.tiles_out = (l->outputs + out - 1) / out;
         c.tiles_in = (l->inputs + in - 1) / in;
-        if (c.tile == 0 || c.tiles_out * c.tiles_in * c.layers >= CHIP) break;
+        groups = c.tiles_out * c.tiles_in * c.layers;
+        if (c.tile == 0 || (c.tile == 2 && groups >= CHIP) || (c.tile == 1 && (groups >= 2 * CHIP || groups * rows >= MUCH))) break;
     }
-    const int64_t groups = c.tiles_out * c.tiles_in * c.layers, rows = l->rows / l->experts;
-    if (groups < CHIP) {
-        int64_t splits = (2 * CHIP + groups - 1) / groups;
-        if (splits > rows / 256) splits = rows / 256;
+    if (groups < (c.tile == 1 ? 2 * CHIP : CHIP)) {
+        int64_t splits = 2 * CHIP / groups;
+        if (splits > rows / PART) splits = rows / PART;
         if (splits > 1) c.splits = (int)splits;
     }
     return c;
