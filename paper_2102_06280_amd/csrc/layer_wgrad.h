@@ -4,6 +4,7 @@
 // matrix instruction is exact, and fp32 sums are all that rounds.
 #pragma once
 
+#include <algorithm>
 #include <type_traits>
 
 #include "global_access.h"
@@ -27,6 +28,7 @@ struct Linear {
     int64_t workers;
     int rows, in, out, experts, tokens, k;                // rows, tokens: of a worker
     int tiles_out, tiles_in, splits;
+    bool cached;                                          // results go through the caches
     float *parts;                                         // [split][weights of all layers, then their biases], where the rows are split
 };
 // The rows of dy of a worker's layer.
@@ -37,7 +39,8 @@ __device__ __forceinline__ Range range_of(const Linear &P, int64_t worker, int e
 {
     const int64_t low = worker * P.rows, high = low + P.rows;
     if (!P.start) return Range{low, high};
-    const int64_t at = worker * (P.experts + 1) + expert, a = P.start[at], b = P.start[at + 1];
+    const auto start = (const __attribute__((address_space(1))) int32_t *)(uint64_t)P.start;
+    const int64_t at = worker * (P.experts + 1) + expert, a = start[at], b = start[at + 1];
     if (a >= low && b <= high && a <= b) return Range{a, b};
     report(P.status);
     return Range{low, low};
@@ -60,45 +63,48 @@ constexpr int XCDS = 8, SORTED_EXPERTS = 64;
 struct Share {
     int64_t worker;
     int expert, split, tile;
+    Range range;
 };
-__device__ __forceinline__ int expert_of_rank(const Linear &P, int64_t worker, int rank)
+__device__ __forceinline__ int64_t from_lane(int64_t v, int lane)
 {
-    const int lane = threadIdx.x & 63;
-    int length = -1;
-    if (lane < P.experts) {
-        const Range range = range_of(P, worker, lane);
-        length = (int)(range.end - range.first);
+    const uint32_t low = __builtin_amdgcn_readlane((int)v, lane), high = __builtin_amdgcn_readlane((int)(v >> 32), lane);
+    return (int64_t)((uint64_t)high << 32 | low);
+}
+__device__ __forceinline__ bool share_of(const Linear &P, Share &s)
+{
+    // (as many workgroups as there are tiles to write: far below 2^32)
+    const uint32_t per_layer = (uint32_t)P.tiles_out * (uint32_t)P.tiles_in, workers = (uint32_t)P.workers, splits = (uint32_t)P.splits;
+    const uint32_t groups = per_layer * splits * workers * (uint32_t)P.experts;
+    uint32_t group = (uint32_t)group_number();
+    if (group >= groups) return false;
+    if (!P.start) {
+        const uint32_t xcd = group % XCDS;
+        group = xcd * (groups / XCDS) + min(xcd, groups % XCDS) + group / XCDS;
     }
+    s.tile = (int)(group % per_layer);
+    group /= per_layer;
+    s.split = (int)(group % splits);
+    group /= splits;
+    s.worker = group % workers;
+    s.expert = (int)(group / workers);
+    if (P.start && per_layer % XCDS == 0) s.tile = s.tile % XCDS * (int)(per_layer / XCDS) + s.tile / XCDS;
+    if (!P.start || P.experts == 1 || P.experts > SORTED_EXPERTS) {
+        s.range = range_of(P, s.worker, s.expert);
+        return true;
+    }
+    // the layer that has as many longer ones before it as `expert` says
+    const int lane = threadIdx.x & 63;
+    Range mine{0, -1};
+    if (lane < P.experts) mine = range_of(P, s.worker, lane);
+    const int length = (int)(mine.end - mine.first);
     int longer = 0;
     for (int e = 0; e < P.experts; ++e) {
         const int other = __builtin_amdgcn_readlane(length, e);
         longer += other > length || (other == length && e < lane);
     }
-    return __builtin_ctzll(__ballot(lane < P.experts && longer == rank));
-}
-__device__ __forceinline__ Share share_of(const Linear &P)
-{
-    const uint32_t per_layer = (uint32_t)P.tiles_out * (uint32_t)P.tiles_in;
-    int64_t group = group_number();
-    Share s;
-    if (!P.start) {
-        const int64_t groups = (int64_t)per_layer * P.splits * P.workers, xcd = group % XCDS;
-        if (group >= groups) return Share{P.workers, 0, 0, 0};
-        group = xcd * (groups / XCDS) + min(xcd, groups % XCDS) + group / XCDS;
-    }
-    s.tile = (int)(group % per_layer);
-    group /= per_layer;
-    s.split = (int)(group % P.splits);
-    group /= P.splits;
-    s.worker = group % P.workers;
-    const int64_t rank = group / P.workers;
-    if (rank >= P.experts) return Share{P.workers, 0, 0, 0};
-    s.expert = (int)rank;
-    if (P.start) {
-        if (per_layer % XCDS == 0) s.tile = s.tile % XCDS * (int)(per_layer / XCDS) + s.tile / XCDS;
-        if (P.experts > 1 && P.experts <= SORTED_EXPERTS) s.expert = expert_of_rank(P, s.worker, s.expert);
-    }
-    return s;
+    s.expert = __builtin_ctzll(__ballot(lane < P.experts && longer == s.expert));
+    s.range = Range{from_lane(mine.first, s.expert), from_lane(mine.end, s.expert)};
+    return true;
 }
 
 // A piece of dy as bf16 planes, the large parts first.
@@ -188,27 +194,28 @@ struct Tile {
 };
 constexpr int BUFFERS = 3;
 template <class E, class T>
-constexpr int tile_lds() { return BUFFERS * T::STEP * 2 * (Planes<E>::COUNT * T::OUT + T::IN) + 2 * T::STEP * 4; }
+constexpr int tile_lds() { return BUFFERS * T::STEP * 2 * (Planes<E>::COUNT * T::OUT + T::IN) + 4 * T::STEP * 4; }
 
 template <class E, class T, bool SOURCED>
 __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
 {
     constexpr int N = Piece<E>::N, PLANES = Planes<E>::COUNT;
     constexpr int A_PIECES = T::OUT / N, A_ROWS = T::THREADS / A_PIECES, A_COUNT = T::STEP / A_ROWS;
-    constexpr int B_PIECES = T::IN / 16, B_ROWS = T::THREADS / B_PIECES, B_COUNT = T::STEP / B_ROWS;
+    constexpr int B_PIECES = T::IN / 16, B_ROWS = std::min(T::THREADS / B_PIECES, T::STEP), B_COUNT = T::STEP / B_ROWS;
+    constexpr bool B_ALL = B_PIECES * B_ROWS == T::THREADS;          // or the first threads only
     static_assert(A_COUNT * A_ROWS == T::STEP && B_COUNT * B_ROWS == T::STEP, "whole turns");
     constexpr int MI = T::OUT / T::WO / 32, NI = T::IN / T::WI / 32;
     constexpr int A_BYTES = T::STEP * T::OUT * 2, B_BYTES = T::STEP * T::IN * 2, BUFFER = PLANES * A_BYTES + B_BYTES;
     extern __shared__ char shared[];
     const lds_bytes lds = (lds_bytes)shared;
-    int32_t *const rows_of = (int32_t *)(shared + BUFFERS * BUFFER);       // [2][STEP]: the checkpoint's rows
+    int32_t *const rows_of = (int32_t *)(shared + BUFFERS * BUFFER);       // [4][STEP]: the checkpoint's rows
 
-    const Share mine = share_of(P);
-    if (mine.worker >= P.workers) return;
+    Share mine;
+    if (!share_of(P, mine)) return;
     const int tile = mine.tile, split = mine.split, expert = mine.expert;
     const int64_t worker = mine.worker;
     const int o0 = tile / P.tiles_in * T::OUT, i0 = tile % P.tiles_in * T::IN;
-    Range range = range_of(P, worker, expert);
+    Range range = mine.range;
     if (P.tokens == 0) range.end = range.first;           // (of which none is a row's)
     if (P.splits > 1) {
         const int64_t part = ((range.end - range.first + P.splits - 1) / P.splits + T::STEP - 1) / T::STEP * T::STEP;
@@ -218,13 +225,16 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     const uint32_t length = (uint32_t)(range.end - range.first), steps = (length + T::STEP - 1) / T::STEP;    // (rows beyond it: below 2^32)
 
     const int t = threadIdx.x;
-    const int ac = t % A_PIECES * N, ar = t / A_PIECES, bc = t % B_PIECES * 16, br = t / B_PIECES;
+    const int ac = t % A_PIECES * N, ar = t / A_PIECES, bc = t % B_PIECES * 16, br = B_ALL ? t / B_PIECES : min(t / B_PIECES, B_ROWS - 1);
     const bool a_in = o0 + ac < P.out, b_in = i0 + bc < P.kept.stride;
     const int64_t exponents_stride = P.kept.stride / BLOCK;
     const int b_column = min(i0 + bc, (int)P.kept.stride - 16);
-    u32x4 a[A_COUNT], b[B_COUNT];
-    uint32_t e[B_COUNT];
-    bool a_on[A_COUNT], b_on[B_COUNT];
+    // A step's rows on their way to LDS, and what of them counts.
+    struct Staged {
+        u32x4 a[A_COUNT], b[B_COUNT];
+        uint32_t e[B_COUNT];
+        bool a_on[A_COUNT], b_on[B_COUNT];
+    };
     const bool with_bias = P.bias_at >= 0 && i0 == 0;
     float bias[N] = {};
 
@@ -233,27 +243,27 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     const auto take = [&](uint32_t step) {
         if (!SOURCED) return;
 #pragma unroll
-        for (int i = 0; i < A_COUNT; ++i) a_row[i] = rows_of[(step & 1) * T::STEP + ar + i * A_ROWS];
+        for (int i = 0; i < A_COUNT; ++i) a_row[i] = rows_of[(step & 3) * T::STEP + ar + i * A_ROWS];
 #pragma unroll
-        for (int i = 0; i < B_COUNT; ++i) b_row[i] = rows_of[(step & 1) * T::STEP + br + i * B_ROWS];
+        for (int i = 0; i < B_COUNT; ++i) b_row[i] = rows_of[(step & 3) * T::STEP + br + i * B_ROWS];
     };
-    // A step's rows: loads without a condition, of rows and columns that are there, and what of them counts.
-    const auto load = [&](uint32_t step) {
+    // Loads without a condition, of rows and columns that are there.
+    const auto load = [&](Staged &to, uint32_t step) {
 #pragma unroll
         for (int i = 0; i < A_COUNT; ++i) {
             const int s = ar + i * A_ROWS;
             const uint32_t at = step * T::STEP + s;
-            a_on[i] = a_in && at < length && (!SOURCED || a_row[i] >= 0);
-            a[i] = load_raw<E, false>((const E *)P.dy + (range.first + min(at, length - 1)) * P.ld, o0 + ac, P.out);
+            to.a_on[i] = a_in && at < length && (!SOURCED || a_row[i] >= 0);
+            to.a[i] = load_raw<E, false>((const E *)P.dy + (range.first + min(at, length - 1)) * P.ld, o0 + ac, P.out);
         }
 #pragma unroll
         for (int i = 0; i < B_COUNT; ++i) {
             const int s = br + i * B_ROWS;
             const uint32_t at = step * T::STEP + s;
             const int64_t r = SOURCED ? max(b_row[i], 0) : range.first + min(at, length - 1);
-            b_on[i] = b_in && at < length && (!SOURCED || b_row[i] >= 0);
-            b[i] = *(const __attribute__((address_space(1))) u32x4 *)(uint64_t)(P.kept.codes + r * P.kept.stride + b_column);
-            e[i] = *(const __attribute__((address_space(1))) uint8_t *)(uint64_t)(P.kept.exponents + r * exponents_stride + b_column / BLOCK);
+            to.b_on[i] = b_in && at < length && (!SOURCED || b_row[i] >= 0);
+            to.b[i] = *(const __attribute__((address_space(1))) u32x4 *)(uint64_t)(P.kept.codes + r * P.kept.stride + b_column);
+            to.e[i] = *(const __attribute__((address_space(1))) uint8_t *)(uint64_t)(P.kept.exponents + r * exponents_stride + b_column / BLOCK);
         }
     };
     int a_to[A_COUNT], b_to[B_COUNT];
@@ -261,11 +271,11 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     for (int i = 0; i < A_COUNT; ++i) a_to[i] = lds_offset<T::OUT>(ar + i * A_ROWS, ac);
 #pragma unroll
     for (int i = 0; i < B_COUNT; ++i) b_to[i] = lds_offset<T::IN>(br + i * B_ROWS, bc);
-    const auto put = [&](auto buffer) {
+    const auto put = [&](const Staged &from, auto buffer) {
         const lds_bytes at = lds + decltype(buffer)::value * BUFFER;
 #pragma unroll
         for (int i = 0; i < A_COUNT; ++i) {
-            const u32x4 w = a_on[i] ? settled<E, false>(a[i], o0 + ac, P.out) : (u32x4)0u;
+            const u32x4 w = from.a_on[i] ? settled<E, false>(from.a[i], o0 + ac, P.out) : (u32x4)0u;
             if constexpr (N == 8) {
                 u32x4 p[PLANES];
                 Planes<E>::split(w, p);
@@ -286,34 +296,42 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
         }
 #pragma unroll
         for (int i = 0; i < B_COUNT; ++i) {
-            const float by = __uint_as_float(e[i] << 23);
+            const float by = __uint_as_float(from.e[i] << 23);
             u32x4 w[2];
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const uint32_t code = b_on[i] ? b[i][q] : 0u;
+                const uint32_t code = from.b_on[i] ? from.b[i][q] : 0u;
                 w[q / 2][q % 2 * 2] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, by, false));
                 w[q / 2][q % 2 * 2 + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(code, by, true));
             }
             const lds_bytes to = at + PLANES * A_BYTES + b_to[i];
-            *(__attribute__((address_space(3))) u32x4 *)to = w[0];
-            *(__attribute__((address_space(3))) u32x4 *)(to + 16) = w[1];
+            if (B_ALL || t < B_PIECES * B_ROWS) {
+                *(__attribute__((address_space(3))) u32x4 *)to = w[0];
+                *(__attribute__((address_space(3))) u32x4 *)(to + 16) = w[1];
+            }
         }
     };
-    // The checkpoint's rows of a step, looked up by its first threads; the next step's slots are asked for a step ahead.
+    // The checkpoint's rows of a step, looked up by the first threads; the next step's slots are asked for a step ahead.
     int32_t next_slot = -1;
-    const auto ask = [&](uint32_t step) {
+    const auto ask = [&](uint32_t step, int threads) {
         const uint32_t s = step * T::STEP + t;
-        if (t < T::STEP && s < length) next_slot = ((const __attribute__((address_space(1))) int32_t *)(uint64_t)P.source)[range.first + s];
+        if (t < threads && s < length) next_slot = ((const __attribute__((address_space(1))) int32_t *)(uint64_t)P.source)[range.first + s];
     };
     const auto look_up = [&](uint32_t step) {
         if (!SOURCED) return;
-        if (t < T::STEP) rows_of[(step & 1) * T::STEP + t] = step * T::STEP + t < length ? input_row(P, worker, next_slot) : -1;
-        ask(step + 1);
+        if (t < T::STEP) rows_of[(step & 3) * T::STEP + t] = step * T::STEP + t < length ? input_row(P, worker, next_slot) : -1;
+        ask(step + 1, T::STEP);
     };
-    if (SOURCED) ask(0);
+    static_assert(4 * T::STEP <= T::THREADS, "four steps' rows at once");
+    if (SOURCED) {
+        ask(0, 4 * T::STEP);
+        if (t < 4 * T::STEP) rows_of[t] = (uint32_t)t < length ? input_row(P, worker, next_slot) : -1;
+        ask(4, T::STEP);
+        __syncthreads();
+    }
 
     f32x16 acc[MI][NI] = {};
-    const int wave = t >> 6, wo = wave / T::WI * (T::OUT / T::WO), wi = wave % T::WI * (T::IN / T::WI);
+    const int wave = __builtin_amdgcn_readfirstlane(t >> 6), wo = wave / T::WI * (T::OUT / T::WO), wi = wave % T::WI * (T::IN / T::WI);
     int d_at[MI], x_at[NI];
 #pragma unroll
     for (int i = 0; i < MI; ++i) d_at[i] = operand_place<T::OUT>(wo + 32 * i);
@@ -346,6 +364,7 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     // before them are multiplied.  The rows that step s + 4 takes of the checkpoint are read from LDS and those of step s + 5 looked up, into the place that
     // step s + 3 had, read in front of the last barrier.
     Operands even, odd;
+    Staged coming;
     const auto turn = [&](uint32_t step, auto buffer) {
         constexpr int B = decltype(buffer)::value;
         typedef std::integral_constant<int, (B + 1) % BUFFERS> Next;
@@ -361,8 +380,8 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
             fetch(odd, buffer, std::integral_constant<int, 48>());
             multiply(even);
         }
-        put(Third());
-        load(step + 3);
+        put(coming, Third());
+        load(coming, step + 3);
         take(step + 4);
         look_up(step + 5);
         fetch(even, Next(), std::integral_constant<int, 0>());
@@ -373,25 +392,20 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
         typedef std::integral_constant<int, 0> First;
         typedef std::integral_constant<int, 1> Second;
         typedef std::integral_constant<int, 2> Third;
-        look_up(0);
-        look_up(1);
-        if (SOURCED) __syncthreads();
+        // (the sums' registers are free as yet)
+        Staged first, second;
         take(0);
-        load(0);
+        load(first, 0);
         take(1);
-        put(First());
-        load(1);
-        put(Second());
-        __syncthreads();
-        look_up(2);
-        look_up(3);
-        if (SOURCED) __syncthreads();
+        load(second, 1);
         take(2);
-        load(2);
+        load(coming, 2);
         take(3);
-        if (SOURCED) __syncthreads();
+        put(first, First());
+        put(second, Second());
+        if (SOURCED) __syncthreads();                     // rows 0 have been read: rows 4 go there
         look_up(4);
-        if (SOURCED) __syncthreads();
+        __syncthreads();
         fetch(even, First(), std::integral_constant<int, 0>());
         for (uint32_t step = 0; step < steps; step += BUFFERS) {
             turn(step, First());
@@ -404,18 +418,24 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     const int64_t all = P.workers * P.experts;
     float *const to = P.splits > 1 ? P.parts + split * all * (weights + P.out) + layer * weights
                                    : P.grads + worker * P.ld_grads + P.weight_at + expert * weights;
-    const int l = t & 63;
+    const auto write = [&](auto cached) {
+        const int l = t & 63;
 #pragma unroll
-    for (int i = 0; i < MI; ++i)
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) {
-            const int o = o0 + wo + 32 * i + 8 * (v / 4) + 4 * (l >> 5) + v % 4;
+            for (int v = 0; v < 16; ++v) {
+                const int o = o0 + wo + 32 * i + 8 * (v / 4) + 4 * (l >> 5) + v % 4;
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                const int c = i0 + wi + 32 * j + (l & 31);
-                if (o < P.out && c < P.in) __builtin_nontemporal_store(acc[i][j][v], to + (int64_t)o * P.in + c);
+                for (int j = 0; j < NI; ++j) {
+                    const int c = i0 + wi + 32 * j + (l & 31);
+                    if (o >= P.out || c >= P.in) continue;
+                    if constexpr (decltype(cached)::value) to[(int64_t)o * P.in + c] = acc[i][j][v];
+                    else __builtin_nontemporal_store(acc[i][j][v], to + (int64_t)o * P.in + c);
+                }
             }
-        }
+    };
+    if (P.cached) write(std::true_type());
+    else write(std::false_type());
     if (with_bias) {
         // the sums of the threads that have the same columns, in their order
         float *const sums = (float *)shared;              // [A_ROWS][OUT]

@@ -423,7 +423,9 @@ int check_linear(const dbw_linear *l, int64_t *ld)
 typedef layer::Tile<256, 256, 2, 4, 32> Large;
 typedef layer::Tile<128, 256, 2, 4, 32> LargeSplit;       // of operands in parts
 typedef layer::Tile<128, 128, 2, 2, 32> Middle;
+typedef layer::Tile<64, 128, 2, 2, 32> MiddleSplit;
 typedef layer::Tile<64, 64, 2, 2, 64> Small;
+typedef layer::Tile<64, 64, 2, 2, 32> SmallSplit;         // in three
 struct Cut {
     int tile;                                             // 0: small, 1: middle, 2: large
     int64_t tiles_out, tiles_in, layers;
@@ -441,7 +443,7 @@ Cut cut_of(const dbw_linear *l)
     const int64_t rows = l->rows / l->experts;
     int64_t groups = 0;
     for (c.tile = 2; c.tile >= 0; --c.tile) {
-        const int out = c.tile == 2 ? (l->type == DBW_TYPE_BF16 ? Large::OUT : LargeSplit::OUT) : c.tile == 1 ? Middle::OUT : Small::OUT;
+        const int out = c.tile == 2 ? (l->type == DBW_TYPE_BF16 ? Large::OUT : LargeSplit::OUT) : c.tile == 1 ? (l->type == DBW_TYPE_BF16 ? Middle::OUT : MiddleSplit::OUT) : Small::OUT;
         const int in = c.tile == 2 ? Large::IN : c.tile == 1 ? Middle::IN : Small::IN;
         c.tiles_out = (l->outputs + out - 1) / out;
         c.tiles_in = (l->inputs + in - 1) / in;
@@ -484,10 +486,14 @@ extern "C" int dbw_checkpoint_weight_grad(const dbw_linear *shape, const void *d
     if (too_long(ld_grads, shape->workers)) return DBW_ERR_UNSUPPORTED;
     const int64_t tokens = (int64_t)shape->workers * shape->tokens;
     const Cut cut = cut_of(shape);
+    // Past the caches (two of eight experts 2 x 4096 x 1024 x 2048 bf16 98 us, through them 127), but for rows that share their lines of 128 bytes with the
+    // next and all of which the last-level cache holds, where a line's parts come together (13 x 14 x 809 x 171, 16 experts, 115 MB, 42 and past them
+    // 59; but 5 x 161 x 2097 x 2192, 8 experts, fp16, 735 MB, 357 and 266).
+    const bool cached = shape->inputs % 32 != 0 && 4 * weights * shape->workers <= (int64_t)256 << 20;
     const int64_t groups = cut.tiles_out * cut.tiles_in * cut.layers * cut.splits;
     const layer::Linear P{dy, layer::kept_of((void *)checkpoint, tokens, shape->inputs), start, source, status_out, grads, ld, ld_grads, weight_at,
                           bias_at, shape->workers, shape->rows, shape->inputs, shape->outputs, shape->experts, shape->tokens, shape->k, (int)cut.tiles_out,
-                          (int)cut.tiles_in, cut.splits, (float *)work};
+                          (int)cut.tiles_in, cut.splits, cached, (float *)work};
     hipStream_t s = (hipStream_t)stream;
     bool fits = true;
     by_type(shape->type, [&](auto v) {
@@ -503,10 +509,14 @@ extern "C" int dbw_checkpoint_weight_grad(const dbw_linear *shape, const void *d
             if (source) run(layer::weight_grad_kernel<E, T, true>);
             else run(layer::weight_grad_kernel<E, T, false>);
         };
-        if (cut.tile == 0) launch(Small());
-        else if (cut.tile == 1) launch(Middle());
-        else if constexpr (layer::Planes<E>::COUNT == 1) launch(Large());
-        else launch(LargeSplit());
+        if (cut.tile == 0) launch(std::conditional_t<layer::Planes<E>::COUNT == 3, SmallSplit, Small>());
+        else if constexpr (layer::Planes<E>::COUNT == 1) {
+            if (cut.tile == 1) launch(Middle());
+            else launch(Large());
+        } else {
+            if (cut.tile == 1) launch(MiddleSplit());
+            else launch(LargeSplit());
+        }
     });
     if (!fits) return DBW_ERR_HIP;
     if (cut.splits > 1) {
