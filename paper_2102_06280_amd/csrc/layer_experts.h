@@ -241,36 +241,40 @@ __global__ __launch_bounds__(MOVE_THREADS) void combine_kernel(Move P, int chunk
     for (int i = 0; i < C; ++i) store_piece<E>((E *)P.out + token.row * P.ld, c0 + i * 64 * N, P.width, Piece<E>::pack(v[i]));
 }
 
-// Here a wave has the whole token, as many columns at a time as its lanes hold; what it has of a few slots' products is summed over the lanes in the end.
-template <class E, int C>
+// Here a wave has the whole token, or, where there are few, a workgroup (WAVES of them); as many columns at a time as the lanes hold.  What they have of a few
+// slots' products is summed in the end.
+template <class E, int C, int WAVES>
 __global__ __launch_bounds__(MOVE_THREADS) void combine_grad_kernel(Move P)
 {
-    constexpr int N = Piece<E>::N, Q = 2;                 // slots at a time
-    const Token token = token_of(1);
-    if (token.row >= P.rows) return;
-    const E *const dy = (const E *)P.tokens + token.row * P.ld;
+    constexpr int N = Piece<E>::N, Q = 2, T = 64 * WAVES;  // Q: slots at a time
+    __shared__ float sums[2][WAVES][Q];
+    const int64_t row = WAVES == 1 ? token_of(1).row : group_number();
+    if (row >= P.rows) return;
+    const int t = threadIdx.x % T;
+    const E *const dy = (const E *)P.tokens + row * P.ld;
+    int turn = 0;
     for (int j0 = 0; j0 < P.k; j0 += 64) {
-        const Slots slots(P, token.row, j0);
+        const Slots slots(P, row, j0);
         const int count = min(64, P.k - j0);
         float mine = 0.f;                                 // of the slot that is the lane's
         for (int j = 0; j < count; j += Q) {
             int p[Q];
             float dot[Q] = {};
             for (int q = 0; q < Q; ++q) p[q] = j + q < count ? slots.place_of(j + q) : -1;
-            for (int c0 = (threadIdx.x & 63) * N; c0 < P.width; c0 += C * 64 * N) {
+            for (int c0 = t * N; c0 < P.width; c0 += C * T * N) {
                 u32x4 d[C], z[Q][C];
 #pragma unroll
-                for (int i = 0; i < C; ++i) d[i] = load_raw<E, false>(dy, c0 + i * 64 * N, P.width);
+                for (int i = 0; i < C; ++i) d[i] = load_raw<E, false>(dy, c0 + i * T * N, P.width);
                 if (P.dweights)
 #pragma unroll
                     for (int q = 0; q < Q; ++q)
                         if (p[q] >= 0)
 #pragma unroll
                             for (int i = 0; i < C; ++i)
-                                z[q][i] = load_raw<E, false>((const E *)P.sorted_in + p[q] * P.ld_sorted, c0 + i * 64 * N, P.width);
+                                z[q][i] = load_raw<E, false>((const E *)P.sorted_in + p[q] * P.ld_sorted, c0 + i * T * N, P.width);
                 float g[C][N];
 #pragma unroll
-                for (int i = 0; i < C; ++i) Piece<E>::unpack(settled<E, false>(d[i], c0 + i * 64 * N, P.width), g[i]);
+                for (int i = 0; i < C; ++i) Piece<E>::unpack(settled<E, false>(d[i], c0 + i * T * N, P.width), g[i]);
 #pragma unroll
                 for (int q = 0; q < Q; ++q) {
                     if (p[q] < 0) continue;
@@ -278,7 +282,7 @@ __global__ __launch_bounds__(MOVE_THREADS) void combine_grad_kernel(Move P)
                     float part = 0.f;
 #pragma unroll
                     for (int i = 0; i < C; ++i) {
-                        const int c = c0 + i * 64 * N;
+                        const int c = c0 + i * T * N;
                         float x[N];
                         if (P.dweights) {
                             Piece<E>::unpack(settled<E, false>(z[q][i], c, P.width), x);
@@ -292,15 +296,98 @@ __global__ __launch_bounds__(MOVE_THREADS) void combine_grad_kernel(Move P)
                     dot[q] += part;
                 }
             }
-            if (P.dweights)
+            if (!P.dweights) continue;
+#pragma unroll
+            for (int q = 0; q < Q; ++q) dot[q] = loss::lanes_sum<64>(dot[q]);
+            if (WAVES > 1) {
+                if ((threadIdx.x & 63) == 0)
+#pragma unroll
+                    for (int q = 0; q < Q; ++q) sums[turn][threadIdx.x >> 6][q] = dot[q];
+                __syncthreads();
+#pragma unroll
                 for (int q = 0; q < Q; ++q) {
-                    const float sum = loss::lanes_sum<64>(dot[q]);
-                    if ((int)(threadIdx.x & 63) == j + q) mine = sum;
+                    dot[q] = sums[turn][0][q];
+                    for (int w = 1; w < WAVES; ++w) dot[q] += sums[turn][w][q];
                 }
+                turn ^= 1;
+            }
+#pragma unroll
+            for (int q = 0; q < Q; ++q)
+                if (t == j + q) mine = dot[q];
         }
-        const int j = threadIdx.x & 63;
-        if (P.dweights && j < count) ((__attribute__((address_space(1))) float *)(uint64_t)P.dweights)[token.row * P.k + j0 + j] = mine;
+        if (P.dweights && t < count) ((__attribute__((address_space(1))) float *)(uint64_t)P.dweights)[row * P.k + j0 + t] = mine;
     }
+}
+
+// Rows of up to 256 bytes: 16 lanes a token, a piece each, and a few slots at a time.  24 x 2351 x 16 fp16
+// with four slots there and back 24.6 us, by a wave a token 50.4.
+constexpr int NARROW_BYTES = 256, NARROW_TOKENS = MOVE_THREADS / 16, NARROW_SLOTS = 4;
+struct NarrowSlots {
+    int64_t place[NARROW_SLOTS];
+    float weight[NARROW_SLOTS];
+    __device__ __forceinline__ NarrowSlots(const Move &P, int64_t row, int j0)
+    {
+        const int64_t first = (uint32_t)row / (uint32_t)P.per_worker * P.slots;
+#pragma unroll
+        for (int q = 0; q < NARROW_SLOTS; ++q) {
+            const int64_t slot = row * P.k + min(j0 + q, P.k - 1);
+            place[q] = ((const __attribute__((address_space(1))) int32_t *)(uint64_t)P.place)[slot];
+            weight[q] = P.weights ? ((const __attribute__((address_space(1))) float *)(uint64_t)P.weights)[slot] : 1.f;
+        }
+#pragma unroll
+        for (int q = 0; q < NARROW_SLOTS; ++q) {
+            const bool there = place[q] >= first && place[q] < first + P.slots;
+            if (place[q] >= 0 && !there) report(P.status);
+            if (!there || j0 + q >= P.k) place[q] = -1;
+        }
+    }
+};
+enum { GATHER, COMBINE, COMBINE_GRAD };
+template <class E, int WHAT>
+__global__ __launch_bounds__(MOVE_THREADS) void narrow_kernel(Move P)
+{
+    constexpr int N = Piece<E>::N;
+    const int64_t row = group_number() * NARROW_TOKENS + (threadIdx.x >> 4);
+    if (row >= P.rows) return;
+    const int c = (threadIdx.x & 15) * N;
+    u32x4 raw = (u32x4)0u;
+    if (WHAT != COMBINE) raw = load_piece<E>((const E *)P.tokens + row * P.ld, c, P.width);
+    float g[N], v[N] = {};
+    Piece<E>::unpack(raw, g);
+    for (int j0 = 0; j0 < P.k; j0 += NARROW_SLOTS) {
+        const NarrowSlots slots(P, row, j0);
+        u32x4 z[NARROW_SLOTS];
+        const bool reads = WHAT == COMBINE || (WHAT == COMBINE_GRAD && P.dweights);
+#pragma unroll
+        for (int q = 0; q < NARROW_SLOTS; ++q) {
+            z[q] = (u32x4)0u;
+            if (reads && slots.place[q] >= 0) z[q] = load_raw<E, false>((const E *)P.sorted_in + slots.place[q] * P.ld_sorted, c, P.width);
+        }
+#pragma unroll
+        for (int q = 0; q < NARROW_SLOTS; ++q) {
+            const bool there = slots.place[q] >= 0;
+            float x[N];
+            Piece<E>::unpack(settled<E, false>(z[q], c, P.width), x);
+            if (WHAT == COMBINE && there)
+#pragma unroll
+                for (int n = 0; n < N; ++n) v[n] = fmaf(slots.weight[q], x[n], v[n]);
+            if (WHAT == COMBINE_GRAD && P.dweights) {
+                float dot = 0.f;
+#pragma unroll
+                for (int n = 0; n < N; ++n) dot = fmaf(g[n], x[n], dot);
+                dot = loss::lanes_sum<16>(dot);
+                if ((threadIdx.x & 15) == 0 && j0 + q < P.k)
+                    ((__attribute__((address_space(1))) float *)(uint64_t)P.dweights)[row * P.k + j0 + q] = there ? dot : 0.f;
+            }
+            if (WHAT != COMBINE && there) {
+                if (WHAT == COMBINE_GRAD)
+#pragma unroll
+                    for (int n = 0; n < N; ++n) x[n] = slots.weight[q] * g[n];
+                store_piece<E>((E *)P.sorted_out + slots.place[q] * P.ld_sorted, c, P.width, WHAT == GATHER ? raw : Piece<E>::pack(x));
+            }
+        }
+    }
+    if (WHAT == COMBINE) store_piece<E>((E *)P.out + row * P.ld, c, P.width, Piece<E>::pack(v));
 }
 
 }  // namespace layer

@@ -296,7 +296,14 @@ int check_move(const dbw_routing *routing, const dbw_rows *shape, const void *to
 }
 dim3 move_grid(int64_t waves) { return grid_of((waves + layer::MOVE_WAVES - 1) / layer::MOVE_WAVES); }
 // Pieces of a lane: rows in chunks of 64 C pieces, a wave each, four pieces a lane where that leaves waves enough.
-constexpr int64_t MOVE_ENOUGH = 4096;
+constexpr int64_t MOVE_ENOUGH = 4096, MOVE_FEW = 1024;
+template <class E, int WHAT>
+bool launch_narrow(int64_t row_bytes, const layer::Move &P, hipStream_t s)
+{
+    if (row_bytes > layer::NARROW_BYTES) return false;
+    hipLaunchKernelGGL((layer::narrow_kernel<E, WHAT>), grid_of((P.rows + layer::NARROW_TOKENS - 1) / layer::NARROW_TOKENS), dim3(layer::MOVE_THREADS), 0, s, P);
+    return true;
+}
 template <class F>
 void by_chunk(int64_t rows, int64_t row_bytes, F f)
 {
@@ -346,6 +353,7 @@ extern "C" int dbw_expert_gather(const dbw_routing *routing, const dbw_rows *sha
     P.tokens = x;
     P.sorted_out = sorted;
     by_type(shape->type, [&](auto e) {
+        if (launch_narrow<decltype(e), layer::GATHER>(S.e * shape->width, P, (hipStream_t)stream)) return;
         by_chunk(S.rows, S.e * shape->width, [&](auto c, int chunks) {
             hipLaunchKernelGGL((layer::gather_kernel<decltype(e), c.value>), move_grid(S.rows * chunks), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P,
                                chunks);
@@ -366,6 +374,7 @@ extern "C" int dbw_expert_combine(const dbw_routing *routing, const dbw_rows *sh
     P.sorted_in = sorted;
     P.out = y;
     by_type(shape->type, [&](auto e) {
+        if (launch_narrow<decltype(e), layer::COMBINE>(S.e * shape->width, P, (hipStream_t)stream)) return;
         by_chunk(S.rows, S.e * shape->width, [&](auto c, int chunks) {
             hipLaunchKernelGGL((layer::combine_kernel<decltype(e), c.value>), move_grid(S.rows * chunks), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P,
                                chunks);
@@ -393,10 +402,13 @@ extern "C" int dbw_expert_combine_grad(const dbw_routing *routing, const dbw_row
     P.dweights = dweights;
     by_type(shape->type, [&](auto e) {
         typedef decltype(e) E;
-        const auto launch = [&](auto kernel) { hipLaunchKernelGGL(kernel, move_grid(S.rows), dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P); };
-        if (S.e * shape->width > 2048) launch(layer::combine_grad_kernel<E, 4>);
-        else if (S.e * shape->width > 1024) launch(layer::combine_grad_kernel<E, 2>);
-        else launch(layer::combine_grad_kernel<E, 1>);
+        const int64_t bytes = S.e * shape->width;
+        if (launch_narrow<E, layer::COMBINE_GRAD>(bytes, P, (hipStream_t)stream)) return;
+        const auto launch = [&](auto kernel, dim3 grid) { hipLaunchKernelGGL(kernel, grid, dim3(layer::MOVE_THREADS), 0, (hipStream_t)stream, P); };
+        if (bytes > 2048 && S.rows <= MOVE_FEW) launch(layer::combine_grad_kernel<E, 2, layer::MOVE_WAVES>, grid_of(S.rows));
+        else if (bytes > 2048) launch(layer::combine_grad_kernel<E, 4, 1>, move_grid(S.rows));
+        else if (bytes > 1024) launch(layer::combine_grad_kernel<E, 2, 1>, move_grid(S.rows));
+        else launch(layer::combine_grad_kernel<E, 1, 1>, move_grid(S.rows));
     });
     DBW_HIP(hipGetLastError());
     return DBW_OK;
