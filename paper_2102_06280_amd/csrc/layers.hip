@@ -68,7 +68,7 @@ int64_t checkpoint_bytes(int64_t rows, int64_t width) { return rows * (layer::pa
 // as its registers hold it: no barriers.  Microseconds, workers x rows x width, bf16 unless said otherwise: forwards 8 x 2048 x 2048 by a wave 23.5, by 256
 // threads, four rows between two barriers, 24.8; 4 x 2048 x 4096 by 256 threads 23.3, by 128 28.5, by 512 28.0; backwards from 8 bits
 // 8 x 2048 x 4096 by 128 threads, two rows at a time, 75.8, by 256 one row at a time 78.7, by 512 79.9.  16 x 64 x 16 fp32 by 16 threads a row, four rows
-// each, 7.9, one each 11.4.
+// each, 7.9, one each 11.4.  4 x 2048 x 12288 backwards by 512 threads 143, by 1024 threads, whose registers do not hold it all, 274.
 template <int T_, int C_, int SLOTS_, int R_>
 struct Plan {
     static constexpr int T = T_, C = C_, SLOTS = SLOTS_, R = R_;
@@ -76,13 +76,13 @@ struct Plan {
 template <bool BACK, class F>
 bool by_row(int64_t bytes, F f)
 {
-    if (bytes <= 16 * 16) f(Plan<16, 1, 16, 4>());
+    if (bytes <= 16 * 16) f(std::conditional_t<BACK, Plan<16, 1, 16, 4>, Plan<16, 1, 16, 1>>());
     else if (bytes <= 64 * 16) f(Plan<64, 1, 4, 1>());
     else if (bytes <= 2 * 64 * 16) f(Plan<64, 2, 4, 1>());
     else if (bytes <= 4 * 64 * 16) f(Plan<64, 4, 4, 1>());
     else if (bytes <= 2 * 256 * 16) f(std::conditional_t<BACK, Plan<128, 4, 2, 1>, Plan<256, 2, 1, 1>>());
     else if (bytes <= 2 * 512 * 16) f(Plan<512, 2, 1, 1>());
-    else if (bytes <= 2 * 1024 * 16) f(Plan<1024, 2, 1, 1>());
+    else if (bytes <= 4 * 512 * 16) f(Plan<512, 4, 1, 1>());
     else return false;
     return true;
 }
