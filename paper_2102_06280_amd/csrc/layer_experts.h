@@ -75,6 +75,7 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_kernel(Sort P)
             if (P.chunks == 1)
                 for (int w = 0; w < SORT_WAVES; ++w) all += count[w * E + e];
             else
+#pragma unroll 8
                 for (int c = 0; c < P.chunks; ++c) {
                     const int n = P.counts[(worker * P.chunks + c) * E + e];
                     all += n;

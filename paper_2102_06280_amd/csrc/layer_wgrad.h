@@ -58,7 +58,7 @@ __device__ __forceinline__ int input_row(const Linear &P, int64_t worker, int32_
 // A workgroup's tile.  Workgroups go to the XCDs in turn, each with an L2 of its own: an XCD gets tiles that follow one another, which read the same rows
 // (4 x 4096 x 2048 x 2048 bf16 145 us, tiles to the XCDs in turn 153).  With experts the work of a workgroup is what its expert has of rows; so
 // every layer's tiles are shared out to all XCDs, and the workers' longest layers come first (2 x 4096 x 1024 x 2048, two of eight experts, the most popular
-// four times as popular as the least NOTE), which a wave finds by counting, up to 64 experts.
+// four times as popular as the least: 140 us, in the experts' own order 174), which a wave finds by counting, up to 64 experts.
 constexpr int XCDS = 8, SORTED_EXPERTS = 64;
 struct Share {
     int64_t worker;
@@ -216,7 +216,10 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     const int64_t worker = mine.worker;
     const int o0 = tile / P.tiles_in * T::OUT, i0 = tile % P.tiles_in * T::IN;
     Range range = mine.range;
-    if (P.tokens == 0) range.end = range.first;           // (of which none is a row's)
+    if (P.tokens == 0 && range.end > range.first) {       // (no row of the checkpoint is any of these rows')
+        range.end = range.first;
+        report(P.status);
+    }
     if (P.splits > 1) {
         const int64_t part = ((range.end - range.first + P.splits - 1) / P.splits + T::STEP - 1) / T::STEP * T::STEP;
         range.first = min(range.first + split * part, range.end);

@@ -264,8 +264,14 @@ extern "C" int dbw_layer_norm_grad(const dbw_rows *shape, const void *dy, const 
 
 namespace {
 
-constexpr int SORT_CHUNK = 1024;                          // slots of a workgroup
-int chunks_of(const dbw_routing *l) { return (int)(((int64_t)l->tokens * l->k + SORT_CHUNK - 1) / SORT_CHUNK); }
+// Slots of a workgroup, of which a worker has 256 at most: each of them adds up what all of them counted.
+constexpr int SORT_CHUNK = 1024, SORT_CHUNKS = 256;
+int chunk_of(const dbw_routing *l)
+{
+    const int64_t each = ((int64_t)l->tokens * l->k + SORT_CHUNKS - 1) / SORT_CHUNKS;
+    return each > SORT_CHUNK ? (int)each : SORT_CHUNK;
+}
+int chunks_of(const dbw_routing *l) { return (int)(((int64_t)l->tokens * l->k + chunk_of(l) - 1) / chunk_of(l)); }
 
 int check_routing(const dbw_routing *l)
 {
@@ -319,7 +325,7 @@ extern "C" int64_t dbw_expert_work_bytes(const dbw_routing *routing)
 {
     const int rc = check_routing(routing);
     if (rc != DBW_OK) return rc;
-    const int64_t chunks = chunks_of(routing);
+    const int64_t chunks = routing->tokens > 0 ? chunks_of(routing) : 1;
     return 16 + (chunks > 1 ? routing->workers * chunks * routing->experts * 4 : 0);
 }
 
@@ -332,7 +338,7 @@ extern "C" int dbw_expert_sort(const dbw_routing *routing, const int32_t *expert
     if (!start_out || !work || (slots > 0 && (!expert || !place_out || !source_out))) return DBW_ERR_NULL;
     if (off(work, 16)) return DBW_ERR_INVALID;
     const int chunks = slots > 0 ? chunks_of(routing) : 1;
-    const layer::Sort P{expert, start_out, place_out, source_out, status_out, (int32_t *)work, routing->workers, (int)slots, routing->experts, SORT_CHUNK,
+    const layer::Sort P{expert, start_out, place_out, source_out, status_out, (int32_t *)work, routing->workers, (int)slots, routing->experts, chunk_of(routing),
                         chunks};
     hipStream_t s = (hipStream_t)stream;
     const dim3 grid = grid_of((int64_t)routing->workers * chunks), block(layer::SORT_THREADS);

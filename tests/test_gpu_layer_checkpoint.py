@@ -264,3 +264,78 @@ def test_on_another_stream_captured_and_twice_the_same(B):
             graph.replay()
             torch.cuda.synchronize()
             assert torch.equal(grads, again)
+
+
+# --------------------------------------------------------------------------- tiles of every size
+
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("workers,rows,width,out,experts,k,pad", [
+    (64, 40, 256, 256, 4, 2, 0), (32, 70, 300, 270, 0, 1, 1), (3, 100, 4097, 1100, 0, 1, 0), (70, 5, 257, 300, 3, 1, 3),       # a workgroup's tile 256 wide
+    (40, 30, 200, 200, 4, 2, 0), (45, 64, 129, 255, 3, 2, 1), (1, 8200, 1000, 1030, 0, 1, 0),                                   # 128 wide; and in parts
+    (1, 3000, 512, 200, 0, 1, 0), (2, 2500, 33, 100, 2, 2, 0), (300, 33, 65, 64, 70, 1, 0)])                                    # 64; in parts; more experts than are sorted
+def test_tiles_of_every_size(B, dtype, workers, rows, width, out, experts, k, pad):
+    """Against 64 bits on the GPU, inputs as in Layer: the bound is that of Layer.check()."""
+    g = torch.Generator(device="cuda").manual_seed(workers * 7 + width)
+    randn = lambda *s: torch.randn(*s, device="cuda", generator=g)
+    r, e = rows * k, max(experts, 1)
+    x = randn(workers * rows, width).to(BF16)
+    shape = B.make_rows(workers, rows, width, BF16)
+    kept = torch.empty(B.dbw_checkpoint_bytes(shape), dtype=torch.uint8, device="cuda")
+    B.dbw_checkpoint_store(shape, x, kept)
+    B.dbw_checkpoint_load(shape, kept, x)
+    x = x.double()
+    flat = torch.full((workers * r, out + pad), math.nan, dtype=dtype, device="cuda")
+    flat[:, :out] = randn(workers * r, out).to(dtype)
+    start = source = None
+    if experts:
+        expert = torch.randint(-1, experts, (workers * r,), device="cuda", generator=g).int()
+        expert[:k * rows // 2] = experts - 1
+        routing = B.make_routing(workers, rows, k, experts)
+        start = torch.empty(workers * (experts + 1), dtype=torch.int32, device="cuda")
+        place, source = (torch.empty(workers * r, dtype=torch.int32, device="cuda") for _ in range(2))
+        B.dbw_expert_sort(routing, expert, start, place, source, torch.empty(B.dbw_expert_work_bytes(routing), dtype=torch.uint8, device="cuda"))
+        flat[source < 0] = math.nan
+    linear = B.make_linear(workers, r, width, out, dtype, experts=e, tokens=rows, k=k, ld=out + pad)
+    work = torch.full((B.dbw_checkpoint_weight_grad_work_bytes(linear),), 255, dtype=torch.uint8, device="cuda")
+    count = e * out
+    grads = torch.full((workers, count * width + count + 7), MARK, device="cuda")
+
+    def run():
+        B.dbw_checkpoint_weight_grad(linear, flat, kept, grads, work, 1, bias_at=count * width + 4, start=start, source=source)
+
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.stream(s):
+        with torch.cuda.graph(graph, stream=s):
+            run()
+    for _ in range(2):
+        grads.fill_(MARK)
+        graph.replay()
+        torch.cuda.synchronize()
+    replayed = grads.clone()
+    grads.fill_(MARK)
+    run()
+    assert torch.equal(grads, replayed)
+    assert (grads[:, 0] == MARK).all() and (grads[:, 1 + count * width:4 + count * width] == MARK).all() and (grads[:, -3:] == MARK).all()
+    weight = grads[:, 1:1 + count * width].view(workers, e, out, width)
+    bias = grads[:, 4 + count * width:4 + count * width + count].view(workers, e, out)
+    starts = start.tolist() if experts else None
+    for i in sorted({0, workers // 2, workers - 1}):
+        for c in sorted({0, e // 2, e - 1}):
+            a, z = starts[i * (e + 1) + c:i * (e + 1) + c + 2] if experts else (i * r, (i + 1) * r)
+            d = flat[a:z, :out].double()
+            u = x[source[a:z].long() // k] if experts else x[a:z]
+            steps = 2 * ref.U * (z - a + 8)
+            for got, want, size in ((weight[i, c], d.t().contiguous() @ u, d.t().abs().contiguous() @ u.abs()), (bias[i, c], d.sum(0), d.abs().sum(0))):
+                assert ((got.double() - want).abs() <= 1.01 * steps * size + ref.U * want.abs() + 1e-40).all(), (i, c)
+
+
+def test_a_checkpoint_of_no_tokens_is_reported(B):
+    linear = B.make_linear(1, 3, 8, 5, F32, tokens=0)
+    grads = torch.full((1, 45), MARK, device="cuda")
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    B.dbw_checkpoint_weight_grad(linear, torch.ones(15, device="cuda"), torch.empty(0, dtype=torch.uint8, device="cuda"), grads,
+                                 torch.empty(B.dbw_checkpoint_weight_grad_work_bytes(linear), dtype=torch.uint8, device="cuda"), 0, bias_at=40,
+                                 source=torch.zeros(3, dtype=torch.int32, device="cuda"), status_out=status)
+    assert (grads == 0).all() and status.item() == B.ERR_INVALID

@@ -31,7 +31,7 @@ def run_sort(B, expert, workers, tokens, k, experts):
 
 @pytest.mark.parametrize("workers,tokens,k,experts", [(1, 1, 1, 1), (2, 3, 2, 4), (1, 64, 1, 2), (3, 65, 1, 3), (1, 1, 8, 8), (5, 100, 3, 17), (2, 511, 2, 64), (1, 4096, 1, 5),
                                                       (2, 4097, 1, 100), (3, 5000, 2, 16), (1, 20000, 3, 600), (40, 7, 4, 1024), (1, 9000, 1, 1024), (1, 300, 1, 512),
-                                                      (2, 300, 40, 513)])
+                                                      (1, 300000, 1, 40),                                                       (2, 300, 40, 513)])
 @pytest.mark.parametrize("some", ["all", "few", "one", "none"])
 def test_sort(B, workers, tokens, k, experts, some):
     g = torch.Generator().manual_seed(tokens * 31 + experts)
