@@ -28,7 +28,6 @@ struct Linear {
     int64_t workers;
     int rows, in, out, experts, tokens, k;                // rows, tokens: of a worker
     int tiles_out, tiles_in, splits;
-    bool cached;                                          // results go through the caches
     float *parts;                                         // [split][weights of all layers, then their biases], where the rows are split
 };
 // The rows of dy of a worker's layer.
@@ -421,24 +420,31 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     const int64_t all = P.workers * P.experts;
     float *const to = P.splits > 1 ? P.parts + split * all * (weights + P.out) + layer * weights
                                    : P.grads + worker * P.ld_grads + P.weight_at + expert * weights;
-    const auto write = [&](auto cached) {
-        const int l = t & 63;
+    // Sums go through LDS, 32 rows of every wave row at a time, and from there to memory as whole rows of the tile.  (From the registers, 32 columns
+    // of two rows at a time, 12 x 1 x 279 x 2960 with 22 experts 448 us instead of 310: the lines that rows share were written in parts.  Past the caches:
+    // two of eight experts 2 x 4096 x 1024 x 2048 bf16 100 us, through them 130.)
+    constexpr int PITCH = T::IN + 8;                      // floats: the two rows that a wave writes at a time lie on different banks
+    static_assert(T::WO * 32 * PITCH * 4 <= BUFFERS * BUFFER, "room for them");
+    float *const held = (float *)shared;                  // [WO * 32][PITCH]
+    const int l = t & 63;
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+    for (int i = 0; i < MI; ++i) {
+        if (i > 0) __syncthreads();
 #pragma unroll
-            for (int v = 0; v < 16; ++v) {
-                const int o = o0 + wo + 32 * i + 8 * (v / 4) + 4 * (l >> 5) + v % 4;
+        for (int v = 0; v < 16; ++v)
 #pragma unroll
-                for (int j = 0; j < NI; ++j) {
-                    const int c = i0 + wi + 32 * j + (l & 31);
-                    if (o >= P.out || c >= P.in) continue;
-                    if constexpr (decltype(cached)::value) to[(int64_t)o * P.in + c] = acc[i][j][v];
-                    else __builtin_nontemporal_store(acc[i][j][v], to + (int64_t)o * P.in + c);
-                }
-            }
-    };
-    if (P.cached) write(std::true_type());
-    else write(std::false_type());
+            for (int j = 0; j < NI; ++j)
+                held[(wave / T::WI * 32 + 8 * (v / 4) + 4 * (l >> 5) + v % 4) * PITCH + wi + 32 * j + (l & 31)] = acc[i][j][v];
+        __syncthreads();
+        constexpr int EACH = T::IN / 4, AT_ONCE = T::THREADS / EACH;
+#pragma unroll
+        for (int r0 = 0; r0 < T::WO * 32; r0 += AT_ONCE) {
+            const int r = r0 + t / EACH, c = t % EACH * 4, o = o0 + r / 32 * (T::OUT / T::WO) + 32 * i + r % 32;
+            if (o >= P.out) continue;
+            const u32x4 w = *(const u32x4 *)(held + r * PITCH + c);
+            store_piece<float>(to + (int64_t)o * P.in + i0, c, P.in - i0, w);
+        }
+    }
     if (with_bias) {
         // the sums of the threads that have the same columns, in their order
         float *const sums = (float *)shared;              // [A_ROWS][OUT]

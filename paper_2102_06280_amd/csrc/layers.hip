@@ -504,14 +504,10 @@ extern "C" int dbw_checkpoint_weight_grad(const dbw_linear *shape, const void *d
     if (too_long(ld_grads, shape->workers)) return DBW_ERR_UNSUPPORTED;
     const int64_t tokens = (int64_t)shape->workers * shape->tokens;
     const Cut cut = cut_of(shape);
-    // Past the caches (two of eight experts 2 x 4096 x 1024 x 2048 bf16 98 us, through them 127), but for rows that share their lines of 128 bytes with the
-    // next and all of which the last-level cache holds, where a line's parts come together (13 x 14 x 809 x 171, 16 experts, 115 MB, 42 and past them
-    // 59; but 5 x 161 x 2097 x 2192, 8 experts, fp16, 735 MB, 357 and 266).
-    const bool cached = shape->inputs % 32 != 0 && 4 * weights * shape->workers <= (int64_t)256 << 20;
     const int64_t groups = cut.tiles_out * cut.tiles_in * cut.layers * cut.splits;
     const layer::Linear P{dy, layer::kept_of((void *)checkpoint, tokens, shape->inputs), start, source, status_out, grads, ld, ld_grads, weight_at,
                           bias_at, shape->workers, shape->rows, shape->inputs, shape->outputs, shape->experts, shape->tokens, shape->k, (int)cut.tiles_out,
-                          (int)cut.tiles_in, cut.splits, cached, (float *)work};
+                          (int)cut.tiles_in, cut.splits, (float *)work};
     hipStream_t s = (hipStream_t)stream;
     bool fits = true;
     by_type(shape->type, [&](auto v) {
