@@ -45,7 +45,8 @@ __global__ __launch_bounds__(SORT_THREADS) void sort_count_kernel(Sort P)
 
 // A chunk's slots to their rows.  A wave has a contiguous part of the chunk and counts its experts; an expert's rows begin behind those of
 // smaller ones, within them a chunk's behind earlier chunks', a wave's behind earlier waves', and a lane's behind the lower lanes that name
-// the same expert.  Counts are integers: nothing depends on the order of the atomics.
+// the same expert.  Counts are integers: nothing depends on the order of the atomics.  The latency of two launches bounds it (4 x 8192 slots 4.6 and 5.1 us), or
+// of one (a chunk's slots or fewer, 3.9).
 __global__ __launch_bounds__(SORT_THREADS) void sort_kernel(Sort P)
 {
     extern __shared__ int32_t count[];                    // [waves][E], and a number a wave
@@ -143,6 +144,8 @@ struct Move {
     int per_worker, width, k;
 };
 
+// Memory bounds all of these: 4 x 4096 x 2048 bf16, two of 16 experts, gathered in 36 us (201 MB, 5.6 TB/s), combined in 36 (5.6), gradient 60 (336 MB, 5.6).
+//
 // A wave has a token, or some of its columns, C pieces a lane at a time.  Of up to 64 slots of the token each lane has one: its sorted row, or -1, and its
 // weight, which go to the whole wave when they are used.
 constexpr int MOVE_WAVES = 4, MOVE_THREADS = 64 * MOVE_WAVES;

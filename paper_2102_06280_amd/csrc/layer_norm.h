@@ -60,6 +60,8 @@ struct Ahead {
 // group at a time, with the weights in registers and the next rows on their way; the rows' sums share their barriers.  The mean comes first, then the
 // sums of the differences from it and of their squares: the first of these is what the rounding of the mean left, which counts where a row's mean is
 // large beside its spread.
+//
+// Memory bounds it: 8 x 2048 x 2048 bf16 23.5 us, keeping 8 bits too 28.5 (134 and 168 MB, 5.7 and 5.9 TB/s), one row of 4096 3.5 us.
 template <class E, int T, int C, int SLOTS, int R>
 __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P)
 {
@@ -297,7 +299,8 @@ __device__ __forceinline__ float *part_of(const NormGrad &P, int worker, int str
 }
 
 // As norm_kernel; every thread's columns are the same in all rows, so that it sums dw and db in registers.  Rows that take no part are zeros with a mean and
-// a scale of zero.
+// a scale of zero.  Memory bounds long batches (8 x 8192 x 2048 bf16 from 8 bits 133 us, 5.0 TB/s); shorter ones pay some 8 us for the first rows' way and
+// for adding up (8 x 2048 x 2048 37 us).
 template <class E, int T, int C, int SLOTS, int R, bool KEPT>
 __global__ __launch_bounds__(T * SLOTS) void norm_grad_kernel(NormGrad P)
 {
@@ -547,6 +550,8 @@ struct Store {
     int width;
     Kept kept;
 };
+// Memory bounds both: 4 x 4096 x 4096 bf16 36.7 and 29.2 us (203 MB each, 5.5 and 7.0 TB/s, the codes still in the last-level cache for the second).
+//
 // A workgroup has STORE_PIECES x STORE_THREADS pieces that follow one another, a thread every STORE_THREADS-th; a row is a multiple of the pieces of a
 // block.  4 x 4096 x 4096 bf16 stored and loaded with one, two and four pieces a thread 73, 67.6 and 71 us.
 constexpr int STORE_THREADS = 256, STORE_PIECES = 2;
