@@ -144,7 +144,8 @@ struct Planes<f16> {                                      // 11 bits: the neares
     }
 };
 template <>
-struct Planes<float> {                                    // 24 bits: the upper eight towards zero, so that they stay finite, the nearest eight of the rest, what is left
+struct Planes<float> {                                    // 24 bits: the upper eight towards zero, so that they stay finite, the nearest eight of the rest,
+                                                          // and what is left
     static constexpr int COUNT = 3;
     static __device__ __forceinline__ void split(const u32x4 &w, u32x2 (&p)[3])
     {

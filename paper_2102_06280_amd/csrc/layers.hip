@@ -178,7 +178,8 @@ extern "C" int dbw_layer_norm(const dbw_rows *shape, const void *x, const uint8_
     if (!(x == y && S.ld == S.ld_out) && overlap(x, S.rows, S.ld, y, S.rows, S.ld_out, shape->width, S.e)) return DBW_ERR_ALIAS;
     if (S.rows == 0) return DBW_OK;
     const int strips = strips_of(shape, rows_at_once<false>(shape, S), NORM_GROUPS, 1);
-    layer::Norm P{x, mask, params, S.ld, S.ld_out, ld_params, weight_at, bias_at, S.rows, shape->rows, shape->width, shape->workers, strips, eps, y, stats_out, kept_of(checkpoint, S, shape)};
+    layer::Norm P{x, mask, params, S.ld, S.ld_out, ld_params, weight_at, bias_at, S.rows, shape->rows, shape->width, shape->workers, strips, eps, y,
+                  stats_out, kept_of(checkpoint, S, shape)};
     if (!checkpoint) P.kept.codes = nullptr;
     hipStream_t s = (hipStream_t)stream;
     by_type(shape->type, [&](auto e) {
@@ -461,7 +462,8 @@ Cut cut_of(const dbw_linear *l)
     const int64_t rows = l->rows / l->experts;
     int64_t groups = 0;
     for (c.tile = 2; c.tile >= 0; --c.tile) {
-        const int out = c.tile == 2 ? (l->type == DBW_TYPE_BF16 ? Large::OUT : LargeSplit::OUT) : c.tile == 1 ? (l->type == DBW_TYPE_BF16 ? Middle::OUT : MiddleSplit::OUT) : Small::OUT;
+        const bool whole = l->type == DBW_TYPE_BF16;
+        const int out = c.tile == 2 ? (whole ? Large::OUT : LargeSplit::OUT) : c.tile == 1 ? (whole ? Middle::OUT : MiddleSplit::OUT) : Small::OUT;
         const int in = c.tile == 2 ? Large::IN : c.tile == 1 ? Middle::IN : Small::IN;
         c.tiles_out = (l->outputs + out - 1) / out;
         c.tiles_in = (l->inputs + in - 1) / in;

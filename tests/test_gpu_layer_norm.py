@@ -214,6 +214,25 @@ def test_on_another_stream_and_twice_the_same(B):
     assert torch.equal(y.flat, y2.flat) and torch.equal(dx.flat, dx2.flat) and torch.equal(grads, grads2)
 
 
+def test_two_calls_at_once_and_masks_of_truth_values(B):
+    """On two streams, with outputs and scratch memory of their own."""
+    a, b = Case(B, BF16, 2, 900, 2048, seed=11), Case(B, F32, 3, 400, 500, seed=12)
+    a.mask_arg = a.mask_arg.bool()
+    want = [(c.forward().flat.clone(), *(v if torch.is_tensor(v) else v.flat for v in c.backward())) for c in (a, b)]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    got = [None, None]
+    for turn in range(3):
+        for i, c in enumerate((a, b)):
+            with torch.cuda.stream(streams[i]):
+                y = c.forward()
+                dx, grads = c.backward()
+                got[i] = (y.flat, dx.flat, grads)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert all(torch.equal(x, w) for x, w in zip(got[i], want[i]))
+
+
 @pytest.mark.parametrize("width", [100, 2048, 20000])
 def test_captured_and_replayed(B, width):
     c = Case(B, BF16, 2, 200, width, seed=10)
