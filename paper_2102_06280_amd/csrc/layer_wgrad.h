@@ -127,8 +127,8 @@ __device__ __forceinline__ uint32_t nearest(float a, float b)
 }
 __device__ __forceinline__ float low_half(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float high_half(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
-// What is left of v without its larger part; nothing of an infinity.
-__device__ __forceinline__ float rest_of(float v, float part) { return fabsf(v) < INFINITY ? v - part : 0.f; }
+// What is left of v without its larger part; nothing of an infinity, and of NaN NaN (whose upper half may be that of an infinity).
+__device__ __forceinline__ float rest_of(float v, float part) { return fabsf(v) == INFINITY ? 0.f : v - part; }
 template <>
 struct Planes<f16> {                                      // 11 bits: the nearest eight and what is left
     static constexpr int COUNT = 2;

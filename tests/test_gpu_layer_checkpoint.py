@@ -237,6 +237,22 @@ def test_nan_stays_in_its_columns(B):
     assert torch.isnan(weight[11]).all() and torch.isnan(weight).sum() == 70 and torch.isnan(bias).sum() == 1 and torch.isnan(bias[11])
 
 
+@pytest.mark.parametrize("dtype,bits", [(F32, (0x7f800001, -0x7f0001, 0x7fffffff)), (F16, (0x7c01, -0x3ff, 0x7fff)), (BF16, (0x7f81, -0x7f, 0x7fff))])
+def test_every_nan_is_one(B, dtype, bits):
+    """Also those whose upper bits alone are an infinity's."""
+    c = Layer(B, dtype, 1, 40, 33, 70, seed=8)
+    dy = c.dy.values.clone()
+    for i, b in enumerate(bits):
+        dy.view(torch.int32 if dtype == F32 else torch.int16)[5 + i, 20 * i] = b
+    assert torch.isnan(dy).sum() == len(bits)
+    c.dy = Rows(dy)
+    got = c.run().cpu()
+    weight, bias = got[0, 3:3 + 70 * 33].view(70, 33), got[0, c.bias_at:c.bias_at + 70]
+    for rows in (weight, bias):
+        nan = torch.isnan(rows).view(70, -1)
+        assert nan[0:60:20].all() and nan.sum() == len(bits) * nan.shape[1]
+
+
 def test_on_another_stream_captured_and_twice_the_same(B):
     for kw in (dict(), dict(experts=4, k=2)):
         c = Layer(B, BF16, 2, 300, 100, 200, seed=7, **kw)
