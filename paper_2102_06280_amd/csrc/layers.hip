@@ -69,6 +69,9 @@ int64_t checkpoint_bytes(int64_t rows, int64_t width) { return rows * (layer::pa
 // threads, four rows between two barriers, 24.8; 4 x 2048 x 4096 by 256 threads 23.3, by 128 28.5, by 512 28.0; backwards from 8 bits
 // 8 x 2048 x 4096 by 128 threads, two rows at a time, 75.8, by 256 one row at a time 78.7, by 512 79.9.  16 x 64 x 16 fp32 by 16 threads a row, four rows
 // each, 7.9, one each 11.4.  4 x 2048 x 12288 backwards by 512 threads 143, by 1024 threads, whose registers do not hold it all, 274.
+// Three pieces a thread where they hold the row: forwards, and backwards from 8 bits, 8 x 2048 x 1536 19.1 and 26.5, with four pieces 23.4 and 29.3; 16 x 1779 x
+// 2983 by 128 threads 75 and 91, by 256 with two pieces 79 and by 128 with four 147; 8 x 2048 x 5296 by 256 threads 73 and 98, by 512 with two 77 and 126;
+// 4 x 2048 x 12288 by 512 87 and 118, with four 105 and 176.
 template <int T_, int C_, int SLOTS_, int R_>
 struct Plan {
     static constexpr int T = T_, C = C_, SLOTS = SLOTS_, R = R_;
@@ -79,9 +82,13 @@ bool by_row(int64_t bytes, F f)
     if (bytes <= 16 * 16) f(std::conditional_t<BACK, Plan<16, 1, 16, 4>, Plan<16, 1, 16, 1>>());
     else if (bytes <= 64 * 16) f(Plan<64, 1, 4, 1>());
     else if (bytes <= 2 * 64 * 16) f(Plan<64, 2, 4, 1>());
+    else if (bytes <= 3 * 64 * 16) f(Plan<64, 3, 4, 1>());
     else if (bytes <= 4 * 64 * 16) f(Plan<64, 4, 4, 1>());
+    else if (bytes <= 3 * 128 * 16) f(Plan<128, 3, 2, 1>());
     else if (bytes <= 2 * 256 * 16) f(std::conditional_t<BACK, Plan<128, 4, 2, 1>, Plan<256, 2, 1, 1>>());
+    else if (bytes <= 3 * 256 * 16) f(Plan<256, 3, 1, 1>());
     else if (bytes <= 2 * 512 * 16) f(Plan<512, 2, 1, 1>());
+    else if (bytes <= 3 * 512 * 16) f(Plan<512, 3, 1, 1>());
     else if (bytes <= 4 * 512 * 16) f(Plan<512, 4, 1, 1>());
     else return false;
     return true;

@@ -124,6 +124,22 @@ def test_many_rows_and_long_ones(B, dtype, workers, rows, width, pad, kept):
     c.check_backward(*c.backward(checkpoint=checkpoint), x=x)
 
 
+# on either side of what 64, 128, 256 and 512 threads hold in one to four pieces of 16 bytes
+@pytest.mark.parametrize("dtype", TYPES)
+@pytest.mark.parametrize("pieces", [64, 128, 192, 256, 384, 512, 768, 1024, 1536, 2048])
+@pytest.mark.parametrize("more", [-3, 0, 1])
+def test_rows_as_long_as_registers(B, dtype, pieces, more):
+    width = pieces * (4 if dtype == F32 else 8) + more
+    c = Case(B, dtype, 2, 37, width, pad=1 - more % 2, seed=12)
+    checkpoint = torch.full((B.dbw_checkpoint_bytes(c.shape),), 255, dtype=torch.uint8, device="cuda")
+    c.check_forward(c.forward(checkpoint=checkpoint), f"{width}")
+    own = torch.full_like(checkpoint, 99)
+    B.dbw_checkpoint_store(c.shape, c.x.arg, own, mask=c.mask_arg)
+    assert torch.equal(checkpoint, own)
+    c.check_backward(*c.backward(), what=f"{width}")
+    c.check_backward(*c.backward(checkpoint=checkpoint), what=f"{width} kept", x=ref.kept(torch.where(c.on[:, None], c.x.values, 0)))
+
+
 @pytest.mark.parametrize("dtype", TYPES)
 @pytest.mark.parametrize("weight,bias", [(False, False), (True, False), (False, True)])
 @pytest.mark.parametrize("width", [20, 3000, 40000])
