@@ -457,25 +457,37 @@ struct Cut {
     int64_t tiles_out, tiles_in, layers;
     int splits;
 };
-// Large tiles where they fill the chip.  Else middle ones where there are two for a compute unit or so much to do that splitting the rows pays: 1 x 4096 x
+// Of the tiles that fill the chip, the one whose tiles take least time for all of the weights, in the time that a large one takes for its area, a hundredth as
+// the unit: 4 x 1024 rows a layer, 16 layers of 1024 x 1024, large, middle and small tiles bf16 200, 228 and 397 us, fp16 340, 399 and 721, fp32 477, 697
+// and 881.  Layers of few rows are bound by a tile's latency, which middle tiles hide better, two and more to a compute unit: 8 x 16 layers bf16 of 64 rows 119 and
+// 106, of 128 137 and 129, of 256 176 and 174 (fp16 of 64 146 and 151).
+//
+// Large tiles fill the chip with one for each compute unit; middle ones with two, or where there is so much to do that splitting the rows pays: 1 x 4096 x
 // 2048 x 2048 bf16 67.7 us (small tiles 82, large ones 71.9), 1 x 8192 x 1024 x 1024 40.9 (50, 53), but 8 x 1024 x 512 x 512 29 and small ones
-// 15.3, 2 x 1024 x 768 x 2304 34 and 25.4.  Parts have 512 rows at least: 2 x 512 x 500 x 700 fp32 whole 15.8, in halves 26.6.
-constexpr int64_t CHIP = 256, MUCH = 400000, PART = 512;
+// 15.3, 2 x 1024 x 768 x 2304 34 and 25.4.  Small ones are taken where neither does.  Parts have 512 rows at least: 2 x 512 x 500 x 700 fp32 whole 15.8, in halves 26.6.
+constexpr int64_t CHIP = 256, MUCH = 400000, PART = 512, FEW_ROWS = 128;
 Cut cut_of(const dbw_linear *l)
 {
+    const bool whole = l->type == DBW_TYPE_BF16, thirds = l->type == DBW_TYPE_F32;
+    const int64_t rows = l->rows / l->experts, layers = (int64_t)l->workers * l->experts;
+    const int outs[3] = {Small::OUT, whole ? Middle::OUT : MiddleSplit::OUT, whole ? Large::OUT : LargeSplit::OUT}, ins[3] = {Small::IN, Middle::IN, Large::IN};
+    const int price[3] = {thirds ? 185 : 200, thirds ? 145 : whole && rows <= FEW_ROWS ? 90 : 115, 100};
     Cut c;
-    c.layers = (int64_t)l->workers * l->experts;
+    c.tile = -1;
+    c.layers = layers;
     c.splits = 1;
-    const int64_t rows = l->rows / l->experts;
+    double least = 0;
     int64_t groups = 0;
-    for (c.tile = 2; c.tile >= 0; --c.tile) {
-        const bool whole = l->type == DBW_TYPE_BF16;
-        const int out = c.tile == 2 ? (whole ? Large::OUT : LargeSplit::OUT) : c.tile == 1 ? (whole ? Middle::OUT : MiddleSplit::OUT) : Small::OUT;
-        const int in = c.tile == 2 ? Large::IN : c.tile == 1 ? Middle::IN : Small::IN;
-        c.tiles_out = (l->outputs + out - 1) / out;
-        c.tiles_in = (l->inputs + in - 1) / in;
-        groups = c.tiles_out * c.tiles_in * c.layers;
-        if (c.tile == 0 || (c.tile == 2 && groups >= CHIP) || (c.tile == 1 && (groups >= 2 * CHIP || groups * rows >= MUCH))) break;
+    for (int tile = 2; tile >= 0; --tile) {
+        const int64_t out = (l->outputs + outs[tile] - 1) / outs[tile], in = (l->inputs + ins[tile] - 1) / ins[tile], n = out * in * layers;
+        const bool fills = tile == 2 ? n >= CHIP : tile == 1 ? n >= 2 * CHIP || n * rows >= MUCH : n >= CHIP || c.tile < 0;
+        const double cost = (double)price[tile] * outs[tile] * ins[tile] * n;
+        if (!fills || (c.tile >= 0 && cost >= least)) continue;
+        c.tile = tile;
+        c.tiles_out = out;
+        c.tiles_in = in;
+        groups = n;
+        least = cost;
     }
     if (groups < (c.tile == 1 ? 2 * CHIP : CHIP)) {
         int64_t splits = 2 * CHIP / groups;

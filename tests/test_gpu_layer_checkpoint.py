@@ -288,7 +288,9 @@ def test_on_another_stream_captured_and_twice_the_same(B):
 @pytest.mark.parametrize("workers,rows,width,out,experts,k,pad", [
     (64, 40, 256, 256, 4, 2, 0), (32, 70, 300, 270, 0, 1, 1), (3, 100, 4097, 1100, 0, 1, 0), (70, 5, 257, 300, 3, 1, 3),       # a workgroup's tile 256 wide
     (40, 30, 200, 200, 4, 2, 0), (45, 64, 129, 255, 3, 2, 1), (1, 8200, 1000, 1030, 0, 1, 0),                                   # 128 wide; and in parts
-    (1, 3000, 512, 200, 0, 1, 0), (2, 2500, 33, 100, 2, 2, 0), (300, 33, 65, 64, 70, 1, 0)])         # 64; in parts; more experts than are sorted
+    (1, 3000, 512, 200, 0, 1, 0), (2, 2500, 33, 100, 2, 2, 0), (300, 33, 65, 64, 70, 1, 0),          # 64; in parts; more experts than are sorted
+    (32, 150, 500, 1024, 0, 1, 1), (64, 300, 250, 256, 4, 2, 0), (30, 280, 500, 1000, 2, 1, 0),                                 # 256 wide, of more rows
+    (16, 64, 64, 64, 16, 2, 0), (40, 100, 100, 48, 16, 1, 1), (256, 40, 130, 30, 0, 1, 0)])                                     # many layers within a tile
 def test_tiles_of_every_size(B, dtype, workers, rows, width, out, experts, k, pad):
     """Against 64 bits on the GPU, inputs as in Layer: the bound is that of Layer.check()."""
     g = torch.Generator(device="cuda").manual_seed(workers * 7 + width)
