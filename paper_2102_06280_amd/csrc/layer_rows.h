@@ -90,13 +90,15 @@ __device__ __forceinline__ u32x4 load_piece(const E *row, int c, int width)
 {
     return settled<E, WIDE>(load_raw<E, WIDE>(row, c, width), c, width);
 }
-template <class E>
+// And back, past the caches or through them.
+template <class E, bool PAST = true>
 __device__ __forceinline__ void store_piece(E *row, int c, int width, const u32x4 &w)
 {
     typedef __attribute__((address_space(1))) typename Piece<E>::raw *place;
     constexpr int N = Piece<E>::N;
     if (c + N <= width) {
-        __builtin_nontemporal_store((typename Piece<E>::raw)w, (place)(uint64_t)(row + c));
+        if constexpr (PAST) __builtin_nontemporal_store((typename Piece<E>::raw)w, (place)(uint64_t)(row + c));
+        else *(place)(uint64_t)(row + c) = (typename Piece<E>::raw)w;
         return;
     }
     if (c >= width) return;

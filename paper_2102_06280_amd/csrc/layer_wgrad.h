@@ -198,7 +198,7 @@ struct Tile {
     static constexpr int OUT = OUT_, IN = IN_, WO = WO_, WI = WI_, STEP = STEP_;
     static constexpr int THREADS = 64 * WO * WI;
 };
-constexpr int BUFFERS = 3;
+constexpr int BUFFERS = 3, LINE = 128;                    // LINE: bytes of a cache line
 template <class E, class T>
 constexpr int tile_lds() { return BUFFERS * T::STEP * 2 * (Planes<E>::COUNT * T::OUT + T::IN) + 4 * T::STEP * 4; }
 
@@ -428,12 +428,15 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
     float *const to = P.splits > 1 ? P.parts + split * all * (weights + P.out) + layer * weights
                                    : P.grads + worker * P.ld_grads + P.weight_at + expert * weights;
     // Sums go through LDS, 32 rows of every wave row at a time, and from there to memory as whole rows of the tile.  (From the registers, 32 columns
-    // of two rows at a time, 12 x 1 x 279 x 2960 with 22 experts 448 us instead of 310: the lines that rows share were written in parts.  Past the caches:
-    // two of eight experts 2 x 4096 x 1024 x 2048 bf16 100 us, through them 130.)
+    // of two rows at a time, 12 x 1 x 279 x 2960 with 22 experts 448 us instead of 269: the lines that rows share were written in parts.)  Rows of whole lines go past
+    // the caches, others through them, where lines that tiles share are put together: bf16, past and through, 12 x 22 layers of 4 x 512 x 2960 270 and
+    // 348 us, with weights that begin 4 or 32 bytes behind a line 512 and 367; of 4 x 279 x 2960 312 and 269; 2 x 8 of 1024 x 1024 x 2048 4 bytes behind one 115 and 102;
+    // 4 x 512 x 2048 x 2048 33.1 and 29.1.  (The other way round 8 x 16 of 64 x 1000 x 1000, whose rows begin on 32 bytes: 141 and 164.)
     constexpr int PITCH = T::IN + 8;                      // floats: the two rows that a wave writes at a time lie on different banks
     static_assert(T::WO * 32 * PITCH * 4 <= BUFFERS * BUFFER, "room for them");
     float *const held = (float *)shared;                  // [WO * 32][PITCH]
     const int l = t & 63;
+    const bool lines = (uintptr_t)to % LINE == 0 && P.in % (LINE / 4) == 0;
 #pragma unroll
     for (int i = 0; i < MI; ++i) {
         if (i > 0) __syncthreads();
@@ -449,7 +452,13 @@ __global__ __launch_bounds__(T::THREADS) void weight_grad_kernel(Linear P)
             const int r = r0 + t / EACH, c = t % EACH * 4, o = o0 + r / 32 * (T::OUT / T::WO) + 32 * i + r % 32;
             if (o >= P.out) continue;
             const u32x4 w = *(const u32x4 *)(held + r * PITCH + c);
-            store_piece<float>(to + (int64_t)o * P.in + i0, c, P.in - i0, w);
+            if (lines) {
+                asm volatile("");                         // (around it: or both stores become one, through the caches)
+                store_piece<float>(to + (int64_t)o * P.in + i0, c, P.in - i0, w);
+                asm volatile("");
+            } else {
+                store_piece<float, false>(to + (int64_t)o * P.in + i0, c, P.in - i0, w);
+            }
         }
     }
     if (with_bias) {
