@@ -59,7 +59,8 @@ struct Ahead {
 // A row in the registers of T threads, C pieces each.  A workgroup has SLOTS such groups of threads and walks over a strip of a worker's rows, R rows a
 // group at a time, with the weights in registers and the next rows on their way; the rows' sums share their barriers.  The mean comes first, then the
 // sums of the differences from it and of their squares: the first of these is what the rounding of the mean left, which counts where a row's mean is
-// large beside its spread.
+// large beside its spread.  Means are sums of shares x / D and not quotients of sums: a product that a difference follows may be contracted with it for
+// some of a row's pieces and not for others, and differences from two centres, half a step of the mean apart, have no such rest.
 //
 // Memory bounds it: 8 x 2048 x 2048 bf16 23.5 us, keeping 8 bits too 28.5 (134 and 168 MB, 5.7 and 5.9 TB/s), one row of 4096 3.5 us.
 template <class E, int T, int C, int SLOTS, int R>
@@ -132,14 +133,13 @@ __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P
                 if (P.kept.codes && row < strip.end && c < (int)P.kept.stride) keep_piece<E>(P.kept, base + row, c, raw[q][i]);
                 Piece<E>::unpack(raw[q][i], v[q][i]);
 #pragma unroll
-                for (int j = 0; j < N; ++j) total[q] += v[q][i][j];
+                for (int j = 0; j < N; ++j) total[q] = fmaf(v[q][i][j], inverse, total[q]);
             }
         }
         load(at + strip.stride);
         row_sums<T>(total, totals[slot]);
 #pragma unroll
         for (int q = 0; q < R; ++q) {
-            total[q] *= inverse;                          // the mean
             s[2 * q] = s[2 * q + 1] = 0.f;
 #pragma unroll
             for (int i = 0; i < C; ++i) {
@@ -151,7 +151,7 @@ __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P
                     for (int j = 0; j < N; ++j) v[q][i][j] = c + j < P.width ? v[q][i][j] : 0.f;
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
-                    s[2 * q] += v[q][i][j];
+                    s[2 * q] = fmaf(v[q][i][j], inverse, s[2 * q]);
                     s[2 * q + 1] = fmaf(v[q][i][j], v[q][i][j], s[2 * q + 1]);
                 }
             }
@@ -162,7 +162,7 @@ __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P
             const int64_t row = at + q * SLOTS + slot;
             if (row >= strip.end) continue;
             const int64_t r = base + row;
-            const float rest = s[2 * q] * inverse;
+            const float rest = s[2 * q];
             const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[2 * q + 1] * inverse) + P.eps);
             if (P.stats && t == 0)
                 *(__attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r) = on[q] ? (f32x2){total[q] + rest, rstd} : (f32x2)0.f;
@@ -192,17 +192,17 @@ __global__ __launch_bounds__(T) void norm_long_kernel(Norm P)
     const bool on = !P.mask || P.mask[r];
     const E *const x = (const E *)P.x + r * P.ld;
     E *const y = (E *)P.y + r * P.ld_out;
+    const float inverse = 1.f / (float)P.width;
     float v[N], total[1] = {0.f};
     if (on)
         for (int c = t * N; c < P.width; c += T * N) {
             Piece<E>::unpack(load_piece<E, true>(x, c, P.width), v);
             float part = 0.f;
-            for (int j = 0; j < N; ++j) part += v[j];
+            for (int j = 0; j < N; ++j) part = fmaf(v[j], inverse, part);
             total[0] += part;
         }
-    const float inverse = 1.f / (float)P.width;
     row_sums<T>(total, totals);
-    const float mean = total[0] * inverse;
+    const float mean = total[0];
     float s[2] = {0.f, 0.f};
     if (on)
         for (int c = t * N; c < P.width; c += T * N) {
@@ -210,14 +210,14 @@ __global__ __launch_bounds__(T) void norm_long_kernel(Norm P)
             float part[2] = {0.f, 0.f};
             for (int j = 0; j < N; ++j) {
                 const float d = c + j < P.width ? v[j] - mean : 0.f;
-                part[0] += d;
+                part[0] = fmaf(d, inverse, part[0]);
                 part[1] = fmaf(d, d, part[1]);
             }
             s[0] += part[0];
             s[1] += part[1];
         }
     row_sums<T>(s, sums);
-    const float rest = s[0] * inverse;
+    const float rest = s[0];
     const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[1] * inverse) + P.eps);
     if (P.stats && t == 0) {
         P.stats[2 * r] = on ? mean + rest : 0.f;
