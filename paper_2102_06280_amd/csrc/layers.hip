@@ -77,7 +77,7 @@ struct Plan {
     static constexpr int T = T_, C = C_, SLOTS = SLOTS_, R = R_;
 };
 template <bool BACK, class F>
-bool by_row(int64_t bytes, F f)
+constexpr bool by_row(int64_t bytes, F f)
 {
     if (bytes <= 16 * 16) f(std::conditional_t<BACK, Plan<16, 1, 16, 4>, Plan<16, 1, 16, 1>>());
     else if (bytes <= 64 * 16) f(Plan<64, 1, 4, 1>());
@@ -93,6 +93,16 @@ bool by_row(int64_t bytes, F f)
     else return false;
     return true;
 }
+// The kernels count on it: all of a plan's pieces but the last are whole.  (A row's last 16 bytes may be 2 or 4 of its own.)
+template <bool BACK>
+constexpr bool pieces_are_whole()
+{
+    bool whole = true;
+    for (int64_t piece = 0; piece < 2048; ++piece)
+        by_row<BACK>(16 * piece + 2, [&](auto p) { whole = whole && 16 * piece + 2 > (p.C - 1) * p.T * 16 && piece < p.C * p.T; });
+    return whole;
+}
+static_assert(pieces_are_whole<false>() && pieces_are_whole<true>(), "rows are longer than all of a plan's pieces but the last");
 constexpr int LONG_THREADS = 1024, LONG_GRAD_THREADS = 256;
 
 // Workgroups of a worker, which take rows_at_once rows each in turn: `groups` for all workers, if there are so many rows for at least `turns` turns.
