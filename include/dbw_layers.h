@@ -12,8 +12,9 @@
  * Rows.  Worker i's token positions are the rows i * T + t, 0 <= t < T.  Activations and their gradients are fp32, bf16 or fp16 and
  * need no alignment beyond an element's; widths and strides may be odd.  Columns between a row's width and its stride are neither
  * read nor written.  What is computed is computed and summed in fp32 and rounded once to the type of its array.  No
- * sum depends on the order in which workgroups run: the same call gives the same bits.  Squares that pass the largest fp32 number make a norm's rho 0.  In the
- * weight gradient from 8 bits fp32 values of magnitude below 2^-110 enter to within 2^-133 each.
+ * sum depends on the order in which workgroups run: the same call gives the same bits.  Squares that pass the largest fp32 number make a norm's rho 0,
+ * and a row with numbers of magnitude 2^124 and more, unless all are equal, may be NaN.  In the weight gradient from 8 bits fp32 values of
+ * magnitude below 2^-110 enter to within 2^-133 each.
  *
  * Rows that take no part.  mask [dev, N*T] uint8 or NULL: a row whose entry is 0 is not read, whatever it holds (infinities, NaN); its outputs
  * are given as zeros and it adds nothing to any sum.  In the other rows infinities and NaN go through the formulas.

@@ -56,6 +56,23 @@ struct Ahead {
     __device__ __forceinline__ bool on(int64_t at, int q) const { return at + q * SLOTS < end && rows[q]; }
 };
 
+// The row's first number, which its mean counts from: of lane 0 where a row is a wave's or 16 lanes', or as it was loaded.
+template <class E, int T>
+__device__ __forceinline__ float first_of(float lane_0, float loaded)
+{
+    if (T == 16) return loss::shifted<0x150, 0xf>(lane_0, 0.f);
+    if (T == 64) return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(lane_0)));
+    return loaded;
+}
+
+// A piece's numbers added up in pairs: of equal numbers exactly.
+template <int N>
+__device__ __forceinline__ float piece_sum(const float (&v)[N])
+{
+    if constexpr (N == 4) return (v[0] + v[1]) + (v[2] + v[3]);
+    else return ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+}
+
 // Piece i of C, all of which but the last are whole: in two steps as load_raw and settled.
 template <class E, bool WIDE, int C>
 __device__ __forceinline__ u32x4 load_turn(const E *row, int i, int c, int width)
@@ -76,6 +93,11 @@ __device__ __forceinline__ u32x4 settled_turn(const u32x4 &w, int i, int c, int 
 // large beside its spread.  Means are sums of shares x / D and not quotients of sums: a product that a difference follows may be contracted with it for
 // some of a row's pieces and not for others, and differences from two centres, half a step of the mean apart, have no such rest.
 //
+// The mean counts from the row's first number x_0: mu = x_0 + mean of (x - x_0), a piece's N numbers added up before N x_0 goes off them.  Equal numbers add up
+// exactly in pairs, so that a row of them has differences of zero, and the mean of other rows is off by a step or two of mu and by what is small beside
+// the spread.  Sums of x over a row leave many steps of mu, and where the spread is less, the squares' mean without the rest's square is rounding, of either
+// sign: rho of NaN, or of a spread that is not there.  As it is, the two differ: numbers that are not all equal lie steps of their own apart.
+//
 // Memory bounds it: 8 x 2048 x 2048 bf16 23.5 us, keeping 8 bits too 28.5 (134 and 168 MB, 5.7 and 5.9 TB/s), one row of 4096 3.5 us.
 template <class E, int T, int C, int SLOTS, int R>
 __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P)
@@ -90,6 +112,7 @@ __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P
     const int64_t base = (int64_t)strip.worker * P.per_worker;
     const float inverse = 1.f / (float)P.width;
     u32x4 next[R][C];
+    typename Bits<E>::type next_first[R];
     bool next_on[R];
     Ahead<R, SLOTS> ahead(P.mask, base + slot, strip.end - slot);
     ahead.look(strip.first);
@@ -98,9 +121,11 @@ __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P
         for (int q = 0; q < R; ++q) {
             const int64_t r = base + at + q * SLOTS + slot;
             next_on[q] = ahead.on(at, q);
-            if (next_on[q])
+            if (next_on[q]) {
+                if (T > 64) next_first[q] = *(const __attribute__((address_space(1))) typename Bits<E>::type *)(uint64_t)((const E *)P.x + r * P.ld);
 #pragma unroll
-                for (int i = 0; i < C; ++i) next[q][i] = load_raw<E, WIDE>((const E *)P.x + r * P.ld, (i * T + t) * N, P.width);
+                for (int i = 0; i < C; ++i) next[q][i] = load_turn<E, WIDE, C>((const E *)P.x + r * P.ld, i, (i * T + t) * N, P.width);
+            }
         }
         ahead.look(at + strip.stride);
     };
@@ -128,13 +153,13 @@ __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P
     };
     for (int64_t at = strip.first; at < strip.end; at += strip.stride) {
         bool on[R];
-        float v[R][C][N], total[R], s[2 * R];
+        float v[R][C][N], first[R], total[R], s[2 * R];
         u32x4 raw[R][C];
 #pragma unroll
         for (int q = 0; q < R; ++q) {
             on[q] = next_on[q];
 #pragma unroll
-            for (int i = 0; i < C; ++i) raw[q][i] = on[q] ? settled<E, WIDE>(next[q][i], (i * T + t) * N, P.width) : (u32x4)0u;
+            for (int i = 0; i < C; ++i) raw[q][i] = on[q] ? settled_turn<E, WIDE, C>(next[q][i], i, (i * T + t) * N, P.width) : (u32x4)0u;
         }
         if (last >= 0) store(last);
 #pragma unroll
@@ -146,21 +171,25 @@ __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P
                 const int c = (i * T + t) * N;
                 if (P.kept.codes && row < strip.end && c < (int)P.kept.stride) keep_piece<E>(P.kept, base + row, c, raw[q][i]);
                 Piece<E>::unpack(raw[q][i], v[q][i]);
+                if (i == 0) first[q] = first_of<E, T>(v[q][0][0], on[q] ? loss::widen(__builtin_bit_cast(E, next_first[q])) : 0.f);
+                if (i == C - 1 && c + N > P.width)
 #pragma unroll
-                for (int j = 0; j < N; ++j) total[q] = fmaf(v[q][i][j], inverse, total[q]);
+                    for (int j = 0; j < N; ++j) v[q][i][j] = c + j < P.width ? v[q][i][j] : first[q];
+                total[q] = fmaf(piece_sum(v[q][i]) - N * first[q], inverse, total[q]);
             }
         }
         load(at + strip.stride);
         row_sums<T>(total, totals[slot]);
 #pragma unroll
         for (int q = 0; q < R; ++q) {
+            total[q] += first[q];                         // the mean
             s[2 * q] = s[2 * q + 1] = 0.f;
 #pragma unroll
             for (int i = 0; i < C; ++i) {
                 const int c = (i * T + t) * N;
 #pragma unroll
                 for (int j = 0; j < N; ++j) v[q][i][j] -= total[q];
-                if (c + N > P.width)
+                if (i == C - 1 && c + N > P.width)
 #pragma unroll
                     for (int j = 0; j < N; ++j) v[q][i][j] = c + j < P.width ? v[q][i][j] : 0.f;
 #pragma unroll
@@ -207,16 +236,19 @@ __global__ __launch_bounds__(T) void norm_long_kernel(Norm P)
     const E *const x = (const E *)P.x + r * P.ld;
     E *const y = (E *)P.y + r * P.ld_out;
     const float inverse = 1.f / (float)P.width;
+    u32x4 next = on ? load_raw<E, true>(x, t * N, P.width) : (u32x4)0u;
+    const float first = on ? loss::widen(*x) : 0.f;       // (asked for beside the first pieces)
     float v[N], total[1] = {0.f};
     if (on)
         for (int c = t * N; c < P.width; c += T * N) {
-            Piece<E>::unpack(load_piece<E, true>(x, c, P.width), v);
-            float part = 0.f;
-            for (int j = 0; j < N; ++j) part = fmaf(v[j], inverse, part);
-            total[0] += part;
+            Piece<E>::unpack(settled<E, true>(next, c, P.width), v);
+            next = load_raw<E, true>(x, c + T * N, P.width);
+            if (c + N > P.width)
+                for (int j = 0; j < N; ++j) v[j] = c + j < P.width ? v[j] : first;
+            total[0] = fmaf(piece_sum(v) - N * first, inverse, total[0]);
         }
     row_sums<T>(total, totals);
-    const float mean = total[0];
+    const float mean = first + total[0];
     float s[2] = {0.f, 0.f};
     if (on)
         for (int c = t * N; c < P.width; c += T * N) {
