@@ -159,6 +159,7 @@ class Study:
         self.shape = B.make_logits(workers, ROWS, VOCAB, B.TYPE_F32, scale=SCALE)
         self.work = torch.empty(B.dbw_loss_work_bytes(self.shape), dtype=torch.uint8, device="cuda")
         self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        self.diverged = torch.zeros((), dtype=torch.int64, device="cuda")      # tokens sampled from no distribution
         self.dlogits = torch.empty(workers, ROWS, VOCAB, device="cuda")
         self.loss = torch.empty(workers, device="cuda")
 
@@ -169,8 +170,11 @@ class Study:
         return torch.randint(0, VOCAB, (self.n, ROWS, 2), device="cuda", generator=self.gen)
 
     def sample(self, logits):
-        # (of a model that has diverged any token is as good as another: multinomial ends the process where a probability is none)
-        p = torch.softmax(logits * SCALE, -1).nan_to_num(nan=1.0).reshape(-1, VOCAB)
+        # (of a model that has diverged any token is as good as another, and is counted: multinomial ends the process where a probability is none)
+        p = torch.softmax(logits * SCALE, -1).reshape(-1, VOCAB)
+        none = torch.isnan(p).any(-1)
+        self.diverged += none.sum()
+        p.masked_fill_(none[:, None], 1.0)
         return torch.multinomial(p, 1, generator=self.gen)[:, 0].int()
 
     def logp(self, models, context, tokens):
@@ -230,7 +234,8 @@ class Study:
 
 
 def run(workers: int = 6, rounds: int = 40, seed: int = 1, experts: int = 0):
-    """Curves of the three stages, as lists of floats, and the status the losses left."""
+    """Curves of the three stages, as lists of floats, the status the losses left, and how many tokens a diverged model was to sample ("diverged": with any,
+    the curves are no result)."""
     study = Study(workers, seed, experts)
     try:
         # Experts' weights multiply the step: with the first rates the ratio of a token with a negative advantage, which nothing bounds, overflows in the
@@ -246,7 +251,7 @@ def run(workers: int = 6, rounds: int = 40, seed: int = 1, experts: int = 0):
         return {"distill_loss": [v.mean().item() for v in distill],
                 "preference_loss": [v[0].mean().item() for v in preference], "margin": [v[1].item() for v in preference],
                 "reward": [v[0].item() for v in policy], "kl": [v[1].item() for v in policy],
-                "status": int(study.status.item()), "params": study.x[0][:, :study.d].cpu().numpy()}
+                "status": int(study.status.item()), "diverged": int(study.diverged.item()), "params": study.x[0][:, :study.d].cpu().numpy()}
     finally:
         study.close()
 
@@ -261,6 +266,8 @@ def main():
     out = run(args.workers, args.rounds, args.seed, args.experts)
     out.pop("params")
     print(json.dumps({k: [round(x, 5) for x in v] if isinstance(v, list) else v for k, v in out.items()}))
+    if out["diverged"]:
+        raise SystemExit(f"models diverged: {out['diverged']} tokens were sampled from no distribution")
 
 
 if __name__ == "__main__":
