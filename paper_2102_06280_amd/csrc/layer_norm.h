@@ -87,8 +87,8 @@ __device__ __forceinline__ u32x4 settled_turn(const u32x4 &w, int i, int c, int 
     return i < C - 1 ? w : settled<E, WIDE>(w, c, width);
 }
 
-// A row in the registers of T threads, C pieces each.  A workgroup has SLOTS such groups of threads and walks over a strip of a worker's rows, R rows a
-// group at a time, with the weights in registers and the next rows on their way; the rows' sums share their barriers.  The mean comes first, then the
+// A row in the registers of T threads, C pieces each.  A workgroup has SLOTS such groups of threads and walks over a strip of a worker's rows, a row a
+// group at a time, with the weights in registers and the next row on its way.  The mean comes first, then the
 // sums of the differences from it and of their squares: the first of these is what the rounding of the mean left, which counts where a row's mean is
 // large beside its spread.  Means are sums of shares x / D and not quotients of sums: a product that a difference follows may be contracted with it for
 // some of a row's pieces and not for others, and differences from two centres, half a step of the mean apart, have no such rest.
@@ -99,33 +99,30 @@ __device__ __forceinline__ u32x4 settled_turn(const u32x4 &w, int i, int c, int 
 // sign: rho of NaN, or of a spread that is not there.  As it is, the two differ: numbers that are not all equal lie steps of their own apart.
 //
 // Memory bounds it: 8 x 2048 x 2048 bf16 23.5 us, keeping 8 bits too 28.5 (134 and 168 MB, 5.7 and 5.9 TB/s), one row of 4096 3.5 us.
-template <class E, int T, int C, int SLOTS, int R>
+template <class E, int T, int C, int SLOTS>
 __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P)
 {
     constexpr int N = Piece<E>::N, WAVES = (T + 63) / 64;
     constexpr bool WIDE = T * C > 16;
-    __shared__ float totals[SLOTS][WAVES][R], sums[SLOTS][WAVES][2 * R];
+    __shared__ float totals[SLOTS][WAVES][1], sums[SLOTS][WAVES][2];
     const int64_t group = group_number();
     if (group >= (int64_t)P.workers * P.strips) return;
-    const Strip strip = strip_of((uint32_t)group, P.strips, R * SLOTS, P.per_worker);
+    const Strip strip = strip_of((uint32_t)group, P.strips, SLOTS, P.per_worker);
     const int t = loss::tid<T>(), slot = slot_of<T>();
     const int64_t base = (int64_t)strip.worker * P.per_worker;
     const float inverse = 1.f / (float)P.width;
-    u32x4 next[R][C];
-    typename Bits<E>::type next_first[R];
-    bool next_on[R];
-    Ahead<R, SLOTS> ahead(P.mask, base + slot, strip.end - slot);
+    u32x4 next[C];
+    typename Bits<E>::type next_first;
+    bool next_on;
+    Ahead<1, SLOTS> ahead(P.mask, base + slot, strip.end - slot);
     ahead.look(strip.first);
     const auto load = [&](int64_t at) {
+        const int64_t r = base + at + slot;
+        next_on = ahead.on(at, 0);
+        if (next_on) {
+            if (T > 64) next_first = *(const __attribute__((address_space(1))) typename Bits<E>::type *)(uint64_t)((const E *)P.x + r * P.ld);
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            const int64_t r = base + at + q * SLOTS + slot;
-            next_on[q] = ahead.on(at, q);
-            if (next_on[q]) {
-                if (T > 64) next_first[q] = *(const __attribute__((address_space(1))) typename Bits<E>::type *)(uint64_t)((const E *)P.x + r * P.ld);
-#pragma unroll
-                for (int i = 0; i < C; ++i) next[q][i] = load_turn<E, WIDE, C>((const E *)P.x + r * P.ld, i, (i * T + t) * N, P.width);
-            }
+            for (int i = 0; i < C; ++i) next[i] = load_turn<E, WIDE, C>((const E *)P.x + r * P.ld, i, (i * T + t) * N, P.width);
         }
         ahead.look(at + strip.stride);
     };
@@ -140,83 +137,62 @@ __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P
     }
     // Rows are written a turn later, in front of the loads of the rows behind the next: waiting for loads is waiting for all that was asked for before
     // them, and nothing then waits for stores that have just begun.  (Backwards from 8 bits with a mask, 8 x 2048 x 2048 bf16: 48 us -> 37.)
-    u32x4 out[R][C];
+    u32x4 out[C];
     int64_t last = -1;
     const auto store = [&](int64_t at) {
+        const int64_t row = at + slot;
+        if (row < strip.end)
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            const int64_t row = at + q * SLOTS + slot;
-            if (row < strip.end)
-#pragma unroll
-                for (int i = 0; i < C; ++i) store_piece<E>((E *)P.y + (base + row) * P.ld_out, (i * T + t) * N, P.width, out[q][i]);
-        }
+            for (int i = 0; i < C; ++i) store_piece<E>((E *)P.y + (base + row) * P.ld_out, (i * T + t) * N, P.width, out[i]);
     };
     for (int64_t at = strip.first; at < strip.end; at += strip.stride) {
-        bool on[R];
-        float v[R][C][N], first[R], total[R], s[2 * R];
-        u32x4 raw[R][C];
+        const bool on = next_on;
+        const int64_t row = at + slot;
+        float v[C][N], first, total[1] = {0.f}, s[2] = {0.f, 0.f};
+        u32x4 raw[C];
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            on[q] = next_on[q];
-#pragma unroll
-            for (int i = 0; i < C; ++i) raw[q][i] = on[q] ? settled_turn<E, WIDE, C>(next[q][i], i, (i * T + t) * N, P.width) : (u32x4)0u;
-        }
+        for (int i = 0; i < C; ++i) raw[i] = on ? settled_turn<E, WIDE, C>(next[i], i, (i * T + t) * N, P.width) : (u32x4)0u;
         if (last >= 0) store(last);
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            const int64_t row = at + q * SLOTS + slot;
-            total[q] = 0.f;
+        for (int i = 0; i < C; ++i) {
+            const int c = (i * T + t) * N;
+            if (P.kept.codes && row < strip.end && c < (int)P.kept.stride) keep_piece<E>(P.kept, base + row, c, raw[i]);
+            Piece<E>::unpack(raw[i], v[i]);
+            if (i == 0) first = first_of<E, T>(v[0][0], on ? loss::widen(__builtin_bit_cast(E, next_first)) : 0.f);
+            if (i == C - 1 && c + N > P.width)
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const int c = (i * T + t) * N;
-                if (P.kept.codes && row < strip.end && c < (int)P.kept.stride) keep_piece<E>(P.kept, base + row, c, raw[q][i]);
-                Piece<E>::unpack(raw[q][i], v[q][i]);
-                if (i == 0) first[q] = first_of<E, T>(v[q][0][0], on[q] ? loss::widen(__builtin_bit_cast(E, next_first[q])) : 0.f);
-                if (i == C - 1 && c + N > P.width)
-#pragma unroll
-                    for (int j = 0; j < N; ++j) v[q][i][j] = c + j < P.width ? v[q][i][j] : first[q];
-                total[q] = fmaf(piece_sum(v[q][i]) - N * first[q], inverse, total[q]);
-            }
+                for (int j = 0; j < N; ++j) v[i][j] = c + j < P.width ? v[i][j] : first;
+            total[0] = fmaf(piece_sum(v[i]) - N * first, inverse, total[0]);
         }
         load(at + strip.stride);
         row_sums<T>(total, totals[slot]);
+        const float mean = total[0] + first;
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            total[q] += first[q];                         // the mean
-            s[2 * q] = s[2 * q + 1] = 0.f;
+        for (int i = 0; i < C; ++i) {
+            const int c = (i * T + t) * N;
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-                const int c = (i * T + t) * N;
+            for (int j = 0; j < N; ++j) v[i][j] -= mean;
+            if (i == C - 1 && c + N > P.width)
 #pragma unroll
-                for (int j = 0; j < N; ++j) v[q][i][j] -= total[q];
-                if (i == C - 1 && c + N > P.width)
+                for (int j = 0; j < N; ++j) v[i][j] = c + j < P.width ? v[i][j] : 0.f;
 #pragma unroll
-                    for (int j = 0; j < N; ++j) v[q][i][j] = c + j < P.width ? v[q][i][j] : 0.f;
-#pragma unroll
-                for (int j = 0; j < N; ++j) {
-                    s[2 * q] = fmaf(v[q][i][j], inverse, s[2 * q]);
-                    s[2 * q + 1] = fmaf(v[q][i][j], v[q][i][j], s[2 * q + 1]);
-                }
+            for (int j = 0; j < N; ++j) {
+                s[0] = fmaf(v[i][j], inverse, s[0]);
+                s[1] = fmaf(v[i][j], v[i][j], s[1]);
             }
         }
         row_sums<T>(s, sums[slot]);
+        const float rest = s[0];
+        const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[1] * inverse) + P.eps);
+        if (P.stats && t == 0 && row < strip.end)
+            *(__attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * (base + row)) = on ? (f32x2){mean + rest, rstd} : (f32x2)0.f;
+        const float less = -rest * rstd;
 #pragma unroll
-        for (int q = 0; q < R; ++q) {
-            const int64_t row = at + q * SLOTS + slot;
-            if (row >= strip.end) continue;
-            const int64_t r = base + row;
-            const float rest = s[2 * q];
-            const float rstd = 1.f / sqrtf(fmaf(-rest, rest, s[2 * q + 1] * inverse) + P.eps);
-            if (P.stats && t == 0)
-                *(__attribute__((address_space(1))) f32x2 *)(uint64_t)(P.stats + 2 * r) = on[q] ? (f32x2){total[q] + rest, rstd} : (f32x2)0.f;
-            const float less = -rest * rstd;
+        for (int i = 0; i < C; ++i) {
 #pragma unroll
-            for (int i = 0; i < C; ++i) {
-#pragma unroll
-                for (int j = 0; j < N; ++j) v[q][i][j] = fmaf(fmaf(v[q][i][j], rstd, less), w[i][j], b[i][j]);
-                const u32x4 packed = Piece<E>::pack(v[q][i]);
-                out[q][i] = on[q] ? packed : (u32x4)0u;
-            }
+            for (int j = 0; j < N; ++j) v[i][j] = fmaf(fmaf(v[i][j], rstd, less), w[i][j], b[i][j]);
+            const u32x4 packed = Piece<E>::pack(v[i]);
+            out[i] = on ? packed : (u32x4)0u;
         }
         last = at;
     }
@@ -347,7 +323,7 @@ __device__ __forceinline__ float *part_of(const NormGrad &P, int worker, int str
     return P.grads + worker * P.ld_grads + at;
 }
 
-// As norm_kernel; every thread's columns are the same in all rows, so that it sums dw and db in registers.  Rows that take no part are zeros with a mean and
+// As norm_kernel, R rows a group at a time, whose sums share their barriers; every thread's columns are the same in all rows, so that it sums dw and db in registers.  Rows that take no part are zeros with a mean and
 // a scale of zero.  Memory bounds long batches (8 x 8192 x 2048 bf16 from 8 bits 133 us, 5.0 TB/s); shorter ones pay some 8 us for the first rows' way and
 // for adding up (8 x 2048 x 2048 37 us).
 template <class E, int T, int C, int SLOTS, int R, bool KEPT>

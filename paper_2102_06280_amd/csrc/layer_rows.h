@@ -16,10 +16,6 @@ typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 
-// Rows of T threads each in a workgroup.
-template <int T>
-constexpr int ROWS_OF = T <= 64 ? 256 / T : 1;
-
 constexpr int BLOCK = 32;                                 // columns that share a power of two
 constexpr int64_t padded(int64_t width) { return (width + BLOCK - 1) / BLOCK * BLOCK; }
 

@@ -13,7 +13,6 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "global_access.h"
 #include "layer_rows.h"
 
 namespace layer {

@@ -64,7 +64,7 @@ bool outside(int64_t at, int64_t count, int64_t ld) { return at >= 0 && (count >
 layer::Kept kept_of(const void *checkpoint, const Shape &S, const dbw_rows *l) { return layer::kept_of((void *)checkpoint, S.rows, l->width); }
 int64_t checkpoint_bytes(int64_t rows, int64_t width) { return rows * (layer::padded(width) + layer::padded(width) / layer::BLOCK); }
 
-// Which kernel takes a row of a norm: T threads, C pieces each, SLOTS such groups of threads in a workgroup, R rows of a group at a time.  A wave a row as long
+// Which kernel takes a row of a norm: T threads, C pieces each, SLOTS such groups of threads in a workgroup, R rows of a group at a time backwards (forwards one).  A wave a row as long
 // as its registers hold it: no barriers.  Microseconds, workers x rows x width, bf16 unless said otherwise: forwards 8 x 2048 x 2048 by a wave 23.5, by 256
 // threads, four rows between two barriers, 24.8; 4 x 2048 x 4096 by 256 threads 23.3, by 128 28.5, by 512 28.0; backwards from 8 bits
 // 8 x 2048 x 4096 by 128 threads, two rows at a time, 75.8, by 256 one row at a time 78.7, by 512 79.9.  16 x 64 x 16 fp32 by 16 threads a row, four rows
@@ -202,7 +202,7 @@ extern "C" int dbw_layer_norm(const dbw_rows *shape, const void *x, const uint8_
     by_type(shape->type, [&](auto e) {
         typedef decltype(e) E;
         if (!by_row<false>(S.e * shape->width, [&](auto p) {
-                hipLaunchKernelGGL((layer::norm_kernel<E, p.T, p.C, p.SLOTS, p.R>), grid_of((int64_t)shape->workers * strips), dim3(p.T * p.SLOTS), 0, s, P);
+                hipLaunchKernelGGL((layer::norm_kernel<E, p.T, p.C, p.SLOTS>), grid_of((int64_t)shape->workers * strips), dim3(p.T * p.SLOTS), 0, s, P);
             }))
             hipLaunchKernelGGL((layer::norm_long_kernel<E, LONG_THREADS>), grid_of(S.rows), dim3(LONG_THREADS), 0, s, P);
     });
