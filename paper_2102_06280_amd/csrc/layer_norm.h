@@ -19,12 +19,19 @@ struct Norm {
     Kept kept;                                            // codes null: not wanted
 };
 
-// Sums of K numbers over a row's T threads.  lds: T / 64 times K floats of the row's that nothing else uses until the next barrier but one.
+// What the first of 16 lanes has.
+__device__ __forceinline__ float of_lane_0(float v) { return loss::shifted<0x150, 0xf>(v, 0.f); }
+
+// Sums of K numbers over a row's T threads, the same in all of them (16 lanes add in as many orders: the first one's).  lds: T / 64 times K floats of the row's
+// that nothing else uses until the next barrier but one.
 template <int T, int K>
 __device__ __forceinline__ void row_sums(float (&v)[K], float (*lds)[K])
 {
 #pragma unroll
-    for (int k = 0; k < K; ++k) v[k] = loss::lanes_sum<T>(v[k]);
+    for (int k = 0; k < K; ++k) {
+        v[k] = loss::lanes_sum<T>(v[k]);
+        if (T == 16) v[k] = of_lane_0(v[k]);
+    }
     if (T <= 64) return;
     if ((threadIdx.x & 63) == 0)
 #pragma unroll
@@ -60,7 +67,7 @@ struct Ahead {
 template <class E, int T>
 __device__ __forceinline__ float first_of(float lane_0, float loaded)
 {
-    if (T == 16) return loss::shifted<0x150, 0xf>(lane_0, 0.f);
+    if (T == 16) return of_lane_0(lane_0);
     if (T == 64) return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(lane_0)));
     return loaded;
 }

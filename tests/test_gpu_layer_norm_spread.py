@@ -134,3 +134,29 @@ def test_squares_beyond_fp32(B, pieces, size):
     assert torch.equal(y[far], c.b.expand(3, -1)[far]) and (stats[far, 1] == 0).all()
     mu, off = x.double().mean(1), (ref.depth(c.d) + 4) * ref.U * x.double().abs().mean(1)
     ref.close(stats[:, 0], mu, off + ref.U * x[:, 0].double().abs(), "mu")
+
+
+@pytest.mark.parametrize("width", [3, 13, 16, 33, 50, 64])
+@pytest.mark.parametrize("loud", [10.0, 1e4])
+@pytest.mark.parametrize("at", [0, -1])
+def test_one_centre_for_all_lanes_of_a_row(B, width, loud, at):
+    """Rows by 16 lanes, one number far from the others.  u = (x - mu) rho: a difference from the one centre (U |u|), without the rest, a sum of 4 products and 4 additions
+    (9 U of the differences' mean magnitude), times rho (the variance's 9 U and two products by half, a sum, a root, a quotient) and rounded (U)."""
+    c = Case(B, F32, 1, 200, width, masked=False, weight=False, bias=False, seed=29)
+    x = torch.randn(c.total, width, generator=c.g)
+    x[:, at] *= loud
+    c.x = Rows(x)
+    y = c.forward().result()
+    eps = torch.tensor(1e-5).double().item()
+    one, none = torch.ones(c.total, width, dtype=torch.float64), torch.zeros(c.total, width, dtype=torch.float64)
+    u = ref.norm(x.double(), one, none, eps)[0]
+    ref.close(y, u, ref.U * ((1 + 5.5 + 3 + 1) * u.abs() + (9 + 1) * u.abs().mean(1, keepdim=True)), "u")
+
+
+@pytest.mark.parametrize("offset", [1000.0, -1e4, 1e6])
+@pytest.mark.parametrize("width", [3, 13, 16, 33, 64])
+def test_a_small_spread_beside_a_large_mean_by_16_lanes(B, width, offset):
+    c = Case(B, F32, 2, 50, width, masked=False, seed=30)
+    c.x = Rows(torch.randn(c.total, width, generator=c.g) + offset)
+    c.check_forward(c.forward())
+    c.check_backward(*c.backward())
