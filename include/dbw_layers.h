@@ -20,7 +20,7 @@
  * are given as zeros and it adds nothing to any sum.  In the other rows infinities and NaN go through the formulas.
  *
  * In place only where an entry point says so: any other overlap of what a call writes with what it reads or writes is DBW_ERR_ALIAS where
- * both are rows of activations, and the caller's to avoid elsewhere.
+ * both are rows of activations (also of rows that lie between one another's), and the caller's to avoid elsewhere.
  *
  * work is scratch memory of the call's, on a 16-byte boundary, of the size that the function next to the entry point gives; what it holds before and
  * after means nothing.  Calls that may overlap in time need one each.
@@ -85,7 +85,8 @@ int64_t dbw_layer_norm_work_bytes(const dbw_rows *shape);
 
 /* Its backward pass, from dy [dev, stride ld_out].  With u_c = rho (x_c - mu) and g_c = w_c dy_c,
  *     dx_c = rho (g_c - mean of g - u_c mean of (g u)),  dw_c = sum over the worker's rows of dy_c u_c,  db_c = sum of dy_c.
- *   x          [dev, stride ld], or NULL: what `checkpoint` stands for is taken for x (one of the two is given)
+ *   x          [dev, stride ld], or NULL: what `checkpoint` stands for is taken for x (one of the two is given).  That is off by 2^-4 of x at most, and so
+ *              u by 2^-4 of |x| rho: where a row's mean is large beside its spread, u is lost by |mu| rho 2^-4, whatever the spread
  *   stats      mu and rho as dbw_layer_norm gave them
  *   dx         [dev, stride ld]; may be x itself, or dy if the strides are equal
  *   grads      [dev, N * ld_grads] float: dw goes to the columns from weight_at on of every worker's row, db to those from

@@ -105,7 +105,7 @@ __device__ __forceinline__ u32x4 settled_turn(const u32x4 &w, int i, int c, int 
 // the spread.  Sums of x over a row leave many steps of mu, and where the spread is less, the squares' mean without the rest's square is rounding, of either
 // sign: rho of NaN, or of a spread that is not there.  As it is, the two differ: numbers that are not all equal lie steps of their own apart.
 //
-// Memory bounds it: 8 x 2048 x 2048 bf16 23.5 us, keeping 8 bits too 28.5 (134 and 168 MB, 5.7 and 5.9 TB/s), one row of 4096 3.5 us.
+// Memory bounds it: 8 x 2048 x 2048 bf16 23.0 us, keeping 8 bits too 32.0 (134 and 168 MB, 5.8 and 5.2 TB/s), one row of 4096 3.3 us.
 template <class E, int T, int C, int SLOTS>
 __global__ __launch_bounds__(T * SLOTS, T == 64 ? 3 : 1) void norm_kernel(Norm P)
 {
@@ -330,9 +330,9 @@ __device__ __forceinline__ float *part_of(const NormGrad &P, int worker, int str
     return P.grads + worker * P.ld_grads + at;
 }
 
-// As norm_kernel, R rows a group at a time, whose sums share their barriers; every thread's columns are the same in all rows, so that it sums dw and db in registers.  Rows that take no part are zeros with a mean and
-// a scale of zero.  Memory bounds long batches (8 x 8192 x 2048 bf16 from 8 bits 133 us, 5.0 TB/s); shorter ones pay some 8 us for the first rows' way and
-// for adding up (8 x 2048 x 2048 37 us).
+// As norm_kernel, R rows a group at a time, whose sums share their barriers; every thread's columns are the same in all rows, so that it sums dw and db in
+// registers.  Rows that take no part are zeros with a mean and a scale of zero.  Memory bounds long batches (8 x 8192 x 2048 bf16 from 8 bits 133 us,
+// 5.0 TB/s); shorter ones pay some 8 us for the first rows' way and for adding up (8 x 2048 x 2048 37 us).
 template <class E, int T, int C, int SLOTS, int R, bool KEPT>
 __global__ __launch_bounds__(T * SLOTS) void norm_grad_kernel(NormGrad P)
 {

@@ -3,9 +3,9 @@
 // What a code stands for is exact in bf16, and so is dy as one (bf16), two (fp16) or three (fp32) bf16 numbers: every product on the bf16
 // matrix instruction is exact, and fp32 sums are all that rounds.
 //
-// 4 x 4096 x 2048 x 2048 bf16 141 us (0.97 PFLOP/s; the library's bf16 product of these sizes, without the decoding, takes 105), matrix cores busy 41 %, LDS
+// 4 x 4096 x 2048 x 2048 bf16 135 us (1.02 PFLOP/s; the library's bf16 product of these sizes, without the decoding, takes 105), matrix cores busy 41 %, LDS
 // 31 %, vector units 29 % of the time under a profiler: what is left are waits, with two waves a SIMD and a barrier every 32 rows.  fp16 and fp32 take two and three
-// products for one: 2 x 4096 x 2048 x 2048 129 and 187 us.  Short batches are bound by writing dW, workgroup after workgroup (1 x 300 x 4096 x 4096 24 us,
+// products for one: 2 x 4096 x 2048 x 2048 125 and 178 us.  Short batches are bound by writing dW, workgroup after workgroup (1 x 300 x 4096 x 4096 24 us,
 // 67 MB).  Tried without gain: wave priorities, four waves of 128 x 128 (spilled), tiles of 128 x 128 with two workgroups a compute unit (216), the
 // next rows put into LDS at a step's beginning or end (within 2 %).
 #pragma once

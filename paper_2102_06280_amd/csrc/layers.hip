@@ -65,13 +65,16 @@ layer::Kept kept_of(const void *checkpoint, const Shape &S, const dbw_rows *l) {
 int64_t checkpoint_bytes(int64_t rows, int64_t width) { return rows * (layer::padded(width) + layer::padded(width) / layer::BLOCK); }
 
 // Which kernel takes a row of a norm: T threads, C pieces each, SLOTS such groups of threads in a workgroup, R rows of a group at a time backwards (forwards one).  A wave a row as long
-// as its registers hold it: no barriers.  Microseconds, workers x rows x width, bf16 unless said otherwise: forwards 8 x 2048 x 2048 by a wave 23.5, by 256
-// threads, four rows between two barriers, 24.8; 4 x 2048 x 4096 by 256 threads 23.3, by 128 28.5, by 512 28.0; backwards from 8 bits
+// as its registers hold it: no barriers.  Microseconds when the plans were chosen, workers x rows x width, bf16 unless said otherwise: forwards
+// 8 x 2048 x 2048 by a wave 23.5, by 256 threads, four rows between two barriers, 24.8; 4 x 2048 x 4096 by 256 threads 23.3, by 128 28.5, by 512 28.0; backwards from 8 bits
 // 8 x 2048 x 4096 by 128 threads, two rows at a time, 75.8, by 256 one row at a time 78.7, by 512 79.9.  16 x 64 x 16 fp32 by 16 threads a row, four rows
 // each, 7.9, one each 11.4.  4 x 2048 x 12288 backwards by 512 threads 143, by 1024 threads, whose registers do not hold it all, 274.
 // Three pieces a thread where they hold the row: forwards, and backwards from 8 bits, 8 x 2048 x 1536 19.1 and 26.5, with four pieces 23.4 and 29.3; 16 x 1779 x
 // 2983 by 128 threads 75 and 91, by 256 with two pieces 79 and by 128 with four 147; 8 x 2048 x 5296 by 256 threads 73 and 98, by 512 with two 77 and 126;
 // 4 x 2048 x 12288 by 512 87 and 118, with four 105 and 176.
+// Since whole pieces are loaded without a look at the width: forwards 8 x 2048 x 2048 23.0, 4 x 2048 x 4096 21.8, 8 x 2048 x 1536 16.8, 16 x 1779 x 2983 75, 8 x 2048 x 5296 72,
+// 4 x 2048 x 12288 83; backwards from 8 bits 8 x 2048 x 4096 73.8, the others as they were.  Four pieces by 512 threads are more than the registers of 16-bit
+// rows backwards hold, 34 of them go to scratch memory from x and 38 from 8 bits: 4 x 2048 x 16000 190 and 165 us, of 121 and 101 by their bytes.
 template <int T_, int C_, int SLOTS_, int R_>
 struct Plan {
     static constexpr int T = T_, C = C_, SLOTS = SLOTS_, R = R_;
