@@ -87,7 +87,7 @@ int64_t dbw_layer_norm_work_bytes(const dbw_rows *shape);
  *     dx_c = rho (g_c - mean of g - u_c mean of (g u)),  dw_c = sum over the worker's rows of dy_c u_c,  db_c = sum of dy_c.
  *   x          [dev, stride ld], or NULL: what `checkpoint` stands for is taken for x (one of the two is given).  That is off by 2^-4 of x at most, and so
  *              u by 2^-4 of |x| rho: where a row's mean is large beside its spread, u is lost by |mu| rho 2^-4, whatever the spread
- *   stats      mu and rho as dbw_layer_norm gave them
+ *   stats      mu and rho as dbw_layer_norm gave them; u takes mu's own rounding, 2^-24 |mu| rho, where the forward pass does not
  *   dx         [dev, stride ld]; may be x itself, or dy if the strides are equal
  *   grads      [dev, N * ld_grads] float: dw goes to the columns from weight_at on of every worker's row, db to those from
  *              bias_at on; the other columns are left as they are.  A part whose column number is negative is not wanted; NULL: neither is

@@ -7,9 +7,8 @@ import torch
 import layer_reference as ref
 
 f = np.float32
-# bytes of a row up to which T threads take it in C pieces each
-PLANS = [(256, 16, 1), (1024, 64, 1), (2048, 64, 2), (3072, 64, 3), (4096, 64, 4), (6144, 128, 3), (8192, 256, 2), (12288, 256, 3), (16384, 512, 2),
-         (24576, 512, 3), (32768, 512, 4)]
+# threads that take a row and pieces of 16 bytes of each: the first with as many pieces as the row has
+PLANS = [(16, 1), (64, 1), (64, 2), (64, 3), (64, 4), (128, 3), (256, 2), (256, 3), (512, 2), (512, 3), (512, 4)]
 WIDTHS = [3, 17, 65, 100, 200, 257, 511, 700, 982, 1500, 2049, 3001, 5000, 8001, 20000]
 
 
@@ -41,7 +40,7 @@ def norm(x, eps, size):
     """mu, rho, the variance and the differences from the mean [rows, width] of fp32 numbers of which a piece of 16 bytes holds 16 / size."""
     n, width = x.shape
     each = 16 // size
-    t, turns = next(((t, c) for most, t, c in PLANS if width * size <= most), (1024, -(-width // (1024 * each))))
+    t, turns = next(((t, c) for t, c in PLANS if width * size <= 16 * t * c), (1024, -(-width // (1024 * each))))
     inverse, first = f(1) / f(width), x[:, :1]
     cut = lambda v: v.reshape(n, turns, t, each)
     row = np.repeat(first, turns * t * each, 1)
